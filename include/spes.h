@@ -296,6 +296,89 @@ SPES_API int spes_expert_warmup_merge_static(int32_t n_experts, int32_t dtype, i
                                              void* const* dst, const int64_t* elems, float* sim,
                                              int32_t* nbr, void* stream);
 
+/* ---- Operators around the expert layer ------------------------------------------------------------------------------
+ * What a training program runs beside the routed layer: the norm ahead of it, routing of other kinds than the layer's own, and an
+ * optimizer step that orthogonalises the update.  Zero rows or tokens are a valid call.
+ */
+
+/* Layer norm (kind SPES_NORM_LAYER) or root-mean-square norm (SPES_NORM_RMS) of every row, with the residual stream's addition:
+ *      v = x + add (rounded to the storage type)   or  v = x  without add
+ *      mean = sum v / cols (layer norm; 0 otherwise)      rstd = (sum (v - mean)^2 / cols + eps)^-1/2
+ *      y = (v - mean) rstd weight + bias
+ *
+ *  rows >= 0; 1 <= cols <= 16384
+ *  x, add     DEVICE [rows, cols], rows x_stride and add_stride elements apart (>= cols); add may be NULL.  Here and in
+ *             spes_norm_bwd a tensor with a stride needs no other alignment than its element's
+ *  weight     DEVICE [cols]      bias  DEVICE [cols] or NULL
+ *  eps        >= 0
+ *  sum        DEVICE [rows, cols] out: v; NULL exactly if add is
+ *  y          DEVICE [rows, cols] out
+ *  mean       DEVICE [rows] f32 out, layer norm only (else NULL)     rstd  DEVICE [rows] f32 out
+ */
+typedef enum { SPES_NORM_LAYER = 0, SPES_NORM_RMS = 1 } spes_norm_kind;
+SPES_API int spes_norm_fwd(int32_t kind, int32_t rows, int32_t cols, int32_t dtype, const void* x,
+                           int64_t x_stride, const void* add, int64_t add_stride,
+                           const void* weight, const void* bias, float eps, void* sum, void* y,
+                           float* mean, float* rstd, void* stream);
+
+/* Backward of spes_norm_fwd for the upstream gradient dy.  With hat = (v - mean) rstd and h = dy weight
+ *      dx = rstd (h - hat (sum h hat / cols) - (sum h / cols, layer norm only)) + dres
+ *      d_weight = sum over rows of dy hat           d_bias = sum over rows of dy
+ * dx is the gradient of v, hence of x and of add alike; dres is the gradient that reaches v along the residual stream.
+ *
+ *  dy, x, dres  DEVICE [rows, cols] with strides as above; x is v (the forward's sum, or its x without add); dres may be NULL
+ *  mean, rstd   as the forward left them
+ *  dx           DEVICE [rows, cols] out
+ *  d_weight     DEVICE [cols] f32, d_bias DEVICE [cols] f32.  d_bias may be NULL; both may (a frozen norm), then scratch may as well
+ *  accumulate   0: d_weight and d_bias are overwritten; 1: added to
+ *  scratch      DEVICE, spes_norm_scratch_bytes(rows, cols) bytes
+ */
+SPES_API size_t spes_norm_scratch_bytes(int32_t rows, int32_t cols);
+SPES_API int spes_norm_bwd(int32_t kind, int32_t rows, int32_t cols, int32_t dtype, const void* dy,
+                           int64_t dy_stride, const void* x, int64_t x_stride, const void* weight,
+                           const float* mean, const float* rstd, const void* dres,
+                           int64_t dres_stride, void* dx, float* d_weight, float* d_bias,
+                           int32_t accumulate, void* scratch, void* stream);
+
+/* Routing to experts from given scores.  Per token, with logits l over M experts
+ *      s = softmax(l) or sigmoid(l)        c = s + bias
+ *      with groups > 1 the experts stand in `groups` groups of M / groups each; a group counts the sum of its two largest c (its
+ *      only one, of a single expert), and only the kept_groups best groups are open, equal ones to the lower group
+ *      idx = the top_k largest c in open groups in descending order, equal ones to the lower expert
+ *      gate = scale * s[idx], with renorm scale * s[idx] / sum of s[idx]
+ * The bias steers the choice only: it enters no gate and has no gradient (a program moves it by the counts to balance the load).
+ * Logits may be -inf (an expert that a token must not get counts 0 then, and is taken only where nothing else is left); a row of
+ * -inf alone has gates 0, as has one whose chosen scores are all 0.  NaN counts below everything: indices are valid and
+ * different from one another whatever the logits hold.
+ *
+ *  Supported: 1 <= top_k <= 16; n_experts <= 512; groups <= 16, dividing n_experts; top_k <= kept_groups * n_experts / groups
+ */
+typedef enum { SPES_SCORE_SOFTMAX = 0, SPES_SCORE_SIGMOID = 1 } spes_score;
+typedef struct {
+  int32_t score;       /* spes_score                                       */
+  int32_t groups;      /* 1: no groups                                     */
+  int32_t kept_groups; /* 1 <= kept_groups <= groups                       */
+  int32_t renorm;      /* 1: gates are renormalised over the chosen ones   */
+  float scale;         /* factor of the gates, finite                      */
+} spes_router_opts;
+
+/*  logits  DEVICE [T, n_experts] f32      bias   DEVICE [n_experts] f32 or NULL
+ *  idx     DEVICE [T, top_k] i32 out      gate   DEVICE [T, top_k] f32 out
+ *  count   DEVICE [n_experts] i32 out: tokens that chose the expert
+ */
+SPES_API int spes_router_fwd(int32_t T, int32_t n_experts, int32_t top_k, const spes_router_opts* opts,
+                             const float* logits, const float* bias, int32_t* idx, float* gate,
+                             int32_t* count, void* stream);
+
+/* Gradient of the gates with respect to the logits, the choice held fixed.  A scale of gates of 0 / 0 has none.
+ *
+ *  logits, idx  as above, idx as the forward left it      dgate  DEVICE [T, top_k] f32
+ *  dlogits      DEVICE [T, n_experts] f32 out
+ */
+SPES_API int spes_router_bwd(int32_t T, int32_t n_experts, int32_t top_k, const spes_router_opts* opts,
+                             const float* logits, const int32_t* idx, const float* dgate,
+                             float* dlogits, void* stream);
+
 SPES_API const char* spes_strerror(int code);
 
 #ifdef __cplusplus

@@ -8,6 +8,7 @@ missing and cannot be built the import fails loudly -- there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional, Sequence
 
@@ -17,6 +18,8 @@ import torch
 from . import build as _build
 
 SPES_F32, SPES_BF16 = 0, 1
+SPES_NORM_LAYER, SPES_NORM_RMS = 0, 1
+SPES_SCORE_SOFTMAX, SPES_SCORE_SIGMOID = 0, 1
 
 
 class SpesError(RuntimeError):
@@ -33,6 +36,10 @@ _LAYOUT_FIELDS = ("total", "logits", "lse", "topk_idx", "topk_gate", "offset", "
 
 class spes_moe_ctx_layout(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in _LAYOUT_FIELDS]
+
+
+class spes_router_opts(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("score", "groups", "kept_groups", "renorm")] + [("scale", ctypes.c_float)]
 
 
 def _load() -> ctypes.CDLL:
@@ -69,6 +76,17 @@ def _load() -> ctypes.CDLL:
     lib.spes_expert_warmup_merge.argtypes = [i32, i32, i32, ctypes.c_float, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp]
     lib.spes_expert_warmup_merge_static.restype = i32
     lib.spes_expert_warmup_merge_static.argtypes = [i32, i32, i32, ctypes.c_float, vp, i64, i32, vp, vp, vp, vp, vp, vp]
+    lib.spes_norm_scratch_bytes.restype = sz
+    lib.spes_norm_scratch_bytes.argtypes = [i32, i32]
+    lib.spes_norm_fwd.restype = i32
+    lib.spes_norm_fwd.argtypes = [i32] * 4 + [vp, i64, vp, i64, vp, vp, ctypes.c_float] + [vp] * 5
+    lib.spes_norm_bwd.restype = i32
+    lib.spes_norm_bwd.argtypes = [i32] * 4 + [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, i32, vp, vp]
+    opts = ctypes.POINTER(spes_router_opts)
+    lib.spes_router_fwd.restype = i32
+    lib.spes_router_fwd.argtypes = [i32, i32, i32, opts] + [vp] * 6
+    lib.spes_router_bwd.restype = i32
+    lib.spes_router_bwd.argtypes = [i32, i32, i32, opts] + [vp] * 5
     lib.spes_ref_mfma_rate.restype = i32
     lib.spes_ref_mfma_rate.argtypes = [vp, i32, i32, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.spes_profile_enable.restype = i32
@@ -98,6 +116,35 @@ def _dev(t: Optional[torch.Tensor]):
     if not t.is_cuda or not t.is_contiguous():
         raise SpesError("device arguments must be contiguous GPU tensors")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _buf(t: Optional[torch.Tensor], dtype: torch.dtype, *size: int):
+    """Pointer of a contiguous tensor of at least this size and of this type."""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or t.numel() < math.prod(size):
+        raise SpesError(f"expected a contiguous GPU tensor of {size} {dtype}, got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _rows(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype):
+    """Pointer and row stride of a matrix whose rows may stand further apart than they are long."""
+    if t is None:
+        return None, 0
+    if t.shape != (rows, cols) or t.dtype != dtype:
+        raise SpesError("a matrix argument has another shape or type than the call says")
+    stride = t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    if not t.is_cuda or (cols > 1 and t.stride(1) != 1) or stride < cols:
+        raise SpesError("matrix arguments must be GPU tensors with contiguous rows that do not overlap")
+    return t.data_ptr(), stride
+
+
+def _scratch(t: Optional[torch.Tensor], bytes_of, *args):
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous() or t.numel() * t.element_size() < bytes_of(*args):
+        raise SpesError("scratch is not a contiguous GPU tensor, or smaller than the call needs")
+    return t.data_ptr()
 
 
 def _stream(stream):
@@ -222,6 +269,48 @@ def spes_expert_warmup_merge_static(n_experts, dtype, top_K, alpha, w_in, elems_
                                                 ctypes.cast(sp, ctypes.c_void_p), ctypes.cast(dp, ctypes.c_void_p),
                                                 el.ctypes.data_as(ctypes.c_void_p), _dev(sim), _dev(nbr), _stream(stream)),
            "spes_expert_warmup_merge_static")
+
+
+def spes_norm_scratch_bytes(rows: int, cols: int) -> int:
+    return int(_lib.spes_norm_scratch_bytes(rows, cols))
+
+
+def spes_norm_fwd(kind, rows, cols, dtype, x, add, weight, bias, eps, sum, y, mean, rstd, stream=None) -> None:
+    """x and add may be views with rows further apart than cols; their strides go into the call."""
+    t, f = torch_dtype(dtype), torch.float32
+    xp, xs = _rows(x, rows, cols, t)
+    ap, as_ = _rows(add, rows, cols, t)
+    _check(_lib.spes_norm_fwd(kind, rows, cols, dtype, xp, xs, ap, as_, _buf(weight, t, cols), _buf(bias, t, cols), eps,
+                              _buf(sum, t, rows, cols), _buf(y, t, rows, cols), _buf(mean, f, rows), _buf(rstd, f, rows), _stream(stream)),
+           "spes_norm_fwd")
+
+
+def spes_norm_bwd(kind, rows, cols, dtype, dy, x, weight, mean, rstd, dres, dx, d_weight, d_bias, accumulate=0, scratch=None,
+                  stream=None) -> None:
+    """dy, x and dres may be views with rows further apart than cols; their strides go into the call."""
+    t, f = torch_dtype(dtype), torch.float32
+    gp, gs = _rows(dy, rows, cols, t)
+    xp, xs = _rows(x, rows, cols, t)
+    rp, rs = _rows(dres, rows, cols, t)
+    _check(_lib.spes_norm_bwd(kind, rows, cols, dtype, gp, gs, xp, xs, _buf(weight, t, cols), _buf(mean, f, rows), _buf(rstd, f, rows), rp, rs,
+                              _buf(dx, t, rows, cols), _buf(d_weight, f, cols), _buf(d_bias, f, cols), int(accumulate),
+                              _scratch(scratch, _lib.spes_norm_scratch_bytes, rows, cols), _stream(stream)), "spes_norm_bwd")
+
+
+def router_opts(score, groups=1, kept_groups=1, renorm=0, scale=1.0) -> spes_router_opts:
+    return spes_router_opts(score, groups, kept_groups, renorm, scale)
+
+
+def spes_router_fwd(T, n_experts, top_k, opts, logits, bias, idx, gate, count, stream=None) -> None:
+    f, i = torch.float32, torch.int32
+    _check(_lib.spes_router_fwd(T, n_experts, top_k, opts, _buf(logits, f, T, n_experts), _buf(bias, f, n_experts), _buf(idx, i, T, top_k),
+                                _buf(gate, f, T, top_k), _buf(count, i, n_experts), _stream(stream)), "spes_router_fwd")
+
+
+def spes_router_bwd(T, n_experts, top_k, opts, logits, idx, dgate, dlogits, stream=None) -> None:
+    f, i = torch.float32, torch.int32
+    _check(_lib.spes_router_bwd(T, n_experts, top_k, opts, _buf(logits, f, T, n_experts), _buf(idx, i, T, top_k), _buf(dgate, f, T, top_k),
+                                _buf(dlogits, f, T, n_experts), _stream(stream)), "spes_router_bwd")
 
 
 def spes_profile_enable(on: bool) -> None:

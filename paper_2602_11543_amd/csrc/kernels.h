@@ -51,6 +51,21 @@ int launch_upcycle_init(int dtype, int n_experts, long elems, const void* dense,
 int launch_expert_pack(int dtype, int n_experts, long elems, void* store, const unsigned char* mask, void* packed, int to_store,
                        hipStream_t s);
 
+// norm.hip
+size_t norm_scratch_bytes(int rows, int cols);
+int launch_norm_fwd(int dtype, int kind, int rows, int cols, const void* x, long x_stride, const void* add, long add_stride, const void* weight,
+                    const void* bias, float eps, void* sum, void* y, float* mean, float* rstd, hipStream_t s);
+// d_weight[cols] (+)=, d_bias[cols] (+)= through partial sums in scratch; either may be NULL
+int launch_norm_bwd(int dtype, int kind, int rows, int cols, const void* dy, long dy_stride, const void* x, long x_stride, const void* weight,
+                    const float* mean, const float* rstd, const void* dres, long dres_stride, void* dx, float* d_weight, float* d_bias,
+                    int accumulate, float* scratch, hipStream_t s);
+
+// router.hip
+int launch_router_fwd(int T, int M, int k, const spes_router_opts& o, const float* logits, const float* bias, int* idx, float* gate, int* count,
+                      hipStream_t s);
+int launch_router_bwd(int T, int M, int k, const spes_router_opts& o, const float* logits, const int* idx, const float* dgate, float* dlogits,
+                      hipStream_t s);
+
 // reference.hip: register-resident MFMA loop (blocks x 4 wavefronts x iters x 64 MFMAs of 16x16x32); *flop = operations launched
 int launch_mfma_rate(const void* data, int blocks, int iters, float* sink, double* flop, hipStream_t s);
 

@@ -1,0 +1,357 @@
+// Routing to experts from given scores, and its gradient.  Per token with logits l
+//      s = softmax(l) or sigmoid(l)            c = s + bias                    (the bias steers the choice and nothing else)
+//      groups: of equal size; a group counts the sum of its two largest c; only the `kept` best groups are open
+//      idx = the k largest c in open groups, equal ones to the lower expert    gate = scale s[idx] (/ sum of s[idx], renorm)
+// Sixteen lanes hold a token, four consecutive experts to a lane and quad, so a wavefront works on four tokens and every
+// reduction stays within a row of lanes, in data-parallel-primitive steps.  What bounds it is the k rounds of the choice (five instructions
+// an expert of the lane and round), not the 4 M bytes of a token.
+//
+// Gradient, the choice held fixed, with g the gates' share (scale taken out) and u = scale dgate.  Every difference is between gradients, weighted by
+// shares, so nothing cancels when one expert takes all:
+//      renorm:   D_j = sum_i g_i (u_j - u_i);  softmax: dl_j = g_j D_j (the other scores do not matter);  sigmoid: dl_j = g_j (1 - s_j) D_j
+//      otherwise sigmoid: dl_j = u_j s_j (1 - s_j);   softmax: dl_j = s_j (sum_i s_i (u_j - u_i) + u_j sum of the s not chosen),
+//                and dl_e = -s_e sum_i s_i u_i for an expert that is not chosen
+#include <type_traits>
+
+#include "kernels.h"
+#include "lds_load.h"
+#include "units.h"
+
+namespace spes {
+namespace {
+
+
+
+constexpr int kRow = 16;                       // lanes of a token
+constexpr int kSkew = 16;                      // floats: one more for every group ahead, so that groups of 32 start in different banks
+
+template <int CTRL> __device__ __forceinline__ int dpp_int(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
+__device__ __forceinline__ unsigned row_max(unsigned v) {
+  v = max(v, (unsigned)dpp_int<0x128>((int)v));       // row_ror 8, 4, 2, 1
+  v = max(v, (unsigned)dpp_int<0x124>((int)v));
+  v = max(v, (unsigned)dpp_int<0x122>((int)v));
+  return max(v, (unsigned)dpp_int<0x121>((int)v));
+}
+__device__ __forceinline__ int row_min(int v) {
+  v = min(v, dpp_int<0x128>(v));
+  v = min(v, dpp_int<0x124>(v));
+  v = min(v, dpp_int<0x122>(v));
+  return min(v, dpp_int<0x121>(v));
+}
+__device__ __forceinline__ float row_max_f(float v) {
+  v = fmaxf(v, dpp_move<0x128>(v));
+  v = fmaxf(v, dpp_move<0x124>(v));
+  v = fmaxf(v, dpp_move<0x122>(v));
+  return fmaxf(v, dpp_move<0x121>(v));
+}
+__device__ __forceinline__ float row_sum(float v) { return lane_group_sum<16>(v); }
+
+// unsigned keys in the order of the floats; NaN below them all, and 0 below that
+__device__ __forceinline__ unsigned order_key(float f) {
+  const unsigned u = __float_as_uint(f);
+  return f != f ? 1u : u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+
+__device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
+
+struct RouterArgs {
+  int T, M, k, groups, kept, size, parts;      // parts: lanes that look through a group, a power of two; groups * parts <= 16
+  unsigned inv_size;                           // e / size = e inv_size >> 20 for e < 512
+  bool renorm;
+  float scale;
+  const float *logits, *bias;
+  int* idx;
+  float* gate;
+  int* count;
+  bool one_block;                              // count is written, not added to
+  const float* dgate;
+  float* dlogits;
+};
+
+// four logits from expert e on, -inf beyond the last one
+__device__ __forceinline__ void load4(const float* row, int e, int M, float* v) {
+  if (e + 4 <= M) {
+    const f32x4_any q = *reinterpret_cast<const f32x4_any*>(row + e);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = q[c];
+  } else {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = e + c < M ? row[e + c] : -INFINITY;
+  }
+}
+
+// softmax of one token: the largest logit and the inverse of the sum.  A row of -inf alone has no largest one: its scores are 0.
+template <int NQ>
+__device__ __forceinline__ void softmax_stats(const float (&v)[NQ * 4], float& mx, float& inv) {
+  mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NQ * 4; ++i) mx = fmaxf(mx, v[i]);
+  mx = row_max_f(mx);
+  if (mx == -INFINITY) mx = 0.f;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < NQ * 4; ++i) sum += expf(v[i] - mx);
+  sum = row_sum(sum);
+  inv = sum == 0.f ? 0.f : 1.f / sum;
+}
+
+template <int NQ, bool SOFTMAX, bool GROUPS, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
+  constexpr int V = NQ * 4, TOKENS = BLOCK / kRow;
+  __shared__ int hist[NQ * 64];
+  __shared__ float choice[GROUPS ? TOKENS : 1][NQ * 64 + kSkew];
+  const int l = threadIdx.x % kRow, at = threadIdx.x / kRow;
+  for (int e = threadIdx.x; e < NQ * 64; e += BLOCK) hist[e] = 0;
+  __syncthreads();
+  for (long t0 = (long)blockIdx.x * TOKENS; t0 < a.T; t0 += (long)gridDim.x * TOKENS) {
+    const long t = t0 + at < a.T ? t0 + at : a.T - 1;          // (surplus rows of lanes repeat the last token and store nothing)
+    const bool live = t0 + at < a.T;
+    const float* const row = a.logits + t * a.M;
+    float v[V];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) load4(row, q * 64 + l * 4, a.M, v + q * 4);
+    float mx = 0.f, inv = 1.f;
+    if (SOFTMAX) softmax_stats<NQ>(v, mx, inv);
+    auto score = [&](float x) { return SOFTMAX ? expf(x - mx) * inv : sigmoid(x); };
+    unsigned key[V];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int e = q * 64 + l * 4 + c, i = q * 4 + c;
+        float x = score(v[i]);
+        if (a.bias && e < a.M) x += a.bias[e];
+        key[i] = e < a.M ? order_key(x) : 0u;
+        if (GROUPS && e < a.M) choice[at][e + (int)((unsigned)e * a.inv_size >> 20)] = x;
+      }
+    if (GROUPS) {
+      // lanes g parts .. look through group g; the first of them ranks it among the others
+      wave_lds_order();
+      const int g = l / a.parts, part = l % a.parts;
+      float first = -INFINITY, second = -INFINITY;
+      if (g < a.groups) {
+        const float* const own = choice[at] + g * (a.size + 1);
+        for (int n = part; n < a.size; n += a.parts) {
+          const float x = own[n];
+          second = fmaxf(second, fminf(first, x));             // (NaN: passed over)
+          first = fmaxf(first, x);
+        }
+      }
+      for (int d = 1; d < a.parts; d *= 2) {
+        const float f2 = __shfl_xor(first, d, kWave), s2 = __shfl_xor(second, d, kWave);
+        second = fmaxf(fmaxf(second, s2), fminf(first, f2));
+        first = fmaxf(first, f2);
+      }
+      wave_lds_order();
+      const unsigned mine = part == 0 && g < a.groups ? order_key(a.size > 1 ? first + second : first) : 0u;
+      int rank = 0;
+      auto against = [&](unsigned other, int lane) { rank += other > mine || (other == mine && lane < l) ? 1 : 0; };
+#define SPES_TURN(r) against((unsigned)dpp_int<0x120 + r>((int)mine), dpp_int<0x120 + r>(l))
+      SPES_TURN(1); SPES_TURN(2); SPES_TURN(3); SPES_TURN(4); SPES_TURN(5); SPES_TURN(6); SPES_TURN(7); SPES_TURN(8);
+      SPES_TURN(9); SPES_TURN(10); SPES_TURN(11); SPES_TURN(12); SPES_TURN(13); SPES_TURN(14); SPES_TURN(15);
+#undef SPES_TURN
+      const unsigned open = (unsigned)(__ballot(mine != 0 && rank < a.kept) >> (threadIdx.x & 48)) & 0xffffu;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const unsigned e = (unsigned)(q * 64 + l * 4 + c);
+          if ((open >> ((e * a.inv_size >> 20) * a.parts) & 1u) == 0) key[q * 4 + c] = 0;
+        }
+    }
+    int chosen = 0;                     // of lane j: the j-th expert
+    for (int j = 0; j < a.k; ++j) {
+      unsigned top = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) top = max(top, key[i]);
+      top = row_max(top);
+      int first = 0x7fffffff;
+#pragma unroll
+      for (int i = V - 1; i >= 0; --i) first = key[i] == top ? (i / 4) * 64 + i % 4 : first;
+      const int e = row_min(first == 0x7fffffff ? first : first + l * 4);
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (e == (i / 4) * 64 + l * 4 + i % 4) key[i] = 0;
+      if (l == j) chosen = e;
+    }
+    const bool mine = l < a.k;
+    const float s = mine ? score(row[chosen]) : 0.f;
+    float share = s;
+    if (a.renorm) {
+      const float total = row_sum(s);
+      share = total == 0.f ? 0.f : s / total;
+    }
+    if (mine && live) {
+      a.idx[t * a.k + l] = chosen;
+      a.gate[t * a.k + l] = share * a.scale;
+      atomicAdd(&hist[chosen], 1);
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.M; e += BLOCK) {
+    if (a.one_block) a.count[e] = hist[e];
+    else if (hist[e] != 0) atomicAdd(&a.count[e], hist[e]);      // (integers: any order gives the same)
+  }
+}
+
+__global__ __launch_bounds__(512) void zero_kernel(int* __restrict__ p, int n) {
+  if (threadIdx.x < n) p[threadIdx.x] = 0;
+}
+
+// sum over the chosen i of w_i (u - u_i), in every lane for its own u
+__device__ __forceinline__ float weighted_differences(float w, float u) {
+  float d = 0.f;
+#define SPES_TURN(r) d = fmaf(dpp_move<0x120 + r>(w), u - dpp_move<0x120 + r>(u), d)
+  SPES_TURN(1); SPES_TURN(2); SPES_TURN(3); SPES_TURN(4); SPES_TURN(5); SPES_TURN(6); SPES_TURN(7); SPES_TURN(8);
+  SPES_TURN(9); SPES_TURN(10); SPES_TURN(11); SPES_TURN(12); SPES_TURN(13); SPES_TURN(14); SPES_TURN(15);
+#undef SPES_TURN
+  return d;
+}
+
+// WHOLE: softmax without renormalisation, where every score has a gradient.  Otherwise only the k chosen ones are read.
+template <int NQ, bool SOFTMAX, bool WHOLE>
+__global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a) {
+  constexpr int V = NQ * 4;
+  __shared__ __align__(16) float out[16][NQ * 64];
+  const int l = threadIdx.x % kRow, at = threadIdx.x / kRow;
+  float* const mine = out[at];
+  for (long t0 = (long)blockIdx.x * 16; t0 < a.T; t0 += (long)gridDim.x * 16) {
+    const long t = t0 + at < a.T ? t0 + at : a.T - 1;
+    const bool live = t0 + at < a.T;
+    const float* const row = a.logits + t * a.M;
+    int e = -1;
+    float u = 0.f, x = 0.f;
+    if (l < a.k) {
+      e = a.idx[t * a.k + l];
+      if (e < 0 || e >= a.M) e = -1;                       // (no expert: no gradient)
+      else { u = a.dgate[t * a.k + l] * a.scale; x = row[e]; }
+    }
+    const bool has = e >= 0;
+    float p[WHOLE ? V : 1], mx = 0.f, inv = 1.f;
+    if (WHOLE) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) load4(row, q * 64 + l * 4, a.M, p + q * 4);
+      if constexpr (WHOLE) softmax_stats<NQ>(p, mx, inv);
+#pragma unroll
+      for (int i = 0; i < (WHOLE ? V : 1); ++i) p[i] = expf(p[i] - mx) * inv;
+    }
+    // marks of the chosen ones, then results
+    wave_lds_order();
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) *reinterpret_cast<float4*>(mine + q * 64 + l * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+    wave_lds_order();
+    float d;
+    if (WHOLE) {
+      if (has) mine[e] = 1.f;
+      wave_lds_order();
+      float rest = 0.f;
+#pragma unroll
+      for (int i = 0; i < (WHOLE ? V : 1); ++i) rest += mine[(i / 4) * 64 + l * 4 + i % 4] == 0.f ? p[i] : 0.f;
+      rest = row_sum(rest);
+      wave_lds_order();
+      const float s = has ? expf(x - mx) * inv : 0.f;
+      d = s * (weighted_differences(s, u) + u * rest);
+      const float dot = row_sum(s * u);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        float* const o = mine + q * 64 + l * 4;
+        const float* const pq = p + (WHOLE ? q * 4 : 0);
+        *reinterpret_cast<float4*>(o) = make_float4(-pq[0] * dot, -pq[WHOLE ? 1 : 0] * dot, -pq[WHOLE ? 2 : 0] * dot, -pq[WHOLE ? 3 : 0] * dot);
+      }
+      wave_lds_order();
+    } else {
+      // the softmax over the chosen ones alone, or sigmoids; 1 - s from the side that does not cancel
+      float s, other;
+      if (SOFTMAX) {
+        const float top = row_max_f(has ? x : -INFINITY);
+        s = has ? expf(x - (top == -INFINITY ? 0.f : top)) : 0.f;
+        other = 1.f;
+      } else {
+        const float small = expf(-fabsf(x)), big = 1.f / (1.f + small);
+        s = has ? (x < 0.f ? small * big : big) : 0.f;
+        other = x < 0.f ? big : small * big;
+      }
+      if (a.renorm) {
+        const float total = row_sum(s), g = total == 0.f ? 0.f : s / total;
+        d = g * other * weighted_differences(g, u);
+      } else {
+        d = s * other * u;
+      }
+    }
+    if (has) mine[e] = d;
+    wave_lds_order();
+    if (live) {
+      float* const dst = a.dlogits + t * a.M;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const int e0 = q * 64 + l * 4;
+        const float4 o = *reinterpret_cast<const float4*>(mine + e0);
+        if (e0 + 4 <= a.M) {
+          *reinterpret_cast<f32x4_any*>(dst + e0) = f32x4_any{o.x, o.y, o.z, o.w};
+        } else {
+          if (e0 < a.M) dst[e0] = o.x;
+          if (e0 + 1 < a.M) dst[e0 + 1] = o.y;
+          if (e0 + 2 < a.M) dst[e0 + 2] = o.z;
+        }
+      }
+    }
+  }
+}
+
+RouterArgs router_args(int T, int M, int k, const spes_router_opts& o) {
+  RouterArgs a = {};
+  a.T = T; a.M = M; a.k = k; a.groups = o.groups; a.kept = o.kept_groups; a.size = M / o.groups;
+  a.parts = 1;
+  while (a.parts * 2 * a.groups <= kRow) a.parts *= 2;
+  a.inv_size = ((1u << 20) + (unsigned)a.size - 1) / (unsigned)a.size;
+  a.renorm = o.renorm != 0;
+  a.scale = o.scale;
+  return a;
+}
+
+template <typename F>
+int with_quads(int M, F launch) {
+  if (M <= 64) return launch(std::integral_constant<int, 1>{});
+  if (M <= 128) return launch(std::integral_constant<int, 2>{});
+  if (M <= 256) return launch(std::integral_constant<int, 4>{});
+  return launch(std::integral_constant<int, 8>{});
+}
+
+}  // namespace
+
+int launch_router_fwd(int T, int M, int k, const spes_router_opts& o, const float* logits, const float* bias, int* idx, float* gate, int* count,
+                      hipStream_t s) {
+  RouterArgs a = router_args(T, M, k, o);
+  a.logits = logits; a.bias = bias; a.idx = idx; a.gate = gate; a.count = count;
+  // A single block counts by itself; several need a launch ahead of theirs that clears the counts.
+  a.one_block = T <= 128;
+  if (!a.one_block) hipLaunchKernelGGL(zero_kernel, dim3(1), dim3(512), 0, s, count, M);
+  const bool groups = o.groups > 1;
+  return with_quads(M, [&](auto nq) {
+    constexpr int NQ = decltype(nq)::value;
+    auto go = [&](auto softmax, auto grouped) {
+      constexpr bool SM = decltype(softmax)::value, GR = decltype(grouped)::value;
+      if (a.one_block) hipLaunchKernelGGL((router_fwd_kernel<NQ, SM, GR, 1024>), dim3(1), dim3(1024), 0, s, a);
+      else hipLaunchKernelGGL((router_fwd_kernel<NQ, SM, GR, 256>), dim3(cdiv(T, 16) < 1024 ? cdiv(T, 16) : 1024), dim3(256), 0, s, a);
+      return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
+    };
+    if (o.score == SPES_SCORE_SOFTMAX) return groups ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+    return groups ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
+  });
+}
+
+int launch_router_bwd(int T, int M, int k, const spes_router_opts& o, const float* logits, const int* idx, const float* dgate, float* dlogits,
+                      hipStream_t s) {
+  RouterArgs a = router_args(T, M, k, o);
+  a.logits = logits; a.idx = const_cast<int*>(idx); a.dgate = dgate; a.dlogits = dlogits;
+  const int grid = cdiv(T, 16) < 4096 ? cdiv(T, 16) : 4096;
+  return with_quads(M, [&](auto nq) {
+    constexpr int NQ = decltype(nq)::value;
+    if (o.score == SPES_SCORE_SIGMOID) hipLaunchKernelGGL((router_bwd_kernel<NQ, false, false>), dim3(grid), dim3(256), 0, s, a);
+    else if (o.renorm) hipLaunchKernelGGL((router_bwd_kernel<NQ, true, false>), dim3(grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((router_bwd_kernel<NQ, true, true>), dim3(grid), dim3(256), 0, s, a);
+    return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
+  });
+}
+
+}  // namespace spes
