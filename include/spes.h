@@ -379,6 +379,44 @@ SPES_API int spes_router_bwd(int32_t T, int32_t n_experts, int32_t top_k, const 
                              const float* logits, const int32_t* idx, const float* dgate,
                              float* dlogits, void* stream);
 
+/* Orthogonalisation of a stack of matrices by Newton-Schulz steps: every matrix is scaled to Frobenius norm 1, then `steps` times
+ *      X <- a X + (b X X^T + c (X X^T)^2) X
+ * which takes each singular value through a s + b s^3 + c s^5 and leaves the singular vectors.  Products and sums: bf16 storage
+ * on fp16 operands with fp32 sums, the result within about 1e-3 of the formula's in norm; fp32 storage to fp32 accuracy.  A matrix of
+ * zeros gives zeros, one that holds an infinity or a NaN gives NaN.
+ *
+ *  1 <= n <= 65535 matrices of rows x cols, each side at most 16384; 1 <= steps <= 64
+ *  src    DEVICE [n, rows, cols] storage dtype      out  DEVICE [n, rows, cols] storage dtype out
+ *  coef   HOST [3] f32: a, b, c, or NULL for 3.4445, -4.7750, 2.0315, which lift small singular values to near 1 in five steps.
+ *         Values that let singular values grow to 5 overflow the stored operands
+ *  scratch DEVICE, spes_orthogonalize_scratch_bytes(n, rows, cols, dtype) bytes
+ */
+SPES_API size_t spes_orthogonalize_scratch_bytes(int32_t n, int32_t rows, int32_t cols, int32_t dtype);
+SPES_API int spes_orthogonalize(int32_t n, int32_t rows, int32_t cols, int32_t dtype, const void* src,
+                                void* out, int32_t steps, const float* coef, void* scratch,
+                                void* stream);
+
+/* Optimizer step with an orthogonalised update on the trainable subset of one parameter matrix of the expert store; state and
+ * gradients are compact, as for spes_masked_adamw.  Per matrix, with g = grad_scale * grad,
+ *      m <- beta m + g       u = nesterov ? g + beta m : m       o = spes_orthogonalize(u)
+ *      w <- w (1 - lr weight_decay) - lr update_scale o
+ * in fp32 (o as above for the storage type), then the expert's row of the full store is overwritten with w rounded to the storage
+ * type.  Frozen experts are not touched.  update_scale is the caller's, commonly 0.2 sqrt(max(rows, cols)).
+ *
+ *  n_experts >= 1; rows, cols: sides of the matrix per expert, each at most 16384
+ *  param        DEVICE [n_experts, rows, cols] storage dtype, in/out
+ *  trainable_mask HOST [n_experts] bytes
+ *  master       DEVICE [n_trainable, rows, cols] f32 in/out; NULL is allowed for dtype f32 only, then param itself is the weight
+ *  m            DEVICE [n_trainable, rows, cols] f32 in/out      grad  DEVICE [n_trainable, rows, cols] f32
+ *  0 <= beta < 1; steps, coef as above
+ *  scratch      DEVICE, spes_orthogonalize_scratch_bytes(n_trainable, rows, cols, dtype) bytes
+ */
+SPES_API int spes_masked_muon(int32_t n_experts, int32_t rows, int32_t cols, int32_t dtype, void* param,
+                              const uint8_t* trainable_mask, float* master, float* m,
+                              const float* grad, float lr, float beta, int32_t nesterov,
+                              float weight_decay, float update_scale, int32_t steps,
+                              const float* coef, float grad_scale, void* scratch, void* stream);
+
 SPES_API const char* spes_strerror(int code);
 
 #ifdef __cplusplus

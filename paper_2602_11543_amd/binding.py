@@ -87,6 +87,12 @@ def _load() -> ctypes.CDLL:
     lib.spes_router_fwd.argtypes = [i32, i32, i32, opts] + [vp] * 6
     lib.spes_router_bwd.restype = i32
     lib.spes_router_bwd.argtypes = [i32, i32, i32, opts] + [vp] * 5
+    lib.spes_orthogonalize_scratch_bytes.restype = sz
+    lib.spes_orthogonalize_scratch_bytes.argtypes = [i32] * 4
+    lib.spes_orthogonalize.restype = i32
+    lib.spes_orthogonalize.argtypes = [i32] * 4 + [vp, vp, i32, vp, vp, vp]
+    lib.spes_masked_muon.restype = i32
+    lib.spes_masked_muon.argtypes = [i32] * 4 + [vp] * 5 + [ctypes.c_float, ctypes.c_float, i32, ctypes.c_float, ctypes.c_float, i32, vp, ctypes.c_float, vp, vp]
     lib.spes_ref_mfma_rate.restype = i32
     lib.spes_ref_mfma_rate.argtypes = [vp, i32, i32, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.spes_profile_enable.restype = i32
@@ -311,6 +317,38 @@ def spes_router_bwd(T, n_experts, top_k, opts, logits, idx, dgate, dlogits, stre
     f, i = torch.float32, torch.int32
     _check(_lib.spes_router_bwd(T, n_experts, top_k, opts, _buf(logits, f, T, n_experts), _buf(idx, i, T, top_k), _buf(dgate, f, T, top_k),
                                 _buf(dlogits, f, T, n_experts), _stream(stream)), "spes_router_bwd")
+
+
+def spes_orthogonalize_scratch_bytes(n: int, rows: int, cols: int, dtype: int) -> int:
+    return int(_lib.spes_orthogonalize_scratch_bytes(n, rows, cols, dtype))
+
+
+def _coef(coef):
+    if coef is None:
+        return None
+    if len(coef) != 3:
+        raise SpesError("coef has three values: a, b, c")
+    return (ctypes.c_float * 3)(*coef)
+
+
+def spes_orthogonalize(n, rows, cols, dtype, src, out, steps=5, coef=None, scratch=None, stream=None) -> None:
+    t = torch_dtype(dtype)
+    _check(_lib.spes_orthogonalize(n, rows, cols, dtype, _buf(src, t, n, rows, cols), _buf(out, t, n, rows, cols), steps, _coef(coef),
+                                   _scratch(scratch, _lib.spes_orthogonalize_scratch_bytes, n, rows, cols, dtype), _stream(stream)),
+           "spes_orthogonalize")
+
+
+def spes_masked_muon(n_experts, rows, cols, dtype, param, trainable_mask, master, m, grad, lr, beta, nesterov, weight_decay, update_scale,
+                     steps=5, coef=None, grad_scale=1.0, scratch=None, stream=None) -> None:
+    mask = np.ascontiguousarray(trainable_mask, dtype=np.uint8)
+    if mask.shape != (n_experts,):
+        raise SpesError("trainable_mask must have one byte per expert")
+    f, n = torch.float32, int(np.count_nonzero(mask))
+    _check(_lib.spes_masked_muon(n_experts, rows, cols, dtype, _buf(param, torch_dtype(dtype), n_experts, rows, cols),
+                                 mask.ctypes.data, _buf(master, f, n, rows, cols), _buf(m, f, n, rows, cols), _buf(grad, f, n, rows, cols),
+                                 lr, beta, int(nesterov), weight_decay, update_scale, steps, _coef(coef), grad_scale,
+                                 _scratch(scratch, _lib.spes_orthogonalize_scratch_bytes, n, rows, cols, dtype) if n else None,
+                                 _stream(stream)), "spes_masked_muon")
 
 
 def spes_profile_enable(on: bool) -> None:

@@ -1,5 +1,6 @@
 // C ABI of the operators around the expert layer: argument checks ahead of any launch.
 #include <cmath>
+#include <new>
 
 #include "kernels.h"
 
@@ -22,6 +23,20 @@ int router_supported(int T, int M, int k, const spes_router_opts* o) {
   if (M > kMaxRouterExperts || k > kMaxRouterChoice || o->groups > 16) return SPES_ESHAPE;
   return SPES_OK;
 }
+
+constexpr int kMaxSide = 16384;      // of a matrix: 32-bit byte offsets into it
+constexpr float kCoef[3] = {3.4445f, -4.7750f, 2.0315f};
+
+int matrices_supported(long n, int rows, int cols, int dtype) {
+  if (n < 1 || rows < 1 || cols < 1 || !dtype_ok(dtype)) return SPES_EINVAL;
+  if (rows > kMaxSide || cols > kMaxSide) return SPES_ESHAPE;
+  if (n > 65535) return SPES_ESHAPE;      // a grid dimension
+  // a launch has one block for 128 x 128 elements and more of a matrix
+  if (n * (((long)rows + 127) / 128) * (((long)cols + 127) / 128) > (1L << 28)) return SPES_ESHAPE;
+  return SPES_OK;
+}
+bool coef_ok(const float* c) { return c == nullptr || (std::isfinite(c[0]) && std::isfinite(c[1]) && std::isfinite(c[2])); }
+bool steps_ok(int steps) { return steps >= 1 && steps <= 64; }
 
 }  // namespace
 
@@ -80,6 +95,40 @@ SPES_API int spes_router_bwd(int32_t T, int32_t n_experts, int32_t top_k, const 
   if (!logits || !idx || !dgate || !dlogits) return SPES_EINVAL;
   if (!aligned16(logits) || !aligned16(idx) || !aligned16(dgate) || !aligned16(dlogits)) return SPES_EALIGN;
   return launch_router_bwd(T, n_experts, top_k, *opts, logits, idx, dgate, dlogits, static_cast<hipStream_t>(stream));
+}
+
+SPES_API size_t spes_orthogonalize_scratch_bytes(int32_t n, int32_t rows, int32_t cols, int32_t dtype) {
+  return matrices_supported(n, rows, cols, dtype) == SPES_OK ? orthogonalize_scratch_bytes(n, rows, cols, dtype) : 0;
+}
+
+SPES_API int spes_orthogonalize(int32_t n, int32_t rows, int32_t cols, int32_t dtype, const void* src, void* out, int32_t steps, const float* coef,
+                                void* scratch, void* stream) {
+  const int rc = matrices_supported(n, rows, cols, dtype);
+  if (rc != SPES_OK) return rc;
+  if (!src || !out || !scratch || !steps_ok(steps) || !coef_ok(coef)) return SPES_EINVAL;
+  if (!aligned16(src) || !aligned16(out) || !aligned16(scratch)) return SPES_EALIGN;
+  return launch_orthogonalize(dtype, n, rows, cols, src, out, steps, coef ? coef : kCoef, scratch, static_cast<hipStream_t>(stream));
+}
+
+SPES_API int spes_masked_muon(int32_t n_experts, int32_t rows, int32_t cols, int32_t dtype, void* param, const uint8_t* trainable_mask, float* master,
+                              float* m, const float* grad, float lr, float beta, int32_t nesterov, float weight_decay, float update_scale, int32_t steps,
+                              const float* coef, float grad_scale, void* scratch, void* stream) {
+  if (n_experts < 1 || !param || !trainable_mask || !(beta >= 0.f && beta < 1.f) || !steps_ok(steps) || !coef_ok(coef)) return SPES_EINVAL;
+  int n = 0;
+  for (int e = 0; e < n_experts; ++e) n += trainable_mask[e] != 0;
+  const int rc = matrices_supported(n > 0 ? n : 1, rows, cols, dtype);
+  if (rc != SPES_OK) return rc;
+  if (n == 0) return SPES_OK;
+  if (!m || !grad || !scratch || (!master && dtype != SPES_F32)) return SPES_EINVAL;
+  if (!aligned16(param) || !aligned16(m) || !aligned16(grad) || !aligned16(master) || !aligned16(scratch)) return SPES_EALIGN;
+  long* const param_at = new (std::nothrow) long[n];
+  if (param_at == nullptr) return SPES_EINVAL;
+  for (int e = 0, i = 0; e < n_experts; ++e)
+    if (trainable_mask[e]) param_at[i++] = (long)e * rows * cols;
+  const int status = launch_masked_muon(dtype, n, rows, cols, param, param_at, master, m, grad, lr, beta, nesterov, weight_decay, update_scale, steps,
+                                        coef ? coef : kCoef, grad_scale, scratch, static_cast<hipStream_t>(stream));
+  delete[] param_at;
+  return status;
 }
 
 }  // extern "C"

@@ -66,6 +66,14 @@ int launch_router_fwd(int T, int M, int k, const spes_router_opts& o, const floa
 int launch_router_bwd(int T, int M, int k, const spes_router_opts& o, const float* logits, const int* idx, const float* dgate, float* dlogits,
                       hipStream_t s);
 
+// orthogonalize.hip
+size_t orthogonalize_scratch_bytes(int n, int rows, int cols, int dtype);
+int launch_orthogonalize(int dtype, int n, int rows, int cols, const void* src, void* out, int steps, const float* coef, void* scratch, hipStream_t s);
+// n matrices; param_at: element offset of each in the full store
+int launch_masked_muon(int dtype, int n, int rows, int cols, void* param, const long* param_at, float* master, float* m, const float* grad, float lr,
+                       float beta, int nesterov, float weight_decay, float update_scale, int steps, const float* coef, float grad_scale, void* scratch,
+                       hipStream_t s);
+
 // reference.hip: register-resident MFMA loop (blocks x 4 wavefronts x iters x 64 MFMAs of 16x16x32); *flop = operations launched
 int launch_mfma_rate(const void* data, int blocks, int iters, float* sink, double* flop, hipStream_t s);
 

@@ -74,3 +74,37 @@ def test_router():
     for bad in (dict(logits=P[0] + 4), dict(idx=P[1] + 4), dict(dgate=P[2] + 8), dict(dlogits=P[3] + 4)):
         assert bwd(**bad) == EALIGN, bad
     assert bwd(T=0, logits=None, idx=None, dgate=None, dlogits=None) == 0
+
+
+def test_orthogonalize_and_muon():
+    fn, mu = LIB.spes_orthogonalize, LIB.spes_masked_muon
+    fn.restype, fn.argtypes = i32, [i32] * 4 + [vp, vp, i32, vp, vp, vp]
+    mu.restype, mu.argtypes = i32, [i32] * 4 + [vp] * 5 + [f32, f32, i32, f32, f32, i32, vp, f32, vp, vp]
+    c3 = lambda *v: (f32 * 3)(*v)  # noqa: E731
+
+    def orth(n=2, rows=64, cols=32, dtype=1, src=P[0], out=P[1], steps=5, coef=None, scratch=P[2]):
+        return fn(n, rows, cols, dtype, src, out, steps, coef, scratch, None)
+
+    for bad in (dict(n=0), dict(rows=0), dict(cols=-1), dict(dtype=2), dict(src=None), dict(out=None), dict(scratch=None), dict(steps=0), dict(steps=65),
+                dict(coef=c3(1, float("nan"), 0))):
+        assert orth(**bad) == EINVAL, bad
+    for bad in (dict(rows=16385), dict(cols=16385), dict(n=65536), dict(n=60000, rows=16384, cols=16384)):
+        assert orth(**bad) == ESHAPE, bad
+    for bad in (dict(src=P[0] + 8), dict(out=P[1] + 2), dict(scratch=P[2] + 4)):
+        assert orth(**bad) == EALIGN, bad
+
+    mask = (ctypes.c_uint8 * 3)(1, 0, 1)
+    none = (ctypes.c_uint8 * 3)(0, 0, 0)
+
+    def muon(E=3, rows=64, cols=32, dtype=1, param=P[0], mask=mask, master=P[1], m=P[2], grad=P[3], beta=0.95, steps=5, coef=None, scratch=P[4]):
+        return mu(E, rows, cols, dtype, param, mask, master, m, grad, 0.1, beta, 1, 0.1, 1.0, steps, coef, 1.0, scratch, None)
+
+    for bad in (dict(E=0), dict(rows=0), dict(dtype=9), dict(param=None), dict(mask=None), dict(master=None), dict(m=None), dict(grad=None), dict(beta=1.0),
+                dict(beta=-0.1), dict(steps=0), dict(scratch=None), dict(coef=c3(float("inf"), 0, 0))):
+        assert muon(**bad) == EINVAL, bad
+    assert muon(rows=20000) == ESHAPE
+    for bad in (dict(param=P[0] + 8), dict(master=P[1] + 4), dict(m=P[2] + 4), dict(grad=P[3] + 4), dict(scratch=P[4] + 4)):
+        assert muon(**bad) == EALIGN, bad
+    assert muon(mask=none, master=None, m=None, grad=None, scratch=None) == 0
+    assert S.spes_orthogonalize_scratch_bytes(0, 8, 8, 0) == 0 and S.spes_orthogonalize_scratch_bytes(1, 8, 20000, 0) == 0
+    assert S.spes_orthogonalize_scratch_bytes(2, 64, 32, 0) > S.spes_orthogonalize_scratch_bytes(2, 64, 32, 1) > 0
