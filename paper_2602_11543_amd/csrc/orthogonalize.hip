@@ -9,8 +9,8 @@
 // grows small singular values 3.4-fold a step, and what rounding adds to them grows alike.  Against 64 bits, on gradients with 16 strong
 // directions above a broad floor, 512 x 1024: bf16 operands leave 1.3e-2 of the result's norm, fp16 ones 1.6e-3; nearly all of that is the
 // rounding of X itself in the first two steps, in the term a X, so while it matters X is carried with its remainder (a second fp16
-// plane, 22 bits together): 1.0e-3.  In the later steps, where singular values are near 1 and P near (b + c) I, what is rounded is P - (b + c) I, and
-// the step is X <- (a + b + c) X + (P - (b + c) I) X: 0.8e-3.  fp32 storage takes every operand as such a pair and every product as three,
+// plane, 22 bits together), which is added at the step's end: 0.8e-3.  The term a X itself stands in P, X <- (P + a I) X + a remainder: where
+// singular values are near 1, P is near (b + c) I and P + a I is rounded to finer steps.  fp32 storage takes every operand as such a pair and every product as three,
 // lo hi + hi lo + hi hi: 3e-7.  Range: X stands scaled by 2^12, G and P by 2^11, which holds singular values below 5, G below 25
 // and P below 31; after the first scaling they are at most 1.21 with the default coefficients.
 #include <cmath>
@@ -18,6 +18,7 @@
 
 #include "kernels.h"
 #include "lds_load.h"
+#include "plan.h"
 #include "units.h"
 
 namespace spes {
@@ -29,10 +30,12 @@ typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 constexpr int kXcds = 8;
 constexpr int kXBits = 12, kGBits = 11;        // X, and G and P, as they are stored, are scaled by these powers of two
 constexpr int kPad = 64;                       // stored matrices have sides that are multiples of this, zeros beyond the matrix
+constexpr int kFewRows = 32;                   // up to so many, operands are pairs in bf16 storage too: rounding is of one sign in a single direction (a
+                                               // 1 x 16 matrix came out 4.4e-3 off), and such matrices wait for launches, not for products
 constexpr int kSumBlocks = 256;                // partial sums of squares of a matrix, at most
 constexpr int kSlots = 64;                     // matrices of an optimizer launch
 
-enum Epi { kGram, kPoly, kStep, kLast, kUpdate };
+enum Epi { kGram, kPoly, kStep, kLast, kUpdate };      // kLast, kUpdate: a step whose result is the caller's, or his weights' update
 
 struct NsArgs {
   const f16 *A, *B, *E;
@@ -41,7 +44,6 @@ struct NsArgs {
   long a_lo, b_lo, e_lo, c_lo;                 // elements from a matrix to its plane of remainders; 0: it has none here
   int lda, ldb, lde, ldc;
   int M, N, K, n;                              // of the products, padded; matrices
-  int passes;                                  // 1: hi hi; 3: lo hi, hi lo, hi hi
   float alpha, beta;                           // result = (alpha product + beta E) factor
   float diagonal;                              // kPoly: added to the diagonal
   const float* factor;                         // of each matrix, NULL: 1.  kGram: squared
@@ -54,26 +56,26 @@ struct NsArgs {
   long param_at[kSlots];                       // of each matrix, in elements
 };
 
-// x as the sum of two fp16 values; 8 at a time.  (x is pinned as it is in 32 bits: a product that is rounded straight to fp16 for one of
+// x as the sum of two fp16 values.  (x is pinned as it is in 32 bits: a product that is rounded straight to fp16 for one of
 // the two uses and by way of fp32 for the other comes out a step apart where the fp32 value lies half way between two, and the remainder is then
 // that of the other one.)
-__device__ __forceinline__ void split8(const float* x, uint4& hi, uint4& lo) {
-  f16x8 h, r;
+template <int N>
+__device__ __forceinline__ void split(const float* x, f16* hi, f16* lo) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < N; ++e) {
     float v = x[e];
     asm("" : "+v"(v));
-    h[e] = (f16)v;
-    r[e] = (f16)(v - (float)h[e]);
+    hi[e] = (f16)v;
+    lo[e] = (f16)(v - (float)hi[e]);
   }
-  hi = __builtin_bit_cast(uint4, h);
-  lo = __builtin_bit_cast(uint4, r);
 }
-__device__ __forceinline__ void add8(float* x, const uint4& v) {
-  const f16x8 h = __builtin_bit_cast(f16x8, v);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] += (float)h[e];
+__device__ __forceinline__ void split8(const float* x, uint4& hi, uint4& lo) {
+  f16 h[8], r[8];
+  split<8>(x, h, r);
+  hi = __builtin_bit_cast(uint4, *reinterpret_cast<f16x8*>(h));
+  lo = __builtin_bit_cast(uint4, *reinterpret_cast<f16x8*>(r));
 }
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 
 template <typename T>
 __device__ __forceinline__ void put_result(const NsArgs& g, int i, long row, int col, const float* o) {
@@ -101,48 +103,76 @@ __device__ __forceinline__ void update(const NsArgs& g, int i, long row, int col
   }
 }
 
-// One BM x BN tile of one product, of a symmetric one (kGram, kPoly) with its mirror image.  Four wavefronts, each a quarter of the tile.
-// Operands come straight into LDS as in gemm_mfma.hip: A, and B with B_KC, as [row][k], else B as [k][column].
-template <Epi EPI, bool B_KC, typename T, int BM, int BN, int NS>
-__global__ __launch_bounds__(256, 2) void ns_gemm_kernel(const NsArgs g) {
-  constexpr int BK = 64, TM = BM / 32, TN = BN / 32, NA = BM / 32, NB = BN / 32, NP = NA + NB;
-  constexpr int A_VEC = BM * 8, B_VEC = BN * 8, STAGE = A_VEC + B_VEC;
-  constexpr int PITCH = BN / 2 + 4, SLAB = 32 * PITCH;
-  constexpr bool SYM = EPI == kGram || EPI == kPoly;
+template <int BM_, int BN_, int NSA_, int NSB_, int MINB_>
+struct Cfg {
+  static constexpr int BM = BM_, BN = BN_, MINB = MINB_;
+  static constexpr int NSA = NSA_, NSB = NSB_;              // LDS slots of each operand, one K-tile each
+  static constexpr int BK = 64, TM = BM / 32, TN = BN / 32; // 16 x 16 MFMA tiles per wavefront along m, n
+  static constexpr int NA = BM / 32, NB = BN / 32;          // 1 KB loads per wavefront and K-tile
+  static constexpr int A_VEC = BM * 8, B_VEC = BN * 8;      // 16-byte units of a slot
+  // epilogue slabs, 32 rows of a wavefront's quarter: floats, or bytes of fp16 (rows 4 or 36 banks apart: the sixteen rows of a write miss each other)
+  static constexpr int PITCH = BN / 2 + 4, SLAB = 32 * PITCH, PITCH16 = BN + 16, SLAB16 = 32 * PITCH16;
+  static constexpr bool PLANES = BM == 64 && MINB == 1;     // both planes of a pair side by side in a slot, see the main loop
+  static constexpr int UNITS = (NSA * A_VEC + NSB * B_VEC) * (PLANES ? 2 : 1);
+  static_assert(4 * SLAB * 4 <= UNITS * 16 && 4 * 4 * SLAB16 <= UNITS * 16, "a float slab, or four of fp16, for every wavefront");
   static_assert(BM == BN, "mirror images of square tiles");
-  __shared__ uint4 smem[NS * STAGE > SLAB ? NS * STAGE : SLAB];
-  static_assert(NS * STAGE * 16 >= 4 * SLAB * 4, "a slab for every wavefront");
+};
+// one block per CU: all 160 KB of LDS, 256 accumulators per lane
+typedef Cfg<256, 256, 3, 2, 1> Tile;
+// two blocks per CU
+typedef Cfg<128, 128, 3, 2, 2> TileSmall;
+// few tiles; on pairs
+typedef Cfg<64, 64, 5, 5, 2> TileTiny;
+typedef Cfg<64, 64, 4, 4, 1> TileTinyPairs;
+
+// One BM x BN tile of one product, of a symmetric one (kGram, kPoly) with its mirror image.  Four wavefronts, each a quarter of the tile as TM x TN
+// MFMA tiles of 16 x 16.  Operands come straight into LDS, K-tiles of 64, three or two of them at a time: A, and B with B_KC, as
+// [row][k], else B as [k][column], read through the transposing read; both permuted within a row against bank conflicts.  The main loop is
+// that of gemm_mfma.hip without its masks and index tables: stored matrices are padded, so every K-tile is whole.  Fragments are read a
+// k-step ahead of their MFMAs, and loads, reads and the scalars of the next K-tiles are dealt out over the gaps between MFMAs.
+// SPLIT: operands are pairs.  IN, OUT: planes of what is read beside the product and of the result
+template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C>
+__global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
+  constexpr int BM = C::BM, BN = C::BN, BK = C::BK, TM = C::TM, TN = C::TN, NSA = C::NSA, NSB = C::NSB, NA = C::NA, NB = C::NB, NP = NA + NB;
+  constexpr int A_VEC = C::A_VEC, B_VEC = C::B_VEC, PITCH = C::PITCH;
+  constexpr bool SYM = EPI == kGram || EPI == kPoly;
+  __shared__ uint4 smem[C::UNITS];
   const int tid = threadIdx.x, lane = tid & 63, wave = (int)uniform(tid >> 6);
   const int l16 = lane & 15, lq = lane >> 4, wm = wave >> 1, wn = wave & 1;
 
+  // ---- which tile: every XCD (workgroups go round the eight) gets one contiguous range ----
   const unsigned mt = (unsigned)cdiv(g.M, BM), nt = (unsigned)cdiv(g.N, BN), per = SYM ? mt * (mt + 1) / 2 : mt * nt;
   const unsigned total = per * (unsigned)g.n, per_xcd = (total + kXcds - 1) / kXcds;
-  const unsigned slot = blockIdx.x / kXcds, t = (blockIdx.x % kXcds) * per_xcd + slot;
-  if (slot >= per_xcd || t >= total) return;
-  const int mat = (int)(t / per);
-  unsigned in = t - (unsigned)mat * per, mi, ni;
+  const unsigned slot = blockIdx.x / kXcds, t_ = (blockIdx.x % kXcds) * per_xcd + slot;
+  if (slot >= per_xcd || t_ >= total) return;
+  const int mat = (int)uniform(t_ / per);
+  const unsigned in = t_ - (unsigned)mat * per;
+  unsigned mi, ni;
   if (SYM) {
     mi = (unsigned)((sqrtf(8.f * (float)in + 1.f) - 1.f) * 0.5f);
     if (mi * (mi + 1) / 2 > in) --mi;
     if ((mi + 1) * (mi + 2) / 2 <= in) ++mi;
     ni = in - mi * (mi + 1) / 2;
   } else {
-    mi = in / nt;
-    ni = in - mi * nt;
+    // row tiles four at a time, the column tiles inside: what an XCD works on at once shares four row panels
+    const unsigned group = in / (4 * nt), within = in - group * 4 * nt, left = mt - group * 4, rows = left < 4 ? left : 4;
+    ni = within / rows;
+    mi = group * 4 + (within - ni * rows);
   }
-  const int m0 = (int)mi * BM, n0 = (int)ni * BN;
+  const int m0 = (int)uniform(mi * BM), n0 = (int)uniform(ni * BN);
 
-  // ---- operands ----
-  const int nk = g.K / BK, nsteps = nk * g.passes;
+  // ---- operands: buffer resources whose base moves with the K-tile and that end with the operand, behind which loads deliver zeros; a lane's
+  // byte offsets are fixed ----
+  const int nk = (int)uniform((unsigned)g.K / BK), nsteps = SPLIT ? 3 * nk : nk;
   auto base_of = [](const f16* p, long elems) -> unsigned long {
     const unsigned long v = reinterpret_cast<unsigned long>(p + elems);
     return (unsigned long)uniform((unsigned)(v >> 32)) << 32 | uniform((unsigned)v);
   };
   const unsigned long a_base = base_of(g.A, mat * g.a_ms), b_base = base_of(g.B, mat * g.b_ms);
   const unsigned a_bytes = uniform((unsigned)g.M * (unsigned)g.lda * 2u), b_bytes = uniform((unsigned)(B_KC ? g.N : g.K) * (unsigned)g.ldb * 2u);
-  const unsigned a_step = 128u, b_step = uniform(B_KC ? 128u : (unsigned)g.ldb * 128u);       // bytes per K-tile
+  const unsigned a_step = BK * 2u, b_step = uniform(B_KC ? BK * 2u : (unsigned)g.ldb * (BK * 2u));       // bytes per K-tile
   const int kc_chunk = (lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7);
-  constexpr int BCH = BN / 8;
+  constexpr int BCH = BN / 8;       // 16-byte chunks per k-row
   unsigned aoff[NA], boff[NB];
 #pragma unroll
   for (int i = 0; i < NA; ++i) aoff[i] = ((unsigned)(m0 + wave * 8 + (lane >> 3) + 32 * i) * (unsigned)g.lda + (unsigned)kc_chunk * 8u) * 2u;
@@ -155,135 +185,362 @@ __global__ __launch_bounds__(256, 2) void ns_gemm_kernel(const NsArgs g) {
       boff[i] = ((unsigned)k * (unsigned)g.ldb + (unsigned)n0 + (unsigned)((lane % BCH) ^ (2 * (k & 3))) * 8u) * 2u;
     }
   }
-  const unsigned lds0 = (unsigned)(unsigned long)(__attribute__((address_space(3))) uint4*)smem + (unsigned)wave * 1024u;
-  auto load_tile = [&](int step, int s) {
-    const int pass = step / nk, k = step - pass * nk;
-    const bool alive = step < nsteps;
-    const unsigned long a = a_base + (g.passes == 3 && pass == 0 ? (unsigned long)g.a_lo * 2 : 0) + (unsigned)k * a_step;
-    const unsigned long b = b_base + (g.passes == 3 && pass == 1 ? (unsigned long)g.b_lo * 2 : 0) + (unsigned long)((unsigned)k * b_step);
-    const rsrc_t ra = make_rsrc(a, alive ? a_bytes - (unsigned)k * a_step : 0u), rb = make_rsrc(b, alive ? b_bytes - (unsigned)k * b_step : 0u);
-    const unsigned dst = lds0 + (unsigned)s * (STAGE * 16u);
-#pragma unroll
-    for (int i = 0; i < NA; ++i) {
-      const unsigned d = set_lds_dest(dst + (unsigned)i * 4096u);
-      one_instruction();
-      load_to_lds(ra, aoff[i], d);
-    }
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const unsigned d = set_lds_dest(dst + A_VEC * 16u + (unsigned)i * 4096u);
-      one_instruction();
-      load_to_lds(rb, boff[i], d);
-    }
-  };
 
   f32x4 acc[TN][TM];
 #pragma unroll
   for (int j = 0; j < TN; ++j)
 #pragma unroll
-    for (int i = 0; i < TM; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int kc_pos = lq ^ (l16 >> 1);
-  const uint4* const a_kc = smem + (wm * (BM / 2) + l16) * 8;
-  const uint4* const b_kc = smem + A_VEC + (wn * (BN / 2) + l16) * 8;
-  const bf16_t* const b_tr = reinterpret_cast<const bf16_t*>(smem + A_VEC) + (lq * 8 + (l16 >> 2)) * BN + (lane & 3) * 4 + wn * (BN / 2);
-  auto tr_pos = [&](int i) { return (i & ~3) * 16 + ((i & 3) ^ (l16 >> 2)) * 16; };
-  for (int s = 0; s < NS - 1; ++s) load_tile(s, s);
-  int cur = 0, fill = NS - 1;
-  for (int step = 0; step < nsteps; ++step) {
-    wait_and_meet<(NS - 2) * NP>();
-    load_tile(step + NS - 1, fill);
+    for (int i = 0; i < TM; ++i) {
+      acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // (zeros that the compiler takes for different values)
+      if (C::MINB == 1) asm("" : "+a"(acc[j][i]));
+      else asm("" : "+v"(acc[j][i]));
+    }
+
+  if constexpr (C::PLANES) {
+    // On the smallest tile a wavefront has eight MFMAs in a K-tile, less than its meeting and its reads take.  So all four planes of a K-tile are
+    // loaded at once, which is 24 MFMAs of a wavefront for one meeting and four loads in place of six, in four stages of LDS.  Against the loop below,
+    // over the pairs one after the other: 4 matrices of 512 x 256, products of 10.2, 6.9 and 7.3 us 7.8, 6.2 and 6.5, the call 122 -> 105.
+    static_assert(SPLIT && NSA == NSB, "whole stages of pairs");
+    constexpr int STAGE = 2 * (A_VEC + B_VEC), STAGES = NSA;
+    const unsigned a_lo = uniform((unsigned)g.a_lo * 2u), b_lo = uniform((unsigned)g.b_lo * 2u);
+    const unsigned lds0 = (unsigned)(unsigned long)(__attribute__((address_space(3))) uint4*)smem + (unsigned)wave * 1024u;
+    auto load_stage = [&](int k, int s) {
+      const unsigned inside = k < nk ? ~0u : 0u;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      f16x8 fa[TM], fb[TN];
+      for (int two = 0; two < 2; ++two) {
+        const unsigned dst = lds0 + (unsigned)(s * STAGE + two * A_VEC) * 16u;
+        const rsrc_t ra = make_rsrc(a_base + (two ? a_lo : 0u) + (unsigned long)((unsigned)k * a_step), (a_bytes - (unsigned)k * a_step) & inside);
+        const rsrc_t rb = make_rsrc(b_base + (two ? b_lo : 0u) + (unsigned long)((unsigned)k * b_step), (b_bytes - (unsigned)k * b_step) & inside);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) fa[i] = __builtin_bit_cast(f16x8, a_kc[cur * STAGE + i * 128 + (kc_pos ^ (ks * 4))]);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        if (B_KC) {
-          fb[j] = __builtin_bit_cast(f16x8, b_kc[cur * STAGE + j * 128 + (kc_pos ^ (ks * 4))]);
-        } else {
-          const bf16_t* p = b_tr + cur * (STAGE * 8) + ks * 32 * BN + tr_pos(j);
-          const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 4 * BN);
-          fb[j] = __builtin_bit_cast(f16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+        for (int i = 0; i < NA; ++i) {
+          const unsigned d = set_lds_dest(dst + (unsigned)i * 4096u);
+          one_instruction();
+          load_to_lds(ra, aoff[i], d);
         }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const unsigned d = set_lds_dest(dst + 2 * A_VEC * 16u + (unsigned)i * 4096u);
+          one_instruction();
+          load_to_lds(rb, boff[i], d);
+        }
+      }
+    };
+    const int kc_pos = lq ^ (l16 >> 1);
+    const uint4* const a_kc = smem + (wm * (BM / 2) + l16) * 8;
+    const uint4* const b_kc = smem + 2 * A_VEC + (wn * (BN / 2) + l16) * 8;
+    const bf16_t* const b_tr = reinterpret_cast<const bf16_t*>(smem + 2 * A_VEC) + (lq * 8 + (l16 >> 2)) * BN + (lane & 3) * 4;
+    for (int s = 0; s < STAGES - 1; ++s) load_stage(s, s);
+    int cur = 0, fill = STAGES - 1;
+    for (int k = 0; k < nk; ++k) {
+      wait_and_meet<(STAGES - 2) * 2 * NP>();
+      load_stage(k + STAGES - 1, fill);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        f16x8 fa[2][TM], fb[2][TN];
+#pragma unroll
+        for (int two = 0; two < 2; ++two) {
+#pragma unroll
+          for (int i = 0; i < TM; ++i) fa[two][i] = __builtin_bit_cast(f16x8, a_kc[cur * STAGE + two * A_VEC + i * 128 + (kc_pos ^ (ks * 4))]);
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            if (B_KC) {
+              fb[two][j] = __builtin_bit_cast(f16x8, b_kc[cur * STAGE + two * B_VEC + j * 128 + (kc_pos ^ (ks * 4))]);
+            } else {
+              const bf16_t* p = b_tr + (cur * STAGE + two * B_VEC) * 8 + ks * 32 * BN + ((wn * (BN / 32) + j) ^ (l16 >> 2)) * 16;
+              const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 4 * BN);
+              fb[two][j] = __builtin_bit_cast(f16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+            }
+          }
+        }
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass)          // lo hi, hi lo, hi hi
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+              acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[pass == 1][j], fa[pass == 0][i], acc[j][i], 0, 0, 0);
+      }
+      cur = cur + 1 == STAGES ? 0 : cur + 1;
+      fill = fill + 1 == STAGES ? 0 : fill + 1;
+    }
+  } else {
+    // ---- the K-tiles being loaded; with SPLIT the pairs lo hi, hi lo, hi hi one after the other ----
+    const unsigned lds0 = (unsigned)(unsigned long)(__attribute__((address_space(3))) uint4*)smem + (unsigned)wave * 1024u;
+    struct Src { unsigned lo, hi, bytes, k, dst; };
+    Src as = {0, 0, 0, 0, 0}, bs = as;
+    struct At { int k, pass; };                         // K-tile within its pass, and the pass
+    auto after = [&](At x) {
+      if (!SPLIT) return At{x.k + 1, 0};
+      int k, end;          // (on the scalar unit, where the compiler would not keep it)
+      asm("s_cmp_eq_u32 %2, %3\n\ts_cselect_b32 %0, 0, %2\n\ts_cselect_b32 %1, 1, 0" : "=&s"(k), "=&s"(end) : "s"(x.k + 1), "s"(nk) : "scc");
+      return At{k, x.pass + end};
+    };
+    // in steps, so that the main loop can deal them out: 0 the k, 1 the base, 2 the size, 3 where to
+    auto next_src = [&](Src& x, int step, At at, unsigned per_tile, unsigned long base, unsigned lo_plane, int lo_pass, unsigned bytes, unsigned dst) {
+      if (step == 0) {
+        x.k = (unsigned)at.k;
+        pin(x.k);
+      } else if (step == 1) {
+        const unsigned plane = SPLIT ? lo_plane & (unsigned)(((at.pass ^ lo_pass) - 1) >> 31) : 0u;
+        const unsigned long v = base + (unsigned long)plane + (unsigned long)(x.k * per_tile);
+        x.lo = (unsigned)v; x.hi = (unsigned)(v >> 32);
+        pin(x.lo); pin(x.hi);
+      } else if (step == 2) {
+        x.bytes = (bytes - x.k * per_tile) & (unsigned)((SPLIT ? at.pass - 3 : at.k - nk) >> 31);
+        pin(x.bytes);
+      } else {
+        x.dst = dst;
+        pin(x.dst);
+      }
+    };
+    const unsigned a_lo = uniform((unsigned)g.a_lo * 2u), b_lo = uniform((unsigned)g.b_lo * 2u);
+    auto next_a = [&](int step, At at, int s) { next_src(as, step, at, a_step, a_base, a_lo, 0, a_bytes, lds0 + (unsigned)s * (A_VEC * 16u)); };
+    auto next_b = [&](int step, At at, int s) {
+      next_src(bs, step, at, b_step, b_base, b_lo, 1, b_bytes, lds0 + NSA * A_VEC * 16u + (unsigned)s * (B_VEC * 16u));
+    };
+    unsigned lds_dest = 0;
+    auto aim = [&](int p) { lds_dest = set_lds_dest((p < NB ? bs.dst + (unsigned)p * 4096u : as.dst + (unsigned)(p - NB) * 4096u)); };
+    auto load = [&](int p) {
+      if (p < NB) load_to_lds(rsrc_t{bs.lo, bs.hi, bs.bytes, 0x00020000u}, boff[p], lds_dest);
+      else load_to_lds(rsrc_t{as.lo, as.hi, as.bytes, 0x00020000u}, aoff[p - NB], lds_dest);
+    };
+
+    f16x8 fa[2][TM], fb[2][TN];
+    const int kc_pos = lq ^ (l16 >> 1);
+    const uint4* const a_kc = smem + (wm * (BM / 2) + l16) * 8;
+    const uint4* const b_kc = smem + NSA * A_VEC + (wn * (BN / 2) + l16) * 8;
+    const bf16_t* const b_tr = reinterpret_cast<const bf16_t*>(smem + NSA * A_VEC) + (lq * 8 + (l16 >> 2)) * BN + (lane & 3) * 4;
+    // (sixteen columns u of a k-row stand at position u ^ (k & 3) of their four)
+    auto tr_pos = [&](int j) { return ((wn * (BN / 32) + j) ^ (l16 >> 2)) * 16; };
+    auto read_frag_b = [&](int s, int ks, int set, int j) {
+      if (B_KC) {
+        fb[set][j] = __builtin_bit_cast(f16x8, b_kc[s * B_VEC + j * 128 + (kc_pos ^ (ks * 4))]);
+      } else {
+        const bf16_t* p = b_tr + s * (B_VEC * 8) + ks * 32 * BN + tr_pos(j);
+        const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 4 * BN);
+        fb[set][j] = __builtin_bit_cast(f16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+      }
+    };
+    // fragment w of a k-step in the order the MFMAs first need them: B0, A0 .. A(TM-1), B1 .. B(TN-1)
+    auto read_frag = [&](int sa, int sb, int ks, int set, int w) {
+      if (w == 0) read_frag_b(sb, ks, set, 0);
+      else if (w <= TM) fa[set][w - 1] = __builtin_bit_cast(f16x8, a_kc[sa * A_VEC + (w - 1) * 128 + (kc_pos ^ (ks * 4))]);
+      else read_frag_b(sb, ks, set, w - TM);
+    };
+
+    // ---- schedule, in gaps between the 2 MF MFMAs of a K-tile (gemm_mfma.hip) ----
+    constexpr int MF = TM * TN, NF = TM + TN;
+    constexpr bool WIDE = MF >= 32;                   // room for a second meeting point
+    constexpr int F0 = MF >= 64 ? 2 : 1;              // gaps per fragment
+    constexpr int QF = NF * F0 + 8 < MF ? NF * F0 + 8 : MF;          // K-tile t is in registers: its slots may be overwritten
+    constexpr int QL = WIDE ? 2 * MF - NF * F0 - (MF >= 64 ? 12 : 6) : QF;    // K-tile t+1 is in LDS: its first fragments may be read
+    constexpr int DG_ALL = 2 * MF / NP, DG_B = (2 * MF - QF) / NB, DG = DG_ALL < DG_B ? DG_ALL : DG_B;      // gaps per load
+    constexpr int R0 = QL < MF ? MF : QL;
+    constexpr int F1 = (2 * MF - R0) / NF < 4 ? (2 * MF - R0) / NF : 4;
+    constexpr int SS = MF >= 32 ? 2 : 1;              // gaps per step of the scalars
+    static_assert(DG >= 1 && F1 >= 1 && QF + NB * DG <= 2 * MF && R0 + NF * F1 <= 2 * MF && QF >= 4 * SS && NB * DG >= 4 * SS, "more fragments or loads than MFMA gaps");
+    constexpr int LATE = QF + NP * DG > 2 * MF ? (QF + NP * DG - 2 * MF + DG - 1) / DG : 0;      // loads of an iteration that the next one issues
+    constexpr int LOADED = QL > QF ? ((QL - QF) / DG < NP ? (QL - QF) / DG : NP) : 0;
+    constexpr int AFTER_A = (NSA - 2) * NP, AFTER_B = NA + (NSB - 2) * NP, AHEAD = AFTER_A < AFTER_B ? AFTER_A : AFTER_B;
+    static_assert(AHEAD + NP < 64, "the counter of outstanding loads");
+    constexpr int FAR = NSA > NSB ? NSA : NSB;
+    At at_a = {0, 0}, at_b = {0, 0};                    // to be loaded next
+#pragma unroll
+    for (int u = -FAR; u < 0; ++u) {
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        if (u + NSB >= 0) next_b(st, at_b, u + NSB);
+        if (u + NSA >= 0) next_a(st, at_a, u + NSA);
+      }
+      if (u + NSB >= 0) at_b = after(at_b);
+      if (u + NSA >= 0) at_a = after(at_a);
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        if ((p < NB ? u + NSB : u + NSA) < 0 || (u == -1 && p >= NP - LATE)) continue;
+        aim(p); one_instruction(); load(p);
+      }
+    }
+    wait_and_meet<AHEAD + NP - LATE>();
+#pragma unroll
+    for (int w = 0; w < NF; ++w) read_frag(0, 0, 0, 0, w);
+    int t = 0, sa = 0, sb = 0;
+    do {
+      const int sa1 = sa + 1 == NSA ? 0 : sa + 1, sb1 = sb + 1 == NSB ? 0 : sb + 1;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int q = 0; q < 2 * MF; ++q) {
+        const int ks = q / MF, j = (q % MF) / TM, i = q % TM;
+        if (q == QF) {
+          wait_and_meet<(WIDE ? 63 : AHEAD)>();
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (WIDE && q == QL) {
+          wait_and_meet<AHEAD + LOADED>();
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[ks][j], fa[ks][i], acc[j][i], 0, 0, 0);
+        // (a use in this gap: the product has no side effects, and the compiler gathers those of many gaps in one place else.  No instruction)
+        if (C::MINB == 1) asm volatile("" :: "a"(acc[j][i]));
+        else asm volatile("" :: "v"(acc[j][i]));
+        if (q < MF && q % F0 == 0 && q / F0 < NF) read_frag(sa, sb, 1, 1, q / F0);
+        if (q >= R0 && (q - R0) % F1 == 0 && (q - R0) / F1 < NF) read_frag(sa1, sb1, 0, 0, (q - R0) / F1);
+        if (q >= QF - 4 * SS && q < QF && (QF - 1 - q) % SS == 0) next_b((q - (QF - 4 * SS)) / SS, at_b, sb);
+        if (q >= QF && q < QF + 4 * SS && (q - QF) % SS == 0) next_a((q - QF) / SS, at_a, sa);
+        {
+          const int at = q >= QF ? q - QF : q - QF + 2 * MF, p = at / DG;
+          if (p < NP && (q >= QF || p >= NP - LATE)) {
+            // (a gap ahead of the load, but in the same iteration)
+            const bool alone = DG == 1 || (q == 0 && at % DG == DG - 1);
+            if (alone || (at % DG == DG - 2 && q < 2 * MF - 1)) aim(p);
+            if (alone) one_instruction();
+            if (at % DG == DG - 1) load(p);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sa = sa1; sb = sb1;
+      at_a = after(at_a); at_b = after(at_b);
+      ++t;
+    } while (t < nsteps);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no load may still write the LDS that the slabs use
+
+  // ---- epilogue: 32 rows of the wavefront's quarter at a time, turned through LDS so that lanes lie along the columns ----
+  const float f1 = g.factor ? g.factor[mat] : 1.f, f = EPI == kGram ? f1 * f1 : f1;
+  constexpr int CPR = BN / 16, RPI = 64 / CPR, NST = 32 / RPI;         // lanes per row (eight columns each), rows at a time
+  const int e_row = m0 + wm * (BM / 2) + lane / CPR, e_col = n0 + wn * (BN / 2) + lane % CPR * 8;
+  if constexpr (EPI == kLast || EPI == kUpdate) {
+    const float alpha = g.alpha * f;
+    float* const slab = reinterpret_cast<float*>(smem) + wave * C::SLAB;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < BM / 64; ++i) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int ii = 0; ii < 2; ++ii) {
+          f32x4 v = acc[j][2 * i + ii];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] *= alpha;
+          *reinterpret_cast<f32x4*>(slab + (ii * 16 + l16) * PITCH + j * 16 + lq * 4) = v;
+        }
+      wave_lds_order();
+      if (!g.tall) {
+#pragma unroll
+        for (int st = 0; st < NST; ++st) {
+          const int r = st * RPI + lane / CPR, c = lane % CPR * 8;
+          float v[8];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const f32x4 q = *reinterpret_cast<const f32x4*>(slab + r * PITCH + c + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * h + e] = q[e];
+          }
+          if (EPI == kLast) put_result<T>(g, mat, e_row + i * 32 + st * RPI, e_col, v);
+          else update<T>(g, mat, e_row + i * 32 + st * RPI, e_col, v);
+        }
+      } else {
+#pragma unroll
+        for (int st = 0; st < BN / 32; ++st) {             // lanes: sixteen columns by four runs of eight rows
+          const int c = st * 16 + l16, r = lq * 8;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = slab[(r + e) * PITCH + c];
+          const int row = n0 + wn * (BN / 2) + c, col = m0 + wm * (BM / 2) + i * 32 + r;
+          if (EPI == kLast) put_result<T>(g, mat, row, col, v);
+          else update<T>(g, mat, row, col, v);
+        }
+      }
+      wave_lds_order();
+    }
+  } else {
+    // All of it on fp16 in LDS, a slab for each plane of what is read beside the product (kPoly: G, kStep: X's remainder) and of the result.  The
+    // arithmetic is done where the products are, four columns to a lane, and rounded there.  Loads and stores go through buffer resources that end
+    // with the matrix: a lane beyond it asks for nothing, and there are no branches.
+    constexpr int PITCH16 = C::PITCH16, SLAB16 = C::SLAB16;
+    char* const slab = reinterpret_cast<char*>(smem) + wave * (4 * SLAB16);
+    const unsigned plane_bytes = uniform((unsigned)g.M * (unsigned)g.ldc * 2u), row_bytes = (unsigned)g.ldc * 2u;
+    const __amdgpu_buffer_rsrc_t in_rs[2] = {tile_rsrc(base_of(g.E, mat * g.e_ms), plane_bytes), tile_rsrc(base_of(g.E, mat * g.e_ms + g.e_lo), plane_bytes)};
+    const __amdgpu_buffer_rsrc_t out_rs[2] = {tile_rsrc(base_of(g.C, mat * g.c_ms), plane_bytes), tile_rsrc(base_of(g.C, mat * g.c_ms + g.c_lo), plane_bytes)};
+    // (a matrix has less than 2^30 bytes, and what is added below stays far from 2^31)
+    const unsigned off0 = e_col < g.N ? (unsigned)e_row * row_bytes + (unsigned)e_col * 2u : 1u << 31;
+    auto off = [&](int i, int st) { return off0 + (unsigned)(i * 32 + st * RPI) * row_bytes; };
+    rsrc_t in0[IN > 0 ? NST : 1], in1[IN > 1 ? NST : 1];
+    auto load_in = [&](int i) {
+#pragma unroll
+      for (int st = 0; st < NST; ++st) {
+        if constexpr (IN > 0) in0[st] = __builtin_amdgcn_raw_buffer_load_b128(in_rs[0], (int)off(i, st), 0, 0);
+        if constexpr (IN > 1) in1[st] = __builtin_amdgcn_raw_buffer_load_b128(in_rs[1], (int)off(i, st), 0, 0);
+      }
+    };
+    load_in(0);
+    const float alpha = g.alpha * f, beta = g.beta * f;
+    const int d0 = m0 + wm * (BM / 2) - n0 - wn * (BN / 2) + l16 - lq * 4;        // row less column of a lane's element r: d0 + 16 (i - j) - r
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < BM / 64; ++i) {
+      if constexpr (IN > 0) {
+#pragma unroll
+        for (int st = 0; st < NST; ++st) {
+          char* const p = slab + (st * RPI + lane / CPR) * PITCH16 + lane % CPR * 16;
+          *reinterpret_cast<rsrc_t*>(p) = in0[st];
+          if constexpr (IN > 1) *reinterpret_cast<rsrc_t*>(p + SLAB16) = in1[st];
+        }
+        wave_lds_order();
+        if (i + 1 < BM / 64) load_in(i + 1);          // ahead of the stores, behind which they would wait
       }
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int i = 0; i < TM; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[j], fa[i], acc[j][i], 0, 0, 0);
-    }
-    cur = cur + 1 == NS ? 0 : cur + 1;
-    fill = fill + 1 == NS ? 0 : fill + 1;
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no load may still write the LDS that the slabs use
-  __syncthreads();
-
-  // ---- epilogue: 32 rows of the wavefront's quarter at a time, turned through LDS so that lanes lie along the columns ----
-  float* const slab = reinterpret_cast<float*>(smem) + wave * SLAB;
-  const float f1 = g.factor ? g.factor[mat] : 1.f, f = EPI == kGram ? f1 * f1 : f1;
-  const bool mirror = SYM ? mi != ni : (EPI == kLast || EPI == kUpdate) && g.tall;
-  const bool direct = SYM || EPI == kStep || !g.tall;
-  const f16* const E = g.E + mat * g.e_ms;
-  f16* const C = g.C + mat * g.c_ms;
-  auto put = [&](int row, int col, const float* v) {
-    if (EPI == kLast || EPI == kUpdate) {
-      if (EPI == kLast) put_result<T>(g, mat, row, col, v);
-      else update<T>(g, mat, row, col, v);
-    } else {
-      uint4 hi, lo;
-      split8(v, hi, lo);
-      *reinterpret_cast<uint4*>(C + (long)row * g.ldc + col) = hi;
-      if (g.c_lo != 0) *reinterpret_cast<uint4*>(C + g.c_lo + (long)row * g.ldc + col) = lo;
-    }
-  };
+        for (int ii = 0; ii < 2; ++ii) {
+          char* const p = slab + (ii * 16 + l16) * PITCH16 + (j * 16 + lq * 4) * 2;
+          float v[4];
 #pragma unroll
-  for (int i = 0; i < BM / 64; ++i) {
+          for (int r = 0; r < 4; ++r) v[r] = acc[j][2 * i + ii][r] * alpha;
+          if constexpr (IN > 0) {
+            const f16x4 x = *reinterpret_cast<const f16x4*>(p);
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+            for (int r = 0; r < 4; ++r) v[r] = fmaf((float)x[r], beta, v[r]);
+          }
+          if constexpr (IN > 1) {
+            const f16x4 x = *reinterpret_cast<const f16x4*>(p + SLAB16);
 #pragma unroll
-      for (int ii = 0; ii < 2; ++ii)
-        *reinterpret_cast<f32x4*>(slab + (ii * 16 + l16) * PITCH + j * 16 + lq * 4) = acc[j][2 * i + ii];
-    wave_lds_order();
-    constexpr int CPR = BN / 16, RPI = 64 / CPR;         // lanes per row, rows at a time
+            for (int r = 0; r < 4; ++r) v[r] = fmaf((float)x[r], beta, v[r]);
+          }
+          if (EPI == kPoly) {
+            const int d = d0 + (2 * i + ii - j) * 16;
 #pragma unroll
-    for (int st = 0; st < 32 / RPI; ++st) {
-      const int r = st * RPI + lane / CPR, c = lane % CPR * 8;
-      const int row = m0 + wm * (BM / 2) + i * 32 + r, col = n0 + wn * (BN / 2) + c;
-      float v[8];
+            for (int r = 0; r < 4; ++r) v[r] += d == r ? g.diagonal : 0.f;
+          }
+          f16 hi[4], lo[4];
+          if constexpr (OUT > 1) {
+            split<4>(v, hi, lo);
+            *reinterpret_cast<f16x4*>(p + (IN + 1) * SLAB16) = f16x4{lo[0], lo[1], lo[2], lo[3]};
+          } else {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 q = *reinterpret_cast<const f32x4*>(slab + r * PITCH + c + 4 * h);
+            for (int r = 0; r < 4; ++r) hi[r] = (f16)v[r];
+          }
+          *reinterpret_cast<f16x4*>(p + IN * SLAB16) = f16x4{hi[0], hi[1], hi[2], hi[3]};
+        }
+      wave_lds_order();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * h + e] = q[e];
-      }
-      const bool in_range = row < g.M && col < g.N;
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (EPI != kGram && in_range) {
-        add8(x, *reinterpret_cast<const uint4*>(E + (long)row * g.lde + col));
-        if (g.e_lo != 0) add8(x, *reinterpret_cast<const uint4*>(E + g.e_lo + (long)row * g.lde + col));
-      }
+      for (int two = 0; two < OUT; ++two) {
+        const char* const from = slab + (IN + two) * SLAB16;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fmaf(g.alpha, v[e], g.beta * x[e]) * f;
-      if (EPI == kPoly) {
+        for (int st = 0; st < NST; ++st)
+          store16(out_rs[two], off(i, st), *reinterpret_cast<const rsrc_t*>(from + (st * RPI + lane / CPR) * PITCH16 + lane % CPR * 16));
+        if (SYM && mi != ni) {
+          // the mirror image through the transposing read: sixteen columns by four runs of eight rows
+          const int col = m0 + wm * (BM / 2) + i * 32 + lq * 8;
+          const unsigned at = col < g.M ? (unsigned)(n0 + wn * (BN / 2) + l16) * row_bytes + (unsigned)col * 2u : 1u << 31;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += row == col + e ? g.diagonal : 0.f;
-      }
-      if (direct && in_range) put(row, col, v);
-      if (mirror) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(slab + r * PITCH + c + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-      }
-    }
-    wave_lds_order();
-    if (mirror) {
-#pragma unroll
-      for (int st = 0; st < BN / 32; ++st) {             // lanes: sixteen columns by four runs of eight rows
-        const int c = st * 16 + l16, r = lq * 8;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = slab[(r + e) * PITCH + c];
-        const int row = n0 + wn * (BN / 2) + c, col = m0 + wm * (BM / 2) + i * 32 + r;
-        if (row < g.N && col < g.M) put(row, col, v);
+          for (int st = 0; st < BN / 32; ++st) {
+            const bf16_t* const p = reinterpret_cast<const bf16_t*>(from + (lq * 8 + (l16 >> 2)) * PITCH16 + (st * 16 + (lane & 3) * 4) * 2);
+            const uint2 x = lds_read_tr(p), y = lds_read_tr(p + 4 * (PITCH16 / 2));
+            store16(out_rs[two], at + (unsigned)(st * 16) * row_bytes, rsrc_t{x.x, x.y, y.x, y.y});
+          }
+        }
       }
       wave_lds_order();
     }
@@ -421,7 +678,9 @@ __global__ __launch_bounds__(256) void ns_scale_kernel(const PrepArgs a) {
 }
 
 struct Buffers {
-  int lo, hi, lo_p, hi_p, planes;     // planes of G and P; X has two
+  int lo, hi, lo_p, hi_p;
+  bool pairs;                         // every operand with its remainder
+  int planes;                         // of G and P; X has two
   int sum_blocks;
   size_t part, factor, x[2], g, p, total;
 };
@@ -430,7 +689,8 @@ Buffers buffers(int n, int rows, int cols, int dtype) {
   Buffers b;
   b.lo = rows < cols ? rows : cols; b.hi = rows < cols ? cols : rows;
   b.lo_p = (int)round_up(b.lo, kPad); b.hi_p = (int)round_up(b.hi, kPad);
-  b.planes = dtype == SPES_F32 ? 2 : 1;
+  b.pairs = dtype == SPES_F32 || b.lo <= kFewRows;
+  b.planes = b.pairs ? 2 : 1;
   const long units = ((long)rows * cols + 7) / 8;
   b.sum_blocks = (int)(units / 1024 < 1 ? 1 : units / 1024 > kSumBlocks ? kSumBlocks : units / 1024);
   size_t off = 0;
@@ -444,28 +704,39 @@ Buffers buffers(int n, int rows, int cols, int dtype) {
   return b;
 }
 
-template <Epi EPI, bool B_KC, typename T>
-int launch_product(const NsArgs& g, hipStream_t s) {
-  constexpr int BM = 128;
-  const long mt = cdiv(g.M, BM), nt = cdiv(g.N, BM);
+template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C>
+int launch_tiles(const NsArgs& g, hipStream_t s) {
+  const long mt = cdiv(g.M, C::BM), nt = cdiv(g.N, C::BN);
   const long total = (EPI == kGram || EPI == kPoly ? mt * (mt + 1) / 2 : mt * nt) * g.n;
-  hipLaunchKernelGGL((ns_gemm_kernel<EPI, B_KC, T, BM, BM, 2>), dim3((unsigned)((total + kXcds - 1) / kXcds * kXcds)), dim3(256), 0, s, g);
+  hipLaunchKernelGGL((ns_gemm_kernel<EPI, B_KC, SPLIT, IN, OUT, T, C>), dim3((unsigned)((total + kXcds - 1) / kXcds * kXcds)), dim3(256), 0, s, g);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
+}
+template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T>
+int launch_product(const NsArgs& g, hipStream_t s) {
+  const int side = plan::square_tile(g.M, g.N, g.n, EPI == kGram || EPI == kPoly);
+  if (side == Tile::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, Tile>(g, s);
+  if (side == TileSmall::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, TileSmall>(g, s);
+  return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, std::conditional_t<SPLIT, TileTinyPairs, TileTiny>>(g, s);
+}
+// a last step; matrices of few rows in bf16 storage, the only ones on pairs there, have few tiles
+template <Epi EPI, typename T>
+int launch_end(bool pairs, const NsArgs& g, hipStream_t s) {
+  if constexpr (sizeof(T) == 4) return launch_product<EPI, false, true, 0, 0, T>(g, s);
+  else return pairs ? launch_tiles<EPI, false, true, 0, 0, T, TileTinyPairs>(g, s) : launch_product<EPI, false, false, 0, 0, T>(g, s);
 }
 
 // carried: steps that take X with its remainder, in bf16 storage
-constexpr int kCarried = 2;
+constexpr int kCarriedSteps = 2;
 
 template <typename T>
 int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool muon, PrepArgs a, NsArgs end, const long* param_at, char* scratch, hipStream_t s) {
-  const bool f32 = sizeof(T) == 4;
   const long xs = (long)b.lo_p * b.hi_p, gs = (long)b.lo_p * b.lo_p;
   f16* X[2] = {reinterpret_cast<f16*>(scratch + b.x[0]), reinterpret_cast<f16*>(scratch + b.x[1])};
   f16 *G = reinterpret_cast<f16*>(scratch + b.g), *P = reinterpret_cast<f16*>(scratch + b.p);
   a.part = reinterpret_cast<double*>(scratch + b.part); a.blocks = b.sum_blocks;
   a.factor = reinterpret_cast<float*>(scratch + b.factor);
   a.X = X[0]; a.ms = 2 * xs; a.lo = b.lo; a.hi = b.hi; a.ld = b.hi_p; a.lo_p = b.lo_p; a.tall = a.rows > a.cols;
-  const bool first_lo = f32 || !exact_start;
+  const bool first_lo = b.pairs || !exact_start;
   a.lo_plane = first_lo ? xs : 0;
   const dim3 sums((unsigned)b.sum_blocks, (unsigned)a.n), tiles((unsigned)(b.lo_p / 64 * (b.hi_p / 64)), (unsigned)a.n);
   if (muon) {
@@ -477,38 +748,42 @@ int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool m
   }
   if (hipGetLastError() != hipSuccess) return SPES_EHIP;
   NsArgs g = end;
-  g.n = a.n; g.passes = f32 ? 3 : 1;
+  g.n = a.n;
   for (int i = 0; i < steps; ++i) {
-    const bool last = i + 1 == steps, x_lo = f32 || (i == 0 ? first_lo : i < kCarried), next_lo = f32 || i + 1 < kCarried;
+    const bool last = i + 1 == steps, x_lo = b.pairs || (i == 0 ? first_lo : i < kCarriedSteps), next_lo = b.pairs || i + 1 < kCarriedSteps;
     f16 *x = X[i & 1], *y = X[(i + 1) & 1];
     const float* factor = i == 0 ? a.factor : nullptr;
     NsArgs q = g;
     q.A = q.B = x; q.a_ms = q.b_ms = 2 * xs; q.a_lo = q.b_lo = xs; q.lda = q.ldb = b.hi_p;
     q.M = q.N = b.lo_p; q.K = b.hi_p;
-    q.C = G; q.c_ms = b.planes * gs; q.c_lo = f32 ? gs : 0; q.ldc = b.lo_p;
+    q.C = G; q.c_ms = b.planes * gs; q.c_lo = b.pairs ? gs : 0; q.ldc = b.lo_p;
     q.alpha = ldexpf(1.f, kGBits - 2 * kXBits); q.beta = 0.f; q.factor = factor;
     q.E = G; q.e_ms = 0; q.e_lo = 0; q.lde = b.lo_p;
-    int rc = launch_product<kGram, true, T>(q, s);
+    int rc = b.pairs ? launch_product<kGram, true, true, 0, 2, float>(q, s) : launch_product<kGram, true, false, 0, 1, float>(q, s);
     if (rc != SPES_OK) return rc;
-    q.A = q.B = q.E = G; q.a_ms = q.b_ms = q.e_ms = b.planes * gs; q.a_lo = q.b_lo = gs; q.e_lo = f32 ? gs : 0; q.lda = q.ldb = b.lo_p;
+    q.A = q.B = q.E = G; q.a_ms = q.b_ms = q.e_ms = b.planes * gs; q.a_lo = q.b_lo = gs; q.e_lo = b.pairs ? gs : 0; q.lda = q.ldb = b.lo_p;
     q.K = b.lo_p; q.C = P;
     q.alpha = coef[2] * ldexpf(1.f, -kGBits); q.beta = coef[1]; q.factor = nullptr;
-    const float shift = f32 || i < kCarried ? 0.f : -(coef[1] + coef[2]);
-    q.diagonal = ldexpf(shift, kGBits);
-    rc = launch_product<kPoly, true, T>(q, s);
+    q.diagonal = ldexpf(coef[0], kGBits);
+    rc = b.pairs ? launch_product<kPoly, true, true, 2, 2, float>(q, s) : launch_product<kPoly, true, false, 1, 1, float>(q, s);
     if (rc != SPES_OK) return rc;
-    q.A = P; q.B = q.E = x; q.b_ms = q.e_ms = 2 * xs; q.b_lo = xs; q.e_lo = x_lo ? xs : 0; q.ldb = q.lde = b.hi_p;
+    q.A = P; q.B = x; q.b_ms = 2 * xs; q.b_lo = xs; q.ldb = b.hi_p;
+    q.E = x + xs; q.e_ms = 2 * xs; q.lde = b.hi_p;             // the remainders
     q.M = b.lo_p; q.N = b.hi_p; q.K = b.lo_p;
     q.C = y; q.c_ms = 2 * xs; q.c_lo = next_lo ? xs : 0; q.ldc = b.hi_p;
-    q.alpha = ldexpf(1.f, -kGBits); q.beta = coef[0] - shift; q.factor = factor;
+    q.alpha = ldexpf(1.f, -kGBits); q.beta = x_lo ? coef[0] : 0.f; q.factor = factor;
     if (!last) {
-      rc = launch_product<kStep, false, T>(q, s);
+      rc = b.pairs           ? launch_product<kStep, false, true, 0, 2, float>(q, s)
+           : x_lo && next_lo ? launch_product<kStep, false, false, 1, 2, float>(q, s)
+           : x_lo            ? launch_product<kStep, false, false, 1, 1, float>(q, s)
+           : next_lo         ? launch_product<kStep, false, false, 0, 2, float>(q, s)
+                             : launch_product<kStep, false, false, 0, 1, float>(q, s);
       if (rc != SPES_OK) return rc;
       continue;
     }
     // out of the scaled form
-    q.alpha = ldexpf(q.alpha, -kXBits); q.beta = ldexpf(q.beta, -kXBits);
-    if (!muon) return launch_product<kLast, false, T>(q, s);
+    q.alpha = ldexpf(q.alpha, -kXBits);
+    if (!muon) return launch_end<kLast, T>(b.pairs, q, s);
     for (int first = 0; first < a.n; first += kSlots) {
       NsArgs u = q;
       u.n = a.n - first < kSlots ? a.n - first : kSlots;
@@ -516,7 +791,7 @@ int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool m
       if (u.factor) u.factor += first;
       if (u.master) u.master += (long)first * a.rows * a.cols;
       for (int k = 0; k < u.n; ++k) u.param_at[k] = param_at[first + k];
-      rc = launch_product<kUpdate, false, T>(u, s);
+      rc = launch_end<kUpdate, T>(b.pairs, u, s);
       if (rc != SPES_OK) return rc;
     }
   }

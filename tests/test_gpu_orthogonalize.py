@@ -153,7 +153,7 @@ def muon_reference(w, m, g, lr, beta, nesterov, wd, scale, grad_scale):
     return w.double() * (1 - lr * wd) - lr * scale * exact(u).to(w.device), m
 
 
-def muon(device, dtype, experts, mask, rows, cols, nesterov, with_master=True, grad_scale=0.5, lr=0.02, wd=0.1, beta=0.9, seed=0):
+def muon(device, dtype, experts, mask, rows, cols, nesterov, with_master=True, grad_scale=0.5, lr=0.02, wd=0.1, beta=0.9, seed=0, check=None):
     n = int(mask.sum())
     at = [e for e in range(experts) if mask[e]]
     g = torch.Generator().manual_seed(seed)
@@ -168,7 +168,7 @@ def muon(device, dtype, experts, mask, rows, cols, nesterov, with_master=True, g
     torch.cuda.synchronize()
     step = 2.0 ** -24
     f = lambda v: float(np.float32(v))  # noqa: E731
-    for i in range(n):
+    for i in range(n) if check is None else check:
         w, mm = muon_reference(w0[i], m0[i], grad[i], f(lr), f(beta), nesterov, f(wd), f(scale), f(grad_scale))
         assert float(((m[i].double() - mm).abs() - 3 * step * (m0[i].abs() + grad[i].abs())).max()) <= 0
         got = master[i] if with_master else param[at[i]]
@@ -210,6 +210,27 @@ def test_larger_matrices(device, dtype, n, rows, cols):
     src = matrices(n, rows, cols, 3).to(dtype).cuda()
     out = run(src)
     near(out[0], exact(src[0]), out_allow(dtype))
+
+
+SIDES = [(40, 520, 780, 256), (40, 780, 520, 256), (3, 1000, 1300, 128), (2, 300, 200, 64)]      # tests/test_operators_plan.py holds the sides
+
+
+@TYPES
+@pytest.mark.parametrize("n,rows,cols,side", SIDES)
+def test_every_tile(device, n, rows, cols, side, dtype):
+    src = matrices(n, rows, cols, side).to(dtype).cuda()
+    out = run(src)
+    for i in {0, 1, n // 2, n - 1}:
+        near(out[i], exact(src[i]), out_allow(dtype))
+    assert torch.equal(out[n - 1:], run(src[n - 1:].clone())) or side != 64
+
+
+@TYPES
+@pytest.mark.parametrize("rows,cols", [(520, 780), (780, 520)])
+def test_optimizer_step_on_full_tiles(device, rows, cols, dtype):
+    mask = np.ones(44, dtype=np.uint8)
+    mask[[0, 7, 20, 43]] = 0
+    muon(device, dtype, 44, mask, rows, cols, True, check=(0, 1, 39))
 
 
 @TYPES

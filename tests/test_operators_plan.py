@@ -1,0 +1,48 @@
+"""The host's choice of tiles for the orthogonalisation's products (csrc/plan.h), checked without a GPU through a small C++ shim."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from test_gpu_orthogonalize import SIDES
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SHIM = """
+#include "plan.h"
+extern "C" int square_tile(int rows, int cols, int n, int symmetric) { return spes::plan::square_tile(rows, cols, n, symmetric != 0); }
+"""
+
+
+@pytest.fixture(scope="module")
+def square_tile(tmp_path_factory):
+    d = tmp_path_factory.mktemp("plan")
+    (d / "shim.cpp").write_text(SHIM)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2602_11543_amd", "csrc"),
+                    str(d / "shim.cpp"), "-o", str(d / "shim.so")], check=True)
+    return ctypes.CDLL(str(d / "shim.so")).square_tile
+
+
+@pytest.mark.parametrize("n,rows,cols,side", SIDES)
+def test_device_tests_reach_every_tile(square_tile, n, rows, cols, side):
+    lo, hi = (-(-v // 64) * 64 for v in sorted((rows, cols)))
+    assert square_tile(lo, hi, n, 0) == side and square_tile(lo, lo, n, 1) == side
+
+
+@pytest.mark.parametrize("rows,cols,n,symmetric,want", [
+    (3584, 4864, 8, 0, 256), (3584, 3584, 8, 1, 256), (1024, 2048, 16, 0, 256), (1024, 1024, 16, 1, 256),      # rounds of full tiles
+    (1280, 1536, 1, 0, 128), (2048, 2048, 1, 0, 128),                                                         # one block per CU of half as wide ones
+    (256, 512, 4, 0, 64), (256, 256, 4, 1, 64), (64, 64, 1, 1, 64), (1280, 1280, 1, 1, 64), (64, 16384, 1, 0, 64)])
+def test_sides(square_tile, rows, cols, n, symmetric, want):
+    assert square_tile(rows, cols, n, symmetric) == want
+
+
+def test_never_more_than_a_round_dearer_than_full_tiles(square_tile):
+    """Full tiles of one round are left only for tiles that are one round as well, or nearly."""
+    for n in (1, 2, 5, 16, 60):
+        for lo in range(64, 2049, 64):
+            for hi in (lo, 2 * lo):
+                full = -(-lo // 256) * -(-hi // 256) * n
+                side = square_tile(lo, hi, n, 0)
+                small = -(-lo // side) * -(-hi // side) * n
+                assert side == 256 or small <= 1024 * -(-full // 256)
