@@ -3,8 +3,8 @@
 //      groups: of equal size; a group counts the sum of its two largest c; only the `kept` best groups are open
 //      idx = the k largest c in open groups, equal ones to the lower expert    gate = scale s[idx] (/ sum of s[idx], renorm)
 // Sixteen lanes hold a token, four consecutive experts to a lane and quad, so a wavefront works on four tokens and every
-// reduction stays within a row of lanes, in data-parallel-primitive steps.  What bounds it is the k rounds of the choice (five instructions
-// an expert of the lane and round), not the 4 M bytes of a token.
+// reduction stays within a row of lanes, in data-parallel-primitive steps.  What bounds it is the instructions of the choice, not the 4 M
+// bytes of a token.
 //
 // Gradient, the choice held fixed, with g the gates' share (scale taken out) and u = scale dgate.  Every difference is between gradients, weighted by
 // shares, so nothing cancels when one expert takes all:
@@ -23,7 +23,10 @@ namespace {
 
 
 constexpr int kRow = 16;                       // lanes of a token
-constexpr int kSkew = 16;                      // floats: one more for every group ahead, so that groups of 32 start in different banks
+// Every block adds its counts to all experts' at its end, and what is added to one address waits in line.  16384 tokens over 256 experts in blocks of
+// 256 threads: 1024 of them 33 us, 512 26; in blocks of 512: 256 of them 23, 128 29.
+constexpr int kBlocks = 256;
+constexpr int kSkew = 20;                      // floats: one more for every group ahead, so that groups of 32 start in different banks
 
 template <int CTRL> __device__ __forceinline__ int dpp_int(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
 __device__ __forceinline__ unsigned row_max(unsigned v) {
@@ -46,13 +49,106 @@ __device__ __forceinline__ float row_max_f(float v) {
 }
 __device__ __forceinline__ float row_sum(float v) { return lane_group_sum<16>(v); }
 
-// unsigned keys in the order of the floats; NaN below them all, and 0 below that
+// A choice is a double: the score's value, which leaves the low 29 bits of the mantissa free, and in these the expert, such that equal scores are in
+// the order of the experts.  Then one comparison decides, and a sorting step is v_max_f64 and v_min_f64, two full-rate instructions instead of the
+// five of a pair (a compare and four selects).  NaN and -inf become the lowest finite values, +inf the highest.
+constexpr double kAbove = 0x1p130, kBelow = -0x1p130, kClosed = -0x1p140;      // beyond all floats
+constexpr int kExpertBits = 511;
+__device__ __forceinline__ double with_low(double v, unsigned low) {
+  const uint2 w = __builtin_bit_cast(uint2, v);
+  return __builtin_bit_cast(double, make_uint2(w.x | low, w.y));
+}
+__device__ __forceinline__ double choice_of(float c, unsigned e) {
+  const double v = fmin(fmax((double)c, kBelow), kAbove);
+  const unsigned sign = (unsigned)((int)__builtin_bit_cast(uint2, v).y >> 31);          // larger low bits: larger, of a negative number smaller
+  return with_low(v, e ^ (kExpertBits & ~sign));
+}
+__device__ __forceinline__ int expert_of(double v) {
+  const uint2 w = __builtin_bit_cast(uint2, v);
+  return (int)((w.x & kExpertBits) ^ (kExpertBits & ~(unsigned)((int)w.y >> 31)));
+}
+// (as instructions: the compiler, which does not know that none of these is a signalling NaN, adds one to quieten each operand that came from another lane)
+__device__ __forceinline__ double larger(double a, double b) {
+  double r;
+  asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ double smaller(double a, double b) {
+  double r;
+  asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ void order(double& a, double& b) {          // the larger one first
+  const double hi = larger(a, b);
+  b = smaller(a, b);
+  a = hi;
+}
+// descending: a bitonic sequence of N (a power of two), or any sequence
+template <int N> __device__ __forceinline__ void sort_bitonic(double* v) {
+#pragma unroll
+  for (int d = N / 2; d > 0; d /= 2)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((i & d) == 0) order(v[i], v[i + d]);
+}
+template <int N> __device__ __forceinline__ void sort(double* v) {
+  if constexpr (N > 1) {
+    sort<N / 2>(v);
+    sort<N / 2>(v + N / 2);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) order(v[i], v[N - 1 - i]);          // both halves descend: the first half gets the largest, either is bitonic now
+    sort_bitonic<N / 2>(v);
+    sort_bitonic<N / 2>(v + N / 2);
+  }
+}
+// the K largest of two descending lists, in `a`
+template <int K> __device__ __forceinline__ void merge(double* a, const double* b) {
+  double hi[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) hi[i] = larger(a[i], b[K - 1 - i]);
+  sort_bitonic<K>(hi);
+#pragma unroll
+  for (int i = 0; i < K; ++i) a[i] = hi[i];
+}
+template <int CTRL> __device__ __forceinline__ double dpp_double(double v) {
+  const uint2 w = __builtin_bit_cast(uint2, v);
+  return __builtin_bit_cast(double, make_uint2((unsigned)dpp_int<CTRL>((int)w.x), (unsigned)dpp_int<CTRL>((int)w.y)));
+}
+// The K largest of a row of lanes, from L descending values in each: lists of neighbours, of pairs, of halves are merged, and grow until they
+// have K.  Every lane ends with the whole list.
+template <int K, int L, int CTRL> __device__ __forceinline__ void merge_lanes(double* v) {
+  double o[K];
+#pragma unroll
+  for (int i = 0; i < L; ++i) o[i] = dpp_double<CTRL>(v[i]);
+  if constexpr (L < K) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {          // the L largest, and the rest, either bitonic
+      v[L + i] = smaller(v[i], o[L - 1 - i]);
+      v[i] = larger(v[i], o[L - 1 - i]);
+    }
+    sort_bitonic<L>(v);
+    sort_bitonic<L>(v + L);
+  } else {
+    merge<K>(v, o);
+  }
+}
+template <int K, int L> __device__ __forceinline__ void merge_row(double* v) {
+  constexpr int L1 = L < K ? 2 * L : K, L2 = L1 < K ? 2 * L1 : K, L3 = L2 < K ? 2 * L2 : K;
+  merge_lanes<K, L, 0xB1>(v);         // quad_perm [1,0,3,2]
+  merge_lanes<K, L1, 0x4E>(v);        // quad_perm [2,3,0,1]
+  merge_lanes<K, L2, 0x141>(v);       // row_half_mirror
+  merge_lanes<K, L3, 0x140>(v);       // row_mirror
+}
+
+// group scores, in the order of their values: unsigned keys, NaN as -inf, 0 below all
 __device__ __forceinline__ unsigned order_key(float f) {
   const unsigned u = __float_as_uint(f);
-  return f != f ? 1u : u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+  return f != f ? 0x007fffffu : u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
 
 __device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
+// of every expert, for the choice: within some steps of 2^-24
+__device__ __forceinline__ float sigmoid_near(float l) { return __builtin_amdgcn_rcpf(1.f + __expf(-l)); }
 
 struct RouterArgs {
   int T, M, k, groups, kept, size, parts;      // parts: lanes that look through a group, a power of two; groups * parts <= 16
@@ -95,7 +191,8 @@ __device__ __forceinline__ void softmax_stats(const float (&v)[NQ * 4], float& m
   inv = sum == 0.f ? 0.f : 1.f / sum;
 }
 
-template <int NQ, bool SOFTMAX, bool GROUPS, int BLOCK>
+// K: a power of two, k at least
+template <int NQ, int K, bool SOFTMAX, bool GROUPS, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
   constexpr int V = NQ * 4, TOKENS = BLOCK / kRow;
   __shared__ int hist[NQ * 64];
@@ -103,6 +200,12 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
   const int l = threadIdx.x % kRow, at = threadIdx.x / kRow;
   for (int e = threadIdx.x; e < NQ * 64; e += BLOCK) hist[e] = 0;
   __syncthreads();
+  float bias[V];
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    if (a.bias) load4(a.bias, q * 64 + l * 4, a.M, bias + q * 4);
+    else bias[q * 4] = bias[q * 4 + 1] = bias[q * 4 + 2] = bias[q * 4 + 3] = 0.f;
+  }
   for (long t0 = (long)blockIdx.x * TOKENS; t0 < a.T; t0 += (long)gridDim.x * TOKENS) {
     const long t = t0 + at < a.T ? t0 + at : a.T - 1;          // (surplus rows of lanes repeat the last token and store nothing)
     const bool live = t0 + at < a.T;
@@ -112,17 +215,16 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
     for (int q = 0; q < NQ; ++q) load4(row, q * 64 + l * 4, a.M, v + q * 4);
     float mx = 0.f, inv = 1.f;
     if (SOFTMAX) softmax_stats<NQ>(v, mx, inv);
-    auto score = [&](float x) { return SOFTMAX ? expf(x - mx) * inv : sigmoid(x); };
-    unsigned key[V];
+    double best[V > K ? V : K];
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const int e = q * 64 + l * 4 + c, i = q * 4 + c;
-        float x = score(v[i]);
-        if (a.bias && e < a.M) x += a.bias[e];
-        key[i] = e < a.M ? order_key(x) : 0u;
-        if (GROUPS && e < a.M) choice[at][e + (int)((unsigned)e * a.inv_size >> 20)] = x;
+        const float x = (SOFTMAX ? __expf(v[i] - mx) * inv : sigmoid_near(v[i])) + bias[i];
+        const double mine = choice_of(x, (unsigned)e);
+        best[i] = e < a.M ? mine : kClosed;
+        if (GROUPS) choice[at][e < a.M ? e + (int)((unsigned)e * a.inv_size >> 20) : NQ * 64 + kSkew - 1] = x;          // (the last one is nobody's)
       }
     if (GROUPS) {
       // lanes g parts .. look through group g; the first of them ranks it among the others
@@ -143,7 +245,7 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
         first = fmaxf(first, f2);
       }
       wave_lds_order();
-      const unsigned mine = part == 0 && g < a.groups ? order_key(a.size > 1 ? first + second : first) : 0u;
+      const unsigned mine = part == 0 && g < a.groups ? order_key(a.size > 1 ? first + second : first) : 0u;      // (-inf + inf counts as -inf)
       int rank = 0;
       auto against = [&](unsigned other, int lane) { rank += other > mine || (other == mine && lane < l) ? 1 : 0; };
 #define SPES_TURN(r) against((unsigned)dpp_int<0x120 + r>((int)mine), dpp_int<0x120 + r>(l))
@@ -156,26 +258,25 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const unsigned e = (unsigned)(q * 64 + l * 4 + c);
-          if ((open >> ((e * a.inv_size >> 20) * a.parts) & 1u) == 0) key[q * 4 + c] = 0;
+          if ((open >> ((e * a.inv_size >> 20) * a.parts) & 1u) == 0) best[q * 4 + c] = kClosed;
         }
     }
-    int chosen = 0;                     // of lane j: the j-th expert
-    for (int j = 0; j < a.k; ++j) {
-      unsigned top = 0;
+    // the K largest of the lane, then of the token
+    constexpr int L = V < K ? V : K;
+    sort<L>(best);
 #pragma unroll
-      for (int i = 0; i < V; ++i) top = max(top, key[i]);
-      top = row_max(top);
-      int first = 0x7fffffff;
-#pragma unroll
-      for (int i = V - 1; i >= 0; --i) first = key[i] == top ? (i / 4) * 64 + i % 4 : first;
-      const int e = row_min(first == 0x7fffffff ? first : first + l * 4);
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (e == (i / 4) * 64 + l * 4 + i % 4) key[i] = 0;
-      if (l == j) chosen = e;
+    for (int i = L; i < V; i += L) {
+      sort<L>(best + i);
+      merge<L>(best, best + i);
     }
+    merge_row<K, L>(best);
+    double pick = best[0];              // of lane j: the j-th
+#pragma unroll
+    for (int j = 1; j < K; ++j) pick = l == j ? best[j] : pick;
+    const int chosen = expert_of(pick);
     const bool mine = l < a.k;
-    const float s = mine ? score(row[chosen]) : 0.f;
+    const float x = mine ? row[chosen] : 0.f;
+    const float s = !mine ? 0.f : SOFTMAX ? expf(x - mx) * inv : sigmoid(x);
     float share = s;
     if (a.renorm) {
       const float total = row_sum(s);
@@ -329,14 +430,22 @@ int launch_router_fwd(int T, int M, int k, const spes_router_opts& o, const floa
   const bool groups = o.groups > 1;
   return with_quads(M, [&](auto nq) {
     constexpr int NQ = decltype(nq)::value;
-    auto go = [&](auto softmax, auto grouped) {
+    auto go = [&](auto choice, auto softmax, auto grouped) {
       constexpr bool SM = decltype(softmax)::value, GR = decltype(grouped)::value;
-      if (a.one_block) hipLaunchKernelGGL((router_fwd_kernel<NQ, SM, GR, 1024>), dim3(1), dim3(1024), 0, s, a);
-      else hipLaunchKernelGGL((router_fwd_kernel<NQ, SM, GR, 256>), dim3(cdiv(T, 16) < 1024 ? cdiv(T, 16) : 1024), dim3(256), 0, s, a);
+      constexpr int K = decltype(choice)::value;
+      constexpr int ONE = NQ <= 2 ? 1024 : 512;          // (of more experts, a block of 1024 would spill registers)
+      const int need = cdiv(T, ONE / kRow);
+      hipLaunchKernelGGL((router_fwd_kernel<NQ, K, SM, GR, ONE>), dim3(a.one_block ? 1 : need < kBlocks ? need : kBlocks), dim3(ONE), 0, s, a);
       return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
     };
-    if (o.score == SPES_SCORE_SOFTMAX) return groups ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
-    return groups ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
+    auto kind = [&](auto choice) {
+      if (o.score == SPES_SCORE_SOFTMAX) return groups ? go(choice, std::true_type{}, std::true_type{}) : go(choice, std::true_type{}, std::false_type{});
+      return groups ? go(choice, std::false_type{}, std::true_type{}) : go(choice, std::false_type{}, std::false_type{});
+    };
+    if (k <= 2) return kind(std::integral_constant<int, 2>{});
+    if (k <= 4) return kind(std::integral_constant<int, 4>{});
+    if (k <= 8) return kind(std::integral_constant<int, 8>{});
+    return kind(std::integral_constant<int, 16>{});
   });
 }
 
