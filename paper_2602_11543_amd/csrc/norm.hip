@@ -3,7 +3,7 @@
 //      mean = sum v / N (layer norm; 0 otherwise)     rstd = (sum (v - mean)^2 / N + eps)^-1/2     hat = (v - mean) rstd     y = hat w + b
 //      dx = rstd (h - hat (sum h hat / N) - sum h / N) + dres      with h = dy w; the last sum for layer norm only
 //      dw = sum over rows of dy hat     db = sum over rows of dy
-// Every sum is fp32.  One pass over memory: a row stays in the registers of its 16, 64 or 256 lanes, eight columns to a lane
+// Every sum is fp32.  One pass over memory: a row stays in the registers of its 16, 64 or 256 lanes, 16 bytes to a lane
 // and unit, so the mean is subtracted before anything is squared.
 #include <type_traits>
 
@@ -30,6 +30,37 @@ __device__ __forceinline__ void row_sums(float* v, float (*red)[N][4], int& turn
   }
 }
 
+// How the rows end: with a whole unit; inside one, which is then read from where it ends with the row and shifted (guarded loads are
+// waited for where they stand: 32768 x 4095 703 us, so 504); or they are shorter than one, and read element by element.
+enum Ends { kWhole, kInside, kNarrow };
+template <typename T, int LPR, int NU, Ends ENDS>
+struct RowUnits {
+  static constexpr int W = 16 / (int)sizeof(T);
+  int cols, l;
+  __device__ __forceinline__ int left(int i) const { return cols - (l + i * LPR) * W; }          // elements of the row from the unit's first on
+  __device__ __forceinline__ int from(int i) const { return min((l + i * LPR) * W, cols - W); }
+  template <bool ONCE> __device__ __forceinline__ void request(Unit<T> (&u)[NU], const T* row) const {
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      if constexpr (ENDS == kNarrow) u[i].load(row, left(i));
+      else u[i].template load<ONCE>(row + from(i));
+    }
+  }
+  template <bool ONCE> __device__ __forceinline__ void put(const Unit<T>& u, int i, T* row) const {
+    T* const p = row + (l + i * LPR) * W;
+    if constexpr (ENDS != kWhole) u.template store<ONCE>(p, left(i));
+    else if (left(i) > 0) u.template store<ONCE>(p);
+  }
+  // before they are used: units beyond the row are zeros
+  __device__ __forceinline__ void cut(Unit<T> (&u)[NU]) const {
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      if constexpr (ENDS == kInside) u[i].drop((l + i * LPR) * W - from(i));
+      if constexpr (ENDS == kWhole) u[i].keep(left(i) > 0);
+    }
+  }
+};
+
 struct FwdArgs {
   int rows, cols;
   const void *x, *add, *weight, *bias;
@@ -39,9 +70,9 @@ struct FwdArgs {
   float *mean, *rstd;
 };
 
-template <typename T, int LPR, int NU, bool LAYER>
+template <typename T, int LPR, int NU, Ends ENDS, bool LAYER, bool ONCE>
 __global__ __launch_bounds__(256) void norm_fwd_kernel(const FwdArgs a) {
-  constexpr int RPB = 256 / LPR;
+  constexpr int RPB = 256 / LPR, W = 16 / (int)sizeof(T);
   __shared__ float red[2][1][4];
   int turn = 0;
   const int l = threadIdx.x % LPR;
@@ -49,39 +80,39 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(const FwdArgs a) {
   const T* const add = static_cast<const T*>(a.add);
   T* const y = static_cast<T*>(a.y);
   T* const sum = static_cast<T*>(a.sum);
-  int left[NU];
+  const RowUnits<T, LPR, NU, ENDS> at = {a.cols, l};
   Unit<T> w[NU], b[NU];
+  at.template request<false>(w, static_cast<const T*>(a.weight));
+  at.cut(w);
+  if (a.bias) {
+    at.template request<false>(b, static_cast<const T*>(a.bias));
+    at.cut(b);
+  } else {
 #pragma unroll
-  for (int i = 0; i < NU; ++i) {
-    const int c = (l + i * LPR) * 8;
-    left[i] = a.cols - c;
-    w[i].load(static_cast<const T*>(a.weight) + (left[i] > 0 ? c : 0), left[i]);
-    b[i].load(static_cast<const T*>(a.bias) + (left[i] > 0 ? c : 0), a.bias ? left[i] : 0);
+    for (int i = 0; i < NU; ++i) b[i].keep(false);
   }
   const float n = (float)a.cols;
   for (long row = (long)blockIdx.x * RPB + threadIdx.x / LPR; row < a.rows; row += (long)gridDim.x * RPB) {
     Unit<T> in[NU], more[NU];
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      const int c = left[i] > 0 ? (l + i * LPR) * 8 : 0;
-      in[i].load(x + row * a.x_stride + c, left[i]);
-      if (add) more[i].load(add + row * a.add_stride + c, left[i]);
-    }
-    float v[NU][8], s = 0.f;
+    at.template request<ONCE>(in, x + row * a.x_stride);
+    if (add) at.template request<ONCE>(more, add + row * a.add_stride);
+    at.cut(in);
+    if (add) at.cut(more);
+    float v[NU][W], s = 0.f;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       in[i].get(v[i]);
       if (add) {
-        float o[8];
+        float o[W];
         more[i].get(o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] += o[e];
+        for (int e = 0; e < W; ++e) v[i][e] += o[e];
         in[i].set(v[i]);
-        in[i].store(sum + row * a.cols + (l + i * LPR) * 8, left[i]);
+        at.template put<ONCE>(in[i], i, sum + row * a.cols);
         in[i].get(v[i]);                  // normalised is what is stored
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += v[i][e];
+      for (int e = 0; e < W; ++e) s += v[i][e];
     }
     float mean = 0.f;
     if (LAYER) {
@@ -92,8 +123,8 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(const FwdArgs a) {
 #pragma unroll
     for (int i = 0; i < NU; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (LAYER) v[i][e] = e < left[i] ? v[i][e] - mean : 0.f;
+      for (int e = 0; e < W; ++e) {
+        if (LAYER) v[i][e] = e < at.left(i) ? v[i][e] - mean : 0.f;
         q = fmaf(v[i][e], v[i][e], q);
       }
     row_sums<LPR, 1>(&q, red, turn);
@@ -104,13 +135,13 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(const FwdArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      float wf[8], bf[8];
+      float wf[W], bf[W];
       w[i].get(wf);
       b[i].get(bf);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * rstd, wf[e], bf[e]);
+      for (int e = 0; e < W; ++e) v[i][e] = fmaf(v[i][e] * rstd, wf[e], bf[e]);
       in[i].set(v[i]);
-      in[i].store(y + row * a.cols + (l + i * LPR) * 8, left[i]);
+      at.template put<ONCE>(in[i], i, y + row * a.cols);
     }
   }
 }
@@ -125,48 +156,45 @@ struct BwdArgs {
   bool bias;
 };
 
-template <typename T, int LPR, int NU, bool LAYER>
+template <typename T, int LPR, int NU, Ends ENDS, bool LAYER, bool ONCE>
 __global__ __launch_bounds__(256) void norm_bwd_kernel(const BwdArgs a) {
-  constexpr int RPB = 256 / LPR, N = LAYER ? 2 : 1;
+  constexpr int RPB = 256 / LPR, N = LAYER ? 2 : 1, W = 16 / (int)sizeof(T);
   __shared__ float red[2][N][4];
-  __shared__ float across[RPB > 1 ? 256 * 8 : 1];
+  __shared__ float across[RPB > 1 ? 256 * W : 1];
   int turn = 0;
   const int l = threadIdx.x % LPR;
   const T* const dy = static_cast<const T*>(a.dy);
   const T* const x = static_cast<const T*>(a.x);
   const T* const dres = static_cast<const T*>(a.dres);
   T* const dx = static_cast<T*>(a.dx);
-  int left[NU];
+  const RowUnits<T, LPR, NU, ENDS> at = {a.cols, l};
   Unit<T> w[NU];
-  float dw[NU][8], db[NU][8];
+  at.template request<false>(w, static_cast<const T*>(a.weight));
+  at.cut(w);
+  float dw[NU][W], db[NU][W];
 #pragma unroll
-  for (int i = 0; i < NU; ++i) {
-    const int c = (l + i * LPR) * 8;
-    left[i] = a.cols - c;
-    w[i].load(static_cast<const T*>(a.weight) + (left[i] > 0 ? c : 0), left[i]);
+  for (int i = 0; i < NU; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.f;
-  }
+    for (int e = 0; e < W; ++e) dw[i][e] = db[i][e] = 0.f;
   const float inv_n = 1.f / (float)a.cols;
   for (long row = (long)blockIdx.x * RPB + threadIdx.x / LPR; row < a.rows; row += (long)gridDim.x * RPB) {
     Unit<T> g[NU], in[NU], res[NU];
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      const int c = left[i] > 0 ? (l + i * LPR) * 8 : 0;
-      g[i].load(dy + row * a.dy_stride + c, left[i]);
-      in[i].load(x + row * a.x_stride + c, left[i]);
-      if (dres) res[i].load(dres + row * a.dres_stride + c, left[i]);
-    }
+    at.template request<ONCE>(g, dy + row * a.dy_stride);
+    at.template request<ONCE>(in, x + row * a.x_stride);
+    if (dres) at.template request<ONCE>(res, dres + row * a.dres_stride);
+    at.cut(g);
+    at.cut(in);
+    if (dres) at.cut(res);
     const float rstd = a.rstd[row], mean = LAYER ? a.mean[row] : 0.f;
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      float gf[8], xf[8], wf[8];
+      float gf[W], xf[W], wf[W];
       g[i].get(gf);
       in[i].get(xf);
       w[i].get(wf);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {        // (columns beyond the row: dy and w are zero)
+      for (int e = 0; e < W; ++e) {        // (columns beyond the row: dy and w are zero)
         const float hat = (xf[e] - mean) * rstd, h = gf[e] * wf[e];
         dw[i][e] = fmaf(gf[e], hat, dw[i][e]);
         db[i][e] += gf[e];
@@ -178,23 +206,23 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const BwdArgs a) {
     const float c0 = s[0] * inv_n, c1 = LAYER ? s[1] * inv_n : 0.f;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      float gf[8], xf[8], wf[8], o[8];
+      float gf[W], xf[W], wf[W], o[W];
       g[i].get(gf);
       in[i].get(xf);
       w[i].get(wf);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < W; ++e) {
         const float hat = (xf[e] - mean) * rstd, h = gf[e] * wf[e];
         o[e] = (h - fmaf(hat, c0, c1)) * rstd;
       }
       if (dres) {
-        float rf[8];
+        float rf[W];
         res[i].get(rf);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] += rf[e];
+        for (int e = 0; e < W; ++e) o[e] += rf[e];
       }
       in[i].set(o);
-      in[i].store(dx + row * a.cols + (l + i * LPR) * 8, left[i]);
+      at.template put<ONCE>(in[i], i, dx + row * a.cols);
     }
   }
   if (a.part == nullptr) return;
@@ -205,41 +233,45 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const BwdArgs a) {
     float* const out = a.part + ((long)which * gridDim.x + blockIdx.x) * a.cols;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      float (&d)[8] = which ? db[i] : dw[i];
+      float (&d)[W] = which ? db[i] : dw[i];
       if (RPB > 1) {
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) across[e * 256 + threadIdx.x] = d[e];
+        for (int e = 0; e < W; ++e) across[e * 256 + threadIdx.x] = d[e];
         __syncthreads();
         if (threadIdx.x < LPR)
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
+          for (int e = 0; e < W; ++e)
             for (int r = 1; r < RPB; ++r) d[e] += across[e * 256 + r * LPR + threadIdx.x];
       }
       if (threadIdx.x < LPR) {
-        Unit<float> u;
-        u.set(d);
-        u.store(out + (l + i * LPR) * 8, left[i]);
+#pragma unroll
+        for (int h = 0; h < W / 4; ++h) {
+          Unit<float> u;
+          u.set(d + 4 * h);
+          u.store(out + (l + i * LPR) * W + 4 * h, at.left(i) - 4 * h);
+        }
       }
     }
   }
 }
 
-// out[c] (+)= sum over p, ascending within each of eight slices and then over these, of part[p][c]: 32 columns to a block
-__global__ __launch_bounds__(256) void norm_columns_kernel(const float* __restrict__ part, int n_part, int cols, float* __restrict__ d_weight,
-                                                           float* __restrict__ d_bias, int accumulate) {
-  __shared__ float acc[8][33];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
+// out[c] (+)= sum over p, ascending within each of 32 slices and then over these, of part[p][c]: 32 columns to a block
+__global__ __launch_bounds__(1024) void norm_columns_kernel(const float* __restrict__ part, int n_part, int cols, float* __restrict__ d_weight,
+                                                            float* __restrict__ d_bias, int accumulate) {
+  __shared__ float acc[32][33];
+  const int x = threadIdx.x & 31, c = blockIdx.x * 32 + x, slice = threadIdx.x >> 5;
   const float* const src = part + (long)blockIdx.y * n_part * cols;
   float s = 0.f;
   if (c < cols) {
-#pragma unroll 8
-    for (int p = slice; p < n_part; p += 8) s += src[(long)p * cols + c];
+#pragma unroll 16
+    for (int p = slice; p < n_part; p += 32) s += src[(long)p * cols + c];
   }
-  acc[slice][threadIdx.x & 31] = s;
+  acc[slice][x] = s;
   __syncthreads();
   if (slice == 0 && c < cols) {
-    for (int i = 1; i < 8; ++i) s += acc[i][threadIdx.x];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) s += acc[i][x];
     float* const out = blockIdx.y ? d_bias : d_weight;
     out[c] = accumulate ? out[c] + s : s;
   }
@@ -253,20 +285,36 @@ int bwd_blocks(int rows, int cols) {
   return need < 512 ? need : 512;
 }
 
+// Streams that the Infinity Cache (256 MB) does not hold carry the non-temporal hint: 32768 x 4096 bf16 with both residual streams, forward
+// and backward, 405 us without, 396 on the loads, 379 on the stores too (5.7 TB/s); 4096 x 768, which it holds, 18.8 us of kernels without and 19.4 with.
+// Not for rows that end inside a line of 128 bytes, whose halves two wavefronts write: with 4095 columns 722 us, without 703.
+constexpr long kCacheBytes = 256l << 20;
+bool streams(int dtype, int rows, int cols, int tensors, long stride0, long stride1, long stride2) {
+  const long size = dtype == SPES_F32 ? 4 : 2;
+  return rows * cols * size * tensors > kCacheBytes && ((cols | stride0 | stride1 | stride2) * size) % 128 == 0;
+}
+
 template <typename F>
-int with_rows(int dtype, int kind, int cols, F launch) {
+int with_rows(int dtype, int kind, int cols, bool once, F launch) {
   auto typed = [&](auto t) {
     using T = decltype(t);
+    constexpr int W = 16 / (int)sizeof(T), UNITS = (int)sizeof(T) / 2;          // fp32: twice as many units
     auto shaped = [&](auto layer) {
-      using L = decltype(layer);
-      if (cols <= 128) return launch(t, std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}, L{});
-      if (cols <= 256) return launch(t, std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{}, L{});
-      if (cols <= 512) return launch(t, std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{}, L{});
-      if (cols <= 1024) return launch(t, std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{}, L{});
-      if (cols <= 2048) return launch(t, std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{}, L{});
-      if (cols <= 4096) return launch(t, std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{}, L{});
-      if (cols <= 8192) return launch(t, std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{}, L{});
-      return launch(t, std::integral_constant<int, 256>{}, std::integral_constant<int, 8>{}, L{});
+      auto with = [&](auto lpr, auto nu) {
+        constexpr std::integral_constant<int, decltype(nu)::value * UNITS> units;
+        if (cols % W != 0) return launch(t, lpr, units, std::integral_constant<Ends, kInside>{}, layer, std::false_type{});
+        if (once) return launch(t, lpr, units, std::integral_constant<Ends, kWhole>{}, layer, std::true_type{});
+        return launch(t, lpr, units, std::integral_constant<Ends, kWhole>{}, layer, std::false_type{});
+      };
+      if (cols < W) return launch(t, std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}, std::integral_constant<Ends, kNarrow>{}, layer, std::false_type{});
+      if (cols <= 128) return with(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+      if (cols <= 256) return with(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
+      if (cols <= 512) return with(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+      if (cols <= 1024) return with(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+      if (cols <= 2048) return with(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+      if (cols <= 4096) return with(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
+      if (cols <= 8192) return with(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+      return with(std::integral_constant<int, 256>{}, std::integral_constant<int, 8>{});
     };
     return kind == SPES_NORM_LAYER ? shaped(std::true_type{}) : shaped(std::false_type{});
   };
@@ -280,11 +328,14 @@ size_t norm_scratch_bytes(int rows, int cols) { return (size_t)2 * (rows > 0 ? b
 int launch_norm_fwd(int dtype, int kind, int rows, int cols, const void* x, long x_stride, const void* add, long add_stride, const void* weight,
                     const void* bias, float eps, void* sum, void* y, float* mean, float* rstd, hipStream_t s) {
   if (rows == 0) return SPES_OK;
+  const bool once = streams(dtype, rows, cols, add ? 4 : 2, x_stride, add ? add_stride : 0, 0);
   FwdArgs a = {rows, cols, x, add, weight, bias, x_stride, add_stride, eps, sum, y, mean, rstd};
-  return with_rows(dtype, kind, cols, [&](auto t, auto lpr, auto nu, auto layer) {
+  return with_rows(dtype, kind, cols, once, [&](auto t, auto lpr, auto nu, auto ends, auto layer, auto streaming) {
     constexpr int LPR = decltype(lpr)::value, RPB = 256 / LPR;
     const int need = cdiv(rows, RPB), grid = need < 2048 ? need : 2048;
-    hipLaunchKernelGGL((norm_fwd_kernel<decltype(t), LPR, decltype(nu)::value, decltype(layer)::value>), dim3(grid), dim3(256), 0, s, a);
+    constexpr int NU = decltype(nu)::value;
+    constexpr bool LAYER = decltype(layer)::value;
+    hipLaunchKernelGGL((norm_fwd_kernel<decltype(t), LPR, NU, decltype(ends)::value, LAYER, decltype(streaming)::value>), dim3(grid), dim3(256), 0, s, a);
     return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
   });
 }
@@ -294,16 +345,19 @@ int launch_norm_bwd(int dtype, int kind, int rows, int cols, const void* dy, lon
                     int accumulate, float* scratch, hipStream_t s) {
   const int grid = rows > 0 ? bwd_blocks(rows, cols) : 0;
   if (grid > 0) {
+    const bool once = streams(dtype, rows, cols, dres ? 4 : 3, x_stride, dy_stride, dres ? dres_stride : 0);
     BwdArgs a = {rows, cols, dy, x, weight, dres, dy_stride, x_stride, dres_stride, mean, rstd, dx, d_weight ? scratch : nullptr, d_bias != nullptr};
-    const int rc = with_rows(dtype, kind, cols, [&](auto t, auto lpr, auto nu, auto layer) {
+    const int rc = with_rows(dtype, kind, cols, once, [&](auto t, auto lpr, auto nu, auto ends, auto layer, auto streaming) {
       constexpr int LPR = decltype(lpr)::value;
-      hipLaunchKernelGGL((norm_bwd_kernel<decltype(t), LPR, decltype(nu)::value, decltype(layer)::value>), dim3(grid), dim3(256), 0, s, a);
+      constexpr int NU = decltype(nu)::value;
+    constexpr bool LAYER = decltype(layer)::value;
+    hipLaunchKernelGGL((norm_bwd_kernel<decltype(t), LPR, NU, decltype(ends)::value, LAYER, decltype(streaming)::value>), dim3(grid), dim3(256), 0, s, a);
       return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
     });
     if (rc != SPES_OK) return rc;
   }
   if (d_weight == nullptr || (grid == 0 && accumulate)) return SPES_OK;
-  hipLaunchKernelGGL(norm_columns_kernel, dim3(cdiv(cols, 32), d_bias ? 2 : 1), dim3(256), 0, s, scratch, grid, cols, d_weight, d_bias, accumulate);
+  hipLaunchKernelGGL(norm_columns_kernel, dim3(cdiv(cols, 32), d_bias ? 2 : 1), dim3(1024), 0, s, scratch, grid, cols, d_weight, d_bias, accumulate);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
 
