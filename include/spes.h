@@ -162,6 +162,25 @@ SPES_API int spes_moe_bwd(const spes_moe_shape* shape, const void* dy, const voi
                           float* d_w_router, float* d_w_gate, float* d_w_up, float* d_w_down,
                           int32_t accumulate, void* stream);
 
+/* The layer behind a routing that the caller made (spes_router_fwd, or another): spes_moe_fwd and spes_moe_bwd without their
+ * router.  Choice and gates come in, the gates' gradient goes out; dx is the experts' part alone.  renorm_topk of the shape is
+ * not looked at, and spes_moe_router_aux has no scores to work on.  An entry of topk_idx that is no expert counts as expert 0
+ * with gate 0.
+ *
+ *  topk_idx   DEVICE [T,k] i32      topk_gate  DEVICE [T,k] f32 (both copied into ctx, for the backward)
+ *  dgate      DEVICE [T,k] f32 out
+ *  all others as above
+ */
+SPES_API int spes_moe_fwd_routed(const spes_moe_shape* shape, const void* x, const int32_t* topk_idx,
+                                 const float* topk_gate, const void* w_gate, const void* w_up,
+                                 const void* w_down, void* y, int32_t* expert_count, void* ctx,
+                                 void* stream);
+SPES_API int spes_moe_bwd_routed(const spes_moe_shape* shape, const void* dy, const void* x,
+                                 const void* w_gate, const void* w_up, const void* w_down, void* ctx,
+                                 const uint8_t* trainable_mask, void* dx, float* dgate,
+                                 float* d_w_gate, float* d_w_up, float* d_w_down, int32_t accumulate,
+                                 void* stream);
+
 /* Auxiliary router losses (Sec. 3.3 "Training Losses"; coefficients App. B: load-balancing
  * 0.01, router z-loss 0.001).  The paper names the two losses and cites their sources; the
  * formulas used are the cited ones:

@@ -56,6 +56,10 @@ def _load() -> ctypes.CDLL:
     lib.spes_moe_fwd.argtypes = [shp] + [vp] * 12
     lib.spes_moe_bwd.restype = i32
     lib.spes_moe_bwd.argtypes = [shp] + [vp] * 13 + [i32, vp]
+    lib.spes_moe_fwd_routed.restype = i32
+    lib.spes_moe_fwd_routed.argtypes = [shp] + [vp] * 10
+    lib.spes_moe_bwd_routed.restype = i32
+    lib.spes_moe_bwd_routed.argtypes = [shp] + [vp] * 12 + [i32, vp]
     lib.spes_moe_permute.restype = i32
     lib.spes_moe_permute.argtypes = [shp, vp, vp, vp, vp]
     lib.spes_moe_grad_scatter.restype = i32
@@ -197,6 +201,23 @@ def spes_moe_bwd(shape, dy, x, w_router, w_gate, w_up, w_down, ctx, trainable_ma
     _check(_lib.spes_moe_bwd(ctypes.byref(shape), _dev(dy), _dev(x), _dev(w_router), _dev(w_gate), _dev(w_up), _dev(w_down),
                              _dev(ctx), mask.ctypes.data_as(ctypes.c_void_p), _dev(dx), _dev(d_w_router), _dev(d_w_gate),
                              _dev(d_w_up), _dev(d_w_down), int(accumulate), _stream(stream)), "spes_moe_bwd")
+
+
+def spes_moe_fwd_routed(shape, x, topk_idx, topk_gate, w_gate, w_up, w_down, y, expert_count, ctx, stream=None) -> None:
+    T, k = shape.T, shape.top_k
+    _check(_lib.spes_moe_fwd_routed(ctypes.byref(shape), _dev(x), _buf(topk_idx, torch.int32, T, k), _buf(topk_gate, torch.float32, T, k),
+                                    _dev(w_gate), _dev(w_up), _dev(w_down), _dev(y), _buf(expert_count, torch.int32, shape.n_experts), _dev(ctx),
+                                    _stream(stream)), "spes_moe_fwd_routed")
+
+
+def spes_moe_bwd_routed(shape, dy, x, w_gate, w_up, w_down, ctx, trainable_mask, dx, dgate, d_w_gate, d_w_up, d_w_down, accumulate=0,
+                        stream=None) -> None:
+    mask = np.ascontiguousarray(trainable_mask, dtype=np.uint8)
+    if mask.shape != (shape.n_experts,):
+        raise SpesError("trainable_mask must have one byte per expert")
+    _check(_lib.spes_moe_bwd_routed(ctypes.byref(shape), _dev(dy), _dev(x), _dev(w_gate), _dev(w_up), _dev(w_down), _dev(ctx),
+                                    mask.ctypes.data_as(ctypes.c_void_p), _dev(dx), _buf(dgate, torch.float32, shape.T, shape.top_k),
+                                    _dev(d_w_gate), _dev(d_w_up), _dev(d_w_down), int(accumulate), _stream(stream)), "spes_moe_bwd_routed")
 
 
 def spes_moe_permute(shape, x, ctx, xp, stream=None) -> None:

@@ -148,62 +148,11 @@ void prof_mark(int which, const char* name, hipStream_t s) {
 
 #define SPES_TRY(expr) do { int rc_ = (expr); if (rc_ != SPES_OK) return rc_; } while (0)
 
-}  // namespace
-
-extern "C" {
-
-SPES_API size_t spes_moe_ctx_bytes(const spes_moe_shape* shape) {
-  if (shape_supported(shape) != SPES_OK) return 0;
-  return make_layout(shape).pub.total;
-}
-
-SPES_API int spes_moe_ctx_describe(const spes_moe_shape* shape, spes_moe_ctx_layout* out) {
-  if (out == nullptr) return SPES_EINVAL;
-  SPES_TRY(shape_supported(shape));
-  *out = make_layout(shape).pub;
-  return SPES_OK;
-}
-
-SPES_API int spes_moe_fwd(const spes_moe_shape* shape, const void* x, const void* w_router, const float* router_bias,
-                          const void* w_gate, const void* w_up, const void* w_down, void* y, int32_t* topk_idx,
-                          float* topk_gate, int32_t* expert_count, void* ctx, void* stream) {
-  SPES_TRY(shape_supported(shape));
-  if (!x || !w_router || !w_gate || !w_up || !w_down || !y || !topk_idx || !topk_gate || !expert_count || !ctx)
-    return SPES_EINVAL;
-  if (!aligned16(x) || !aligned16(w_router) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(w_down) || !aligned16(y) ||
-      !aligned16(topk_idx) || !aligned16(topk_gate) || !aligned16(expert_count) || !aligned16(ctx) ||
-      (router_bias && !aligned16(router_bias)))
-    return SPES_EALIGN;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  const Layout L = make_layout(shape);
+// the expert part of the forward: tables from the choice and gates in ctx, the two grouped GEMMs, the weighted sum
+int run_experts_fwd(const spes_moe_shape* shape, const Layout& L, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y,
+                    const int* topk_idx, const float* topk_gate, int32_t* expert_count, void* ctx, hipStream_t s) {
   const int T = shape->T, d = shape->d_model, M = shape->n_experts, f = shape->d_ff, k = shape->top_k, dt = shape->dtype;
   const long R = (long)T * k;
-
-  prof_begin(0, s);
-  int logit_parts = 1;
-  // router scores: logits[T,M] = x W_r^T
-  {
-    GemmArgs g = blank();
-    g.A[0] = x; g.a_ms = d; g.a_ks = 1; g.a_elems = (long)T * d;
-    g.B[0] = w_router; g.b_ns = d; g.b_ks = 1; g.b_elems = (long)M * d;
-    g.Kdim = d; g.kchunk = d; g.Mdim = T; g.Ndim = M;
-    g.C[0] = at<float>(ctx, L.pub.logits); g.c_ms = M; g.c_f32 = 1;
-    // the matrix-core epilogue stores four columns at a time; with only M <= 64 output columns the row tiles alone
-    // would occupy a quarter of the CUs, so d_model is cut into partial products that the gating kernel adds up
-    if (dt == SPES_BF16 && M % 4 == 0) {
-      g.kchunk = (cdiv(d, kLogitSplit) + 63) / 64 * 64; g.n_groups = cdiv(d, g.kchunk); g.c_gs = (long)T * M;
-      logit_parts = g.n_groups;
-      SPES_TRY(launch_gemm_mfma(kGroupedK, kEpiStore, true, true, g, s));
-    } else if (L.f32_mfma) {
-      SPES_TRY(launch_gemm_f32(kGroupedK, kEpiStore, true, true, g, s));
-    } else {
-      SPES_TRY(launch_gemm_simt(dt, dt, kGroupedK, kEpiStore, g, s));
-    }
-  }
-  prof_mark(0, "router_gemm", s);
-  SPES_TRY(launch_topk_gate(at<float>(ctx, L.pub.logits), logit_parts, router_bias, T, M, k, shape->renorm_topk, topk_idx, topk_gate,
-                            at<int>(ctx, L.pub.topk_idx), at<float>(ctx, L.pub.topk_gate), at<float>(ctx, L.pub.lse), s));
-  prof_mark(0, "softmax_topk", s);
   SPES_TRY(launch_routing_tables(topk_idx, topk_gate, (int)R, M, k, at<int>(ctx, L.block_counts), expert_count,
                                  at<int>(ctx, L.pub.offset), at<int>(ctx, L.pub.perm), at<int>(ctx, L.pub.inv),
                                  at<int>(ctx, L.row_token), at<float>(ctx, L.row_gate),
@@ -239,6 +188,202 @@ SPES_API int spes_moe_fwd(const spes_moe_shape* shape, const void* x, const void
   SPES_TRY(launch_combine(dt, at<void>(ctx, L.pub.yp), at<int>(ctx, L.pub.inv), topk_gate, y, T, d, k, s));
   prof_mark(0, "combine", s);
   return SPES_OK;
+}
+
+// given_dgate: out, of a routing that the caller made, whose scores are none of this layer's; NULL: the layer's own router
+int run_bwd(const spes_moe_shape* shape, const void* dy, const void* x, const void* w_router, const void* w_gate, const void* w_up, const void* w_down,
+            void* ctx, const uint8_t* trainable_mask, void* dx, float* d_w_router, float* d_w_gate, float* d_w_up, float* d_w_down, float* given_dgate,
+            int32_t accumulate, void* stream) {
+  SPES_TRY(shape_supported(shape));
+  const bool own_router = given_dgate == nullptr;
+  if (!dy || !x || !w_gate || !w_up || !w_down || !ctx || !trainable_mask || !dx || (own_router && (!w_router || !d_w_router))) return SPES_EINVAL;
+  const int T = shape->T, d = shape->d_model, M = shape->n_experts, f = shape->d_ff, k = shape->top_k, dt = shape->dtype;
+  int n_train = 0;
+  unsigned char train_list[kMaxExperts];
+  for (int e = 0; e < M; ++e)
+    if (trainable_mask[e]) train_list[n_train++] = (unsigned char)e;
+  if (n_train > 0 && (!d_w_gate || !d_w_up || !d_w_down)) return SPES_EINVAL;
+  if (!aligned16(dy) || !aligned16(x) || !aligned16(w_router) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(w_down) ||
+      !aligned16(ctx) || !aligned16(dx) || !aligned16(d_w_router) || !aligned16(d_w_gate) || !aligned16(d_w_up) ||
+      !aligned16(d_w_down) || !aligned16(given_dgate))
+    return SPES_EALIGN;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const Layout L = make_layout(shape);
+  const int* inv = at<int>(ctx, L.pub.inv);
+  const float* gate = at<float>(ctx, L.pub.topk_gate);   // the forward's own copies: its outputs belong to the caller
+  const int* idx = at<int>(ctx, L.pub.topk_idx);
+
+  // u = dy[token] W_d per routed row; its epilogue yields the gate gradient <u, h> (per column tile) and,
+  // through the SwiGLU, da and db of the gate-scaled upstream gradient
+  const long R = (long)T * k;
+  const int n_part = dt == SPES_BF16 ? plan::rowdot_parts(f, L.row_tile_mfma, L.est_tiles_mfma)
+                                      : cdiv(f, L.f32_mfma ? plan::kF32RowdotCols : simt_col_tile());
+  // bf16 storage: the two router contractions run on the matrix cores from a bf16 copy of dlogits
+  const bool router_mfma = own_router && dt == SPES_BF16 && M % 8 == 0;
+  prof_begin(1, s);
+  {
+    GemmArgs g = blank();
+    g.A[0] = dy; g.a_ms = d; g.a_ks = 1; g.a_rows = at<int>(ctx, L.row_token); g.a_elems = (long)T * d;
+    g.B[0] = w_down; g.b_ns = 1; g.b_ks = f; g.b_gs = (long)d * f; g.b_elems = (long)M * d * f;
+    g.Kdim = d; g.Ndim = f;
+    g.E[0] = at<void>(ctx, L.pub.a); g.E[1] = at<void>(ctx, L.pub.b); g.E[2] = at<void>(ctx, L.hcorr);
+    g.C[0] = at<void>(ctx, L.da); g.C[1] = at<void>(ctx, L.db); g.C[2] = at<void>(ctx, L.hg); g.c_ms = f;
+    g.row_scale = at<float>(ctx, L.row_gate);
+    g.rowdot = at<float>(ctx, L.dgate_part); g.rowdot_stride = R;
+    // gate * h feeds only the down-projection weight gradient, which exists for the trainable experts alone
+    for (int e = 0; e < M; ++e)
+      if (!trainable_mask[e]) g.c2_skip |= 1ull << e;
+    ragged_tables(g, ctx, L, dt);
+    SPES_TRY(expert_gemm(L, dt, kRaggedM, kEpiDSwiglu, true, false, g, s));
+  }
+  prof_mark(1, "gemm_dgrad_down_dswiglu", s);
+  if (own_router)
+    SPES_TRY(launch_gating_bwd(at<float>(ctx, L.pub.logits), at<float>(ctx, L.pub.lse), idx, gate, at<float>(ctx, L.dgate_part),
+                             n_part, R, inv, at<float>(ctx, L.pub.dgate), T, M, k, shape->renorm_topk,
+                             at<float>(ctx, L.aux), at<float>(ctx, L.pub.dlogits), router_mfma ? at<bf16_t>(ctx, L.dlogits_bf) : nullptr, s));
+  else
+    SPES_TRY(launch_gate_gradient(at<float>(ctx, L.dgate_part), n_part, R, inv, (int)R, given_dgate, at<float>(ctx, L.pub.dgate), s));
+  prof_mark(1, "gating_bwd", s);
+  // dxp = da W_g + db W_u
+  {
+    GemmArgs g = blank();
+    g.npairs = 2;
+    g.A[0] = at<void>(ctx, L.da); g.A[1] = at<void>(ctx, L.db); g.a_ms = f; g.a_ks = 1; g.a_elems = R * f;
+    g.B[0] = w_gate; g.B[1] = w_up; g.b_ns = 1; g.b_ks = d; g.b_gs = (long)f * d; g.b_elems = (long)M * f * d;
+    g.Kdim = f; g.Ndim = d;
+    g.C[0] = at<void>(ctx, L.dxp); g.c_ms = d;
+    ragged_tables(g, ctx, L, dt);
+    SPES_TRY(expert_gemm(L, dt, kRaggedM, kEpiStore, true, false, g, s));
+  }
+  prof_mark(1, "gemm_dgrad_gate_up", s);
+  // weight gradients of the trainable experts only, into their compact slots
+  if (n_train > 0) {
+    GemmArgs g = blank();
+    g.n_groups = n_train;
+    memcpy(g.group_expert, train_list, n_train);
+    g.n_experts = M;
+    for (int i = 0; i < n_train; ++i) g.groups |= 1ull << train_list[i];
+    g.offset = at<int>(ctx, L.pub.offset);
+    g.mean_k = cdiv(R, M); g.max_k = T;
+    g.c_f32 = 1; g.accumulate = accumulate;
+    // dW_d[d,f] = dy[token]^T (gate * h), dW_g[f,d] = da^T xp, dW_u[f,d] = db^T xp over the expert's rows, as one launch:
+    // a layer of a few thousand tokens has fewer tiles per matrix than the chip has CUs
+    g.n_sets = 3;
+    g.k_rows = at<int>(ctx, L.row_token);
+    g.a_ms = 1; g.b_ns = 1; g.Mdim = d; g.Ndim = f; g.c_gs = (long)d * f;
+    const long x_elems = (long)T * d, h_elems = R * f;
+    g.set[0] = {dy, at<void>(ctx, L.hg), d_w_down, x_elems, h_elems, d, f, f, d, f, 1, 0};
+    g.set[1] = {at<void>(ctx, L.da), x, d_w_gate, h_elems, x_elems, f, d, d, f, d, 0, 1};
+    g.set[2] = {at<void>(ctx, L.db), x, d_w_up, h_elems, x_elems, f, d, d, f, d, 0, 1};
+    SPES_TRY(expert_gemm(L, dt, kGroupedK, kEpiStore, false, false, g, s));
+    prof_mark(1, "wgrad", s);
+  }
+  // dW_r[M,d] = dlogits^T x; the token axis is cut into chunks whose partial products are then added in a fixed order
+  int wr_parts = 0;
+  if (own_router) {
+    GemmArgs g = blank();
+    g.a_ms = 1; g.a_ks = M; g.a_elems = (long)T * M;
+    g.B[0] = x; g.b_ns = 1; g.b_ks = d; g.b_elems = (long)T * d;
+    g.Kdim = T; g.Mdim = M; g.Ndim = d;
+    g.C[0] = at<float>(ctx, L.wr_part); g.c_ms = d; g.c_gs = (long)M * d; g.c_f32 = 1;
+    if (router_mfma) {
+      g.A[0] = at<void>(ctx, L.dlogits_bf);
+      g.kchunk = (cdiv(T, kRouterSplit / 2) + 63) / 64 * 64; g.n_groups = cdiv(T, g.kchunk);
+      SPES_TRY(launch_gemm_mfma(kGroupedK, kEpiStore, false, false, g, s));
+    } else {
+      g.A[0] = at<float>(ctx, L.pub.dlogits);
+      if (L.f32_mfma && M % 4 == 0) {       // (its 16-byte vectors lie along the experts)
+        // chunks of at least a K-tile of its deepest tile
+        g.kchunk = cdiv(T, kRouterSplit) > 128 ? (cdiv(T, kRouterSplit) + 127) / 128 * 128 : 128; g.n_groups = cdiv(T, g.kchunk);
+        SPES_TRY(launch_gemm_f32(kGroupedK, kEpiStore, false, false, g, s));
+      } else {
+        g.kchunk = cdiv(T, kRouterSplit); g.n_groups = cdiv(T, g.kchunk);
+        SPES_TRY(launch_gemm_simt(SPES_F32, dt, kGroupedK, kEpiStore, g, s));
+      }
+    }
+    wr_parts = g.n_groups;
+  }
+  prof_mark(1, "router_wgrad", s);
+  // dx = unpermuted sum of dxp + dlogits W_r; in the same launch the sum of dW_r's partial products
+  SPES_TRY(launch_dx_gather(dt, at<void>(ctx, L.dxp), inv, at<float>(ctx, L.pub.dlogits), router_mfma ? at<bf16_t>(ctx, L.dlogits_bf) : nullptr,
+                            w_router, dx, T, d, k, own_router ? M : 0, at<float>(ctx, L.wr_part), wr_parts, d_w_router, accumulate, s));
+  prof_mark(1, "unpermute_sum_router_dgrad", s);
+  return SPES_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+SPES_API size_t spes_moe_ctx_bytes(const spes_moe_shape* shape) {
+  if (shape_supported(shape) != SPES_OK) return 0;
+  return make_layout(shape).pub.total;
+}
+
+SPES_API int spes_moe_ctx_describe(const spes_moe_shape* shape, spes_moe_ctx_layout* out) {
+  if (out == nullptr) return SPES_EINVAL;
+  SPES_TRY(shape_supported(shape));
+  *out = make_layout(shape).pub;
+  return SPES_OK;
+}
+
+SPES_API int spes_moe_fwd(const spes_moe_shape* shape, const void* x, const void* w_router, const float* router_bias,
+                          const void* w_gate, const void* w_up, const void* w_down, void* y, int32_t* topk_idx,
+                          float* topk_gate, int32_t* expert_count, void* ctx, void* stream) {
+  SPES_TRY(shape_supported(shape));
+  if (!x || !w_router || !w_gate || !w_up || !w_down || !y || !topk_idx || !topk_gate || !expert_count || !ctx)
+    return SPES_EINVAL;
+  if (!aligned16(x) || !aligned16(w_router) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(w_down) || !aligned16(y) ||
+      !aligned16(topk_idx) || !aligned16(topk_gate) || !aligned16(expert_count) || !aligned16(ctx) ||
+      (router_bias && !aligned16(router_bias)))
+    return SPES_EALIGN;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const Layout L = make_layout(shape);
+  const int T = shape->T, d = shape->d_model, M = shape->n_experts, k = shape->top_k, dt = shape->dtype;
+
+  prof_begin(0, s);
+  int logit_parts = 1;
+  // router scores: logits[T,M] = x W_r^T
+  {
+    GemmArgs g = blank();
+    g.A[0] = x; g.a_ms = d; g.a_ks = 1; g.a_elems = (long)T * d;
+    g.B[0] = w_router; g.b_ns = d; g.b_ks = 1; g.b_elems = (long)M * d;
+    g.Kdim = d; g.kchunk = d; g.Mdim = T; g.Ndim = M;
+    g.C[0] = at<float>(ctx, L.pub.logits); g.c_ms = M; g.c_f32 = 1;
+    // the matrix-core epilogue stores four columns at a time; with only M <= 64 output columns the row tiles alone
+    // would occupy a quarter of the CUs, so d_model is cut into partial products that the gating kernel adds up
+    if (dt == SPES_BF16 && M % 4 == 0) {
+      g.kchunk = (cdiv(d, kLogitSplit) + 63) / 64 * 64; g.n_groups = cdiv(d, g.kchunk); g.c_gs = (long)T * M;
+      logit_parts = g.n_groups;
+      SPES_TRY(launch_gemm_mfma(kGroupedK, kEpiStore, true, true, g, s));
+    } else if (L.f32_mfma) {
+      SPES_TRY(launch_gemm_f32(kGroupedK, kEpiStore, true, true, g, s));
+    } else {
+      SPES_TRY(launch_gemm_simt(dt, dt, kGroupedK, kEpiStore, g, s));
+    }
+  }
+  prof_mark(0, "router_gemm", s);
+  SPES_TRY(launch_topk_gate(at<float>(ctx, L.pub.logits), logit_parts, router_bias, T, M, k, shape->renorm_topk, topk_idx, topk_gate,
+                            at<int>(ctx, L.pub.topk_idx), at<float>(ctx, L.pub.topk_gate), at<float>(ctx, L.pub.lse), s));
+  prof_mark(0, "softmax_topk", s);
+  return run_experts_fwd(shape, L, x, w_gate, w_up, w_down, y, topk_idx, topk_gate, expert_count, ctx, s);
+}
+
+SPES_API int spes_moe_fwd_routed(const spes_moe_shape* shape, const void* x, const int32_t* topk_idx, const float* topk_gate, const void* w_gate,
+                                 const void* w_up, const void* w_down, void* y, int32_t* expert_count, void* ctx, void* stream) {
+  SPES_TRY(shape_supported(shape));
+  if (!x || !topk_idx || !topk_gate || !w_gate || !w_up || !w_down || !y || !expert_count || !ctx) return SPES_EINVAL;
+  if (!aligned16(x) || !aligned16(topk_idx) || !aligned16(topk_gate) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(w_down) || !aligned16(y) ||
+      !aligned16(expert_count) || !aligned16(ctx))
+    return SPES_EALIGN;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const Layout L = make_layout(shape);
+  int* const idx = at<int>(ctx, L.pub.topk_idx);
+  float* const gate = at<float>(ctx, L.pub.topk_gate);
+  prof_begin(0, s);
+  SPES_TRY(launch_take_routing(topk_idx, topk_gate, shape->T * shape->top_k, shape->n_experts, idx, gate, s));
+  prof_mark(0, "take_routing", s);
+  return run_experts_fwd(shape, L, x, w_gate, w_up, w_down, y, idx, gate, expert_count, ctx, s);
 }
 
 SPES_API int spes_moe_permute(const spes_moe_shape* shape, const void* x, const void* ctx, void* xp, void* stream) {
@@ -277,117 +422,15 @@ SPES_API int spes_moe_bwd(const spes_moe_shape* shape, const void* dy, const voi
                           const void* w_gate, const void* w_up, const void* w_down, void* ctx,
                           const uint8_t* trainable_mask, void* dx, float* d_w_router, float* d_w_gate, float* d_w_up,
                           float* d_w_down, int32_t accumulate, void* stream) {
-  SPES_TRY(shape_supported(shape));
-  if (!dy || !x || !w_router || !w_gate || !w_up || !w_down || !ctx || !trainable_mask || !dx || !d_w_router) return SPES_EINVAL;
-  const int T = shape->T, d = shape->d_model, M = shape->n_experts, f = shape->d_ff, k = shape->top_k, dt = shape->dtype;
-  int n_train = 0;
-  unsigned char train_list[kMaxExperts];
-  for (int e = 0; e < M; ++e)
-    if (trainable_mask[e]) train_list[n_train++] = (unsigned char)e;
-  if (n_train > 0 && (!d_w_gate || !d_w_up || !d_w_down)) return SPES_EINVAL;
-  if (!aligned16(dy) || !aligned16(x) || !aligned16(w_router) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(w_down) ||
-      !aligned16(ctx) || !aligned16(dx) || !aligned16(d_w_router) || !aligned16(d_w_gate) || !aligned16(d_w_up) ||
-      !aligned16(d_w_down))
-    return SPES_EALIGN;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  const Layout L = make_layout(shape);
-  const int* inv = at<int>(ctx, L.pub.inv);
-  const float* gate = at<float>(ctx, L.pub.topk_gate);   // the forward's own copies: its outputs belong to the caller
-  const int* idx = at<int>(ctx, L.pub.topk_idx);
+  return run_bwd(shape, dy, x, w_router, w_gate, w_up, w_down, ctx, trainable_mask, dx, d_w_router, d_w_gate, d_w_up, d_w_down, nullptr, accumulate, stream);
+}
 
-  // u = dy[token] W_d per routed row; its epilogue yields the gate gradient <u, h> (per column tile) and,
-  // through the SwiGLU, da and db of the gate-scaled upstream gradient
-  const long R = (long)T * k;
-  const int n_part = dt == SPES_BF16 ? plan::rowdot_parts(f, L.row_tile_mfma, L.est_tiles_mfma)
-                                      : cdiv(f, L.f32_mfma ? plan::kF32RowdotCols : simt_col_tile());
-  // bf16 storage: the two router contractions run on the matrix cores from a bf16 copy of dlogits
-  const bool router_mfma = dt == SPES_BF16 && M % 8 == 0;
-  prof_begin(1, s);
-  {
-    GemmArgs g = blank();
-    g.A[0] = dy; g.a_ms = d; g.a_ks = 1; g.a_rows = at<int>(ctx, L.row_token); g.a_elems = (long)T * d;
-    g.B[0] = w_down; g.b_ns = 1; g.b_ks = f; g.b_gs = (long)d * f; g.b_elems = (long)M * d * f;
-    g.Kdim = d; g.Ndim = f;
-    g.E[0] = at<void>(ctx, L.pub.a); g.E[1] = at<void>(ctx, L.pub.b); g.E[2] = at<void>(ctx, L.hcorr);
-    g.C[0] = at<void>(ctx, L.da); g.C[1] = at<void>(ctx, L.db); g.C[2] = at<void>(ctx, L.hg); g.c_ms = f;
-    g.row_scale = at<float>(ctx, L.row_gate);
-    g.rowdot = at<float>(ctx, L.dgate_part); g.rowdot_stride = R;
-    // gate * h feeds only the down-projection weight gradient, which exists for the trainable experts alone
-    for (int e = 0; e < M; ++e)
-      if (!trainable_mask[e]) g.c2_skip |= 1ull << e;
-    ragged_tables(g, ctx, L, dt);
-    SPES_TRY(expert_gemm(L, dt, kRaggedM, kEpiDSwiglu, true, false, g, s));
-  }
-  prof_mark(1, "gemm_dgrad_down_dswiglu", s);
-  SPES_TRY(launch_gating_bwd(at<float>(ctx, L.pub.logits), at<float>(ctx, L.pub.lse), idx, gate, at<float>(ctx, L.dgate_part),
-                             n_part, R, inv, at<float>(ctx, L.pub.dgate), T, M, k, shape->renorm_topk,
-                             at<float>(ctx, L.aux), at<float>(ctx, L.pub.dlogits), router_mfma ? at<bf16_t>(ctx, L.dlogits_bf) : nullptr, s));
-  prof_mark(1, "gating_bwd", s);
-  // dxp = da W_g + db W_u
-  {
-    GemmArgs g = blank();
-    g.npairs = 2;
-    g.A[0] = at<void>(ctx, L.da); g.A[1] = at<void>(ctx, L.db); g.a_ms = f; g.a_ks = 1; g.a_elems = R * f;
-    g.B[0] = w_gate; g.B[1] = w_up; g.b_ns = 1; g.b_ks = d; g.b_gs = (long)f * d; g.b_elems = (long)M * f * d;
-    g.Kdim = f; g.Ndim = d;
-    g.C[0] = at<void>(ctx, L.dxp); g.c_ms = d;
-    ragged_tables(g, ctx, L, dt);
-    SPES_TRY(expert_gemm(L, dt, kRaggedM, kEpiStore, true, false, g, s));
-  }
-  prof_mark(1, "gemm_dgrad_gate_up", s);
-  // weight gradients of the trainable experts only, into their compact slots
-  if (n_train > 0) {
-    GemmArgs g = blank();
-    g.n_groups = n_train;
-    memcpy(g.group_expert, train_list, n_train);
-    g.n_experts = M;
-    for (int i = 0; i < n_train; ++i) g.groups |= 1ull << train_list[i];
-    g.offset = at<int>(ctx, L.pub.offset);
-    g.mean_k = cdiv(R, M); g.max_k = T;
-    g.c_f32 = 1; g.accumulate = accumulate;
-    // dW_d[d,f] = dy[token]^T (gate * h), dW_g[f,d] = da^T xp, dW_u[f,d] = db^T xp over the expert's rows, as one launch:
-    // a layer of a few thousand tokens has fewer tiles per matrix than the chip has CUs
-    g.n_sets = 3;
-    g.k_rows = at<int>(ctx, L.row_token);
-    g.a_ms = 1; g.b_ns = 1; g.Mdim = d; g.Ndim = f; g.c_gs = (long)d * f;
-    const long x_elems = (long)T * d, h_elems = R * f;
-    g.set[0] = {dy, at<void>(ctx, L.hg), d_w_down, x_elems, h_elems, d, f, f, d, f, 1, 0};
-    g.set[1] = {at<void>(ctx, L.da), x, d_w_gate, h_elems, x_elems, f, d, d, f, d, 0, 1};
-    g.set[2] = {at<void>(ctx, L.db), x, d_w_up, h_elems, x_elems, f, d, d, f, d, 0, 1};
-    SPES_TRY(expert_gemm(L, dt, kGroupedK, kEpiStore, false, false, g, s));
-    prof_mark(1, "wgrad", s);
-  }
-  // dW_r[M,d] = dlogits^T x; the token axis is cut into chunks whose partial products are then added in a fixed order
-  int wr_parts = 0;
-  {
-    GemmArgs g = blank();
-    g.a_ms = 1; g.a_ks = M; g.a_elems = (long)T * M;
-    g.B[0] = x; g.b_ns = 1; g.b_ks = d; g.b_elems = (long)T * d;
-    g.Kdim = T; g.Mdim = M; g.Ndim = d;
-    g.C[0] = at<float>(ctx, L.wr_part); g.c_ms = d; g.c_gs = (long)M * d; g.c_f32 = 1;
-    if (router_mfma) {
-      g.A[0] = at<void>(ctx, L.dlogits_bf);
-      g.kchunk = (cdiv(T, kRouterSplit / 2) + 63) / 64 * 64; g.n_groups = cdiv(T, g.kchunk);
-      SPES_TRY(launch_gemm_mfma(kGroupedK, kEpiStore, false, false, g, s));
-    } else {
-      g.A[0] = at<float>(ctx, L.pub.dlogits);
-      if (L.f32_mfma && M % 4 == 0) {       // (its 16-byte vectors lie along the experts)
-        // chunks of at least a K-tile of its deepest tile
-        g.kchunk = cdiv(T, kRouterSplit) > 128 ? (cdiv(T, kRouterSplit) + 127) / 128 * 128 : 128; g.n_groups = cdiv(T, g.kchunk);
-        SPES_TRY(launch_gemm_f32(kGroupedK, kEpiStore, false, false, g, s));
-      } else {
-        g.kchunk = cdiv(T, kRouterSplit); g.n_groups = cdiv(T, g.kchunk);
-        SPES_TRY(launch_gemm_simt(SPES_F32, dt, kGroupedK, kEpiStore, g, s));
-      }
-    }
-    wr_parts = g.n_groups;
-  }
-  prof_mark(1, "router_wgrad", s);
-  // dx = unpermuted sum of dxp + dlogits W_r; in the same launch the sum of dW_r's partial products
-  SPES_TRY(launch_dx_gather(dt, at<void>(ctx, L.dxp), inv, at<float>(ctx, L.pub.dlogits), router_mfma ? at<bf16_t>(ctx, L.dlogits_bf) : nullptr,
-                            w_router, dx, T, d, k, M, at<float>(ctx, L.wr_part), wr_parts, d_w_router, accumulate, s));
-  prof_mark(1, "unpermute_sum_router_dgrad", s);
-  return SPES_OK;
+SPES_API int spes_moe_bwd_routed(const spes_moe_shape* shape, const void* dy, const void* x, const void* w_gate, const void* w_up, const void* w_down,
+                                 void* ctx, const uint8_t* trainable_mask, void* dx, float* dgate, float* d_w_gate, float* d_w_up, float* d_w_down,
+                                 int32_t accumulate, void* stream) {
+  SPES_TRY(shape_supported(shape));
+  if (!dgate) return SPES_EINVAL;
+  return run_bwd(shape, dy, x, nullptr, w_gate, w_up, w_down, ctx, trainable_mask, dx, nullptr, d_w_gate, d_w_up, d_w_down, dgate, accumulate, stream);
 }
 
 SPES_API int spes_masked_adamw(int32_t n_experts, int64_t elems, int32_t dtype, void* param, const uint8_t* trainable_mask,

@@ -19,6 +19,10 @@ int launch_gating_bwd(const float* logits, const float* lse, const int* idx, con
 int launch_router_aux(const float* logits, const float* lse, const int* offset, int T, int M, int k, float lb_coef, float z_coef,
                       float grad_scale, float* part, float* losses, float* aux, hipStream_t s);
 
+// a routing that the caller made, and the gradient of its gates
+int launch_take_routing(const int* idx, const float* gate, int R, int M, int* idx_copy, float* gate_copy, hipStream_t s);
+int launch_gate_gradient(const float* part, int n_part, long part_stride, const int* inv, int R, float* dgate, float* dgate_copy, hipStream_t s);
+
 // movement.hip (dtype = spes_dtype of the storage type)
 int launch_permute(int dtype, const void* x, const int* inv, int k, void* xp, int T, int d, hipStream_t s);
 int launch_combine(int dtype, const void* yp, const int* inv, const float* gate, void* y, int T, int d, int k, hipStream_t s);

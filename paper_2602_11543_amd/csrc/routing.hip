@@ -344,6 +344,31 @@ __global__ __launch_bounds__(256) void gating_bwd_kernel(const float* __restrict
   }
 }
 
+// A routing that the caller made: copies of its choice and gates.  An entry that is no expert counts as expert 0 with gate 0, so that no table
+// built from it reaches beyond its end.
+__global__ __launch_bounds__(256) void take_routing_kernel(const int* __restrict__ idx, const float* __restrict__ gate, int R, int M,
+                                                           int* __restrict__ idx_copy, float* __restrict__ gate_copy) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= R) return;
+  const int e = idx[i];
+  const bool valid = e >= 0 && e < M;
+  idx_copy[i] = valid ? e : 0;
+  gate_copy[i] = valid ? gate[i] : 0.f;
+}
+
+// Gradient of such gates: the column-tile partials of a pair's row, in the order in which gating_bwd_kernel adds them
+__global__ __launch_bounds__(256) void gate_gradient_kernel(const float* __restrict__ part, int n_part, long part_stride, const int* __restrict__ inv,
+                                                            int R, float* __restrict__ dgate, float* __restrict__ dgate_copy) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= R) return;
+  const float* const q = part + inv[i];
+  float sum = 0.f;
+#pragma unroll 8
+  for (int p = 0; p < n_part; ++p) sum += q[p * part_stride];
+  dgate[i] = sum;
+  dgate_copy[i] = sum;
+}
+
 // Partial sums for the auxiliary router losses: per block, sum_t p_te for every expert and sum_t lse_t^2.
 __global__ __launch_bounds__(256) void aux_partial_kernel(const float* __restrict__ logits, const float* __restrict__ lse, int T,
                                                           int M, float* __restrict__ part) {
@@ -443,6 +468,16 @@ int launch_gating_bwd(const float* logits, const float* lse, const int* idx, con
                       float* dlogits, bf16_t* dlogits_bf, hipStream_t s) {
   hipLaunchKernelGGL(gating_bwd_kernel, dim3(cdiv(T, 4)), dim3(256), 0, s, logits, lse, idx, gate, dgate_part, n_part, part_stride,
                      inv, dgate, T, M, k, renorm, aux, dlogits, dlogits_bf);
+  return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
+}
+
+int launch_take_routing(const int* idx, const float* gate, int R, int M, int* idx_copy, float* gate_copy, hipStream_t s) {
+  hipLaunchKernelGGL(take_routing_kernel, dim3(cdiv(R, 256)), dim3(256), 0, s, idx, gate, R, M, idx_copy, gate_copy);
+  return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
+}
+
+int launch_gate_gradient(const float* part, int n_part, long part_stride, const int* inv, int R, float* dgate, float* dgate_copy, hipStream_t s) {
+  hipLaunchKernelGGL(gate_gradient_kernel, dim3(cdiv(R, 256)), dim3(256), 0, s, part, n_part, part_stride, inv, R, dgate, dgate_copy);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
 

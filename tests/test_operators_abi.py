@@ -108,3 +108,30 @@ def test_orthogonalize_and_muon():
     assert muon(mask=none, master=None, m=None, grad=None, scratch=None) == 0
     assert S.spes_orthogonalize_scratch_bytes(0, 8, 8, 0) == 0 and S.spes_orthogonalize_scratch_bytes(1, 8, 20000, 0) == 0
     assert S.spes_orthogonalize_scratch_bytes(2, 64, 96, 0) > S.spes_orthogonalize_scratch_bytes(2, 64, 96, 1) > 0
+
+
+def test_layer_behind_a_given_routing():
+    fwd_, bwd_ = LIB.spes_moe_fwd_routed, LIB.spes_moe_bwd_routed
+    fwd_.restype, fwd_.argtypes = i32, [vp] * 11
+    bwd_.restype, bwd_.argtypes = i32, [vp] * 13 + [i32, vp]
+    shape = S.moe_shape(64, 64, 8, 64, 2, S.SPES_BF16, 0)
+    mask = (ctypes.c_uint8 * 8)(1)
+
+    def fwd(sh=shape, **over):
+        a = {n: P[i] for i, n in enumerate(("x", "idx", "gate", "wg", "wu", "wd", "y", "count", "ctx"))}
+        a.update(over)
+        return fwd_(ctypes.byref(sh), *a.values(), None)
+
+    def bwd(sh=shape, **over):
+        a = dict(dy=P[0], x=P[1], wg=P[2], wu=P[3], wd=P[4], ctx=P[5], mask=ctypes.cast(mask, vp), dx=P[6], dgate=P[7], dg=P[8], du=P[9], dd=P[10])
+        a.update(over)
+        return bwd_(ctypes.byref(sh), *a.values(), 0, None)
+
+    for n in ("x", "idx", "gate", "wg", "wu", "wd", "y", "count", "ctx"):
+        assert fwd(**{n: None}) == EINVAL and fwd(**{n: 0x10008}) == EALIGN, n
+    for n in ("dy", "x", "wg", "wu", "wd", "ctx", "mask", "dx", "dgate", "dg"):
+        assert bwd(**{n: None}) == EINVAL, n
+    for n in ("dy", "x", "wg", "wu", "wd", "ctx", "dx", "dgate", "dg", "du", "dd"):
+        assert bwd(**{n: 0x10008}) == EALIGN, n
+    for f in (fwd, bwd):
+        assert f(S.moe_shape(64, 64, 8, 64, 9, 1, 0)) == EINVAL and f(S.moe_shape(64, 64, 128, 64, 2, 1, 0)) == ESHAPE
