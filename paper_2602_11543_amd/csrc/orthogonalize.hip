@@ -89,10 +89,11 @@ struct Cfg {
   static constexpr bool PLANES = BM == 64 && MINB == 1;     // both planes of a pair side by side in a slot, see the main loop
   static constexpr int UNITS = (NSA * A_VEC + NSB * B_VEC) * (PLANES ? 2 : 1);
   static_assert(4 * SLAB * 4 <= UNITS * 16 && 4 * 4 * SLAB16 <= UNITS * 16, "a float slab, or four of fp16, for every wavefront");
-  static_assert(BM == BN, "mirror images of square tiles");
+  static_assert(BM == BN || 2 * BM == BN, "square tiles, and halves of them");
 };
-// one block per CU: all 160 KB of LDS, 256 accumulators per lane
+// one block per CU: all 160 KB of LDS, 256 accumulators per lane; half of such a tile
 typedef Cfg<256, 256, 3, 2, 1> Tile;
+typedef Cfg<128, 256, 3, 3, 1> TileHalf;
 // two blocks per CU
 typedef Cfg<128, 128, 3, 2, 2> TileSmall;
 // few tiles; on pairs
@@ -105,22 +106,14 @@ typedef Cfg<64, 64, 4, 4, 1> TileTinyPairs;
 // that of gemm_mfma.hip without its masks and index tables: stored matrices are padded, so every K-tile is whole.  Fragments are read a
 // k-step ahead of their MFMAs, and loads, reads and the scalars of the next K-tiles are dealt out over the gaps between MFMAs.
 // SPLIT: operands are pairs.  IN, OUT: planes of what is read beside the product and of the result
+// Tile `in` of matrix `mat`, in squares of BN, of which `half` is the upper or the lower half if BM is less
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C>
-__global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
+__device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, const int mat, const unsigned in, const int half) {
   constexpr int BM = C::BM, BN = C::BN, BK = C::BK, TM = C::TM, TN = C::TN, NSA = C::NSA, NSB = C::NSB, NA = C::NA, NB = C::NB, NP = NA + NB;
   constexpr int A_VEC = C::A_VEC, B_VEC = C::B_VEC, PITCH = C::PITCH;
   constexpr bool SYM = EPI == kGram || EPI == kPoly;
-  __shared__ uint4 smem[C::UNITS];
   const int tid = threadIdx.x, lane = tid & 63, wave = (int)uniform(tid >> 6);
   const int l16 = lane & 15, lq = lane >> 4, wm = wave >> 1, wn = wave & 1;
-
-  // ---- which tile: every XCD (workgroups go round the eight) gets one contiguous range ----
-  const unsigned mt = (unsigned)cdiv(g.M, BM), nt = (unsigned)cdiv(g.N, BN), per = SYM ? mt * (mt + 1) / 2 : mt * nt;
-  const unsigned total = per * (unsigned)g.n, per_xcd = (total + kXcds - 1) / kXcds;
-  const unsigned slot = blockIdx.x / kXcds, t_ = (blockIdx.x % kXcds) * per_xcd + slot;
-  if (slot >= per_xcd || t_ >= total) return;
-  const int mat = (int)uniform(t_ / per);
-  const unsigned in = t_ - (unsigned)mat * per;
   unsigned mi, ni;
   if (SYM) {
     mi = (unsigned)((sqrtf(8.f * (float)in + 1.f) - 1.f) * 0.5f);
@@ -129,11 +122,13 @@ __global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
     ni = in - mi * (mi + 1) / 2;
   } else {
     // row tiles four at a time, the column tiles inside: what an XCD works on at once shares four row panels
+    const unsigned mt = (unsigned)cdiv(g.M, BN), nt = (unsigned)cdiv(g.N, BN);
     const unsigned group = in / (4 * nt), within = in - group * 4 * nt, left = mt - group * 4, rows = left < 4 ? left : 4;
     ni = within / rows;
     mi = group * 4 + (within - ni * rows);
   }
-  const int m0 = (int)uniform(mi * BM), n0 = (int)uniform(ni * BN);
+  const int m0 = (int)uniform(mi * BN + (unsigned)half * BM), n0 = (int)uniform(ni * BN);
+  if (BM != BN && m0 >= g.M) return;
 
   // ---- operands: buffer resources whose base moves with the K-tile and that end with the operand, behind which loads deliver zeros; a lane's
   // byte offsets are fixed ----
@@ -562,6 +557,31 @@ __global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
   }
 }
 
+// Every XCD (workgroups go round the eight) gets one contiguous range of the tiles.  A last round of full tiles that is at most half full runs on
+// halves of them (CH, plan::tiles_cut), dealt out by themselves: 8 of 3584 x 4864, 840 tiles of G 498 -> 465 us, of P 387 -> 366.
+template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C, typename CH>
+__global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
+  __shared__ uint4 smem[C::UNITS > CH::UNITS ? C::UNITS : CH::UNITS];
+  constexpr bool SYM = EPI == kGram || EPI == kPoly;
+  const unsigned mt = (unsigned)cdiv(g.M, C::BN), nt = (unsigned)cdiv(g.N, C::BN), per = SYM ? mt * (mt + 1) / 2 : mt * nt;
+  const unsigned total = per * (unsigned)g.n, cut = C::BM != CH::BM ? plan::tiles_cut(total, 0) : 0, whole = total - cut;
+  const unsigned first_half = (whole + kXcds - 1) / kXcds * kXcds;
+  const bool halves = C::BM != CH::BM && blockIdx.x >= first_half;
+  const unsigned block = halves ? blockIdx.x - first_half : blockIdx.x, count = halves ? 2 * cut : whole;
+  const unsigned per_xcd = (count + kXcds - 1) / kXcds, slot = block / kXcds, at = (block % kXcds) * per_xcd + slot;
+  if (slot >= per_xcd || at >= count) return;
+  const unsigned tile = halves ? whole + at / 2 : at;
+  const int mat = (int)uniform(tile / per);
+  const unsigned in = tile - (unsigned)mat * per;
+  if constexpr (C::BM != CH::BM) {
+    if (halves) {
+      ns_tile<EPI, B_KC, SPLIT, IN, OUT, T, CH>(g, smem, mat, in, (int)(at & 1));
+      return;
+    }
+  }
+  ns_tile<EPI, B_KC, SPLIT, IN, OUT, T, C>(g, smem, mat, in, 0);
+}
+
 // ---- into the scaled form, and the momentum ----
 
 struct PrepArgs {
@@ -747,17 +767,18 @@ Buffers buffers(int n, int rows, int cols, int dtype) {
   return b;
 }
 
-template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C>
+template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C, typename CH = C>
 int launch_tiles(const NsArgs& g, hipStream_t s) {
-  const long mt = cdiv(g.M, C::BM), nt = cdiv(g.N, C::BN);
-  const long total = (EPI == kGram || EPI == kPoly ? mt * (mt + 1) / 2 : mt * nt) * g.n;
-  hipLaunchKernelGGL((ns_gemm_kernel<EPI, B_KC, SPLIT, IN, OUT, T, C>), dim3((unsigned)((total + kXcds - 1) / kXcds * kXcds)), dim3(256), 0, s, g);
+  const long mt = cdiv(g.M, C::BN), nt = cdiv(g.N, C::BN);
+  const long total = (EPI == kGram || EPI == kPoly ? mt * (mt + 1) / 2 : mt * nt) * g.n, cut = C::BM != CH::BM ? plan::tiles_cut((unsigned)total, 0) : 0;
+  const long blocks = (long)round_up(total - cut, kXcds) + (long)round_up(2 * cut, kXcds);
+  hipLaunchKernelGGL((ns_gemm_kernel<EPI, B_KC, SPLIT, IN, OUT, T, C, CH>), dim3((unsigned)blocks), dim3(256), 0, s, g);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T>
 int launch_product(const NsArgs& g, hipStream_t s) {
   const int side = plan::square_tile(g.M, g.N, g.n, EPI == kGram || EPI == kPoly);
-  if (side == Tile::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, Tile>(g, s);
+  if (side == Tile::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, Tile, TileHalf>(g, s);
   if (side == TileSmall::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, TileSmall>(g, s);
   return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, std::conditional_t<SPLIT, TileTinyPairs, TileTiny>>(g, s);
 }

@@ -145,6 +145,7 @@ inline int f32_row_tile(long rows, int n_experts, int d_model, int d_ff) {
 //   128   0.45 and 0.77 (one 1280 x 1536 matrix, 55 and 120 tiles, 24 and 20 K-tiles: 15.9 and 13.3 us against 34.1 and 28.4; 8 of 3584 x
 //         4864, 3248 tiles, 76 K-tiles: 614 against 498, in rounds of 97 and 124)
 //   64    0.27 and 0.47 (that matrix's 210 and 480 tiles: 9.3 and 13.7 us)
+// and 0.65 for a last round of 256-wide ones that tiles_cut halves.
 constexpr int square_tile(int rows, int cols, int n, bool symmetric) {
   constexpr int side[3] = {256, 128, 64};
   constexpr double alone[3] = {1.0, 0.45, 0.27}, paired[3] = {1.0, 0.77, 0.47};
@@ -153,7 +154,8 @@ constexpr int square_tile(int rows, int cols, int n, bool symmetric) {
   for (int i = 0; i < 3; ++i) {
     const long mt = (rows + side[i] - 1) / side[i], nt = (cols + side[i] - 1) / side[i];
     const long count = (symmetric ? mt * (mt + 1) / 2 : mt * nt) * n, at_once = i == 0 ? 256 : 512, rest = count % at_once;
-    const double cost = (count / at_once) * paired[i] + (rest == 0 ? 0.0 : rest <= 256 ? alone[i] : paired[i]);
+    const double last = rest == 0 ? 0.0 : i == 0 ? (2 * rest <= 256 ? 0.65 : 1.0) : rest <= 256 ? alone[i] : paired[i];
+    const double cost = (count / at_once) * paired[i] + last;
     if (i == 0 || cost < least) { least = cost; best = side[i]; }
   }
   return best;

@@ -212,7 +212,7 @@ def test_larger_matrices(device, dtype, n, rows, cols):
     near(out[0], exact(src[0]), out_allow(dtype))
 
 
-SIDES = [(40, 520, 780, 256), (40, 780, 520, 256), (3, 1000, 1300, 128), (2, 300, 200, 64)]      # tests/test_operators_plan.py holds the sides
+SIDES = [(40, 520, 780, 256), (40, 780, 520, 256), (180, 500, 761, 256), (2, 1000, 1300, 128), (2, 300, 200, 64)]      # tests/test_operators_plan.py holds the sides
 
 
 @TYPES
