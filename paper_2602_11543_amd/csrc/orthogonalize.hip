@@ -94,8 +94,9 @@ struct Cfg {
 // one block per CU: all 160 KB of LDS, 256 accumulators per lane; half of such a tile
 typedef Cfg<256, 256, 3, 2, 1> Tile;
 typedef Cfg<128, 256, 3, 3, 1> TileHalf;
-// two blocks per CU
+// two blocks per CU; half of such a tile
 typedef Cfg<128, 128, 3, 2, 2> TileSmall;
+typedef Cfg<64, 128, 4, 3, 2> TileSmallHalf;
 // few tiles; on pairs
 typedef Cfg<64, 64, 5, 5, 2> TileTiny;
 typedef Cfg<64, 64, 4, 4, 1> TileTinyPairs;
@@ -557,14 +558,15 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
   }
 }
 
-// Every XCD (workgroups go round the eight) gets one contiguous range of the tiles.  A last round of full tiles that is at most half full runs on
-// halves of them (CH, plan::tiles_cut), dealt out by themselves: 8 of 3584 x 4864, 840 tiles of G 498 -> 465 us, of P 387 -> 366.
+// Every XCD (workgroups go round the eight) gets one contiguous range of the tiles.  A last round of tiles that leaves half of the CUs or more
+// without one runs on halves of them (CH, plan::square_cut), dealt out by themselves: 8 of 3584 x 4864, 840 tiles of G 498 -> 465 us, of P
+// 387 -> 366; one of 1280 x 1536, 120 tiles of the step 13.9 -> 11.4.
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C, typename CH>
 __global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
   __shared__ uint4 smem[C::UNITS > CH::UNITS ? C::UNITS : CH::UNITS];
   constexpr bool SYM = EPI == kGram || EPI == kPoly;
   const unsigned mt = (unsigned)cdiv(g.M, C::BN), nt = (unsigned)cdiv(g.N, C::BN), per = SYM ? mt * (mt + 1) / 2 : mt * nt;
-  const unsigned total = per * (unsigned)g.n, cut = C::BM != CH::BM ? plan::tiles_cut(total, 0) : 0, whole = total - cut;
+  const unsigned total = per * (unsigned)g.n, cut = C::BM != CH::BM ? (unsigned)plan::square_cut(C::BM, total) : 0, whole = total - cut;
   const unsigned first_half = (whole + kXcds - 1) / kXcds * kXcds;
   const bool halves = C::BM != CH::BM && blockIdx.x >= first_half;
   const unsigned block = halves ? blockIdx.x - first_half : blockIdx.x, count = halves ? 2 * cut : whole;
@@ -770,7 +772,7 @@ Buffers buffers(int n, int rows, int cols, int dtype) {
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C, typename CH = C>
 int launch_tiles(const NsArgs& g, hipStream_t s) {
   const long mt = cdiv(g.M, C::BN), nt = cdiv(g.N, C::BN);
-  const long total = (EPI == kGram || EPI == kPoly ? mt * (mt + 1) / 2 : mt * nt) * g.n, cut = C::BM != CH::BM ? plan::tiles_cut((unsigned)total, 0) : 0;
+  const long total = (EPI == kGram || EPI == kPoly ? mt * (mt + 1) / 2 : mt * nt) * g.n, cut = C::BM != CH::BM ? plan::square_cut(C::BM, total) : 0;
   const long blocks = (long)round_up(total - cut, kXcds) + (long)round_up(2 * cut, kXcds);
   hipLaunchKernelGGL((ns_gemm_kernel<EPI, B_KC, SPLIT, IN, OUT, T, C, CH>), dim3((unsigned)blocks), dim3(256), 0, s, g);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
@@ -779,7 +781,7 @@ template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T>
 int launch_product(const NsArgs& g, hipStream_t s) {
   const int side = plan::square_tile(g.M, g.N, g.n, EPI == kGram || EPI == kPoly);
   if (side == Tile::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, Tile, TileHalf>(g, s);
-  if (side == TileSmall::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, TileSmall>(g, s);
+  if (side == TileSmall::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, TileSmall, TileSmallHalf>(g, s);
   return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, std::conditional_t<SPLIT, TileTinyPairs, TileTiny>>(g, s);
 }
 // a last step; matrices of few rows in bf16 storage, the only ones on pairs there, have few tiles

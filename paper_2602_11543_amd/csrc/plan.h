@@ -139,22 +139,29 @@ inline int f32_row_tile(long rows, int n_experts, int d_model, int d_ff) {
   return est * (cols_d < cols_f ? cols_d : cols_f) >= kF32Blocks ? kF32Rows : kF32ShortRows;
 }
 
+// Square tiles of a symmetric or plain product of several matrices that run as two halves: a last round of 256-wide ones (one block per CU, 256 at
+// once) or of 128-wide ones (two, 512) that leaves half of the CUs or more without a tile.
+constexpr long square_cut(int side, long count) {
+  const long rest = count % (side == 256 ? 256 : 512);
+  return side >= 128 && rest <= 128 ? rest : 0;
+}
+
 // Side of the square tiles of a product of n matrices, rows x cols each, of a symmetric one only the tiles on and below the diagonal: 256 (one
 // block per CU), 128 or 64 (two).  A launch costs its number of rounds; what a round costs relative to one of 256-wide tiles, where no CU has
 // a second block and where some have:
 //   128   0.45 and 0.77 (one 1280 x 1536 matrix, 55 and 120 tiles, 24 and 20 K-tiles: 15.9 and 13.3 us against 34.1 and 28.4; 8 of 3584 x
 //         4864, 3248 tiles, 76 K-tiles: 614 against 498, in rounds of 97 and 124)
 //   64    0.27 and 0.47 (that matrix's 210 and 480 tiles: 9.3 and 13.7 us)
-// and 0.65 for a last round of 256-wide ones that tiles_cut halves.
+// A last round that square_cut halves costs 0.65 and 0.36 (3 of 1000 x 1300, 108 tiles, 21 and 16 K-tiles: 14.6 -> 10.2 and 12.8 -> 9.3 us).
 constexpr int square_tile(int rows, int cols, int n, bool symmetric) {
   constexpr int side[3] = {256, 128, 64};
-  constexpr double alone[3] = {1.0, 0.45, 0.27}, paired[3] = {1.0, 0.77, 0.47};
+  constexpr double alone[3] = {1.0, 0.45, 0.27}, paired[3] = {1.0, 0.77, 0.47}, halved[3] = {0.65, 0.36, 0};
   int best = 256;
   double least = 0;
   for (int i = 0; i < 3; ++i) {
     const long mt = (rows + side[i] - 1) / side[i], nt = (cols + side[i] - 1) / side[i];
     const long count = (symmetric ? mt * (mt + 1) / 2 : mt * nt) * n, at_once = i == 0 ? 256 : 512, rest = count % at_once;
-    const double last = rest == 0 ? 0.0 : i == 0 ? (2 * rest <= 256 ? 0.65 : 1.0) : rest <= 256 ? alone[i] : paired[i];
+    const double last = rest == 0 ? 0.0 : square_cut(side[i], count) ? halved[i] : rest <= 256 ? alone[i] : paired[i];
     const double cost = (count / at_once) * paired[i] + last;
     if (i == 0 || cost < least) { least = cost; best = side[i]; }
   }

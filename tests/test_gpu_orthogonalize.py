@@ -265,3 +265,11 @@ def test_binding_refuses_wrong_tensors(device):
         k.update(bad)
         with pytest.raises(S.SpesError):
             S.spes_orthogonalize(2, 32, 48, S.SPES_F32, **k)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,cols", [(1100, 1300), (1300, 1100)])
+def test_optimizer_step_on_halves_of_small_tiles(device, rows, cols, dtype):
+    muon(device, dtype, 2, np.array([0, 1], dtype=np.uint8), rows, cols, True, check=(0,))
+    src = matrices(1, rows, cols, 5).to(dtype).cuda()
+    near(run(src)[0], exact(src[0]), out_allow(dtype))

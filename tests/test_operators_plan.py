@@ -11,16 +11,22 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SHIM = """
 #include "plan.h"
 extern "C" int square_tile(int rows, int cols, int n, int symmetric) { return spes::plan::square_tile(rows, cols, n, symmetric != 0); }
+extern "C" int square_cut(int side, int count) { return (int)spes::plan::square_cut(side, count); }
 """
 
 
 @pytest.fixture(scope="module")
-def square_tile(tmp_path_factory):
+def lib(tmp_path_factory):
     d = tmp_path_factory.mktemp("plan")
     (d / "shim.cpp").write_text(SHIM)
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2602_11543_amd", "csrc"),
                     str(d / "shim.cpp"), "-o", str(d / "shim.so")], check=True)
-    return ctypes.CDLL(str(d / "shim.so")).square_tile
+    return ctypes.CDLL(str(d / "shim.so"))
+
+
+@pytest.fixture(scope="module")
+def square_tile(lib):
+    return lib.square_tile
 
 
 @pytest.mark.parametrize("n,rows,cols,side", SIDES)
@@ -46,3 +52,19 @@ def test_never_more_than_a_round_dearer_than_full_tiles(square_tile):
                 side = square_tile(lo, hi, n, 0)
                 small = -(-lo // side) * -(-hi // side) * n
                 assert side == 256 or small <= 1024 * -(-full // 256)
+
+
+def test_halves(lib):
+    """Of 256-wide and 128-wide tiles, a last round of 256 or 512 that has at most one tile for every second CU."""
+    for side, count, want in [(256, 840, 72), (256, 896, 128), (256, 897, 0), (256, 512, 0), (128, 120, 120), (128, 129, 0), (128, 512 + 64, 64),
+                              (128, 512, 0), (64, 100, 0)]:
+        assert lib.square_cut(side, count) == want, (side, count)
+
+
+def test_device_tests_reach_halves(lib, square_tile):
+    reached = set()
+    for n, rows, cols, side in SIDES + [(1, 1100, 1300, 128)]:
+        lo, hi = (-(-v // 64) * 64 for v in sorted((rows, cols)))
+        mt, nt = -(-lo // side), -(-hi // side)
+        reached |= {(side, symmetric) for symmetric, count in ((0, mt * nt * n), (1, mt * (mt + 1) // 2 * n)) if lib.square_cut(side, count)}
+    assert reached >= {(256, 0), (256, 1), (128, 0), (128, 1)}
