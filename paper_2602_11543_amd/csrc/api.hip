@@ -614,7 +614,7 @@ SPES_API const char* spes_strerror(int code) {
   switch (code) {
     case SPES_OK: return "ok";
     case SPES_EINVAL: return "invalid argument (null pointer, non-positive size, top_k > n_experts or unknown dtype)";
-    case SPES_ESHAPE: return "unsupported shape (n_experts > 64, a feature size not a multiple of 8, or too many rows/trainers)";
+    case SPES_ESHAPE: return "unsupported shape (a size beyond the limit of the call; of the expert layer n_experts > 64, a feature size not a multiple of 8, or too many rows/trainers)";
     case SPES_EALIGN: return "device pointer not 16-byte aligned";
     case SPES_EHIP: return "HIP kernel launch failed";
     default: return "unknown error";

@@ -70,6 +70,8 @@ struct FwdArgs {
   float *mean, *rstd;
 };
 
+// Bound by memory where there are many rows: 32768 x 4096 bf16, both residual streams, 197 us, 1.07 GB at 5.4 TB/s (a copy of 2 GiB runs at 4.9).  4096 x
+// 768 6.7 us, 200 x 2048 3.8, most of it the launch and one way to memory and back.
 template <typename T, int LPR, int NU, Ends ENDS, bool LAYER, bool ONCE>
 __global__ __launch_bounds__(256) void norm_fwd_kernel(const FwdArgs a) {
   constexpr int RPB = 256 / LPR, W = 16 / (int)sizeof(T);
@@ -156,6 +158,9 @@ struct BwdArgs {
   bool bias;
 };
 
+// At most 512 blocks, each with its sums of dw and db in registers until its rows are done: 32768 x 4096 bf16, 176 us, 1.07 GB at 6.1 TB/s; 4096 x 768 7.1 us.
+// Then norm_columns_kernel adds the blocks' sums in a fixed order, 3.6 us of 768 columns, 4.8 of 4096: atomics would save that launch and give
+// another gradient every time.
 template <typename T, int LPR, int NU, Ends ENDS, bool LAYER, bool ONCE>
 __global__ __launch_bounds__(256) void norm_bwd_kernel(const BwdArgs a) {
   constexpr int RPB = 256 / LPR, N = LAYER ? 2 : 1, W = 16 / (int)sizeof(T);

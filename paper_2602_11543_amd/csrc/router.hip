@@ -4,7 +4,8 @@
 //      idx = the k largest c in open groups, equal ones to the lower expert    gate = scale s[idx] (/ sum of s[idx], renorm)
 // Sixteen lanes hold a token, four consecutive experts to a lane and quad, so a wavefront works on four tokens and every
 // reduction stays within a row of lanes, in data-parallel-primitive steps.  What bounds it is the instructions of the choice, not the 4 M
-// bytes of a token.
+// bytes of a token: 32768 tokens over 64 experts, top-8, 12.6 us for 10 MB; 16384 over 256 in 8 groups of which 4 are open, 17.4 us for
+// 18 MB (each with 1.4 to 2.6 us for the launch that clears the counts); 48 over 64 4.2 us.
 //
 // Gradient, the choice held fixed, with g the gates' share (scale taken out) and u = scale dgate.  Every difference is between gradients, weighted by
 // shares, so nothing cancels when one expert takes all:
@@ -19,8 +20,6 @@
 
 namespace spes {
 namespace {
-
-
 
 constexpr int kRow = 16;                       // lanes of a token
 // Every block adds its counts to all experts' at its end, and what is added to one address waits in line.  16384 tokens over 256 experts in blocks of
@@ -309,7 +308,8 @@ __device__ __forceinline__ float weighted_differences(float w, float u) {
   return d;
 }
 
-// WHOLE: softmax without renormalisation, where every score has a gradient.  Otherwise only the k chosen ones are read.
+// WHOLE: softmax without renormalisation, where every score has a gradient.  Otherwise only the k chosen ones are read, and
+// the row of dlogits is put together in LDS and goes out whole: 16384 x 256 5.9 us, 32768 x 64 4.8 (17 and 8 MB written).
 template <int NQ, bool SOFTMAX, bool WHOLE>
 __global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a) {
   constexpr int V = NQ * 4;
