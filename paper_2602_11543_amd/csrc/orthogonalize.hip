@@ -81,13 +81,14 @@ template <int BM_, int BN_, int NSA_, int NSB_, int MINB_>
 struct Cfg {
   static constexpr int BM = BM_, BN = BN_, MINB = MINB_;
   static constexpr int NSA = NSA_, NSB = NSB_;              // LDS slots of each operand, one K-tile each
-  static constexpr int BK = 64, TM = BM / 32, TN = BN / 32; // 16 x 16 MFMA tiles per wavefront along m, n
+  static constexpr int WM = BM < 64 ? 1 : 2, QM = BM / WM, QN = BN * WM / 4;      // wavefronts along m, and the part of the tile that each has
+  static constexpr int BK = 64, TM = QM / 16, TN = QN / 16; // 16 x 16 MFMA tiles per wavefront along m, n
   static constexpr int NA = BM / 32, NB = BN / 32;          // 1 KB loads per wavefront and K-tile
   static constexpr int A_VEC = BM * 8, B_VEC = BN * 8;      // 16-byte units of a slot
   // epilogue slabs, 32 rows of a wavefront's quarter: floats, or bytes of fp16 (rows 4 or 36 banks apart: the sixteen rows of a write miss each other)
-  static constexpr int PITCH = BN / 2 + 4, SLAB = 32 * PITCH, PITCH16 = BN + 16, SLAB16 = 32 * PITCH16;
-  static constexpr bool PLANES = BM == 64 && MINB == 1;     // both planes of a pair side by side in a slot, see the main loop
-  static constexpr int UNITS = (NSA * A_VEC + NSB * B_VEC) * (PLANES ? 2 : 1);
+  static constexpr int PITCH = QN + 4, SLAB = 32 * PITCH, PITCH16 = 2 * QN + 16, SLAB16 = 32 * PITCH16;
+  static constexpr bool STAGED = BN == 64 && (BM < 64 || MINB == 1);      // both planes of a pair, or two K-tiles, side by side in a slot, see the main loop
+  static constexpr int UNITS = (NSA * A_VEC + NSB * B_VEC) * (STAGED ? 2 : 1);
   static_assert(4 * SLAB * 4 <= UNITS * 16 && 4 * 4 * SLAB16 <= UNITS * 16, "a float slab, or four of fp16, for every wavefront");
   static_assert(BM == BN || 2 * BM == BN, "square tiles, and halves of them");
 };
@@ -99,9 +100,11 @@ typedef Cfg<128, 128, 3, 2, 2> TileSmall;
 typedef Cfg<64, 128, 4, 3, 2> TileSmallHalf;
 // few tiles; on pairs
 typedef Cfg<64, 64, 5, 5, 2> TileTiny;
+typedef Cfg<32, 64, 3, 3, 2> TileTinyHalf;
 typedef Cfg<64, 64, 4, 4, 1> TileTinyPairs;
+typedef Cfg<32, 64, 4, 4, 1> TileTinyPairsHalf;
 
-// One BM x BN tile of one product, of a symmetric one (kGram, kPoly) with its mirror image.  Four wavefronts, each a quarter of the tile as TM x TN
+// One BM x BN tile of one product, of a symmetric one (kGram, kPoly) with its mirror image.  Four wavefronts, each a quarter of the tile (QM x QN) as TM x TN
 // MFMA tiles of 16 x 16.  Operands come straight into LDS, K-tiles of 64, three or two of them at a time: A, and B with B_KC, as
 // [row][k], else B as [k][column], read through the transposing read; both permuted within a row against bank conflicts.  The main loop is
 // that of gemm_mfma.hip without its masks and index tables: stored matrices are padded, so every K-tile is whole.  Fragments are read a
@@ -113,11 +116,11 @@ typedef Cfg<64, 64, 4, 4, 1> TileTinyPairs;
 // Tile `in` of matrix `mat`, in squares of BN, of which `half` is the upper or the lower half if BM is less
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C>
 __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, const int mat, const unsigned in, const int half) {
-  constexpr int BM = C::BM, BN = C::BN, BK = C::BK, TM = C::TM, TN = C::TN, NSA = C::NSA, NSB = C::NSB, NA = C::NA, NB = C::NB, NP = NA + NB;
+  constexpr int BM = C::BM, BN = C::BN, QM = C::QM, QN = C::QN, BK = C::BK, TM = C::TM, TN = C::TN, NSA = C::NSA, NSB = C::NSB, NA = C::NA, NB = C::NB, NP = NA + NB;
   constexpr int A_VEC = C::A_VEC, B_VEC = C::B_VEC, PITCH = C::PITCH;
   constexpr bool SYM = EPI == kGram || EPI == kPoly;
   const int tid = threadIdx.x, lane = tid & 63, wave = (int)uniform(tid >> 6);
-  const int l16 = lane & 15, lq = lane >> 4, wm = wave >> 1, wn = wave & 1;
+  const int l16 = lane & 15, lq = lane >> 4, wm = C::WM == 1 ? 0 : wave >> 1, wn = C::WM == 1 ? wave : wave & 1;
   unsigned mi, ni;
   if (SYM) {
     mi = (unsigned)((sqrtf(8.f * (float)in + 1.f) - 1.f) * 0.5f);
@@ -170,69 +173,73 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
       else asm("" : "+v"(acc[j][i]));
     }
 
-  if constexpr (C::PLANES) {
-    // On the smallest tile a wavefront has eight MFMAs in a K-tile, less than its meeting and its reads take.  So all four planes of a K-tile are
-    // loaded at once, which is 24 MFMAs of a wavefront for one meeting and four loads in place of six, in four stages of LDS.  Against the loop below,
-    // over the pairs one after the other: 4 matrices of 512 x 256, products of 10.2, 6.9 and 7.3 us 7.8, 6.2 and 6.5, the call 122 -> 105.
-    static_assert(SPLIT && NSA == NSB, "whole stages of pairs");
+  if constexpr (C::STAGED) {
+    // On the smallest tiles a wavefront has four or eight MFMAs in a K-tile, less than its meeting and its reads take.  So all four planes of
+    // a K-tile are loaded at once, which is 24 MFMAs of a wavefront for one meeting and four loads in place of six, in four stages of LDS; where operands
+    // are not pairs, two K-tiles, in the order of the loop below.  Against that loop, over the pairs one after the other: 4 matrices of 512 x 256 in
+    // fp32, products of 10.2, 6.9 and 7.3 us 7.8, 6.2 and 6.5, the call 122 -> 105.  (On squares of 64 without pairs it takes 9.7 us for that one's 8.9, 210 tiles.)
+    static_assert(NSA == NSB, "whole stages");
     constexpr int STAGE = 2 * (A_VEC + B_VEC), STAGES = NSA;
     const unsigned a_lo = uniform((unsigned)g.a_lo * 2u), b_lo = uniform((unsigned)g.b_lo * 2u);
     const unsigned lds0 = (unsigned)(unsigned long)(__attribute__((address_space(3))) uint4*)smem + (unsigned)wave * 1024u;
     auto load_stage = [&](int k, int s) {
-      const unsigned inside = k < nk ? ~0u : 0u;
 #pragma unroll
       for (int two = 0; two < 2; ++two) {
-        const unsigned dst = lds0 + (unsigned)(s * STAGE + two * A_VEC) * 16u;
-        const rsrc_t ra = make_rsrc(a_base + (two ? a_lo : 0u) + (unsigned long)((unsigned)k * a_step), (a_bytes - (unsigned)k * a_step) & inside);
-        const rsrc_t rb = make_rsrc(b_base + (two ? b_lo : 0u) + (unsigned long)((unsigned)k * b_step), (b_bytes - (unsigned)k * b_step) & inside);
+        const int t = SPLIT ? k : 2 * k + two;
+        const unsigned inside = t < nk ? ~0u : 0u, ahead = (unsigned)t;
+        const unsigned a_dst = lds0 + (unsigned)(s * STAGE + two * A_VEC) * 16u, b_dst = lds0 + (unsigned)(s * STAGE + 2 * A_VEC + two * B_VEC) * 16u;
+        const rsrc_t ra = make_rsrc(a_base + (SPLIT && two ? a_lo : 0u) + (unsigned long)(ahead * a_step), (a_bytes - ahead * a_step) & inside);
+        const rsrc_t rb = make_rsrc(b_base + (SPLIT && two ? b_lo : 0u) + (unsigned long)(ahead * b_step), (b_bytes - ahead * b_step) & inside);
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
-          const unsigned d = set_lds_dest(dst + (unsigned)i * 4096u);
+          const unsigned d = set_lds_dest(a_dst + (unsigned)i * 4096u);
           one_instruction();
           load_to_lds(ra, aoff[i], d);
         }
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          const unsigned d = set_lds_dest(dst + 2 * A_VEC * 16u + (unsigned)i * 4096u);
+          const unsigned d = set_lds_dest(b_dst + (unsigned)i * 4096u);
           one_instruction();
           load_to_lds(rb, boff[i], d);
         }
       }
     };
     const int kc_pos = lq ^ (l16 >> 1);
-    const uint4* const a_kc = smem + (wm * (BM / 2) + l16) * 8;
-    const uint4* const b_kc = smem + 2 * A_VEC + (wn * (BN / 2) + l16) * 8;
+    const uint4* const a_kc = smem + (wm * QM + l16) * 8;
+    const uint4* const b_kc = smem + 2 * A_VEC + (wn * QN + l16) * 8;
     const bf16_t* const b_tr = reinterpret_cast<const bf16_t*>(smem + 2 * A_VEC) + (lq * 8 + (l16 >> 2)) * BN + (lane & 3) * 4;
     for (int s = 0; s < STAGES - 1; ++s) load_stage(s, s);
     int cur = 0, fill = STAGES - 1;
-    for (int k = 0; k < nk; ++k) {
+    const int ns = SPLIT ? nk : (nk + 1) / 2;
+    for (int k = 0; k < ns; ++k) {
       wait_and_meet<(STAGES - 2) * 2 * NP>();
       load_stage(k + STAGES - 1, fill);
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
+      for (int turn = 0; turn < 2; ++turn) {
         f16x8 fa[2][TM], fb[2][TN];
 #pragma unroll
-        for (int two = 0; two < 2; ++two) {
+        for (int x = 0; x < 2; ++x) {
+          const int two = SPLIT ? x : turn, ks = SPLIT ? turn : x;         // both planes at a k-step, or both k-steps of a K-tile
 #pragma unroll
-          for (int i = 0; i < TM; ++i) fa[two][i] = __builtin_bit_cast(f16x8, a_kc[cur * STAGE + two * A_VEC + i * 128 + (kc_pos ^ (ks * 4))]);
+          for (int i = 0; i < TM; ++i) fa[x][i] = __builtin_bit_cast(f16x8, a_kc[cur * STAGE + two * A_VEC + i * 128 + (kc_pos ^ (ks * 4))]);
 #pragma unroll
           for (int j = 0; j < TN; ++j) {
             if (B_KC) {
-              fb[two][j] = __builtin_bit_cast(f16x8, b_kc[cur * STAGE + two * B_VEC + j * 128 + (kc_pos ^ (ks * 4))]);
+              fb[x][j] = __builtin_bit_cast(f16x8, b_kc[cur * STAGE + two * B_VEC + j * 128 + (kc_pos ^ (ks * 4))]);
             } else {
-              const bf16_t* p = b_tr + (cur * STAGE + two * B_VEC) * 8 + ks * 32 * BN + ((wn * (BN / 32) + j) ^ (l16 >> 2)) * 16;
+              const bf16_t* p = b_tr + (cur * STAGE + two * B_VEC) * 8 + ks * 32 * BN + ((wn * TN + j) ^ (l16 >> 2)) * 16;
               const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 4 * BN);
-              fb[two][j] = __builtin_bit_cast(f16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+              fb[x][j] = __builtin_bit_cast(f16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
             }
           }
         }
 #pragma unroll
-        for (int pass = 0; pass < 3; ++pass)          // lo hi, hi lo, hi hi
+        for (int pass = 0; pass < (SPLIT ? 3 : 2); ++pass)          // lo hi, hi lo, hi hi; or the k-steps
 #pragma unroll
           for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int i = 0; i < TM; ++i)
-              acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[pass == 1][j], fa[pass == 0][i], acc[j][i], 0, 0, 0);
+              acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fb[pass == 1][j], fa[SPLIT ? pass == 0 : pass][i], acc[j][i], 0, 0, 0);
       }
       cur = cur + 1 == STAGES ? 0 : cur + 1;
       fill = fill + 1 == STAGES ? 0 : fill + 1;
@@ -281,11 +288,11 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
 
     f16x8 fa[2][TM], fb[2][TN];
     const int kc_pos = lq ^ (l16 >> 1);
-    const uint4* const a_kc = smem + (wm * (BM / 2) + l16) * 8;
-    const uint4* const b_kc = smem + NSA * A_VEC + (wn * (BN / 2) + l16) * 8;
+    const uint4* const a_kc = smem + (wm * QM + l16) * 8;
+    const uint4* const b_kc = smem + NSA * A_VEC + (wn * QN + l16) * 8;
     const bf16_t* const b_tr = reinterpret_cast<const bf16_t*>(smem + NSA * A_VEC) + (lq * 8 + (l16 >> 2)) * BN + (lane & 3) * 4;
     // (sixteen columns u of a k-row stand at position u ^ (k & 3) of their four)
-    auto tr_pos = [&](int j) { return ((wn * (BN / 32) + j) ^ (l16 >> 2)) * 16; };
+    auto tr_pos = [&](int j) { return ((wn * TN + j) ^ (l16 >> 2)) * 16; };
     auto read_frag_b = [&](int s, int ks, int set, int j) {
       if (B_KC) {
         fb[set][j] = __builtin_bit_cast(f16x8, b_kc[s * B_VEC + j * 128 + (kc_pos ^ (ks * 4))]);
@@ -381,8 +388,8 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
 
   // ---- epilogue: 32 rows of the wavefront's quarter at a time, turned through LDS so that lanes lie along the columns ----
   const float f1 = g.factor ? g.factor[mat] : 1.f, f = EPI == kGram ? f1 * f1 : f1;
-  constexpr int CPR = BN / 16, RPI = 64 / CPR, NST = 32 / RPI;         // lanes per row (eight columns each), rows at a time
-  const int e_row = m0 + wm * (BM / 2) + lane / CPR, e_col = n0 + wn * (BN / 2) + lane % CPR * 8;
+  constexpr int CPR = QN / 8, RPI = 64 / CPR, NST = 32 / RPI;         // lanes per row (eight columns each), rows at a time
+  const int e_row = m0 + wm * QM + lane / CPR, e_col = n0 + wn * QN + lane % CPR * 8;
   if constexpr (EPI == kLast || EPI == kUpdate) {
     // The result goes to the caller's matrix, turned if it is tall: W columns of a row of it to a lane.  kUpdate: w <- keep w - rate o in 32 bits, and
     // its copy in the expert store; the weights of 32 rows are requested ahead of the stores of those before.  Tiles inside the
@@ -391,14 +398,14 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
     const float alpha = g.alpha * f;
     float* const slab = reinterpret_cast<float*>(smem) + wave * C::SLAB;
     constexpr int W = EPI == kUpdate ? 4 : 16 / (int)sizeof(T);
-    constexpr int LPR = BN / 2 / W, RUNS = 32 / W;       // lanes per row; turned: runs of W rows, which are columns of the result
-    constexpr int STEPS = BN / 2 * 32 / W / 64;
+    constexpr int LPR = QN / W, RUNS = 32 / W;       // lanes per row; turned: runs of W rows, which are columns of the result
+    constexpr int STEPS = QN * 32 / W / 64;
     const long first = (long)mat * g.rows * g.cols;
     __syncthreads();
     auto finish = [&](auto whole_c, auto tall_c) {
       constexpr bool WHOLE = decltype(whole_c)::value, TALL = decltype(tall_c)::value;
-      auto row_of = [&](int i, int st) { return TALL ? n0 + wn * (BN / 2) + st * (64 / RUNS) + lane / RUNS : m0 + wm * (BM / 2) + i * 32 + st * (64 / LPR) + lane / LPR; };
-      auto col_of = [&](int i) { return TALL ? m0 + wm * (BM / 2) + i * 32 + lane % RUNS * W : n0 + wn * (BN / 2) + lane % LPR * W; };
+      auto row_of = [&](int i, int st) { return TALL ? n0 + wn * QN + st * (64 / RUNS) + lane / RUNS : m0 + wm * QM + i * 32 + st * (64 / LPR) + lane / LPR; };
+      auto col_of = [&](int i) { return TALL ? m0 + wm * QM + i * 32 + lane % RUNS * W : n0 + wn * QN + lane % LPR * W; };
       auto left_of = [&](int i, int st) { return WHOLE ? W : row_of(i, st) < g.rows ? g.cols - col_of(i) : 0; };
       auto at = [&](int i, int st) { return left_of(i, st) > 0 ? (long)row_of(i, st) * g.cols + col_of(i) : 0l; };
       T* const param = static_cast<T*>(g.param) + (EPI == kUpdate ? g.param_at[mat] : 0l);
@@ -412,7 +419,7 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
       };
       load_w(0);
 #pragma unroll
-      for (int i = 0; i < BM / 64; ++i) {
+      for (int i = 0; i < QM / 32; ++i) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -444,7 +451,7 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
             for (int e = 0; e < W; ++e) o[st][e] = fmaf(-g.rate, o[st][e], g.keep * x[e]);
           }
         }
-        if (i + 1 < BM / 64) load_w(i + 1);
+        if (i + 1 < QM / 32) load_w(i + 1);
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
           if constexpr (EPI == kUpdate) {
@@ -490,10 +497,10 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
     };
     load_in(0);
     const float alpha = g.alpha * f, beta = g.beta * f;
-    const int d0 = m0 + wm * (BM / 2) - n0 - wn * (BN / 2) + l16 - lq * 4;        // row less column of a lane's element r: d0 + 16 (i - j) - r
+    const int d0 = m0 + wm * QM - n0 - wn * QN + l16 - lq * 4;        // row less column of a lane's element r: d0 + 16 (i - j) - r
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < BM / 64; ++i) {
+    for (int i = 0; i < QM / 32; ++i) {
       if constexpr (IN > 0) {
 #pragma unroll
         for (int st = 0; st < NST; ++st) {
@@ -502,7 +509,7 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
           if constexpr (IN > 1) *reinterpret_cast<rsrc_t*>(p + SLAB16) = in1[st];
         }
         wave_lds_order();
-        if (i + 1 < BM / 64) load_in(i + 1);          // ahead of the stores, behind which they would wait
+        if (i + 1 < QM / 32) load_in(i + 1);          // ahead of the stores, behind which they would wait
       }
 #pragma unroll
       for (int j = 0; j < TN; ++j)
@@ -546,10 +553,10 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
           store16(out_rs[two], off(i, st), *reinterpret_cast<const rsrc_t*>(from + (st * RPI + lane / CPR) * PITCH16 + lane % CPR * 16));
         if (SYM && mi != ni) {
           // the mirror image through the transposing read: sixteen columns by four runs of eight rows
-          const int col = m0 + wm * (BM / 2) + i * 32 + lq * 8;
-          const unsigned at = col < g.M ? (unsigned)(n0 + wn * (BN / 2) + l16) * row_bytes + (unsigned)col * 2u : 1u << 31;
+          const int col = m0 + wm * QM + i * 32 + lq * 8;
+          const unsigned at = col < g.M ? (unsigned)(n0 + wn * QN + l16) * row_bytes + (unsigned)col * 2u : 1u << 31;
 #pragma unroll
-          for (int st = 0; st < BN / 32; ++st) {
+          for (int st = 0; st < TN; ++st) {
             const bf16_t* const p = reinterpret_cast<const bf16_t*>(from + (lq * 8 + (l16 >> 2)) * PITCH16 + (st * 16 + (lane & 3) * 4) * 2);
             const uint2 x = lds_read_tr(p), y = lds_read_tr(p + 4 * (PITCH16 / 2));
             store16(out_rs[two], at + (unsigned)(st * 16) * row_bytes, rsrc_t{x.x, x.y, y.x, y.y});
@@ -563,7 +570,8 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
 
 // Every XCD (workgroups go round the eight) gets one contiguous range of the tiles.  A last round of tiles that leaves half of the CUs or more
 // without one runs on halves of them (CH, plan::square_cut), dealt out by themselves: 8 of 3584 x 4864, 840 tiles of G 498 -> 465 us, of P
-// 387 -> 366; one of 1280 x 1536, 120 tiles of the step 13.9 -> 11.4.
+// 387 -> 366; one of 1280 x 1536, 120 tiles of the step 13.9 -> 11.4; 4 of 512 x 256, 40, 40 and 128 tiles of 64,
+// fp32 8.2, 6.2, 6.2 -> 6.4, 4.9, 5.6, the call 106 -> 88, bf16 5.2, 4.5, 4.4 -> 4.4, 3.9, 3.9.
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C, typename CH>
 __global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
   __shared__ uint4 smem[C::UNITS > CH::UNITS ? C::UNITS : CH::UNITS];
@@ -788,13 +796,13 @@ int launch_product(const NsArgs& g, hipStream_t s) {
   const int side = plan::square_tile(g.M, g.N, g.n, EPI == kGram || EPI == kPoly);
   if (side == Tile::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, Tile, TileHalf>(g, s);
   if (side == TileSmall::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, TileSmall, TileSmallHalf>(g, s);
-  return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, std::conditional_t<SPLIT, TileTinyPairs, TileTiny>>(g, s);
+  return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, std::conditional_t<SPLIT, TileTinyPairs, TileTiny>, std::conditional_t<SPLIT, TileTinyPairsHalf, TileTinyHalf>>(g, s);
 }
 // a last step; matrices of few rows in bf16 storage, the only ones on pairs there, have few tiles
 template <Epi EPI, typename T>
 int launch_end(bool pairs, const NsArgs& g, hipStream_t s) {
   if constexpr (sizeof(T) == 4) return launch_product<EPI, false, true, 0, 0, T>(g, s);
-  else return pairs ? launch_tiles<EPI, false, true, 0, 0, T, TileTinyPairs>(g, s) : launch_product<EPI, false, false, 0, 0, T>(g, s);
+  else return pairs ? launch_tiles<EPI, false, true, 0, 0, T, TileTinyPairs, TileTinyPairsHalf>(g, s) : launch_product<EPI, false, false, 0, 0, T>(g, s);
 }
 
 // carried: steps that take X with its remainder, in bf16 storage

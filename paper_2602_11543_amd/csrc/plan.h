@@ -140,10 +140,10 @@ inline int f32_row_tile(long rows, int n_experts, int d_model, int d_ff) {
 }
 
 // Square tiles of a symmetric or plain product of several matrices that run as two halves: a last round of 256-wide ones (one block per CU, 256 at
-// once) or of 128-wide ones (two, 512) that leaves half of the CUs or more without a tile.
+// once), of 128-wide or 64-wide ones (two, 512) that leaves half of the CUs or more without a tile.
 constexpr long square_cut(int side, long count) {
   const long rest = count % (side == 256 ? 256 : 512);
-  return side >= 128 && rest <= 128 ? rest : 0;
+  return rest <= 128 ? rest : 0;
 }
 
 // Side of the square tiles of a product of n matrices, rows x cols each, of a symmetric one only the tiles on and below the diagonal: 256 (one
@@ -152,10 +152,11 @@ constexpr long square_cut(int side, long count) {
 //   128   0.45 and 0.77 (one 1280 x 1536 matrix, 55 and 120 tiles, 24 and 20 K-tiles: 15.9 and 13.3 us against 34.1 and 28.4; 8 of 3584 x
 //         4864, 3248 tiles, 76 K-tiles: 614 against 498, in rounds of 97 and 124)
 //   64    0.27 and 0.47 (that matrix's 210 and 480 tiles: 9.3 and 13.7 us)
-// A last round that square_cut halves costs 0.65 and 0.36 (3 of 1000 x 1300, 108 tiles, 21 and 16 K-tiles: 14.6 -> 10.2 and 12.8 -> 9.3 us).
+// A last round that square_cut halves costs 0.65 and 0.36 (3 of 1000 x 1300, 108 tiles, 21 and 16 K-tiles: 14.6 -> 10.2 and 12.8 -> 9.3 us); what one of
+// 64-wide ones costs decides nothing, those are taken in any case.
 constexpr int square_tile(int rows, int cols, int n, bool symmetric) {
   constexpr int side[3] = {256, 128, 64};
-  constexpr double alone[3] = {1.0, 0.45, 0.27}, paired[3] = {1.0, 0.77, 0.47}, halved[3] = {0.65, 0.36, 0};
+  constexpr double alone[3] = {1.0, 0.45, 0.27}, paired[3] = {1.0, 0.77, 0.47}, halved[3] = {0.65, 0.36, 0.27};
   int best = 256;
   double least = 0;
   for (int i = 0; i < 3; ++i) {

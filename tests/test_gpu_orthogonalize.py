@@ -212,7 +212,8 @@ def test_larger_matrices(device, dtype, n, rows, cols):
     near(out[0], exact(src[0]), out_allow(dtype))
 
 
-SIDES = [(40, 520, 780, 256), (40, 780, 520, 256), (180, 500, 761, 256), (2, 1000, 1300, 128), (2, 300, 200, 64)]      # tests/test_operators_plan.py holds the sides
+# tests/test_operators_plan.py holds the sides
+SIDES = [(40, 520, 780, 256), (40, 780, 520, 256), (180, 500, 761, 256), (2, 1000, 1300, 128), (4, 1000, 990, 128), (2, 300, 200, 64), (15, 250, 256, 64)]
 
 
 @TYPES

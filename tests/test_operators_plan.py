@@ -55,9 +55,9 @@ def test_never_more_than_a_round_dearer_than_full_tiles(square_tile):
 
 
 def test_halves(lib):
-    """Of 256-wide and 128-wide tiles, a last round of 256 or 512 that has at most one tile for every second CU."""
+    """Of 256-wide tiles a last round of 256, of others of 512, that has at most one tile for every second CU."""
     for side, count, want in [(256, 840, 72), (256, 896, 128), (256, 897, 0), (256, 512, 0), (128, 120, 120), (128, 129, 0), (128, 512 + 64, 64),
-                              (128, 512, 0), (64, 100, 0)]:
+                              (128, 512, 0), (64, 100, 100), (64, 150, 0)]:
         assert lib.square_cut(side, count) == want, (side, count)
 
 
@@ -66,5 +66,7 @@ def test_device_tests_reach_halves(lib, square_tile):
     for n, rows, cols, side in SIDES + [(1, 1100, 1300, 128)]:
         lo, hi = (-(-v // 64) * 64 for v in sorted((rows, cols)))
         mt, nt = -(-lo // side), -(-hi // side)
-        reached |= {(side, symmetric) for symmetric, count in ((0, mt * nt * n), (1, mt * (mt + 1) // 2 * n)) if lib.square_cut(side, count)}
-    assert reached >= {(256, 0), (256, 1), (128, 0), (128, 1)}
+        for symmetric, count in ((0, mt * nt * n), (1, mt * (mt + 1) // 2 * n)):
+            cut = lib.square_cut(side, count)
+            reached |= {(side, symmetric, kind) for kind, tiles in (("whole", count - cut), ("halves", cut)) if tiles}
+    assert reached == {(side, symmetric, kind) for side in (256, 128, 64) for symmetric in (0, 1) for kind in ("whole", "halves")}
