@@ -35,7 +35,8 @@ constexpr int kFewRows = 32;                   // up to so many, operands are pa
 constexpr int kSumBlocks = 256;                // partial sums of squares of a matrix, at most
 constexpr int kSlots = 64;                     // matrices of an optimizer launch
 
-enum Epi { kGram, kPoly, kStep, kLast, kUpdate };      // kLast, kUpdate: a step whose result is the caller's, or his weights' update
+enum Epi { kGram, kPoly, kStep, kLast, kUpdate, kPart };      // kLast, kUpdate: a step whose result is the caller's, or his weights' update; kPart: a
+                                                              // part of kGram's sum, of K-tiles that blockIdx.y says
 
 struct NsArgs {
   const f16 *A, *B, *E;
@@ -47,6 +48,8 @@ struct NsArgs {
   float alpha, beta;                           // result = (alpha product + beta E) factor
   float diagonal;                              // kPoly: added to the diagonal
   const float* factor;                         // of each matrix, NULL: 1.  kGram: squared
+  float* part;                                 // kPart: [parts][n][M][M]
+  int k_tiles;                                 // kPart: of a part
   // the end: rows x cols as the caller has them
   void *out, *param;
   float* master;
@@ -118,7 +121,7 @@ template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename 
 __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, const int mat, const unsigned in, const int half) {
   constexpr int BM = C::BM, BN = C::BN, QM = C::QM, QN = C::QN, BK = C::BK, TM = C::TM, TN = C::TN, NSA = C::NSA, NSB = C::NSB, NA = C::NA, NB = C::NB, NP = NA + NB;
   constexpr int A_VEC = C::A_VEC, B_VEC = C::B_VEC, PITCH = C::PITCH;
-  constexpr bool SYM = EPI == kGram || EPI == kPoly;
+  constexpr bool SYM = EPI == kGram || EPI == kPoly || EPI == kPart;
   const int tid = threadIdx.x, lane = tid & 63, wave = (int)uniform(tid >> 6);
   const int l16 = lane & 15, lq = lane >> 4, wm = C::WM == 1 ? 0 : wave >> 1, wn = C::WM == 1 ? wave : wave & 1;
   unsigned mi, ni;
@@ -139,13 +142,16 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
 
   // ---- operands: buffer resources whose base moves with the K-tile and that end with the operand, behind which loads deliver zeros; a lane's
   // byte offsets are fixed ----
-  const int nk = (int)uniform((unsigned)g.K / BK), nsteps = SPLIT ? 3 * nk : nk;
+  static_assert(EPI != kPart || B_KC, "parts along the rows of both operands");
+  const int k0 = EPI == kPart ? (int)blockIdx.y * g.k_tiles : 0;
+  const int nk = (int)uniform(EPI == kPart ? (unsigned)min(g.k_tiles, g.K / BK - k0) : (unsigned)g.K / BK), nsteps = SPLIT ? 3 * nk : nk;
   auto base_of = [](const f16* p, long elems) -> unsigned long {
     const unsigned long v = reinterpret_cast<unsigned long>(p + elems);
     return (unsigned long)uniform((unsigned)(v >> 32)) << 32 | uniform((unsigned)v);
   };
-  const unsigned long a_base = base_of(g.A, mat * g.a_ms), b_base = base_of(g.B, mat * g.b_ms);
-  const unsigned a_bytes = uniform((unsigned)g.M * (unsigned)g.lda * 2u), b_bytes = uniform((unsigned)(B_KC ? g.N : g.K) * (unsigned)g.ldb * 2u);
+  const unsigned long a_base = base_of(g.A, mat * g.a_ms + k0 * BK), b_base = base_of(g.B, mat * g.b_ms + k0 * BK);
+  const unsigned a_bytes = uniform(((unsigned)g.M * (unsigned)g.lda - (unsigned)(k0 * BK)) * 2u);
+  const unsigned b_bytes = uniform(((unsigned)(B_KC ? g.N : g.K) * (unsigned)g.ldb - (unsigned)(k0 * BK)) * 2u);
   const unsigned a_step = BK * 2u, b_step = uniform(B_KC ? BK * 2u : (unsigned)g.ldb * (BK * 2u));       // bytes per K-tile
   const int kc_chunk = (lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7);
   constexpr int BCH = BN / 8;       // 16-byte chunks per k-row
@@ -390,7 +396,13 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
   const float f1 = g.factor ? g.factor[mat] : 1.f, f = EPI == kGram ? f1 * f1 : f1;
   constexpr int CPR = QN / 8, RPI = 64 / CPR, NST = 32 / RPI;         // lanes per row (eight columns each), rows at a time
   const int e_row = m0 + wm * QM + lane / CPR, e_col = n0 + wn * QN + lane % CPR * 8;
-  if constexpr (EPI == kLast || EPI == kUpdate) {
+  if constexpr (EPI == kPart) {
+    float* const out = g.part + ((long)blockIdx.y * g.n + mat) * g.M * g.M + (long)(m0 + wm * QM + l16) * g.M + n0 + wn * QN + lq * 4;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int i = 0; i < TM; ++i) *reinterpret_cast<f32x4*>(out + (long)(i * 16) * g.M + j * 16) = acc[j][i];
+  } else if constexpr (EPI == kLast || EPI == kUpdate) {
     // The result goes to the caller's matrix, turned if it is tall: W columns of a row of it to a lane.  kUpdate: w <- keep w - rate o in 32 bits, and
     // its copy in the expert store; the weights of 32 rows are requested ahead of the stores of those before.  Tiles inside the
     // matrix (WHOLE) have no guards, behind which every load would be waited for by itself: 16 of 1024 x 2048, the last step 132 -> 107 us, 8 of
@@ -575,7 +587,7 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C, typename CH>
 __global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
   __shared__ uint4 smem[C::UNITS > CH::UNITS ? C::UNITS : CH::UNITS];
-  constexpr bool SYM = EPI == kGram || EPI == kPoly;
+  constexpr bool SYM = EPI == kGram || EPI == kPoly || EPI == kPart;
   const unsigned mt = (unsigned)cdiv(g.M, C::BN), nt = (unsigned)cdiv(g.N, C::BN), per = SYM ? mt * (mt + 1) / 2 : mt * nt;
   const unsigned total = per * (unsigned)g.n, cut = C::BM != CH::BM ? (unsigned)plan::square_cut(C::BM, total) : 0, whole = total - cut;
   const unsigned first_half = (whole + kXcds - 1) / kXcds * kXcds;
@@ -592,7 +604,41 @@ __global__ __launch_bounds__(256, C::MINB) void ns_gemm_kernel(const NsArgs g) {
       return;
     }
   }
-  ns_tile<EPI, B_KC, SPLIT, IN, OUT, T, C>(g, smem, mat, in, 0);
+  if constexpr (EPI != kPart) ns_tile<EPI, B_KC, SPLIT, IN, OUT, T, C>(g, smem, mat, in, 0);      // (parts are of few tiles: halves)
+}
+
+// kGram from its parts, added in their order: four columns of a row to a thread, eight parts requested at once (beyond the last one through the
+// buffer's end: zeros).  Below the diagonal's tiles the mirror image is written too.
+template <int OUT>
+__global__ __launch_bounds__(256) void ns_join_kernel(const NsArgs g, int parts) {
+  const int at = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4, size = g.M * g.M, mat = blockIdx.y;
+  const int r = at / g.M, c = at - r * g.M;
+  if (at >= size || r / 64 < c / 64) return;
+  const unsigned step = (unsigned)(g.n * size) * 4u;
+  const __amdgpu_buffer_rsrc_t rs = tile_rsrc(reinterpret_cast<unsigned long>(g.part + (long)mat * size), (unsigned)(parts * g.n - mat) * (unsigned)size * 4u);
+  float v[4] = {};
+  for (int first = 0; first < parts; first += 8) {
+    f32x4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)((unsigned)at * 4u + (unsigned)(first + k) * step), 0, 0));
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += x[k][e];
+  }
+  const float f = g.factor ? g.factor[mat] : 1.f, alpha = g.alpha * (f * f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] *= alpha;
+  f16 plane[2][4];
+  split<4>(v, plane[0], plane[1]);
+#pragma unroll
+  for (int two = 0; two < OUT; ++two) {
+    f16* const out = g.C + mat * g.c_ms + two * g.c_lo;
+    *reinterpret_cast<f16x4*>(out + (long)r * g.ldc + c) = f16x4{plane[two][0], plane[two][1], plane[two][2], plane[two][3]};
+    if (r / 64 > c / 64)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[(long)(c + e) * g.ldc + r] = plane[two][e];
+  }
 }
 
 // ---- into the scaled form, and the momentum ----
@@ -760,8 +806,8 @@ struct Buffers {
   int lo, hi, lo_p, hi_p;
   bool pairs;                         // every operand with its remainder
   int planes;                         // of G and P; X has two
-  int sum_blocks;
-  size_t part, factor, x[2], g, p, total;
+  int sum_blocks, gram_parts;
+  size_t part, factor, x[2], g, p, gram, total;
 };
 
 Buffers buffers(int n, int rows, int cols, int dtype) {
@@ -779,16 +825,18 @@ Buffers buffers(int n, int rows, int cols, int dtype) {
   for (int i = 0; i < 2; ++i) b.x[i] = take((size_t)n * 2 * b.lo_p * b.hi_p * 2);
   b.g = take((size_t)n * b.planes * b.lo_p * b.lo_p * 2);
   b.p = take((size_t)n * b.planes * b.lo_p * b.lo_p * 2);
+  b.gram_parts = plan::gram_parts(b.lo_p, b.hi_p, n, b.pairs);
+  b.gram = take(b.gram_parts > 1 ? (size_t)b.gram_parts * n * b.lo_p * b.lo_p * 4 : 0);
   b.total = off;
   return b;
 }
 
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T, typename C, typename CH = C>
-int launch_tiles(const NsArgs& g, hipStream_t s) {
+int launch_tiles(const NsArgs& g, hipStream_t s, int parts = 1) {
   const long mt = cdiv(g.M, C::BN), nt = cdiv(g.N, C::BN);
-  const long total = (EPI == kGram || EPI == kPoly ? mt * (mt + 1) / 2 : mt * nt) * g.n, cut = C::BM != CH::BM ? plan::square_cut(C::BM, total) : 0;
+  const long total = (EPI == kGram || EPI == kPoly || EPI == kPart ? mt * (mt + 1) / 2 : mt * nt) * g.n, cut = C::BM != CH::BM ? plan::square_cut(C::BM, total) : 0;
   const long blocks = (long)round_up(total - cut, kXcds) + (long)round_up(2 * cut, kXcds);
-  hipLaunchKernelGGL((ns_gemm_kernel<EPI, B_KC, SPLIT, IN, OUT, T, C, CH>), dim3((unsigned)blocks), dim3(256), 0, s, g);
+  hipLaunchKernelGGL((ns_gemm_kernel<EPI, B_KC, SPLIT, IN, OUT, T, C, CH>), dim3((unsigned)blocks, (unsigned)parts), dim3(256), 0, s, g);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T>
@@ -803,6 +851,14 @@ template <Epi EPI, typename T>
 int launch_end(bool pairs, const NsArgs& g, hipStream_t s) {
   if constexpr (sizeof(T) == 4) return launch_product<EPI, false, true, 0, 0, T>(g, s);
   else return pairs ? launch_tiles<EPI, false, true, 0, 0, T, TileTinyPairs, TileTinyPairsHalf>(g, s) : launch_product<EPI, false, false, 0, 0, T>(g, s);
+}
+
+template <bool SPLIT, int OUT>
+int launch_gram_parts(const NsArgs& g, int parts, hipStream_t s) {
+  const int rc = launch_tiles<kPart, true, SPLIT, 0, 0, float, std::conditional_t<SPLIT, TileTinyPairs, TileTiny>, std::conditional_t<SPLIT, TileTinyPairsHalf, TileTinyHalf>>(g, s, parts);
+  if (rc != SPES_OK) return rc;
+  hipLaunchKernelGGL((ns_join_kernel<OUT>), dim3((unsigned)(g.M * g.M / 1024), (unsigned)g.n), dim3(256), 0, s, g, parts);
+  return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
 
 // carried: steps that take X with its remainder, in bf16 storage
@@ -842,7 +898,14 @@ int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool m
     q.C = G; q.c_ms = b.planes * gs; q.c_lo = b.pairs ? gs : 0; q.ldc = b.lo_p;
     q.alpha = ldexpf(1.f, kGBits - 2 * kXBits); q.beta = 0.f; q.factor = factor;
     q.E = G; q.e_ms = 0; q.e_lo = 0; q.lde = b.lo_p;
-    int rc = b.pairs ? launch_product<kGram, true, true, 0, 2, float>(q, s) : launch_product<kGram, true, false, 0, 1, float>(q, s);
+    int rc;
+    if (b.gram_parts > 1) {
+      q.part = reinterpret_cast<float*>(scratch + b.gram);
+      q.k_tiles = cdiv(b.hi_p / 64, b.gram_parts);
+      rc = b.pairs ? launch_gram_parts<true, 2>(q, b.gram_parts, s) : launch_gram_parts<false, 1>(q, b.gram_parts, s);
+    } else {
+      rc = b.pairs ? launch_product<kGram, true, true, 0, 2, float>(q, s) : launch_product<kGram, true, false, 0, 1, float>(q, s);
+    }
     if (rc != SPES_OK) return rc;
     q.A = q.B = q.E = G; q.a_ms = q.b_ms = q.e_ms = b.planes * gs; q.a_lo = q.b_lo = gs; q.e_lo = b.pairs ? gs : 0; q.lda = q.ldb = b.lo_p;
     q.K = b.lo_p; q.C = P;

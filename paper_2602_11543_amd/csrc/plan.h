@@ -169,5 +169,16 @@ constexpr int square_tile(int rows, int cols, int n, bool symmetric) {
   return best;
 }
 
+// Parts of the contraction of a symmetric product of n matrices, sides lo, over hi (multiples of 64), where few tiles have a long one: as many as there
+// are CUs for, of four K-tiles at least.  Their sums pass through memory (up to 4 MB) and a launch of its own adds them up, about 3.5 us, which 22
+// K-tiles of pairs or 44 others gain and fewer do not: 4 of 128 x 2320 in fp32 (36 K-tiles) 15.6 -> 5.2 + 3.4 us, one of 300 x 4864 in bf16 (76) 14.8 -> 5.3
+// + 3.5, but one of 64 x 1024 (16) 4.7 -> 3.5 + 2.6.
+constexpr int gram_parts(int lo, int hi, int n, bool pairs) {
+  const long mt = lo / 64, halves = mt * (mt + 1) * n, k_tiles = hi / 64;
+  if (halves > 64 || k_tiles * (pairs ? 2 : 1) < 44) return 1;
+  const long by_cus = 256 / halves, by_length = k_tiles / 4, parts = by_cus < by_length ? by_cus : by_length, each = (k_tiles + parts - 1) / parts;
+  return (int)((k_tiles + each - 1) / each);
+}
+
 }  // namespace plan
 }  // namespace spes

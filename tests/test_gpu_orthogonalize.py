@@ -274,3 +274,18 @@ def test_optimizer_step_on_halves_of_small_tiles(device, rows, cols, dtype):
     muon(device, dtype, 2, np.array([0, 1], dtype=np.uint8), rows, cols, True, check=(0,))
     src = matrices(1, rows, cols, 5).to(dtype).cuda()
     near(run(src)[0], exact(src[0]), out_allow(dtype))
+
+
+# parts where operands are pairs, which tests/test_operators_plan.py holds; others have as many from 44 K-tiles on
+PARTS = [(1, 64, 2900, 10), (4, 128, 2900, 10), (4, 2900, 128, 10), (1, 300, 4864, 8), (2, 35, 3300, 13), (1, 20, 2900, 10), (3, 100, 1500, 6)]
+
+
+@TYPES
+@pytest.mark.parametrize("n,rows,cols,parts", PARTS)
+def test_long_contraction_in_parts(device, n, rows, cols, parts, dtype):
+    src = matrices(n, rows, cols, parts).to(dtype).cuda()
+    out = run(src)
+    for i in {0, n - 1}:
+        near(out[i], exact(src[i]), out_allow(dtype))
+    assert torch.equal(out, run(src))
+    muon(device, dtype, n + 1, np.array([1] * n + [0], dtype=np.uint8), rows, cols, False, check=(0,))

@@ -5,13 +5,14 @@ import subprocess
 
 import pytest
 
-from test_gpu_orthogonalize import SIDES
+from test_gpu_orthogonalize import PARTS, SIDES
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SHIM = """
 #include "plan.h"
 extern "C" int square_tile(int rows, int cols, int n, int symmetric) { return spes::plan::square_tile(rows, cols, n, symmetric != 0); }
 extern "C" int square_cut(int side, int count) { return (int)spes::plan::square_cut(side, count); }
+extern "C" int gram_parts(int lo, int hi, int n, int pairs) { return spes::plan::gram_parts(lo, hi, n, pairs != 0); }
 """
 
 
@@ -70,3 +71,12 @@ def test_device_tests_reach_halves(lib, square_tile):
             cut = lib.square_cut(side, count)
             reached |= {(side, symmetric, kind) for kind, tiles in (("whole", count - cut), ("halves", cut)) if tiles}
     assert reached == {(side, symmetric, kind) for side in (256, 128, 64) for symmetric in (0, 1) for kind in ("whole", "halves")}
+
+
+@pytest.mark.parametrize("n,rows,cols,parts", PARTS + [(1, 64, 1344, 1), (40, 64, 4864, 1), (1, 512, 4864, 1), (32, 64, 4864, 4)])
+def test_parts(lib, n, rows, cols, parts):
+    """Few tiles with a long contraction; every part has K-tiles, and halves of all the tiles at once have a CU each."""
+    lo, hi = (-(-v // 64) * 64 for v in sorted((rows, cols)))
+    assert lib.gram_parts(lo, hi, n, 1) == parts and lib.gram_parts(lo, hi, n, 0) == (parts if hi // 64 >= 44 else 1)
+    each = -(-(hi // 64) // parts)
+    assert (parts - 1) * each < hi // 64 and (parts == 1 or parts * n * (lo // 64) * (lo // 64 + 1) <= 256)
