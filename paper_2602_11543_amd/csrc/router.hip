@@ -220,7 +220,8 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const int e = q * 64 + l * 4 + c, i = q * 4 + c;
-        const float x = (SOFTMAX ? __expf(v[i] - mx) * inv : sigmoid_near(v[i])) + bias[i];
+        float x = (SOFTMAX ? __expf(v[i] - mx) * inv : sigmoid_near(v[i])) + bias[i];
+        x = x != x ? -INFINITY : x;                          // (of a minimum with a NaN the other one is left: a NaN would stand for it in the scan below)
         const double mine = choice_of(x, (unsigned)e);
         best[i] = e < a.M ? mine : kClosed;
         if (GROUPS) choice[at][e < a.M ? e + (int)((unsigned)e * a.inv_size >> 20) : NQ * 64 + kSkew - 1] = x;          // (the last one is nobody's)
@@ -234,7 +235,7 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
         const float* const own = choice[at] + g * (a.size + 1);
         for (int n = part; n < a.size; n += a.parts) {
           const float x = own[n];
-          second = fmaxf(second, fminf(first, x));             // (NaN: passed over)
+          second = fmaxf(second, fminf(first, x));
           first = fmaxf(first, x);
         }
       }
