@@ -361,14 +361,16 @@ SPES_API int spes_norm_bwd(int32_t kind, int32_t rows, int32_t cols, int32_t dty
 
 /* Routing to experts from given scores.  Per token, with logits l over M experts
  *      s = softmax(l) or sigmoid(l)        c = s + bias
- *      with groups > 1 the experts stand in `groups` groups of M / groups each; a group counts the sum of its two largest c (its
- *      only one, of a single expert), and only the kept_groups best groups are open, equal ones to the lower group
+ *      c = -inf where l is -inf or the lowest finite value, which keep an expert from a token, and where it would be NaN
+ *      with groups > 1 the experts stand in `groups` groups of M / groups each; a group counts the sum of its two largest c that are
+ *      not -inf (its only one, where there is one; -inf, where there is none), and only the kept_groups best groups are open,
+ *      equal ones to the lower group
  *      idx = the top_k largest c in open groups in descending order, equal ones to the lower expert
  *      gate = scale * s[idx], with renorm scale * s[idx] / sum of s[idx]
  * The bias steers the choice only: it enters no gate and has no gradient (a program moves it by the counts to balance the load).
- * Logits may be -inf (an expert that a token must not get counts 0 then, and is taken only where nothing else is left); a row of
- * -inf alone has gates 0, as has one whose chosen scores are all 0.  NaN counts below everything: indices are valid and
- * different from one another whatever the logits hold.
+ * An expert whose logit is -inf, the lowest finite value or NaN is taken only where nothing else is left in the open groups,
+ * whatever its bias; indices are valid and different from one another whatever the logits hold.  A row of -inf alone has gates 0,
+ * as has one whose chosen scores are all 0.
  *
  *  Supported: 1 <= top_k <= 16; n_experts <= 512; groups <= 16, dividing n_experts; top_k <= kept_groups * n_experts / groups
  */

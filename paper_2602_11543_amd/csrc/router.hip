@@ -1,6 +1,7 @@
 // Routing to experts from given scores, and its gradient.  Per token with logits l
 //      s = softmax(l) or sigmoid(l)            c = s + bias                    (the bias steers the choice and nothing else)
-//      groups: of equal size; a group counts the sum of its two largest c; only the `kept` best groups are open
+//      c = -inf where l masks the expert (-inf or the type's lowest value: no bias brings it back) and where it would be NaN
+//      groups: of equal size; a group counts the sum of its two largest c that are not -inf; only the `kept` best groups are open
 //      idx = the k largest c in open groups, equal ones to the lower expert    gate = scale s[idx] (/ sum of s[idx], renorm)
 // Sixteen lanes hold a token, four consecutive experts to a lane and quad, so a wavefront works on four tokens and every
 // reduction stays within a row of lanes, in data-parallel-primitive steps.  What bounds it is the instructions of the choice, not the 4 M
@@ -12,6 +13,7 @@
 //      renorm:   D_j = sum_i g_i (u_j - u_i);  softmax: dl_j = g_j D_j (the other scores do not matter);  sigmoid: dl_j = g_j (1 - s_j) D_j
 //      otherwise sigmoid: dl_j = u_j s_j (1 - s_j);   softmax: dl_j = s_j (sum_i s_i (u_j - u_i) + u_j sum of the s not chosen),
 //                and dl_e = -s_e sum_i s_i u_i for an expert that is not chosen
+#include <cfloat>
 #include <type_traits>
 
 #include "kernels.h"
@@ -50,7 +52,7 @@ __device__ __forceinline__ float row_sum(float v) { return lane_group_sum<16>(v)
 
 // A choice is a double: the score's value, which leaves the low 29 bits of the mantissa free, and in these the expert, such that equal scores are in
 // the order of the experts.  Then one comparison decides, and a sorting step is v_max_f64 and v_min_f64, two full-rate instructions instead of the
-// five of a pair (a compare and four selects).  NaN and -inf become the lowest finite values, +inf the highest.
+// five of a pair (a compare and four selects).  -inf becomes the lowest finite value, +inf the highest.
 constexpr double kAbove = 0x1p130, kBelow = -0x1p130, kClosed = -0x1p140;      // beyond all floats
 constexpr int kExpertBits = 511;
 __device__ __forceinline__ double with_low(double v, unsigned low) {
@@ -139,11 +141,14 @@ template <int K, int L> __device__ __forceinline__ void merge_row(double* v) {
   merge_lanes<K, L3, 0x140>(v);       // row_mirror
 }
 
-// group scores, in the order of their values: unsigned keys, NaN as -inf, 0 below all
+// group scores (no NaN among them), in the order of their values: unsigned keys, 0 below all
 __device__ __forceinline__ unsigned order_key(float f) {
   const unsigned u = __float_as_uint(f);
-  return f != f ? 0x007fffffu : u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
+
+// a logit that keeps its expert from the token
+__device__ __forceinline__ bool masks(float l) { return l <= -FLT_MAX; }
 
 __device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
 // of every expert, for the choice: within some steps of 2^-24
@@ -221,7 +226,7 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
       for (int c = 0; c < 4; ++c) {
         const int e = q * 64 + l * 4 + c, i = q * 4 + c;
         float x = (SOFTMAX ? __expf(v[i] - mx) * inv : sigmoid_near(v[i])) + bias[i];
-        x = x != x ? -INFINITY : x;                          // (of a minimum with a NaN the other one is left: a NaN would stand for it in the scan below)
+        x = masks(v[i]) || x != x ? -INFINITY : x;           // (of a minimum with a NaN the other one is left: a NaN would stand for it in the scan below)
         const double mine = choice_of(x, (unsigned)e);
         best[i] = e < a.M ? mine : kClosed;
         if (GROUPS) choice[at][e < a.M ? e + (int)((unsigned)e * a.inv_size >> 20) : NQ * 64 + kSkew - 1] = x;          // (the last one is nobody's)
@@ -245,7 +250,7 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
         first = fmaxf(first, f2);
       }
       wave_lds_order();
-      const unsigned mine = part == 0 && g < a.groups ? order_key(a.size > 1 ? first + second : first) : 0u;      // (-inf + inf counts as -inf)
+      const unsigned mine = part == 0 && g < a.groups ? order_key(second == -INFINITY ? first : first + second) : 0u;
       int rank = 0;
       auto against = [&](unsigned other, int lane) { rank += other > mine || (other == mine && lane < l) ? 1 : 0; };
 #define SPES_TURN(r) against((unsigned)dpp_int<0x120 + r>((int)mine), dpp_int<0x120 + r>(l))

@@ -9,9 +9,84 @@ import pytest
 import torch
 
 import paper_2602_11543_amd as S
-from test_gpu_router import SIGMOID, forward
+from test_gpu_router import SIGMOID, SOFTMAX, forward
 
 pytestmark = pytest.mark.gpu
+
+INF, LOWEST = math.inf, torch.finfo(torch.float32).min
+SCORES = pytest.mark.parametrize("score", [SOFTMAX, SIGMOID], ids=["softmax", "sigmoid"])
+
+
+def counts(logits, bias, score):
+    """c in 64 bits: s + bias, -inf where the logit is -inf, the type's lowest value or a NaN, or the sum is a NaN."""
+    l = logits.double()
+    s = torch.sigmoid(l) if score == SIGMOID else torch.softmax(l, 1)
+    c = s if bias is None else s + bias.double()
+    return torch.where((logits <= LOWEST) | c.isnan(), -INF, c)
+
+
+def choose(c, groups, kept, k):
+    """Indices, and whether a token's choice is clear of rounding.  Equal sums are clear where they are -inf."""
+    T, M = c.shape
+    size = 1 + c.abs().masked_fill(c.isinf(), 0).amax(1, keepdim=True)
+    clear = torch.ones(T, dtype=torch.bool, device=c.device)
+
+    def apart(v):
+        return ((v[:, :-1] - v[:, 1:] > 2.0 ** -18 * size) | (v[:, 1:] == -INF)).all(1)
+
+    if groups > 1:
+        two = c.view(T, groups, M // groups).sort(2, descending=True).values[:, :, :2]
+        best = torch.where(two == -INF, 0.0, two).sum(2).masked_fill(two[:, :, 0] == -INF, -INF).sort(dim=1, descending=True, stable=True)
+        if kept < groups:
+            clear &= apart(best.values[:, kept - 1: kept + 1])
+        open_ = torch.zeros(T, groups, dtype=torch.bool, device=c.device).scatter_(1, best.indices[:, :kept], True)
+        inside = open_.repeat_interleave(M // groups, 1)
+    else:
+        inside = torch.ones_like(c, dtype=torch.bool)
+    # in open groups first, then by c, then by number
+    order = c.sort(dim=1, descending=True, stable=True)
+    first = inside.gather(1, order.indices).to(torch.int8).sort(dim=1, descending=True, stable=True).indices
+    idx, v = order.indices.gather(1, first), order.values.gather(1, first)
+    n = min(k + 1, kept * (M // groups))
+    return idx[:, :k], clear & apart(v[:, :n])
+
+
+@SCORES
+@pytest.mark.parametrize("groups,kept,k", [(1, 1, 6), (6, 2, 6), (6, 6, 16), (16, 3, 4), (3, 1, 2)])
+@pytest.mark.parametrize("low", [-INF, LOWEST], ids=["inf", "lowest"])
+def test_masked_experts_with_a_bias(device, score, groups, kept, k, low):
+    """An expert that a token must not get is not chosen for its bias, and does not open its group."""
+    T, M = 200, 48
+    g = torch.Generator().manual_seed(groups)
+    bias = (0.5 * torch.randn(M, generator=g)).cuda()
+    hide = torch.rand(T, M, generator=g) < torch.rand(T, 1, generator=g)          # from a few experts to nearly all
+    hide[3] = True
+    for b in (bias, None):
+        logits = torch.randn(T, M, generator=g)
+        for _ in range(60):
+            dev = logits.masked_fill(hide, low).cuda()
+            bad = ~choose(counts(dev, b, score), groups, kept, k)[1].cpu()
+            if not bool(bad.any()):
+                break
+            logits[bad] = torch.randn(int(bad.sum()), M, generator=g)
+        assert not bool(bad.any())
+        want = choose(counts(dev, b, score), groups, kept, k)[0]
+        for renorm in (0, 1):
+            idx, gate, count = forward(dev, b, k, S.router_opts(score, groups, kept, renorm, 1.0))
+            assert torch.equal(idx.long(), want)
+            assert torch.equal(count.long(), torch.bincount(want.reshape(-1), minlength=M))
+            masked = hide.cuda().gather(1, want)
+            masked[hide.all(1)] = False
+            assert bool((gate[masked] == 0).all()) and bool(torch.isfinite(gate).all())
+
+
+def test_underflowing_scores_without_a_bias(device):
+    """An expert whose probability is too small for 32 bits is still ahead of a masked one of a lower number."""
+    logits = torch.full((5, 40), -INF, device="cuda")
+    logits[:, 30], logits[:, 20], logits[:, 25] = 400.0, 0.0, -300.0
+    idx, gate, _ = forward(logits, None, 3, S.router_opts(SOFTMAX))
+    assert torch.equal(idx.long(), torch.tensor([30, 20, 25], device="cuda").expand(5, 3))
+    assert torch.equal(gate, torch.tensor([1.0, 0.0, 0.0], device="cuda").expand(5, 3))
 
 
 def test_a_group_of_bad_numbers_does_not_open(device):
