@@ -150,9 +150,17 @@ __device__ __forceinline__ unsigned order_key(float f) {
 // a logit that keeps its expert from the token
 __device__ __forceinline__ bool masks(float l) { return l <= -FLT_MAX; }
 
-__device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
-// of every expert, for the choice: within some steps of 2^-24
-__device__ __forceinline__ float sigmoid_near(float l) { return __builtin_amdgcn_rcpf(1.f + __expf(-l)); }
+// 1 / d, within a step, of 1 <= d <= 2: the hardware's and one Newton step, where a division takes three times as many instructions
+__device__ __forceinline__ float inverse(float d) {
+  const float r = __builtin_amdgcn_rcpf(d);
+  return fmaf(fmaf(-d, r, 1.f), r, r);
+}
+// The choice is made from the same bits as the gates: with the hardware's exponential and reciprocal for every expert and these for the chosen ones, scores a
+// few steps apart came out in another order than their gates.
+__device__ __forceinline__ float sigmoid(float l) {
+  const float small = expf(-fabsf(l)), big = inverse(1.f + small);
+  return l < 0.f ? small * big : big;
+}
 
 struct RouterArgs {
   int T, M, k, groups, kept, size, parts;      // parts: lanes that look through a group, a power of two; groups * parts <= 16
@@ -180,9 +188,10 @@ __device__ __forceinline__ void load4(const float* row, int e, int M, float* v) 
   }
 }
 
-// softmax of one token: the largest logit and the inverse of the sum.  A row of -inf alone has no largest one: its scores are 0.
-template <int NQ>
-__device__ __forceinline__ void softmax_stats(const float (&v)[NQ * 4], float& mx, float& inv) {
+// softmax of one token: the largest logit, the inverse of the sum, and exponentials in place of the logits, MARK: -inf of masked ones.  A row of -inf alone
+// has no largest one: its scores are 0.
+template <int NQ, bool MARK>
+__device__ __forceinline__ void softmax_terms(float (&v)[NQ * 4], float& mx, float& inv) {
   mx = -INFINITY;
 #pragma unroll
   for (int i = 0; i < NQ * 4; ++i) mx = fmaxf(mx, v[i]);
@@ -190,7 +199,11 @@ __device__ __forceinline__ void softmax_stats(const float (&v)[NQ * 4], float& m
   if (mx == -INFINITY) mx = 0.f;
   float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < NQ * 4; ++i) sum += expf(v[i] - mx);
+  for (int i = 0; i < NQ * 4; ++i) {
+    const float e = expf(v[i] - mx);
+    sum += e;
+    v[i] = MARK && masks(v[i]) ? -INFINITY : e;
+  }
   sum = row_sum(sum);
   inv = sum == 0.f ? 0.f : 1.f / sum;
 }
@@ -218,14 +231,14 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) load4(row, q * 64 + l * 4, a.M, v + q * 4);
     float mx = 0.f, inv = 1.f;
-    if (SOFTMAX) softmax_stats<NQ>(v, mx, inv);
+    if constexpr (SOFTMAX) softmax_terms<NQ, true>(v, mx, inv);
     double best[V > K ? V : K];
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const int e = q * 64 + l * 4 + c, i = q * 4 + c;
-        float x = (SOFTMAX ? __expf(v[i] - mx) * inv : sigmoid_near(v[i])) + bias[i];
+        float x = (SOFTMAX ? v[i] * inv : sigmoid(v[i])) + bias[i];
         x = masks(v[i]) || x != x ? -INFINITY : x;           // (of a minimum with a NaN the other one is left: a NaN would stand for it in the scan below)
         const double mine = choice_of(x, (unsigned)e);
         best[i] = e < a.M ? mine : kClosed;
@@ -338,9 +351,9 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a) {
     if (WHOLE) {
 #pragma unroll
       for (int q = 0; q < NQ; ++q) load4(row, q * 64 + l * 4, a.M, p + q * 4);
-      if constexpr (WHOLE) softmax_stats<NQ>(p, mx, inv);
+      if constexpr (WHOLE) softmax_terms<NQ, false>(p, mx, inv);
 #pragma unroll
-      for (int i = 0; i < (WHOLE ? V : 1); ++i) p[i] = expf(p[i] - mx) * inv;
+      for (int i = 0; i < (WHOLE ? V : 1); ++i) p[i] *= inv;
     }
     // marks of the chosen ones, then results
     wave_lds_order();
@@ -374,7 +387,7 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a) {
         s = has ? expf(x - (top == -INFINITY ? 0.f : top)) : 0.f;
         other = 1.f;
       } else {
-        const float small = expf(-fabsf(x)), big = 1.f / (1.f + small);
+        const float small = expf(-fabsf(x)), big = inverse(1.f + small);
         s = has ? (x < 0.f ? small * big : big) : 0.f;
         other = x < 0.f ? big : small * big;
       }

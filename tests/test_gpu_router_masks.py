@@ -103,3 +103,18 @@ def test_a_group_of_bad_numbers_does_not_open(device):
             idx, gate, _ = forward(logits, None, 3, S.router_opts(SIGMOID, groups, 1))
             assert idx.tolist() == [[10, 13, 8]], (at, other)
             assert bool(torch.isfinite(gate).all())
+
+
+@SCORES
+def test_the_choice_agrees_with_the_gates(device, score):
+    """Logits a few steps of 2^-24 apart: gates without renormalisation, which are the scores, descend, equal ones by expert; none is left out for
+    a smaller one."""
+    T, M = 4000, 16
+    g = torch.Generator().manual_seed(5)
+    base = 2 * torch.randn(T, 1, generator=g)
+    logits = (base * (1 + 2.0 ** -23 * torch.randint(-6, 7, (T, M), generator=g))).cuda()
+    idx, gate, _ = forward(logits, None, 16, S.router_opts(score))
+    ahead, behind = gate[:, :-1], gate[:, 1:]
+    assert bool(((ahead > behind) | ((ahead == behind) & (idx[:, :-1] < idx[:, 1:]))).all())
+    few, fgate, _ = forward(logits, None, 5, S.router_opts(score))
+    assert torch.equal(few, idx[:, :5]) and torch.equal(fgate, gate[:, :5])
