@@ -369,8 +369,9 @@ SPES_API int spes_norm_bwd(int32_t kind, int32_t rows, int32_t cols, int32_t dty
  *      gate = scale * s[idx], with renorm scale * s[idx] / sum of s[idx]
  * The bias steers the choice only: it enters no gate and has no gradient (a program moves it by the counts to balance the load).
  * An expert whose logit is -inf, the lowest finite value or NaN is taken only where nothing else is left in the open groups,
- * whatever its bias; indices are valid and different from one another whatever the logits hold.  A row of -inf alone has gates 0,
- * as has one whose chosen scores are all 0.
+ * whatever its bias; indices are valid and different from one another whatever the logits hold.  A row of -inf alone has gates 0.
+ * With renorm, shares keep their bits however small the chosen scores are beside the others, as do their gradients; sigmoid scores lose
+ * bits below e^-187 and are 0 below e^-204, and where all chosen ones are, the gates are.
  *
  *  Supported: 1 <= top_k <= 16; n_experts <= 512; groups <= 16, dividing n_experts; top_k <= kept_groups * n_experts / groups
  */
@@ -391,7 +392,7 @@ SPES_API int spes_router_fwd(int32_t T, int32_t n_experts, int32_t top_k, const 
                              const float* logits, const float* bias, int32_t* idx, float* gate,
                              int32_t* count, void* stream);
 
-/* Gradient of the gates with respect to the logits, the choice held fixed.  A scale of gates of 0 / 0 has none.
+/* Gradient of the gates with respect to the logits, the choice held fixed.  A gate of 0 has none.
  *
  *  logits, idx  as above, idx as the forward left it      dgate  DEVICE [T, top_k] f32
  *  dlogits      DEVICE [T, n_experts] f32 out

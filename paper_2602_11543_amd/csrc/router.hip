@@ -208,6 +208,18 @@ __device__ __forceinline__ void softmax_terms(float (&v)[NQ * 4], float& mx, flo
   inv = sum == 0.f ? 0.f : 1.f / sum;
 }
 
+// Score of a token's chosen expert, one to a lane, and what it lacks to 1 (of softmax: 1), for the gates and for their gradient.  RENORM: up to a factor that
+// all of them have, so that shares keep their bits where the scores underflow: a softmax over the chosen ones alone; sigmoids times e to the
+// power of -top, top the largest logit between 0 and -100.  What is 0 here has neither gate nor gradient.
+struct Score { float s, other; };
+template <bool SOFTMAX, bool RENORM>
+__device__ __forceinline__ Score chosen_score(float x, bool has) {
+  const float largest = RENORM ? row_max_f(has ? x : -INFINITY) : 0.f;
+  if (SOFTMAX) return {has ? expf(x - (largest == -INFINITY ? 0.f : largest)) : 0.f, 1.f};
+  const float small = expf(-fabsf(x)), big = inverse(1.f + small), top = fmaxf(fminf(largest, 0.f), -100.f);
+  return {!has ? 0.f : x < 0.f ? (RENORM ? expf(x - top) : small) * big : big, x < 0.f ? big : small * big};
+}
+
 // K: a power of two, k at least
 template <int NQ, int K, bool SOFTMAX, bool GROUPS, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
@@ -294,11 +306,13 @@ __global__ __launch_bounds__(BLOCK) void router_fwd_kernel(const RouterArgs a) {
     const int chosen = expert_of(pick);
     const bool mine = l < a.k;
     const float x = mine ? row[chosen] : 0.f;
-    const float s = !mine ? 0.f : SOFTMAX ? expf(x - mx) * inv : sigmoid(x);
-    float share = s;
+    float share;
     if (a.renorm) {
-      const float total = row_sum(s);
+      const float s = chosen_score<SOFTMAX, true>(x, mine).s, total = row_sum(s);
       share = total == 0.f ? 0.f : s / total;
+      if (SOFTMAX && inv != inv) share = inv;               // (a NaN or +inf anywhere in the row)
+    } else {
+      share = !mine ? 0.f : SOFTMAX ? expf(x - mx) * inv : sigmoid(x);
     }
     if (mine && live) {
       a.idx[t * a.k + l] = chosen;
@@ -380,22 +394,13 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a) {
       }
       wave_lds_order();
     } else {
-      // the softmax over the chosen ones alone, or sigmoids; 1 - s from the side that does not cancel
-      float s, other;
-      if (SOFTMAX) {
-        const float top = row_max_f(has ? x : -INFINITY);
-        s = has ? expf(x - (top == -INFINITY ? 0.f : top)) : 0.f;
-        other = 1.f;
+      if (SOFTMAX || a.renorm) {
+        const Score c = chosen_score<SOFTMAX, true>(x, has);
+        const float total = row_sum(c.s), g = total == 0.f ? 0.f : c.s / total;
+        d = g * c.other * weighted_differences(g, u);
       } else {
-        const float small = expf(-fabsf(x)), big = inverse(1.f + small);
-        s = has ? (x < 0.f ? small * big : big) : 0.f;
-        other = x < 0.f ? big : small * big;
-      }
-      if (a.renorm) {
-        const float total = row_sum(s), g = total == 0.f ? 0.f : s / total;
-        d = g * other * weighted_differences(g, u);
-      } else {
-        d = s * other * u;
+        const Score c = chosen_score<false, false>(x, has);
+        d = c.s * c.other * u;
       }
     }
     if (has) mine[e] = d;

@@ -3,13 +3,14 @@
 The choice is compared exactly with the definition in 64 bits, a masked expert left out first.  A score in 32 bits is within some 20 steps of
 2^-24; sums c of a score and a bias that are nearer than 2^-18 of their size are drawn again.  Gates and gradients have K = 64 steps of their
 terms, and half a step of its distance for every score that is e to the power of one."""
+import itertools
 import math
 
 import pytest
 import torch
 
 import paper_2602_11543_amd as S
-from test_gpu_router import SIGMOID, SOFTMAX, forward
+from test_gpu_router import K, SIGMOID, SOFTMAX, STEP, backward, forward
 
 pytestmark = pytest.mark.gpu
 
@@ -118,3 +119,69 @@ def test_the_choice_agrees_with_the_gates(device, score):
     assert bool(((ahead > behind) | ((ahead == behind) & (idx[:, :-1] < idx[:, 1:]))).all())
     few, fgate, _ = forward(logits, None, 5, S.router_opts(score))
     assert torch.equal(few, idx[:, :5]) and torch.equal(fgate, gate[:, :5])
+
+
+@SCORES
+@pytest.mark.parametrize("depth", [-60.0, -88.0, -95.0, -120.0, -150.0])
+def test_shares_far_below_the_largest_logit(device, score, depth):
+    """A bias takes experts whose logits are far down: their shares are as if nothing were above them, and so is the gradient."""
+    T, M, k = 64, 32, 4
+    g = torch.Generator().manual_seed(int(-depth))
+    logits = torch.randn(T, M, generator=g)
+    if score == SIGMOID:
+        logits += depth
+    else:
+        logits[:, 8:] += depth
+    logits = logits.cuda()
+    bias = torch.zeros(M, device="cuda")
+    for place, e in enumerate((9, 15, 20, 31)):
+        bias[e] = 3.0 - 0.25 * place
+    o = S.router_opts(score, 1, 1, 1, 2.5)
+    idx, gate, _ = forward(logits, bias, k, o)
+    assert torch.equal(idx.long(), torch.tensor([9, 15, 20, 31], device="cuda").expand(T, k))
+    x = logits.double().gather(1, idx.long()).requires_grad_(True)
+    share = torch.softmax(x, 1) if score == SOFTMAX else torch.sigmoid(x) / torch.sigmoid(x).sum(1, keepdim=True)
+    allow = (K + 1 + x.detach().abs().amax()) * STEP
+    assert bool(((gate - 2.5 * share).abs() <= allow * 2.5 * share).all())
+    dgate = torch.randn(T, k, generator=g).cuda()
+    d = backward(logits, idx, dgate, o)
+    want, = torch.autograd.grad((2.5 * share * dgate.double()).sum(), x)
+    size = 2.5 * share.detach() * (dgate.abs().amax(1, keepdim=True) * 2)
+    assert bool(((d.gather(1, idx.long()) - want).abs() <= 2 * allow * size).all())
+    rest = torch.ones_like(d, dtype=torch.bool).scatter(1, idx.long(), False)
+    assert bool((d[rest] == 0).all())
+
+
+@SCORES
+def test_gates_of_zero_have_no_gradient(device, score):
+    """Where nothing is left of the scores, forward and backward say so alike."""
+    M, k = 32, 4
+    logits = torch.randn(6, M, generator=torch.Generator().manual_seed(1)).cuda()
+    logits[0] = -INF
+    if score == SIGMOID:
+        logits[1] -= 300
+        logits[2] = LOWEST
+    else:
+        logits[1, 8:] = -INF
+    bias = torch.zeros(M, device="cuda")
+    bias[10:14] = 2.0
+    for renorm, b in itertools.product((0, 1), (bias, None)):
+        o = S.router_opts(score, 1, 1, renorm, 1.0)
+        idx, gate, _ = forward(logits, b, k, o)
+        d = backward(logits, idx, torch.arange(1.0, 7 * k - k + 1, device="cuda").view(6, k), o)
+        none = (gate == 0).all(1)
+        assert bool(none[0]) and torch.isfinite(gate).all() and torch.isfinite(d).all()
+        assert bool((d[none] == 0).all())
+        if score == SIGMOID:
+            assert bool(none[1]) and bool(none[2])
+        assert not bool(none[3:].any())
+        assert bool(((gate != 0) | (d.gather(1, idx.long()) == 0)).all())
+
+
+def test_a_bad_logit_shows_in_the_gates(device):
+    """One NaN or +inf among a token's logits: every softmax score is NaN, and so are the gates, whichever experts stand there."""
+    logits = torch.randn(4, 64, device="cuda")
+    logits[1, 40], logits[2, 50] = math.nan, INF
+    for renorm in (0, 1):
+        _, gate, _ = forward(logits, None, 4, S.router_opts(SOFTMAX, 1, 1, renorm, 1.0))
+        assert torch.isnan(gate[1:3]).all() and torch.isfinite(gate[[0, 3]]).all()
