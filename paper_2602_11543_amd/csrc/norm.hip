@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "kernels.h"
+#include "plan.h"
 #include "units.h"
 
 namespace spes {
@@ -290,15 +291,6 @@ int bwd_blocks(int rows, int cols) {
   return need < 512 ? need : 512;
 }
 
-// Streams that the Infinity Cache (256 MB) does not hold carry the non-temporal hint: 32768 x 4096 bf16 with both residual streams, forward
-// and backward, 405 us without, 396 on the loads, 379 on the stores too (5.7 TB/s); 4096 x 768, which it holds, 18.8 us of kernels without and 19.4 with.
-// Not for rows that end inside a line of 128 bytes, whose halves two wavefronts write: with 4095 columns 722 us, without 703.
-constexpr long kCacheBytes = 256l << 20;
-bool streams(int dtype, int rows, int cols, int tensors, long stride0, long stride1, long stride2) {
-  const long size = dtype == SPES_F32 ? 4 : 2;
-  return rows * cols * size * tensors > kCacheBytes && ((cols | stride0 | stride1 | stride2) * size) % 128 == 0;
-}
-
 template <typename F>
 int with_rows(int dtype, int kind, int cols, bool once, F launch) {
   auto typed = [&](auto t) {
@@ -333,7 +325,7 @@ size_t norm_scratch_bytes(int rows, int cols) { return (size_t)2 * (rows > 0 ? b
 int launch_norm_fwd(int dtype, int kind, int rows, int cols, const void* x, long x_stride, const void* add, long add_stride, const void* weight,
                     const void* bias, float eps, void* sum, void* y, float* mean, float* rstd, hipStream_t s) {
   if (rows == 0) return SPES_OK;
-  const bool once = streams(dtype, rows, cols, add ? 4 : 2, x_stride, add ? add_stride : 0, 0);
+  const bool once = plan::norm_streams(dtype == SPES_F32 ? 4 : 2, rows, cols, add ? 4 : 2, x_stride, add ? add_stride : 0, 0);
   FwdArgs a = {rows, cols, x, add, weight, bias, x_stride, add_stride, eps, sum, y, mean, rstd};
   return with_rows(dtype, kind, cols, once, [&](auto t, auto lpr, auto nu, auto ends, auto layer, auto streaming) {
     constexpr int LPR = decltype(lpr)::value, RPB = 256 / LPR;
@@ -350,7 +342,7 @@ int launch_norm_bwd(int dtype, int kind, int rows, int cols, const void* dy, lon
                     int accumulate, float* scratch, hipStream_t s) {
   const int grid = rows > 0 ? bwd_blocks(rows, cols) : 0;
   if (grid > 0) {
-    const bool once = streams(dtype, rows, cols, dres ? 4 : 3, x_stride, dy_stride, dres ? dres_stride : 0);
+    const bool once = plan::norm_streams(dtype == SPES_F32 ? 4 : 2, rows, cols, dres ? 4 : 3, x_stride, dy_stride, dres ? dres_stride : 0);
     BwdArgs a = {rows, cols, dy, x, weight, dres, dy_stride, x_stride, dres_stride, mean, rstd, dx, d_weight ? scratch : nullptr, d_bias != nullptr};
     const int rc = with_rows(dtype, kind, cols, once, [&](auto t, auto lpr, auto nu, auto ends, auto layer, auto streaming) {
       constexpr int LPR = decltype(lpr)::value;
