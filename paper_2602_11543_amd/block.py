@@ -40,7 +40,7 @@ class DeviceBlock:
         self.chosen, self.count = new(n_experts, t=torch.int32), new(n_experts, t=torch.int32)
         self.dlogits = new(T, n_experts)
         self.dh, self.dx = new(T, d_model, t=st), new(T, d_model, t=st)
-        self.d_norm_w, self.d_w_router = new(d_model), None
+        self.d_norm_w, self.d_w_router = torch.zeros(d_model, device=device), torch.zeros(n_experts, d_model, device=device)
         self.ctx = new(S.spes_moe_ctx_bytes(self.shape), t=torch.uint8)
         self.norm_scratch = new(S.spes_norm_scratch_bytes(T, d_model), t=torch.uint8)
         sides = ((d_ff, d_model), (d_model, d_ff))
@@ -64,7 +64,7 @@ class DeviceBlock:
                               *(self.grad.values() if len(self.master["gate"]) else (None,) * 3), accumulate)
         S.spes_router_bwd(T, self.M, self.k, self.opts, self.logits, self.idx, self.dgate, self.dlogits)
         d_w_router = self.dlogits.t() @ self.h.float()
-        self.d_w_router = self.d_w_router + d_w_router if accumulate else d_w_router
+        self.d_w_router = self.d_w_router + d_w_router if accumulate else d_w_router          # (like the other gradients zeros ahead of the first batch)
         dh = (self.dh.float() + self.dlogits @ self.w_router.float()).to(self.dh.dtype)
         S.spes_norm_bwd(S.SPES_NORM_RMS, T, d, self.dt, dh, self.sum, self.norm_w, None, self.rstd, d_out, self.dx, self.d_norm_w, None, accumulate,
                         self.norm_scratch)
