@@ -405,7 +405,8 @@ SPES_API int spes_router_bwd(int32_t T, int32_t n_experts, int32_t top_k, const 
  *      X <- a X + (b X X^T + c (X X^T)^2) X
  * which takes each singular value through a s + b s^3 + c s^5 and leaves the singular vectors.  Products and sums: bf16 storage
  * on fp16 operands with fp32 sums, the result within about 1e-3 of the formula's in norm; fp32 storage to fp32 accuracy.  A matrix of
- * zeros gives zeros, one that holds an infinity or a NaN gives NaN.
+ * zeros gives zeros, one that holds an infinity or a NaN gives NaN.  Copies of a matrix in a call get the same bits, whatever stands
+ * beside them; n decides how products are cut, so in a call with another n the last bits of the same matrix can be others.
  *
  *  1 <= n <= 65535 matrices of rows x cols, each side at most 16384; 1 <= steps <= 64
  *  src    DEVICE [n, rows, cols] storage dtype      out  DEVICE [n, rows, cols] storage dtype out

@@ -839,18 +839,19 @@ int launch_tiles(const NsArgs& g, hipStream_t s, int parts = 1) {
   hipLaunchKernelGGL((ns_gemm_kernel<EPI, B_KC, SPLIT, IN, OUT, T, C, CH>), dim3((unsigned)blocks, (unsigned)parts), dim3(256), 0, s, g);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
+// of: matrices of the whole product, where a launch has only some of them.  One tile for all: in pairs the order of the sums goes by it.
 template <Epi EPI, bool B_KC, bool SPLIT, int IN, int OUT, typename T>
-int launch_product(const NsArgs& g, hipStream_t s) {
-  const int side = plan::square_tile(g.M, g.N, g.n, EPI == kGram || EPI == kPoly);
+int launch_product(const NsArgs& g, int of, hipStream_t s) {
+  const int side = plan::square_tile(g.M, g.N, of, EPI == kGram || EPI == kPoly);
   if (side == Tile::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, Tile, TileHalf>(g, s);
   if (side == TileSmall::BM) return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, TileSmall, TileSmallHalf>(g, s);
   return launch_tiles<EPI, B_KC, SPLIT, IN, OUT, T, std::conditional_t<SPLIT, TileTinyPairs, TileTiny>, std::conditional_t<SPLIT, TileTinyPairsHalf, TileTinyHalf>>(g, s);
 }
 // a last step; matrices of few rows in bf16 storage, the only ones on pairs there, have few tiles
 template <Epi EPI, typename T>
-int launch_end(bool pairs, const NsArgs& g, hipStream_t s) {
-  if constexpr (sizeof(T) == 4) return launch_product<EPI, false, true, 0, 0, T>(g, s);
-  else return pairs ? launch_tiles<EPI, false, true, 0, 0, T, TileTinyPairs, TileTinyPairsHalf>(g, s) : launch_product<EPI, false, false, 0, 0, T>(g, s);
+int launch_end(bool pairs, const NsArgs& g, int of, hipStream_t s) {
+  if constexpr (sizeof(T) == 4) return launch_product<EPI, false, true, 0, 0, T>(g, of, s);
+  else return pairs ? launch_tiles<EPI, false, true, 0, 0, T, TileTinyPairs, TileTinyPairsHalf>(g, s) : launch_product<EPI, false, false, 0, 0, T>(g, of, s);
 }
 
 template <bool SPLIT, int OUT>
@@ -904,14 +905,14 @@ int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool m
       q.k_tiles = cdiv(b.hi_p / 64, b.gram_parts);
       rc = b.pairs ? launch_gram_parts<true, 2>(q, b.gram_parts, s) : launch_gram_parts<false, 1>(q, b.gram_parts, s);
     } else {
-      rc = b.pairs ? launch_product<kGram, true, true, 0, 2, float>(q, s) : launch_product<kGram, true, false, 0, 1, float>(q, s);
+      rc = b.pairs ? launch_product<kGram, true, true, 0, 2, float>(q, a.n, s) : launch_product<kGram, true, false, 0, 1, float>(q, a.n, s);
     }
     if (rc != SPES_OK) return rc;
     q.A = q.B = q.E = G; q.a_ms = q.b_ms = q.e_ms = b.planes * gs; q.a_lo = q.b_lo = gs; q.e_lo = b.pairs ? gs : 0; q.lda = q.ldb = b.lo_p;
     q.K = b.lo_p; q.C = P;
     q.alpha = coef[2] * ldexpf(1.f, -kGBits); q.beta = coef[1]; q.factor = nullptr;
     q.diagonal = ldexpf(coef[0], kGBits);
-    rc = b.pairs ? launch_product<kPoly, true, true, 2, 2, float>(q, s) : launch_product<kPoly, true, false, 1, 1, float>(q, s);
+    rc = b.pairs ? launch_product<kPoly, true, true, 2, 2, float>(q, a.n, s) : launch_product<kPoly, true, false, 1, 1, float>(q, a.n, s);
     if (rc != SPES_OK) return rc;
     q.A = P; q.B = x; q.b_ms = 2 * xs; q.b_lo = xs; q.ldb = b.hi_p;
     q.E = x + xs; q.e_ms = 2 * xs; q.lde = b.hi_p;             // the remainders
@@ -919,17 +920,17 @@ int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool m
     q.C = y; q.c_ms = 2 * xs; q.c_lo = next_lo ? xs : 0; q.ldc = b.hi_p;
     q.alpha = ldexpf(1.f, -kGBits); q.beta = x_lo ? coef[0] : 0.f; q.factor = factor;
     if (!last) {
-      rc = b.pairs           ? launch_product<kStep, false, true, 0, 2, float>(q, s)
-           : x_lo && next_lo ? launch_product<kStep, false, false, 1, 2, float>(q, s)
-           : x_lo            ? launch_product<kStep, false, false, 1, 1, float>(q, s)
-           : next_lo         ? launch_product<kStep, false, false, 0, 2, float>(q, s)
-                             : launch_product<kStep, false, false, 0, 1, float>(q, s);
+      rc = b.pairs           ? launch_product<kStep, false, true, 0, 2, float>(q, a.n, s)
+           : x_lo && next_lo ? launch_product<kStep, false, false, 1, 2, float>(q, a.n, s)
+           : x_lo            ? launch_product<kStep, false, false, 1, 1, float>(q, a.n, s)
+           : next_lo         ? launch_product<kStep, false, false, 0, 2, float>(q, a.n, s)
+                             : launch_product<kStep, false, false, 0, 1, float>(q, a.n, s);
       if (rc != SPES_OK) return rc;
       continue;
     }
     // out of the scaled form
     q.alpha = ldexpf(q.alpha, -kXBits);
-    if (!muon) return launch_end<kLast, T>(b.pairs, q, s);
+    if (!muon) return launch_end<kLast, T>(b.pairs, q, a.n, s);
     for (int first = 0; first < a.n; first += kSlots) {
       NsArgs u = q;
       u.n = a.n - first < kSlots ? a.n - first : kSlots;
@@ -937,7 +938,7 @@ int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool m
       if (u.factor) u.factor += first;
       if (u.master) u.master += (long)first * a.rows * a.cols;
       for (int k = 0; k < u.n; ++k) u.param_at[k] = param_at[first + k];
-      rc = launch_end<kUpdate, T>(b.pairs, u, s);
+      rc = launch_end<kUpdate, T>(b.pairs, u, a.n, s);
       if (rc != SPES_OK) return rc;
     }
   }
