@@ -5,13 +5,16 @@
 //      G = X X^T      P = b G + c G G      X <- a X + P X
 // so a step is three matrix products of lo^2 hi, lo^3 and 2 lo^2 hi operations, of the symmetric ones half the tiles.
 //
-// The products run on the matrix cores on fp16 operands with fp32 sums.  fp16 because its step, 2^-11, is what the polynomial forgives: it
-// grows small singular values 3.4-fold a step, and what rounding adds to them grows alike.  Against 64 bits, on gradients with 16 strong
-// directions above a broad floor, 512 x 1024: bf16 operands leave 1.3e-2 of the result's norm, fp16 ones 1.6e-3; nearly all of that is the
-// rounding of X itself in the first two steps, in the term a X, so while it matters X is carried with its remainder (a second fp16
-// plane, 22 bits together), which is added at the step's end: 0.8e-3.  The term a X itself stands in P, X <- (P + a I) X + a remainder: where
-// singular values are near 1, P is near (b + c) I and P + a I is rounded to finer steps.  fp32 storage takes every operand as such a pair and every product as three,
-// lo hi + hi lo + hi hi: 3e-7.  Range: X stands scaled by 2^12, G and P by 2^11, which holds singular values below 5, G below 25
+// The products run on the matrix cores on fp16 operands with fp32 sums.  What limits them is not the directions that the matrix has but those that it
+// lacks: the polynomial grows small singular values 3.4-fold a step, and rounding noise in empty directions alike.  An expert that got
+// few tokens has a gradient of low rank, and there the fp16 rounding of X alone, 2e-4 of its norm, would end as 1.4e-2 (512 x 1024, rank 1; bf16
+// operands leave 1.3e-2 even of a broad spectrum).  So X goes from step to step with its remainder (a second fp16 plane, 22 bits together), which is added, times a, at the
+// step's end.  The term a X itself stands in P, X <- (P + a I) X + a remainder: where singular values are near 1, P is near (b + c) I and
+// P + a I is rounded to finer steps; what its diagonal loses in that, up to 2^-10, is kept in 32 bits and multiplied with X at the step's end too
+// (without: 2.3e-3).  The last step, behind which nothing grows, does without both.  Left are, against 64 bits after five steps, in the update
+// of fp32 weights: rank 1 1.4e-3, 8 0.7e-3, 128 1.2e-3, full rank 1.1e-3, 16 strong directions above a broad floor 0.8e-3 (512 x 1024; rank 1 of 96 x 96
+// 1.6e-3).  fp32 storage takes every operand as such a pair and every product as three,
+// lo hi + hi lo + hi hi: full rank 2e-6, rank 1 1.2e-4, as products in fp32.  Range: X stands scaled by 2^12, G and P by 2^11, which holds singular values below 5, G below 25
 // and P below 31; after the first scaling they are at most 1.21 with the default coefficients.
 #include <cmath>
 #include <type_traits>
@@ -47,6 +50,7 @@ struct NsArgs {
   int M, N, K, n;                              // of the products, padded; matrices
   float alpha, beta;                           // result = (alpha product + beta E) factor
   float diagonal;                              // kPoly: added to the diagonal
+  float* rest;                                 // [n][M], operands that are not pairs: what P's diagonal lost when it was rounded
   const float* factor;                         // of each matrix, NULL: 1.  kGram: squared
   float* part;                                 // kPart: [parts][n][M][M]
   int k_tiles;                                 // kPart: of a part
@@ -488,7 +492,7 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
     if (whole) g.tall ? finish(std::true_type{}, std::true_type{}) : finish(std::true_type{}, std::false_type{});
     else g.tall ? finish(std::false_type{}, std::true_type{}) : finish(std::false_type{}, std::false_type{});
   } else {
-    // All of it on fp16 in LDS, a slab for each plane of what is read beside the product (kPoly: G, kStep: X's remainder) and of the result.  The
+    // All of it on fp16 in LDS, a slab for each plane of what is read beside the product (kPoly: G, kStep: X and its remainder) and of the result.  The
     // arithmetic is done where the products are, four columns to a lane, and rounded there.  Loads and stores go through buffer resources that end
     // with the matrix: a lane beyond it asks for nothing, and there are no branches.
     constexpr int PITCH16 = C::PITCH16, SLAB16 = C::SLAB16;
@@ -509,7 +513,16 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
     };
     load_in(0);
     const float alpha = g.alpha * f, beta = g.beta * f;
-    const int d0 = m0 + wm * QM - n0 - wn * QN + l16 - lq * 4;        // row less column of a lane's element r: d0 + 16 (i - j) - r
+    constexpr bool KEEPS = EPI == kPoly && OUT == 1, TAKES = EPI == kStep && IN > 0;        // the rest of P's diagonal, which kStep multiplies X with
+    const __amdgpu_buffer_rsrc_t rest_rs = tile_rsrc(base_of(reinterpret_cast<const f16*>(g.rest), 2l * mat * g.M), KEEPS || TAKES ? (unsigned)g.M * 4u : 0u);
+    const unsigned rest_row = (unsigned)(m0 + wm * QM + l16) * 4u;
+    float rest[TAKES ? TM : 1];
+    if constexpr (TAKES) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) rest[i] = load4(rest_rs, rest_row + (unsigned)i * 64u) * alpha;
+    }
+    // (the diagonal passes through the MFMA tiles i, j with j - i = tile_d, in a lane's element r through r = in_d)
+    const int tile_d = (m0 + wm * QM - n0 - wn * QN) / 16, in_d = l16 - lq * 4;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < QM / 32; ++i) {
@@ -533,26 +546,29 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
           for (int r = 0; r < 4; ++r) v[r] = acc[j][2 * i + ii][r] * alpha;
           if constexpr (IN > 0) {
             const f16x4 x = *reinterpret_cast<const f16x4*>(p);
+            const float times = TAKES ? rest[TAKES ? 2 * i + ii : 0] : beta;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = fmaf((float)x[r], beta, v[r]);
+            for (int r = 0; r < 4; ++r) v[r] = fmaf((float)x[r], times, v[r]);
           }
           if constexpr (IN > 1) {
             const f16x4 x = *reinterpret_cast<const f16x4*>(p + SLAB16);
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] = fmaf((float)x[r], beta, v[r]);
           }
-          if (EPI == kPoly) {
-            const int d = d0 + (2 * i + ii - j) * 16;
+          const bool diagonal = EPI == kPoly && j - 2 * i - ii == tile_d;
+          if (diagonal) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] += d == r ? g.diagonal : 0.f;
+            for (int r = 0; r < 4; ++r) v[r] += in_d == r ? g.diagonal : 0.f;
           }
+          // (pinned in 32 bits for every tile alike: see split)
           f16 hi[4], lo[4];
-          if constexpr (OUT > 1) {
-            split<4>(v, hi, lo);
-            *reinterpret_cast<f16x4*>(p + (IN + 1) * SLAB16) = f16x4{lo[0], lo[1], lo[2], lo[3]};
-          } else {
+          split<4>(v, hi, lo);
+          if constexpr (OUT > 1) *reinterpret_cast<f16x4*>(p + (IN + 1) * SLAB16) = f16x4{lo[0], lo[1], lo[2], lo[3]};
+          if (KEEPS && diagonal) {
+            float lost = 0.f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) hi[r] = (f16)v[r];
+            for (int r = 0; r < 4; ++r) lost = in_d == r ? v[r] - (float)hi[r] : lost;
+            store4(rest_rs, (unsigned)in_d < 4u ? rest_row + (unsigned)(2 * i + ii) * 64u : 1u << 31, lost);
           }
           *reinterpret_cast<f16x4*>(p + IN * SLAB16) = f16x4{hi[0], hi[1], hi[2], hi[3]};
         }
@@ -807,7 +823,7 @@ struct Buffers {
   bool pairs;                         // every operand with its remainder
   int planes;                         // of G and P; X has two
   int sum_blocks, gram_parts;
-  size_t part, factor, x[2], g, p, gram, total;
+  size_t part, factor, x[2], g, p, rest, gram, total;
 };
 
 Buffers buffers(int n, int rows, int cols, int dtype) {
@@ -825,6 +841,7 @@ Buffers buffers(int n, int rows, int cols, int dtype) {
   for (int i = 0; i < 2; ++i) b.x[i] = take((size_t)n * 2 * b.lo_p * b.hi_p * 2);
   b.g = take((size_t)n * b.planes * b.lo_p * b.lo_p * 2);
   b.p = take((size_t)n * b.planes * b.lo_p * b.lo_p * 2);
+  b.rest = take(b.pairs ? 0 : (size_t)n * b.lo_p * 4);
   b.gram_parts = plan::gram_parts(b.lo_p, b.hi_p, n, b.pairs);
   b.gram = take(b.gram_parts > 1 ? (size_t)b.gram_parts * n * b.lo_p * b.lo_p * 4 : 0);
   b.total = off;
@@ -862,9 +879,6 @@ int launch_gram_parts(const NsArgs& g, int parts, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
 
-// carried: steps that take X with its remainder, in bf16 storage
-constexpr int kCarriedSteps = 2;
-
 template <typename T>
 int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool muon, PrepArgs a, NsArgs end, const long* param_at, char* scratch, hipStream_t s) {
   const long xs = (long)b.lo_p * b.hi_p, gs = (long)b.lo_p * b.lo_p;
@@ -890,7 +904,7 @@ int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool m
   NsArgs g = end;
   g.n = a.n;
   for (int i = 0; i < steps; ++i) {
-    const bool last = i + 1 == steps, x_lo = b.pairs || (i == 0 ? first_lo : i < kCarriedSteps), next_lo = b.pairs || i + 1 < kCarriedSteps;
+    const bool last = i + 1 == steps, x_lo = i > 0 || first_lo, next_lo = b.pairs || i + 2 < steps;         // X's remainder; the last step has none
     f16 *x = X[i & 1], *y = X[(i + 1) & 1];
     const float* factor = i == 0 ? a.factor : nullptr;
     NsArgs q = g;
@@ -911,20 +925,20 @@ int run(const Buffers& b, int steps, const float* coef, bool exact_start, bool m
     q.A = q.B = q.E = G; q.a_ms = q.b_ms = q.e_ms = b.planes * gs; q.a_lo = q.b_lo = gs; q.e_lo = b.pairs ? gs : 0; q.lda = q.ldb = b.lo_p;
     q.K = b.lo_p; q.C = P;
     q.alpha = coef[2] * ldexpf(1.f, -kGBits); q.beta = coef[1]; q.factor = nullptr;
-    q.diagonal = ldexpf(coef[0], kGBits);
+    q.diagonal = ldexpf(coef[0], kGBits); q.rest = reinterpret_cast<float*>(scratch + b.rest);
     rc = b.pairs ? launch_product<kPoly, true, true, 2, 2, float>(q, a.n, s) : launch_product<kPoly, true, false, 1, 1, float>(q, a.n, s);
     if (rc != SPES_OK) return rc;
     q.A = P; q.B = x; q.b_ms = 2 * xs; q.b_lo = xs; q.ldb = b.hi_p;
-    q.E = x + xs; q.e_ms = 2 * xs; q.lde = b.hi_p;             // the remainders
+    q.E = x; q.e_ms = 2 * xs; q.e_lo = xs; q.lde = b.hi_p;
     q.M = b.lo_p; q.N = b.hi_p; q.K = b.lo_p;
     q.C = y; q.c_ms = 2 * xs; q.c_lo = next_lo ? xs : 0; q.ldc = b.hi_p;
-    q.alpha = ldexpf(1.f, -kGBits); q.beta = x_lo ? coef[0] : 0.f; q.factor = factor;
+    q.alpha = ldexpf(1.f, -kGBits); q.beta = coef[0]; q.factor = factor;
     if (!last) {
       rc = b.pairs           ? launch_product<kStep, false, true, 0, 2, float>(q, a.n, s)
-           : x_lo && next_lo ? launch_product<kStep, false, false, 1, 2, float>(q, a.n, s)
-           : x_lo            ? launch_product<kStep, false, false, 1, 1, float>(q, a.n, s)
-           : next_lo         ? launch_product<kStep, false, false, 0, 2, float>(q, a.n, s)
-                             : launch_product<kStep, false, false, 0, 1, float>(q, a.n, s);
+           : x_lo && next_lo ? launch_product<kStep, false, false, 2, 2, float>(q, a.n, s)
+           : x_lo            ? launch_product<kStep, false, false, 2, 1, float>(q, a.n, s)
+           : next_lo         ? launch_product<kStep, false, false, 1, 2, float>(q, a.n, s)
+                             : launch_product<kStep, false, false, 1, 1, float>(q, a.n, s);
       if (rc != SPES_OK) return rc;
       continue;
     }
