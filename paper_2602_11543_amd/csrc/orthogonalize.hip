@@ -116,8 +116,8 @@ typedef Cfg<32, 64, 4, 4, 1> TileTinyPairsHalf;
 // [row][k], else B as [k][column], read through the transposing read; both permuted within a row against bank conflicts.  The main loop is
 // that of gemm_mfma.hip without its masks and index tables: stored matrices are padded, so every K-tile is whole.  Fragments are read a
 // k-step ahead of their MFMAs, and loads, reads and the scalars of the next K-tiles are dealt out over the gaps between MFMAs.
-// Bound by the matrix cores at the clock that their power allows where there are many tiles: 8 of 3584 x 4864, 842 us of a step are 1.19 PFLOP/s, 465 of
-// G 1.15 (a library product of 8192^3 in fp16: 1.24).  With few tiles by operands on their way, which every die fetches for itself: one of
+// Bound by the matrix cores at the clock that their power allows where there are many tiles: 8 of 3584 x 4864, 842 us of a step are 1.19 PFLOP/s, 895 with X in two
+// planes read and written beside it 1.12, 465 of G 1.15 (a library product of 8192^3 in fp16: 1.24).  With few tiles by operands on their way, which every die fetches for itself: one of
 // 1280 x 1536, 210 tiles of 64 x 64, 9.3 us of G for 2.1 of multiplying.
 // SPLIT: operands are pairs.  IN, OUT: planes of what is read beside the product and of the result
 // Tile `in` of matrix `mat`, in squares of BN, of which `half` is the upper or the lower half if BM is less
@@ -410,7 +410,7 @@ __device__ __forceinline__ void ns_tile(const NsArgs& g, uint4* const smem, cons
     // The result goes to the caller's matrix, turned if it is tall: W columns of a row of it to a lane.  kUpdate: w <- keep w - rate o in 32 bits, and
     // its copy in the expert store; the weights of 32 rows are requested ahead of the stores of those before.  Tiles inside the
     // matrix (WHOLE) have no guards, behind which every load would be waited for by itself: 16 of 1024 x 2048, the last step 132 -> 107 us, 8 of
-    // 4864 x 3584 1152 -> 990.
+    // 4864 x 3584 1152 -> 990.  (On 256-wide tiles the weights and results of 32 rows, beside 256 accumulators, spill 26 registers of bf16 storage, 31 of fp32.)
     const float alpha = g.alpha * f;
     float* const slab = reinterpret_cast<float*>(smem) + wave * C::SLAB;
     constexpr int W = EPI == kUpdate ? 4 : 16 / (int)sizeof(T);

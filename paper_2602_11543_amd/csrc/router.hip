@@ -4,9 +4,10 @@
 //      groups: of equal size; a group counts the sum of its two largest c that are not -inf; only the `kept` best groups are open
 //      idx = the k largest c in open groups, equal ones to the lower expert    gate = scale s[idx] (/ sum of s[idx], renorm)
 // Sixteen lanes hold a token, four consecutive experts to a lane and quad, so a wavefront works on four tokens and every
-// reduction stays within a row of lanes, in data-parallel-primitive steps.  What bounds it is the instructions of the choice, not the 4 M
-// bytes of a token: 32768 tokens over 64 experts, top-8, 12.6 us for 10 MB; 16384 over 256 in 8 groups of which 4 are open, 17.4 us for
-// 18 MB (each with 1.4 to 2.6 us for the launch that clears the counts); 48 over 64 4.2 us.
+// reduction stays within a row of lanes, in data-parallel-primitive steps.  What bounds it is the choice, not the 4 M
+// bytes of a token: 32768 tokens over 64 experts, top-8, 13.6 us for 10 MB, vector instructions in 72 % of the CUs' cycles; 16384 over 256 in 8 groups of which
+// 4 are open, 18.5 us for 18 MB, 59 % (each with 1.2 to 2.3 us for the launch that clears the counts); 48 over 64 4.2 us.  Wavefronts wait half of their time: for the
+// bias, which is asked for quad by quad, for the row and for the chosen logits, which are read again; two or four of them to a SIMD cover only part of it.
 //
 // Gradient, the choice held fixed, with g the gates' share (scale taken out) and u = scale dgate.  Every difference is between gradients, weighted by
 // shares, so nothing cancels when one expert takes all:
