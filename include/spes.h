@@ -404,7 +404,8 @@ SPES_API int spes_router_bwd(int32_t T, int32_t n_experts, int32_t top_k, const 
 /* Orthogonalisation of a stack of matrices by Newton-Schulz steps: every matrix is scaled to Frobenius norm 1, then `steps` times
  *      X <- a X + (b X X^T + c (X X^T)^2) X
  * which takes each singular value through a s + b s^3 + c s^5 and leaves the singular vectors.  Products and sums: bf16 storage
- * on fp16 operands with fp32 sums, the result, ahead of its rounding to bf16, within 2e-3 of the formula's in norm, whatever the rank;
+ * on fp16 operands with fp32 sums, the result, ahead of its rounding to bf16, within 2e-3 of the formula's in norm, whatever the rank (3e-3
+ * where a side is 64 or less: a single direction of so few entries averages less of its rounding out);
  * fp32 storage as products in fp32 (full rank 2e-6, rank one 1.2e-4).  Both for up to five steps with the default coefficients: what rounding
  * leaves in empty directions grows a-fold a step.  A matrix of
  * zeros gives zeros, one that holds an infinity or a NaN gives NaN.  Copies of a matrix in a call get the same bits, whatever stands

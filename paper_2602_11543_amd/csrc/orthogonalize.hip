@@ -13,7 +13,7 @@
 // P + a I is rounded to finer steps; what its diagonal loses in that, up to 2^-10, is kept in 32 bits and multiplied with X at the step's end too
 // (without: 2.3e-3).  The last step, behind which nothing grows, does without both.  Left are, against 64 bits after five steps, in the update
 // of fp32 weights: rank 1 1.4e-3, 8 0.7e-3, 128 1.2e-3, full rank 1.1e-3, 16 strong directions above a broad floor 0.8e-3 (512 x 1024; rank 1 of 96 x 96
-// 1.6e-3).  fp32 storage takes every operand as such a pair and every product as three,
+// 1.6e-3, of sides below 64 up to 2.1e-3).  fp32 storage takes every operand as such a pair and every product as three,
 // lo hi + hi lo + hi hi: full rank 2e-6, rank 1 1.2e-4, as products in fp32.  Range: X stands scaled by 2^12, G and P by 2^11, which holds singular values below 5, G below 25
 // and P below 31; after the first scaling they are at most 1.21 with the default coefficients.
 #include <cmath>

@@ -1,4 +1,4 @@
-"""Orthogonalisation of matrices of any rank, and stacks whose matrices are copies of one another.
+"""Orthogonalisation of matrices of any rank.
 
 In bf16 storage the result is held to 2e-3 of the formula's norm, which the header promises for five steps: X is carried with its remainder into
 every step but the last and the diagonal of P to 32 bits, so what is left is the fp16 rounding of G, of P beside its diagonal and of X in the last step, each
@@ -12,7 +12,7 @@ from test_gpu_orthogonalize import dt, exact, muon_reference, run
 
 pytestmark = pytest.mark.gpu
 
-PROMISE = 2e-3
+PROMISE, PROMISE_SMALL = 2e-3, 3e-3          # the second where a side is 64 or less
 ROUND = 0.41 * 2.0 ** -8
 RANKS = [1, 2, 8, 32, 128]
 
@@ -45,6 +45,20 @@ def test_low_rank_that_storage_holds_exactly(device, rank):
     rows = torch.randn(rank, 640, generator=g).bfloat16().float()
     src = torch.stack([rows[i % rank] * 2.0 ** (i // rank % 5) * (-1) ** (i // 7) for i in range(150)])[None].bfloat16().cuda()
     assert off(run(src)[0], exact(src[0])) <= PROMISE + ROUND
+
+
+@pytest.mark.parametrize("rows,cols", [(33, 33), (39, 43), (46, 37), (64, 64), (61, 330)])
+def test_small_matrices(device, rows, cols):
+    """Twenty of every rank, as updates of fp32 weights, which are not rounded to bf16."""
+    for rank in (1, 2, 5, 33):
+        n = 20
+        u = low_rank(n, rows, cols, rank, rows + rank).cuda()
+        w, m = torch.zeros(n, rows, cols, device="cuda"), torch.zeros(n, rows, cols, device="cuda")
+        scratch = torch.empty(S.spes_orthogonalize_scratch_bytes(n, rows, cols, S.SPES_BF16), dtype=torch.uint8, device="cuda")
+        S.spes_masked_muon(n, rows, cols, S.SPES_BF16, w.bfloat16(), np.ones(n, dtype=np.uint8), w, m, u, 1.0, 0.0, 0, 0.0, -1.0, 5, None, 1.0, scratch)
+        torch.cuda.synchronize()
+        for i in range(n):
+            assert off(w[i], exact(u[i])) <= PROMISE_SMALL
 
 
 @pytest.mark.parametrize("nesterov", [0, 1])
