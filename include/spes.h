@@ -443,6 +443,105 @@ SPES_API int spes_masked_muon(int32_t n_experts, int32_t rows, int32_t cols, int
                               float weight_decay, float update_scale, int32_t steps,
                               const float* coef, float grad_scale, void* scratch, void* stream);
 
+/* ---- The attention half of a block -----------------------------------------------------------------------------------
+ * What stands between the projections of a block's attention: the norm of every head of the queries and keys with the rotation by
+ * the token's position, and attention over sequences of unequal length with its gradients.
+ */
+
+/* Norm and rotation of T tokens' queries (heads of them) and keys (kv_heads).  Per head x of head_dim elements
+ *      hat = x (sum x^2 / head_dim + eps)^-1/2        y = hat weight      (without weights y = x)
+ *      pair i < rot_dim / 2 of y, (a, b), becomes (a cos - b sin, a sin + b cos) with cos = table[pos][i], sin = table[pos][rot_dim / 2 + i]
+ * A pair is elements i and i + rot_dim / 2, or with `interleaved` elements 2 i and 2 i + 1; elements from rot_dim on are not rotated.
+ * What angles the table holds is the caller's.  A position that it does not have gives NaN in what is rotated.
+ *
+ *  Supported: head_dim a multiple of 8, at most 256; rot_dim a multiple of 16, at most head_dim, or 0; T (heads + kv_heads) below 2^31
+ */
+typedef struct {
+  int64_t q_row, k_row; /* elements from one token's q and k to the next one's, where the projection wrote them (a token's heads stand
+                           side by side): multiples of 16 bytes                                     */
+  int32_t T;            /* tokens, >= 0                                                             */
+  int32_t heads, kv_heads, head_dim, rot_dim;
+  int32_t dtype;        /* spes_dtype of q, k, weights and results                                  */
+  int32_t interleaved;
+  int32_t n_pos;        /* rows of the table                                                        */
+  float eps;            /* >= 0                                                                     */
+} spes_qk_shape;
+
+/*  q         DEVICE [T, heads, head_dim], k DEVICE [T, kv_heads, head_dim], rows q_row and k_row elements apart
+ *  q_weight, k_weight  DEVICE [head_dim], or both NULL
+ *  table     DEVICE [n_pos, rot_dim] f32       pos  DEVICE [T] i32, or NULL: token t has position t (then n_pos >= T).  rot_dim 0: both NULL
+ *  q_out     DEVICE [T, heads, head_dim] out   k_out  DEVICE [T, kv_heads, head_dim] out
+ */
+SPES_API int spes_qk_rope_fwd(const spes_qk_shape* shape, const void* q, const void* k, const void* q_weight,
+                              const void* k_weight, const float* table, const int32_t* pos, void* q_out,
+                              void* k_out, void* stream);
+
+/* Its backward for the upstream gradients dq and dk of q_out and k_out.
+ *
+ *  dq        DEVICE [T, heads, head_dim]       dk  DEVICE [T, kv_heads, head_dim]
+ *  q, k      as above (NULL is allowed without weights)
+ *  dq_in, dk_in  DEVICE out, laid out as q and k are (q_row, k_row)
+ *  d_q_weight, d_k_weight  DEVICE [head_dim] f32; both NULL without weights or where they are frozen, then scratch may be NULL as well
+ *  accumulate    0: d_q_weight and d_k_weight are overwritten; 1: added to
+ *  scratch   DEVICE, spes_qk_rope_scratch_bytes(shape) bytes
+ */
+SPES_API size_t spes_qk_rope_scratch_bytes(const spes_qk_shape* shape);
+SPES_API int spes_qk_rope_bwd(const spes_qk_shape* shape, const void* dq, const void* dk, const void* q,
+                              const void* k, const void* q_weight, const void* k_weight, const float* table,
+                              const int32_t* pos, void* dq_in, void* dk_in, float* d_q_weight,
+                              float* d_k_weight, int32_t accumulate, void* scratch, void* stream);
+
+/* Attention of n_seq sequences' queries over their keys.  Per query and head, over the keys j that the query sees,
+ *      s_j = scale <q, k_j>        lse = ln sum_j exp s_j        o = sum_j exp(s_j - lse) v_j
+ * Head h of the queries reads head h / (heads / kv_heads) of keys and values.  Sequence b has the queries in rows q_start[b] up to q_start[b+1], and
+ * its keys and values in rows k_start[b] up to k_start[b+1], or, where k_len is given, in k_len[b] rows from k_start[b] on (a cache with room for more;
+ * in the forward sequences may share rows of it).  With `causal` the last query sees the last key and every one before it a key less: query i of
+ * lq sees the keys up to i + lk - lq, with a window the last `window` of these.  A query that sees no key has o = 0 and lse = -infinity, its dq is 0.
+ * Rows outside of all sequences are not read, and those of o, lse, dq, dk and dv are left as they are.  What the descriptors
+ * hold is cut to the tensors' rows; queries of two sequences must not overlap, nor in the backward keys.  Rows of a sequence must be finite: an
+ * infinity or a NaN in one can reach other rows of its sequence, whether they see it or not.
+ * Products in bf16 storage take bf16 operands, the probabilities and their gradient among them, and are summed in fp32; in fp32 storage they are fp32.
+ *
+ *  Supported: head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, at most 1024; q_rows heads below 2^31; strides multiples of 16 bytes,
+ *  rows at most 2^20 elements apart, heads / kv_heads heads of q within 2^28 elements
+ */
+typedef struct {
+  int64_t q_row, q_head; /* elements from a token's q to the next one's, and from a head's to the next one's; of dq as well     */
+  int64_t k_row, k_head; /* the same of k and dk                                                                                */
+  int64_t v_row, v_head; /* the same of v and dv                                                                                */
+  int32_t n_seq;         /* >= 0                                                                                                */
+  int32_t q_rows;        /* rows of q, o and lse                                                                                */
+  int32_t k_rows;        /* rows of k and v                                                                                     */
+  int32_t heads, kv_heads, head_dim;
+  int32_t dtype;         /* spes_dtype                                                                                          */
+  int32_t causal;
+  int32_t window;        /* 0: none; > 0 with causal only                                                                       */
+  float scale;           /* > 0, finite                                                                                         */
+} spes_attn_shape;
+
+/*  q         DEVICE [q_rows, heads, head_dim]     k, v  DEVICE [k_rows, kv_heads, head_dim], strides in the shape
+ *  q_start   DEVICE [n_seq + 1] i32, ascending    k_start  DEVICE [n_seq + 1] i32 ([n_seq] with k_len)      k_len  DEVICE [n_seq] i32 or NULL
+ *  o         DEVICE [q_rows, heads, head_dim] out
+ *  lse       DEVICE [heads, q_rows] f32 out
+ *  scratch   DEVICE, spes_attn_scratch_bytes(shape, 0) bytes
+ */
+SPES_API size_t spes_attn_scratch_bytes(const spes_attn_shape* shape, int32_t backward);
+SPES_API int spes_attn_fwd(const spes_attn_shape* shape, const void* q, const void* k, const void* v,
+                           const int32_t* q_start, const int32_t* k_start, const int32_t* k_len, void* o,
+                           float* lse, void* scratch, void* stream);
+
+/* Its backward for the upstream gradient d_o of o.  The probabilities are formed again from q, k and lse.
+ *
+ *  d_o       DEVICE [q_rows, heads, head_dim]
+ *  o, lse    as the forward left them; all other inputs as above
+ *  dq        DEVICE out, laid out as q is;  dk, dv  DEVICE out, laid out as k and v are.  They are overwritten
+ *  scratch   DEVICE, spes_attn_scratch_bytes(shape, 1) bytes
+ */
+SPES_API int spes_attn_bwd(const spes_attn_shape* shape, const void* d_o, const void* q, const void* k,
+                           const void* v, const int32_t* q_start, const int32_t* k_start,
+                           const int32_t* k_len, const void* o, const float* lse, void* dq, void* dk,
+                           void* dv, void* scratch, void* stream);
+
 SPES_API const char* spes_strerror(int code);
 
 #ifdef __cplusplus

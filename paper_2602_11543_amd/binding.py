@@ -42,6 +42,16 @@ class spes_router_opts(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("score", "groups", "kept_groups", "renorm")] + [("scale", ctypes.c_float)]
 
 
+class spes_qk_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("q_row", "k_row")] + \
+        [(n, ctypes.c_int32) for n in ("T", "heads", "kv_heads", "head_dim", "rot_dim", "dtype", "interleaved", "n_pos")] + [("eps", ctypes.c_float)]
+
+
+class spes_attn_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head")] + \
+        [(n, ctypes.c_int32) for n in ("n_seq", "q_rows", "k_rows", "heads", "kv_heads", "head_dim", "dtype", "causal", "window")] + [("scale", ctypes.c_float)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(_build.LIB):
         _build.build_library(verbose=False)      # raises if hipcc is unavailable
@@ -97,6 +107,19 @@ def _load() -> ctypes.CDLL:
     lib.spes_orthogonalize.argtypes = [i32] * 4 + [vp, vp, i32, vp, vp, vp]
     lib.spes_masked_muon.restype = i32
     lib.spes_masked_muon.argtypes = [i32] * 4 + [vp] * 5 + [ctypes.c_float, ctypes.c_float, i32, ctypes.c_float, ctypes.c_float, i32, vp, ctypes.c_float, vp, vp]
+    qk, attn = ctypes.POINTER(spes_qk_shape), ctypes.POINTER(spes_attn_shape)
+    lib.spes_qk_rope_fwd.restype = i32
+    lib.spes_qk_rope_fwd.argtypes = [qk] + [vp] * 9
+    lib.spes_qk_rope_scratch_bytes.restype = sz
+    lib.spes_qk_rope_scratch_bytes.argtypes = [qk]
+    lib.spes_qk_rope_bwd.restype = i32
+    lib.spes_qk_rope_bwd.argtypes = [qk] + [vp] * 12 + [i32, vp, vp]
+    lib.spes_attn_scratch_bytes.restype = sz
+    lib.spes_attn_scratch_bytes.argtypes = [attn, i32]
+    lib.spes_attn_fwd.restype = i32
+    lib.spes_attn_fwd.argtypes = [attn] + [vp] * 10
+    lib.spes_attn_bwd.restype = i32
+    lib.spes_attn_bwd.argtypes = [attn] + [vp] * 14
     lib.spes_ref_mfma_rate.restype = i32
     lib.spes_ref_mfma_rate.argtypes = [vp, i32, i32, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.spes_profile_enable.restype = i32
@@ -147,6 +170,26 @@ def _rows(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype):
     if not t.is_cuda or (cols > 1 and t.stride(1) != 1) or stride < cols:
         raise SpesError("matrix arguments must be GPU tensors with contiguous rows that do not overlap")
     return t.data_ptr(), stride
+
+
+def _heads(t: Optional[torch.Tensor], rows: int, heads: int, dim: int, dtype: torch.dtype):
+    """Pointer, row stride and head stride of a [rows, heads, dim] tensor that may be a view."""
+    if t is None:
+        return None, heads * dim, dim
+    if t.shape != (rows, heads, dim) or t.dtype != dtype:
+        raise SpesError(f"expected a GPU tensor of {(rows, heads, dim)} {dtype}, got {tuple(t.shape)} {t.dtype}")
+    row, head, one = t.stride()
+    if not t.is_cuda or (dim > 1 and one != 1):
+        raise SpesError("head tensors must be GPU tensors with contiguous elements")
+    return t.data_ptr(), row if rows > 1 else heads * dim, head if heads > 1 else dim
+
+
+def _like(t: Optional[torch.Tensor], strides, *want):
+    """Pointer of an output that is laid out as its input is."""
+    p, *got = _heads(t, *want)
+    if t is not None and tuple(got) != tuple(strides):
+        raise SpesError("the gradient of a tensor must be laid out as the tensor is")
+    return p
 
 
 def _scratch(t: Optional[torch.Tensor], bytes_of, *args):
@@ -371,6 +414,89 @@ def spes_masked_muon(n_experts, rows, cols, dtype, param, trainable_mask, master
                                  lr, beta, int(nesterov), weight_decay, update_scale, steps, _coef(coef), grad_scale,
                                  _scratch(scratch, _lib.spes_orthogonalize_scratch_bytes, n, rows, cols, dtype) if n else None,
                                  _stream(stream)), "spes_masked_muon")
+
+
+def qk_shape(T, heads, kv_heads, head_dim, rot_dim, dtype, interleaved=0, n_pos=0, eps=1e-6) -> spes_qk_shape:
+    """Rows as far apart as they are long; a call takes the strides of its tensors."""
+    return spes_qk_shape(heads * head_dim, kv_heads * head_dim, T, heads, kv_heads, head_dim, rot_dim, dtype, int(interleaved), n_pos, eps)
+
+
+def _qk(shape, q, k):
+    """The shape with the strides of q and k, and their pointers."""
+    t = torch_dtype(shape.dtype)
+    qp, q_row, q_head = _heads(q, shape.T, shape.heads, shape.head_dim, t)
+    kp, k_row, k_head = _heads(k, shape.T, shape.kv_heads, shape.head_dim, t)
+    if q_head != shape.head_dim or k_head != shape.head_dim:
+        raise SpesError("a token's heads must stand side by side")
+    own = spes_qk_shape.from_buffer_copy(shape)
+    own.q_row, own.k_row = q_row, k_row
+    return own, qp, kp
+
+
+def spes_qk_rope_fwd(shape, q, k, q_weight, k_weight, table, pos, q_out, k_out, stream=None) -> None:
+    """q and k may be views of the projection's output; their strides go into the call."""
+    t, D, f = torch_dtype(shape.dtype), shape.head_dim, torch.float32
+    own, qp, kp = _qk(shape, q, k)
+    _check(_lib.spes_qk_rope_fwd(own, qp, kp, _buf(q_weight, t, D), _buf(k_weight, t, D), _buf(table, f, shape.n_pos, shape.rot_dim),
+                                 _buf(pos, torch.int32, shape.T), _buf(q_out, t, shape.T, shape.heads, D), _buf(k_out, t, shape.T, shape.kv_heads, D),
+                                 _stream(stream)), "spes_qk_rope_fwd")
+
+
+def spes_qk_rope_scratch_bytes(shape) -> int:
+    return int(_lib.spes_qk_rope_scratch_bytes(shape))
+
+
+def spes_qk_rope_bwd(shape, dq, dk, q, k, q_weight, k_weight, table, pos, dq_in, dk_in, d_q_weight, d_k_weight, accumulate=0, scratch=None,
+                     stream=None) -> None:
+    """dq_in and dk_in may be views of the gradient of the projection's output, with the strides of q and k."""
+    t, D, f = torch_dtype(shape.dtype), shape.head_dim, torch.float32
+    own, op, okp = _qk(shape, dq_in, dk_in)
+    qp = _like(q, (own.q_row, D), shape.T, shape.heads, D, t)
+    kp = _like(k, (own.k_row, D), shape.T, shape.kv_heads, D, t)
+    _check(_lib.spes_qk_rope_bwd(own, _buf(dq, t, shape.T, shape.heads, D), _buf(dk, t, shape.T, shape.kv_heads, D), qp, kp, _buf(q_weight, t, D),
+                                 _buf(k_weight, t, D), _buf(table, f, shape.n_pos, shape.rot_dim), _buf(pos, torch.int32, shape.T), op, okp,
+                                 _buf(d_q_weight, f, D), _buf(d_k_weight, f, D), int(accumulate), _scratch(scratch, _lib.spes_qk_rope_scratch_bytes, shape),
+                                 _stream(stream)), "spes_qk_rope_bwd")
+
+
+def attn_shape(n_seq, q_rows, k_rows, heads, kv_heads, head_dim, dtype, causal=1, window=0, scale=None) -> spes_attn_shape:
+    """Rows and heads as far apart as they are long; a call takes the strides of its tensors.  scale: 1 / sqrt(head_dim) if not given."""
+    return spes_attn_shape(heads * head_dim, head_dim, kv_heads * head_dim, head_dim, kv_heads * head_dim, head_dim, n_seq, q_rows, k_rows, heads, kv_heads,
+                           head_dim, dtype, int(causal), window, head_dim ** -0.5 if scale is None else scale)
+
+
+def spes_attn_scratch_bytes(shape, backward=0) -> int:
+    return int(_lib.spes_attn_scratch_bytes(shape, int(backward)))
+
+
+def _attn(shape, q, k, v, q_start, k_start, k_len):
+    """The shape with the strides of q, k and v, and the pointers of these and of the descriptors."""
+    t, i, n, D = torch_dtype(shape.dtype), torch.int32, shape.n_seq, shape.head_dim
+    own = spes_attn_shape.from_buffer_copy(shape)
+    qp, own.q_row, own.q_head = _heads(q, shape.q_rows, shape.heads, D, t)
+    kp, own.k_row, own.k_head = _heads(k, shape.k_rows, shape.kv_heads, D, t)
+    vp, own.v_row, own.v_head = _heads(v, shape.k_rows, shape.kv_heads, D, t)
+    return own, qp, kp, vp, _buf(q_start, i, n + 1), _buf(k_start, i, n + (k_len is None)), _buf(k_len, i, n)
+
+
+def spes_attn_fwd(shape, q, k, v, q_start, k_start, k_len, o, lse, scratch, stream=None) -> None:
+    """q, k and v may be views; their strides go into the call."""
+    t, D = torch_dtype(shape.dtype), shape.head_dim
+    own, *inputs = _attn(shape, q, k, v, q_start, k_start, k_len)
+    _check(_lib.spes_attn_fwd(own, *inputs, _buf(o, t, shape.q_rows, shape.heads, D), _buf(lse, torch.float32, shape.heads, shape.q_rows),
+                              _scratch(scratch, _lib.spes_attn_scratch_bytes, shape, 0), _stream(stream)), "spes_attn_fwd")
+
+
+def spes_attn_bwd(shape, d_o, q, k, v, q_start, k_start, k_len, o, lse, dq, dk, dv, scratch, stream=None) -> None:
+    """q, k and v may be views; dq, dk and dv are laid out as they are."""
+    t, D = torch_dtype(shape.dtype), shape.head_dim
+    own, *inputs = _attn(shape, q, k, v, q_start, k_start, k_len)
+    _check(_lib.spes_attn_bwd(own, _buf(d_o, t, shape.q_rows, shape.heads, D), *inputs, _buf(o, t, shape.q_rows, shape.heads, D),
+                              _buf(lse, torch.float32, shape.heads, shape.q_rows),
+                              _like(dq, (own.q_row, own.q_head), shape.q_rows, shape.heads, D, t),
+                              _like(dk, (own.k_row, own.k_head), shape.k_rows, shape.kv_heads, D, t),
+                              _like(dv, (own.v_row, own.v_head), shape.k_rows, shape.kv_heads, D, t),
+                              _scratch(scratch, _lib.spes_attn_scratch_bytes, shape, 1), _stream(stream)), "spes_attn_bwd")
 
 
 def spes_profile_enable(on: bool) -> None:

@@ -1,0 +1,201 @@
+// What the attention kernels share: how a problem is cut into tiles, tiles in LDS, operand fragments of the 32 x 32 matrix instructions.
+//
+// Rows.  The heads that share keys stand side by side: row r of a sequence is query r / G under head kvh * G + r % G, G = heads / kv_heads, so a tile of rows
+// meets every key once for all of them, and a sum over the rows is one over the heads as well.
+//
+// Orientation.  Scores are formed as S^T = K Q^T (queries' kernels: keys down, rows across) or S = Q K^T (keys' kernel), so that a lane holds sixteen
+// scores of one column, 8 (i / 4) + 4 (lane / 32) + i % 4 for its register i.  The contraction that follows runs over just these: as its order is free, a
+// lane's registers 0..7 and 8..15 are its operand fragments as they stand, and the other operand is read from LDS in the same order.
+#pragma once
+#include "lds_load.h"
+#include "kernels.h"
+
+namespace spes {
+namespace attn {
+
+constexpr int kRows = 128;       // rows of a block of four wavefronts, 32 each
+constexpr int kStep = 64;        // keys (rows, in the keys' kernel) that pass through LDS at a time
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+struct f32x8 { float v[8]; };
+
+template <typename T> struct Mma;
+template <> struct Mma<bf16_t> {
+  typedef bf16x8 Frag;           // sixteen of the contraction: eight of each half of the lanes
+  static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, const f32x16& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ Frag zero() { return __builtin_bit_cast(Frag, make_uint4(0, 0, 0, 0)); }
+  static __device__ __forceinline__ Frag load(const bf16_t* p) { return __builtin_bit_cast(Frag, *reinterpret_cast<const uint4*>(p)); }
+  // registers 8 n .. 8 n + 7 of a tile of results, rounded to the operands' type
+  static __device__ __forceinline__ Frag of(const f32x16& s, int n) {
+    return __builtin_bit_cast(Frag, make_uint4(pack_bf16x2(s[8 * n], s[8 * n + 1]), pack_bf16x2(s[8 * n + 2], s[8 * n + 3]),
+                                               pack_bf16x2(s[8 * n + 4], s[8 * n + 5]), pack_bf16x2(s[8 * n + 6], s[8 * n + 7])));
+  }
+  static __device__ __forceinline__ float get(const Frag& f, int j) { return (float)f[j]; }
+};
+template <> struct Mma<float> {
+  typedef f32x8 Frag;
+  static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ Frag zero() { return Frag{}; }
+  static __device__ __forceinline__ Frag load(const float* p) {
+    const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+    return Frag{{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}};
+  }
+  static __device__ __forceinline__ Frag of(const f32x16& s, int n) {
+    Frag f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.v[j] = s[8 * n + j];
+    return f;
+  }
+  static __device__ __forceinline__ float get(const Frag& f, int j) { return f.v[j]; }
+};
+
+__device__ __forceinline__ unsigned lds_address(void* p) { return uniform((unsigned)(unsigned long)(__attribute__((address_space(3))) char*)p); }
+// from `base` on, for offsets below 2^31
+__device__ __forceinline__ rsrc_t open_rsrc(unsigned long base) {
+  return rsrc_t{uniform((unsigned)base), uniform((unsigned)(base >> 32)), 0x80000000u, 0x00020000u};
+}
+
+// A tile in LDS: rows of DH elements, chunk c (16 bytes) of row r at position c ^ turn(r).  LDS has 64 banks of four bytes, a read of 16 bytes a lane
+// takes sixteen lanes at a time: sixteen rows at one chunk, and in the transposing reads four rows of 64 bytes (fp32: two of 128), meet every bank once.
+template <typename T, int DH>
+struct Tile {
+  static constexpr int kRowBytes = DH * (int)sizeof(T), kChunks = kRowBytes / 16, kRowsPerLoad = 64 / kChunks;
+  static __device__ __forceinline__ int turn(int r) {
+    if (sizeof(T) == 4) return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3);
+    if (DH == 64) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+    return (r & 3) << 2 | ((r >> 2) & 3);
+  }
+  // fragments of rows: lane (x = lane % 32, h = lane / 32) takes elements 16 kc + 8 h .. + 7 of row 32 n + x
+  static __device__ __forceinline__ unsigned row_base(int lane) {
+    const int x = lane & 31, h = lane >> 5;
+    return (unsigned)(x * kRowBytes + (((sizeof(T) == 4 ? 2 * h : h) ^ turn(x)) << 4));
+  }
+  static __device__ __forceinline__ typename Mma<T>::Frag row_frag(const char* slot, unsigned base, int n, int kc) {
+    if constexpr (sizeof(T) == 2) {
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(slot + (base ^ (unsigned)(kc << 5)) + n * 32 * kRowBytes));
+    } else {
+      const float4 p = *reinterpret_cast<const float4*>(slot + (base ^ (unsigned)((4 * kc) << 4)) + n * 32 * kRowBytes);
+      const float4 q = *reinterpret_cast<const float4*>(slot + (base ^ (unsigned)((4 * kc + 1) << 4)) + n * 32 * kRowBytes);
+      return f32x8{{p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w}};
+    }
+  }
+  // fragments of columns: lane (x, h) takes column 32 db + x of rows 16 kk + 4 h + 0..3 and 16 kk + 8 + 4 h + 0..3
+  static __device__ __forceinline__ unsigned col_base(int lane) {
+    const int h = lane >> 5;
+    if (sizeof(T) == 4) return (unsigned)(4 * h * kRowBytes + ((((lane & 31) >> 2) ^ (h << 3)) << 4) + (lane & 3) * 4);
+    const int s = lane & 15, r = 4 * h + (s >> 2);
+    return (unsigned)(r * kRowBytes + (((((lane >> 4) & 1) * 2 + ((s & 3) >> 1)) ^ turn(r)) << 4) + (s & 1) * 8);
+  }
+  static __device__ __forceinline__ typename Mma<T>::Frag col_frag(const char* slot, unsigned base, int db, int kk) {
+    if constexpr (sizeof(T) == 2) {
+      const uint2 p = lds_read_tr(reinterpret_cast<const bf16_t*>(slot + (base ^ (unsigned)(db << 6)) + 16 * kk * kRowBytes));
+      const uint2 q = lds_read_tr(reinterpret_cast<const bf16_t*>(slot + (base ^ (unsigned)(db << 6 | 32)) + (16 * kk + 8) * kRowBytes));
+      return __builtin_bit_cast(bf16x8, make_uint4(p.x, p.y, q.x, q.y));
+    } else {
+      f32x8 f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        f.v[j] = *reinterpret_cast<const float*>(slot + (base ^ (unsigned)((8 * db ^ (j & 4) ^ (j & 3)) << 4)) + (16 * kk + (j & 3) + 8 * (j >> 2)) * kRowBytes);
+      return f;
+    }
+  }
+  // one wavefront's load i of a slot: lane l brings the chunk that belongs at position l % kChunks of row `row(i, l)`
+  static constexpr int kLoads = kStep / (4 * kRowsPerLoad);                 // of each of four wavefronts for kStep rows
+  static __device__ __forceinline__ int load_row(int wave, int i, int lane) { return (wave * kLoads + i) * kRowsPerLoad + lane / kChunks; }
+  static __device__ __forceinline__ int load_chunk(int row, int lane) { return (lane % kChunks) ^ turn(row); }
+  // byte offset from a slot's first row in memory, rows `stride` elements apart, of `dim` elements
+  static __device__ __forceinline__ unsigned load_off(int wave, int i, int lane, long stride, int dim) {
+    const int r = load_row(wave, i, lane), ch = load_chunk(r, lane);
+    return ch * (16 / (int)sizeof(T)) < dim ? (unsigned)(r * stride * (long)sizeof(T) + ch * 16) : kOutOfRange;
+  }
+  // rows j kStep .. of the `rows` rows from `base` into the slot at `dst`; zeros beyond the last row and element
+  static __device__ __forceinline__ void load_rows(unsigned long base, int j, long stride, int rows, const unsigned (&off)[kLoads], unsigned dst, int wave,
+                                                   int lane) {
+    const rsrc_t rs = open_rsrc(base + (unsigned long)((long)j * kStep * stride * (long)sizeof(T)));
+    const int left = rows - j * kStep;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const unsigned o = load_row(wave, i, lane) < left ? off[i] : kOutOfRange;
+      const unsigned m = set_lds_dest(uniform(dst + (unsigned)((wave * kLoads + i) * 1024)));
+      one_instruction();
+      load_to_lds(rs, o, m);
+    }
+  }
+};
+
+__device__ __forceinline__ float both_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+
+__device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
+__device__ __forceinline__ void put4(bf16_t* p, float a, float b, float c, float d) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+}
+__device__ __forceinline__ void put2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
+__device__ __forceinline__ void put2(bf16_t* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(a, b); }
+
+// A sequence as the descriptors give it, cut to the rows that there are, so that whatever they hold no access leaves the tensors
+struct Seq { int q0, lq, k0, lk; };
+__device__ __forceinline__ Seq sequence(const AttnShape& a, int b) {
+  Seq s;
+  s.q0 = min(max(a.q_start[b], 0), a.q_rows);
+  s.lq = min(max(a.q_start[b + 1], s.q0), a.q_rows) - s.q0;
+  s.k0 = min(max(a.k_start[b], 0), a.k_rows);
+  const int len = a.k_len ? a.k_len[b] : max(a.k_start[b + 1], s.k0) - s.k0;
+  s.lk = min(max(len, 0), a.k_rows - s.k0);
+  return s;
+}
+
+// Item t of the list of all sequences' tiles, `per` rows (or keys) each: the sequence, and which of its tiles.  Every wavefront goes over the
+// sequences for itself, 64 at a time.  False beyond the list's end.
+template <bool KEYS>
+__device__ __forceinline__ bool find_tile(const AttnShape& a, int t, int per, int lane, Seq& seq, int& tile, int& tiles) {
+  int before = 0;
+  for (int b0 = 0; b0 < a.n_seq; b0 += kWave) {
+    const int b = b0 + lane;
+    Seq s = {0, 0, 0, 0};
+    if (b < a.n_seq) s = sequence(a, b);
+    const int n = KEYS ? cdiv(s.lk, per) : cdiv((long)s.lq * a.group, per);
+    int sum = n;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      const int up = __shfl_up(sum, d, kWave);
+      if (lane >= d) sum += up;
+    }
+    const unsigned long has = __ballot(t < before + sum);
+    if (has) {
+      const int at = __builtin_ctzl(has);
+      auto pick = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+      seq = Seq{pick(s.q0), pick(s.lq), pick(s.k0), pick(s.lk)};
+      tiles = pick(n);
+      tile = t - before - (pick(sum) - tiles);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  return false;
+}
+
+// Keys [lo, hi) that query i of a sequence sees
+struct Reach { int lo, hi; };
+__device__ __forceinline__ Reach reach(const AttnShape& a, const Seq& s, int i) {
+  if (!a.causal) return Reach{0, s.lk};
+  const int end = min(max(i + s.lk - s.lq + 1, 0), s.lk);
+  return Reach{a.window > 0 ? max(end - a.window, 0) : 0, end};
+}
+
+}  // namespace attn
+}  // namespace spes

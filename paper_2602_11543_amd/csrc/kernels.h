@@ -78,6 +78,33 @@ int launch_masked_muon(int dtype, int n, int rows, int cols, void* param, const 
                        float beta, int nesterov, float weight_decay, float update_scale, int steps, const float* coef, float grad_scale, void* scratch,
                        hipStream_t s);
 
+// attention.hip, attention_bwd.hip
+struct AttnShape {
+  const int *q_start, *k_start, *k_len;
+  long q_row, q_head, k_row, k_head, v_row, v_head;      // strides in elements
+  int n_seq, q_rows, k_rows, heads, kv_heads, group, dim, causal, window;
+  float scale;
+};
+size_t attn_fwd_scratch_bytes(int dtype, const AttnShape& a);
+int launch_attn_fwd(int dtype, const AttnShape& a, const void* q, const void* k, const void* v, void* o, float* lse, void* scratch, hipStream_t s);
+size_t attn_bwd_scratch_bytes(int dtype, const AttnShape& a);
+// dq, dk, dv laid out as q, k, v are
+int launch_attn_bwd(int dtype, const AttnShape& a, const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse, void* dq,
+                    void* dk, void* dv, void* scratch, hipStream_t s);
+
+// qk_rope.hip: norm and rotation of T x (heads + kv_heads) heads; a NULL weight: no norm
+struct QkShape {
+  long q_row, k_row;
+  int T, heads, kv_heads, dim, rot, interleaved, n_pos;
+  float eps;
+};
+int launch_qk_rope_fwd(int dtype, const QkShape& a, const void* q, const void* k, const void* q_weight, const void* k_weight, const float* table,
+                       const int* pos, void* q_out, void* k_out, hipStream_t s);
+size_t qk_rope_scratch_bytes(const QkShape& a);
+int launch_qk_rope_bwd(int dtype, const QkShape& a, const void* dq, const void* dk, const void* q, const void* k, const void* q_weight,
+                       const void* k_weight, const float* table, const int* pos, void* dq_in, void* dk_in, float* d_q_weight, float* d_k_weight,
+                       int accumulate, float* scratch, hipStream_t s);
+
 // reference.hip: register-resident MFMA loop (blocks x 4 wavefronts x iters x 64 MFMAs of 16x16x32); *flop = operations launched
 int launch_mfma_rate(const void* data, int blocks, int iters, float* sink, double* flop, hipStream_t s);
 
