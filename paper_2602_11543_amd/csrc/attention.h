@@ -15,6 +15,7 @@ namespace attn {
 
 constexpr int kRows = 128;       // rows of a block of four wavefronts, 32 each
 constexpr int kStep = 64;        // keys (rows, in the keys' kernel) that pass through LDS at a time
+constexpr int kNone = 1 << 24;   // the number of a tile that no sequence has (2^30 keys: behind the last of them, or its loads are not used)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -58,8 +59,21 @@ template <> struct Mma<float> {
 
 __device__ __forceinline__ unsigned lds_address(void* p) { return uniform((unsigned)(unsigned long)(__attribute__((address_space(3))) char*)p); }
 // from `base` on, for offsets below 2^31
-__device__ __forceinline__ rsrc_t open_rsrc(unsigned long base) {
-  return rsrc_t{uniform((unsigned)base), uniform((unsigned)(base >> 32)), 0x80000000u, 0x00020000u};
+__device__ __forceinline__ rsrc_t open_rsrc(unsigned long base, bool any = true) {
+  return rsrc_t{uniform((unsigned)base), uniform((unsigned)(base >> 32)), any ? 0x80000000u : 0u, 0x00020000u};
+}
+
+// The order of a stretch of code with N matrix instructions, READS LDS reads and VALU other instructions to each: the first AHEAD
+// instructions' reads come first, the others' one instruction after another
+template <int N, int READS, int AHEAD, int VALU>
+__device__ __forceinline__ void interleave() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (i + AHEAD < N) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    if (VALU) __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
+  }
 }
 
 // A tile in LDS: rows of DH elements, chunk c (16 bytes) of row r at position c ^ turn(r).  LDS has 64 banks of four bytes, a read of 16 bytes a lane
@@ -110,19 +124,17 @@ struct Tile {
   static constexpr int kLoads = kStep / (4 * kRowsPerLoad);                 // of each of four wavefronts for kStep rows
   static __device__ __forceinline__ int load_row(int wave, int i, int lane) { return (wave * kLoads + i) * kRowsPerLoad + lane / kChunks; }
   static __device__ __forceinline__ int load_chunk(int row, int lane) { return (lane % kChunks) ^ turn(row); }
-  // byte offset from a slot's first row in memory, rows `stride` elements apart, of `dim` elements
+  // byte offset from a slot's first row in memory, rows `stride` bytes apart, of `dim` elements
   static __device__ __forceinline__ unsigned load_off(int wave, int i, int lane, long stride, int dim) {
     const int r = load_row(wave, i, lane), ch = load_chunk(r, lane);
-    return ch * (16 / (int)sizeof(T)) < dim ? (unsigned)(r * stride * (long)sizeof(T) + ch * 16) : kOutOfRange;
+    return ch * (16 / (int)sizeof(T)) < dim ? (unsigned)(r * stride + ch * 16) : kOutOfRange;
   }
-  // rows j kStep .. of the `rows` rows from `base` into the slot at `dst`; zeros beyond the last row and element
-  static __device__ __forceinline__ void load_rows(unsigned long base, int j, long stride, int rows, const unsigned (&off)[kLoads], unsigned dst, int wave,
-                                                   int lane) {
-    const rsrc_t rs = open_rsrc(base + (unsigned long)((long)j * kStep * stride * (long)sizeof(T)));
-    const int left = rows - j * kStep;
+  // kStep rows, at most `rows` of them real, from `base` on into LDS at `dst`; zeros beyond
+  static __device__ __forceinline__ void load_rows(unsigned long base, long stride, int rows, int dim, unsigned dst, int wave, int lane) {
+    const rsrc_t rs = {uniform((unsigned)base), uniform((unsigned)(base >> 32)), uniform((unsigned)(max(min(rows, kStep), 0) * stride)), 0x00020000u};
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const unsigned o = load_row(wave, i, lane) < left ? off[i] : kOutOfRange;
+      const unsigned o = load_off(wave, i, lane, stride, dim);
       const unsigned m = set_lds_dest(uniform(dst + (unsigned)((wave * kLoads + i) * 1024)));
       one_instruction();
       load_to_lds(rs, o, m);
@@ -130,6 +142,44 @@ struct Tile {
   }
 };
 
+// Two tensors' tiles on their way into a slot, one wavefront's load at a time: the vector-memory path takes a load of a wavefront in sixteen clocks, and a
+// wavefront that issues one behind the other stands still (eight in a row: 440 clocks), so callers deal them out over their matrix instructions
+template <typename T, int DH>
+struct PairLoad {
+  typedef Tile<T, DH> L;
+  static constexpr int kPieces = 2 * L::kLoads;
+  const unsigned (&off)[2][L::kLoads];
+  rsrc_t rs[2];
+  unsigned dst;
+  // rows j kStep .. of `rows` rows, stride[i] bytes apart from base[i]; zeros beyond the last one (the resource ends there) and beyond a row's elements.
+  // Where there is no such tile the loads bring zeros: a loop issues them to its end, without a branch in the middle of its matrix instructions
+  __device__ __forceinline__ PairLoad(const unsigned (&off_)[2][L::kLoads], const unsigned long (&base)[2], const long (&stride)[2], int rows, int j, unsigned slot,
+                                      int wave)
+      : off(off_), dst(slot + (unsigned)(wave * L::kLoads * 1024)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned long at = base[i] + (unsigned long)((long)j * kStep * stride[i]);
+      const unsigned bytes = (unsigned)(max(min(rows - j * kStep, kStep), 0) * stride[i]);
+      rs[i] = rsrc_t{uniform((unsigned)at), uniform((unsigned)(at >> 32)), uniform(bytes), 0x00020000u};
+    }
+  }
+  // from resources that are there
+  __device__ __forceinline__ PairLoad(const unsigned (&off_)[2][L::kLoads], const rsrc_t& first, const rsrc_t& second, unsigned slot, int wave)
+      : off(off_), rs{first, second}, dst(slot + (unsigned)(wave * L::kLoads * 1024)) {}
+  __device__ __forceinline__ void piece(int p) const {
+    const int i = p / L::kLoads, n = p % L::kLoads;
+    const unsigned m = set_lds_dest(uniform(dst + (unsigned)((i * kStep * L::kRowBytes) + n * 1024)));
+    one_instruction();
+    load_to_lds(rs[i], off[i][n], m);
+  }
+  __device__ __forceinline__ void all() const {
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) piece(p);
+  }
+};
+
+// The last loads into LDS, before a block may end
+__device__ __forceinline__ void drain() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ float both_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -139,6 +189,23 @@ __device__ __forceinline__ float both_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// Fragments loaded from memory are waited for here, not at their first use inside a loop, where the wait would be for the loads into LDS behind them as well
+template <typename F, int N>
+__device__ __forceinline__ void settle(F (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (sizeof(F) == 16) {
+      rsrc_t r = __builtin_bit_cast(rsrc_t, f[i]);
+      asm volatile("" : "+v"(r));
+      f[i] = __builtin_bit_cast(F, r);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(f[i].v[j]));
+    }
+  }
+}
+__device__ __forceinline__ void settle(float& v) { asm volatile("" : "+v"(v)); }
 
 __device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ __forceinline__ void put4(bf16_t* p, float a, float b, float c, float d) {

@@ -61,39 +61,53 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(c
     for (int kc = 0; kc < KC; ++kc) qf[kc] = real && 16 * kc + 8 * half < a.dim ? Mma<T>::load(qp + 16 * kc) : Mma<T>::zero();
   }
 
-  const unsigned long k_base = (unsigned long)g.k + (unsigned long)((long)s.k0 * a.k_row + (long)kvh * a.k_head) * ES;
-  const unsigned long v_base = (unsigned long)g.v + (unsigned long)((long)s.k0 * a.v_row + (long)kvh * a.v_head) * ES;
+  // keys and values on their way into LDS
+  const long stride[2] = {a.k_row * ES, a.v_row * ES};
+  const unsigned long base[2] = {(unsigned long)g.k + (unsigned long)(s.k0 * stride[0] + (long)kvh * a.k_head * ES),
+                                 (unsigned long)g.v + (unsigned long)(s.k0 * stride[1] + (long)kvh * a.v_head * ES)};
   const unsigned lds0 = lds_address(smem);
-  unsigned k_off[L::kLoads], v_off[L::kLoads];
+  unsigned off[2][L::kLoads];
 #pragma unroll
-  for (int i = 0; i < L::kLoads; ++i) {
-    k_off[i] = L::load_off(wave, i, lane, a.k_row, a.dim);
-    v_off[i] = L::load_off(wave, i, lane, a.v_row, a.dim);
-  }
-  auto load = [&](int j, int slot) {
-    L::load_rows(k_base, j, a.k_row, s.lk, k_off, lds0 + (unsigned)(slot * 2 * SLOT), wave, lane);
-    L::load_rows(v_base, j, a.v_row, s.lk, v_off, lds0 + (unsigned)(slot * 2 * SLOT + SLOT), wave, lane);
-  };
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int n = 0; n < L::kLoads; ++n) off[i][n] = L::load_off(wave, n, lane, stride[i], a.dim);
+  auto fetch = [&](int j, int slot) { return PairLoad<T, DH>(off, base, stride, s.lk, j, lds0 + (unsigned)(slot * 2 * SLOT), wave); };
+  constexpr int PER = PairLoad<T, DH>::kPieces / KC;
 
   f32x16 acc[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
-  float m = -INFINITY, l = 0.f;             // of this lane's row, in units of log2; l: this half's share
+  float m = -INFINITY, l[4] = {0.f, 0.f, 0.f, 0.f};             // of this lane's row, in units of log2; l: this half's share
   const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
-  if (j0 < j1) load(j0, 0);
+  settle(qf);
+  if (j0 < j1) fetch(j0, 0).all();
   int slot = 0;
   for (int j = j0; j < j1; ++j, slot ^= 1) {
     wait_and_meet<0>();
-    if (j + 1 < j1) load(j + 1, slot ^ 1);
     const int key0 = j * kStep;
-    if (!w_real || key0 >= w1.hi || key0 + kStep <= w0.lo) continue;
+    const PairLoad<T, DH> next = fetch(j + 1 < j1 ? j + 1 : kNone, slot ^ 1);
+    if (!w_real || key0 >= w1.hi || key0 + kStep <= w0.lo) {
+      next.all();
+      continue;
+    }
     const char* const ks = smem + slot * 2 * SLOT;
     const char* const vs = ks + SLOT;
     f32x16 sc[2] = {f32x16{}, f32x16{}};
+    Frag kf[3][2];             // read two steps ahead
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc)
+    for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
-      for (int n = 0; n < 2; ++n) sc[n] = Mma<T>::mma(L::row_frag(ks, rb, n, kc), qf[kc], sc[n]);
+      for (int n = 0; n < 2; ++n) kf[kc][n] = L::row_frag(ks, rb, n, kc);
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      if (kc + 2 < KC)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) kf[(kc + 2) % 3][n] = L::row_frag(ks, rb, n, kc + 2);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) sc[n] = Mma<T>::mma(kf[kc % 3][n], qf[kc], sc[n]);
+#pragma unroll
+      for (int p = 0; p < PER; ++p) next.piece(PER * kc + p);
+    }
     if (key0 < w1.lo || key0 + kStep > w0.hi) {
       const int from = mine.lo - key0 - 4 * half, to = mine.hi - key0 - 4 * half;
 #pragma unroll
@@ -104,15 +118,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(c
           if (at < from || at >= to) sc[n][i] = -INFINITY;
         }
     }
-    float top = sc[0][0];
+    float tops[4] = {sc[0][0], sc[0][8], sc[1][0], sc[1][8]};          // (four chains of eight, as the sums below: one chain would be waited for)
 #pragma unroll
-    for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i / 16][i % 16]);
-    top = both_max(top) * g.c;
+    for (int i = 1; i < 8; ++i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) tops[u] = fmaxf(tops[u], sc[u / 2][8 * (u % 2) + i]);
+    const float top = both_max(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * g.c;
     if (__any(top > m + kLazy)) {
       const bool raise = top > m + kLazy;
       const float f = raise ? exp2_(m - top) : 1.f;
       if (raise) m = top;
-      l *= f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) l[u] *= f;
 #pragma unroll
       for (int d = 0; d < DB; ++d) acc[d] *= f;
     }
@@ -122,7 +139,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(c
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         sc[n][i] = exp2_(fmaf(sc[n][i], g.c, -base));
-        l += sc[n][i];
+        l[2 * n + i / 8] += sc[n][i];
       }
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
@@ -132,9 +149,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(c
     }
   }
 
-  l = both_sum(l);
+  drain();
+  const float sum = both_sum((l[0] + l[1]) + (l[2] + l[3]));
   if (!real) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l, lse = (m + log2f(l)) * kLn2;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum, lse = (m + log2f(sum)) * kLn2;
   const long token = s.q0 + query;
   if (g.parts > 1) {
     float* const op = g.part_o + (((long)part * a.q_rows + token) * a.heads + head) * a.dim;

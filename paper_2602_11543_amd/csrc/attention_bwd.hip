@@ -3,7 +3,7 @@
 //      dv = p^T do      dk = scale ds^T q      dq = scale ds k
 // Two kernels, so that every sum has one owner and one order: by queries (delta and dq) and by keys (dk and dv, over the rows of all heads that share
 // them).  That is 14 D operations a pair for the 10 D of the formulas: s and do v^T are formed twice.
-#include <algorithm>
+#include <type_traits>
 
 #include "attention.h"
 
@@ -69,33 +69,38 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
   }
   delta = both_sum(delta);
   if (real && half == 0) g.delta[(long)head * a.q_rows + token] = delta;
-  const float base = g.lse[(long)head * a.q_rows + token] * kLog2e;
 
-  const unsigned long k_base = (unsigned long)g.k + (unsigned long)((long)s.k0 * a.k_row + (long)kvh * a.k_head) * ES;
-  const unsigned long v_base = (unsigned long)g.v + (unsigned long)((long)s.k0 * a.v_row + (long)kvh * a.v_head) * ES;
+  const long stride[2] = {a.k_row * ES, a.v_row * ES};
+  const unsigned long source[2] = {(unsigned long)g.k + (unsigned long)(s.k0 * stride[0] + (long)kvh * a.k_head * ES),
+                                   (unsigned long)g.v + (unsigned long)(s.k0 * stride[1] + (long)kvh * a.v_head * ES)};
   const unsigned lds0 = lds_address(smem);
-  unsigned k_off[L::kLoads], v_off[L::kLoads];
+  unsigned off[2][L::kLoads];
 #pragma unroll
-  for (int i = 0; i < L::kLoads; ++i) {
-    k_off[i] = L::load_off(wave, i, lane, a.k_row, a.dim);
-    v_off[i] = L::load_off(wave, i, lane, a.v_row, a.dim);
-  }
-  auto load = [&](int j, int slot) {
-    L::load_rows(k_base, j, a.k_row, s.lk, k_off, lds0 + (unsigned)(slot * 2 * SLOT), wave, lane);
-    L::load_rows(v_base, j, a.v_row, s.lk, v_off, lds0 + (unsigned)(slot * 2 * SLOT + SLOT), wave, lane);
-  };
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int n = 0; n < L::kLoads; ++n) off[i][n] = L::load_off(wave, n, lane, stride[i], a.dim);
+  auto fetch = [&](int j, int slot) { return PairLoad<T, DH>(off, source, stride, s.lk, j, lds0 + (unsigned)(slot * 2 * SLOT), wave); };
+  constexpr int PER = PairLoad<T, DH>::kPieces / KC;
 
   f32x16 acc[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
   const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
-  if (j0 < j1) load(j0, 0);
+  float base = g.lse[(long)head * a.q_rows + token] * kLog2e;
+  settle(qf);
+  settle(df);
+  settle(base);
+  settle(delta);
+  if (j0 < j1) fetch(j0, 0).all();
   int slot = 0;
   for (int j = j0; j < j1; ++j, slot ^= 1) {
     wait_and_meet<0>();
-    if (j + 1 < j1) load(j + 1, slot ^ 1);
     const int key0 = j * kStep;
-    if (!w_real || key0 >= w1.hi || key0 + kStep <= w0.lo) continue;
+    const PairLoad<T, DH> next = fetch(j + 1 < j1 ? j + 1 : kNone, slot ^ 1);
+    if (!w_real || key0 >= w1.hi || key0 + kStep <= w0.lo) {
+      next.all();
+      continue;
+    }
     const bool cut = key0 < w1.lo || key0 + kStep > w0.hi;
     const int from = mine.lo - key0 - 4 * half, to = mine.hi - key0 - 4 * half;
     const char* const ks = smem + slot * 2 * SLOT;
@@ -109,6 +114,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
       for (int kc = 0; kc < KC; ++kc) {
         sc = Mma<T>::mma(L::row_frag(ks, rb, n, kc), qf[kc], sc);
         ds = Mma<T>::mma(L::row_frag(vs, rb, n, kc), df[kc], ds);
+        if (n == 0)
+#pragma unroll
+          for (int p = 0; p < PER; ++p) next.piece(PER * kc + p);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) ds[i] *= exp2_(fmaf(sc[i], g.c, -base));
@@ -127,6 +135,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
       }
     }
   }
+  drain();
   if (!real) return;
   T* const dq = static_cast<T*>(g.dq) + token * a.q_row + (long)head * a.q_head;
 #pragma unroll
@@ -138,166 +147,263 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
     }
 }
 
+// Four wavefronts, two by two: two groups of NB x 32 keys, and in each one wavefront for the first 32 of the 64 rows that are in LDS and one for the
+// others, whose sums are joined at the end.
+template <typename T, int DH>
+struct KvTile {
+  static constexpr int NB = 1, kKeys = 2 * NB * 32;
+  static constexpr bool kValuesInLds = false;      // dk, dv and the keys take 320 of a lane's 512 registers, the values would take 64
+};
+
 template <typename T, int DH>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kernel(const BwdArgs g) {
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DH / 16, DB = DH / 32, SLOT = kStep * L::kRowBytes;
+  constexpr int ES = sizeof(T), KC = DH / 16, DB = DH / 32, SLOT = kStep * L::kRowBytes, NB = KvTile<T, DH>::NB, KEYS = KvTile<T, DH>::kKeys;
   __shared__ __align__(1024) char smem[4 * SLOT];
-  __shared__ __align__(16) float stats[2][2][kStep];         // of each slot's rows: -lse / scale, -delta
+  constexpr bool V_LDS = KvTile<T, DH>::kValuesInLds;
+  __shared__ __align__(1024) char values[V_LDS ? KEYS * L::kRowBytes : 16];
+  __shared__ __align__(16) float stats[2][2][kStep];         // of each slot's rows: -lse / scale (fp32: -lse log2 e), -delta
   const AttnShape& a = g.a;
-  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), x = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), x = lane & 31, half = lane >> 5, kw = wave & 1, rw = wave >> 1;
   const int kvh = blockIdx.x % a.kv_heads;
   Seq s;
   int tile, tiles;
-  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, kRows, lane, s, tile, tiles)) return;
+  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, KEYS, lane, s, tile, tiles)) return;
 
-  const int G = a.group, n_rows = s.lq * G, key0 = tile * kRows, first = key0 + wave * 32, key = first + x;
-  const bool real = key < s.lk;
+  const int G = a.group, n_rows = s.lq * G, key0 = tile * KEYS, first = key0 + kw * NB * 32, tail = s.lk - 1;
   // Rows [from, to) see a key: with causal masks r / G + lk - lq >= key, hence r >= (key - (lk - lq)) G, and likewise for the window
   auto rows_of = [&](int at) {
     Reach r = {0, n_rows};
     if (a.causal) {
-      const long first_query = (long)at - (s.lk - s.lq), end = a.window > 0 ? min(first_query + a.window, (long)s.lq) : (long)s.lq;
+      const long first_query = (long)min(at, tail) - (s.lk - s.lq), end = a.window > 0 ? min(first_query + a.window, (long)s.lq) : (long)s.lq;
       r.lo = (int)max(first_query, 0l) * G;
       r.hi = (int)max(end, 0l) * G;
     }
     return r;
   };
-  const int tail = s.lk - 1;
-  const Reach mine = rows_of(min(key, tail)), w0 = rows_of(min(first, tail)), w1 = rows_of(min(first + 31, tail));      // some: [w0.lo, w1.hi), all: [w1.lo, w0.hi)
-  const int lo = rows_of(key0).lo, hi = rows_of(min(key0 + kRows - 1, tail)).hi;
-  const bool w_real = first < s.lk;
+  const int lo = rows_of(key0).lo, hi = rows_of(key0 + KEYS - 1).hi;
   const int j0 = lo / kStep, j1 = hi > lo ? cdiv(hi, kStep) : j0;
 
-  Frag kf[KC], vf[KC];
-  {
-    const T* const kp = static_cast<const T*>(g.k) + (long)(s.k0 + min(key, tail)) * a.k_row + (long)kvh * a.k_head + 8 * half;
-    const T* const vp = static_cast<const T*>(g.v) + (long)(s.k0 + min(key, tail)) * a.v_row + (long)kvh * a.v_head + 8 * half;
+  Frag kf[NB][KC], vf[NB][V_LDS ? 1 : KC];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int key = min(first + 32 * b + x, tail);
+    const T* const kp = static_cast<const T*>(g.k) + (long)(s.k0 + key) * a.k_row + (long)kvh * a.k_head + 8 * half;
+    const T* const vp = static_cast<const T*>(g.v) + (long)(s.k0 + key) * a.v_row + (long)kvh * a.v_head + 8 * half;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const bool in = real && 16 * kc + 8 * half < a.dim;
-      kf[kc] = in ? Mma<T>::load(kp + 16 * kc) : Mma<T>::zero();
-      vf[kc] = in ? Mma<T>::load(vp + 16 * kc) : Mma<T>::zero();
+      const bool in = 16 * kc + 8 * half < a.dim;
+      kf[b][kc] = in ? Mma<T>::load(kp + 16 * kc) : Mma<T>::zero();
+      if constexpr (!V_LDS) vf[b][kc] = in ? Mma<T>::load(vp + 16 * kc) : Mma<T>::zero();
     }
   }
 
+  // rows on their way into LDS: row r of a tile is query r / G, head r % G.  Rows behind the last one repeat it (their probabilities are nothing)
   const unsigned long q_base = (unsigned long)g.q + (unsigned long)((long)s.q0 * a.q_row + (long)kvh * G * a.q_head) * ES;
   const unsigned long d_base = (unsigned long)g.d_o + (unsigned long)(((long)s.q0 * a.heads + (long)kvh * G) * a.dim) * ES;
   const unsigned lds0 = lds_address(smem);
   const unsigned magic = (1u << 22) / (unsigned)G + 1;       // n / G = n magic >> 22 for n < 64 + G, G <= 1024
-  const unsigned q_row = (unsigned)(a.q_row * ES), q_head = (unsigned)(a.q_head * ES), d_row = (unsigned)(a.heads * a.dim * ES), d_head = (unsigned)(a.dim * ES);
-  auto load = [&](int j, int slot) {
-    const int r0 = j * kStep, query = r0 / G, rem = r0 - query * G;
-    const rsrc_t rq = open_rsrc(q_base + (unsigned long)((long)query * a.q_row * ES)), rd = open_rsrc(d_base + (unsigned long)((long)query * a.heads * a.dim * ES));
-    const unsigned dst = lds0 + (unsigned)(slot * 2 * SLOT + wave * L::kLoads * 1024);
+  unsigned off[2][L::kLoads];
+  auto aim = [&](int rem, int left) {
 #pragma unroll
     for (int i = 0; i < L::kLoads; ++i) {
       const int r = L::load_row(wave, i, lane), ch = L::load_chunk(r, lane);
-      const unsigned n = (unsigned)(r + rem), q = n * magic >> 22, h = n - q * G;
-      const bool in = r0 + r < n_rows && ch * (16 / ES) < a.dim;
-      const unsigned q_off = in ? q * q_row + h * q_head + ch * 16 : kOutOfRange, d_off = in ? q * d_row + h * d_head + ch * 16 : kOutOfRange;
-      const unsigned m = set_lds_dest(uniform(dst + i * 1024));
-      one_instruction();
-      load_to_lds(rq, q_off, m);
-      const unsigned m2 = set_lds_dest(uniform(dst + SLOT + i * 1024));
-      one_instruction();
-      load_to_lds(rd, d_off, m2);
+      const unsigned n = (unsigned)(min(r, left - 1) + rem), q = n * magic >> 22, h = n - q * G;
+      const bool in = ch * (16 / ES) < a.dim;
+      off[0][i] = in ? q * (unsigned)(a.q_row * ES) + h * (unsigned)(a.q_head * ES) + ch * 16 : kOutOfRange;
+      off[1][i] = in ? q * (unsigned)(a.heads * a.dim * ES) + h * (unsigned)(a.dim * ES) + ch * 16 : kOutOfRange;
     }
   };
+  auto fetch = [&](int j, int slot, bool there) {
+    const int r0 = j * kStep, query = r0 / G, rem = r0 - query * G;
+    if (there && (j == j0 || rem != 0 || kStep % G != 0 || r0 + kStep > n_rows)) aim(rem, n_rows - r0);
+    return PairLoad<T, DH>(off, open_rsrc(q_base + (unsigned long)((long)query * a.q_row * ES), there),
+                           open_rsrc(d_base + (unsigned long)((long)query * a.heads * a.dim * ES), there), lds0 + (unsigned)(slot * 2 * SLOT), wave);
+  };
+  constexpr int PER = PairLoad<T, DH>::kPieces / KC;
   // one row's number to a lane of the first two wavefronts, on its way while the step before is worked on
   auto number = [&](int j) {
     const int r = j * kStep + lane;
     if (r >= n_rows) return wave == 0 ? -INFINITY : 0.f;
     const long at = (long)(kvh * G + r % G) * a.q_rows + s.q0 + r / G;
-    return wave == 0 ? -g.lse[at] / a.scale : -g.delta[at];
+    return wave == 0 ? g.lse[at] : -g.delta[at];
+  };
+  auto keep = [&](int slot, float v) {
+    if (wave == 0) v = v == -INFINITY ? -INFINITY : ES == 2 ? -v / a.scale : -v * kLog2e;      // a row without keys has no probabilities
+    if (wave < 2) stats[slot][wave][lane] = v;
   };
 
-  f32x16 dk[DB], dv[DB];
+  f32x16 dk[NB][DB], dv[NB][DB];
 #pragma unroll
-  for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x16{};
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dk[b][d] = dv[b][d] = f32x16{};
   const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    settle(kf[b]);
+    if constexpr (!V_LDS) settle(vf[b]);
+  }
+  if constexpr (V_LDS)
+#pragma unroll
+    for (int t = 0; t < KEYS / kStep; ++t)
+      L::load_rows((unsigned long)g.v + (unsigned long)(((long)(s.k0 + key0 + t * kStep) * a.v_row + (long)kvh * a.v_head) * ES), a.v_row * ES,
+                   s.lk - key0 - t * kStep, a.dim, lds_address(values) + (unsigned)(t * SLOT), wave, lane);
   if (j0 < j1) {
-    load(j0, 0);
-    if (wave < 2) {
-      const float v = number(j0);
-      stats[0][wave][lane] = wave == 0 && v == INFINITY ? -INFINITY : v;      // a row without keys has no probabilities
-    }
+    fetch(j0, 0, true).all();
+    if (wave < 2) keep(0, number(j0));
   }
-  int slot = 0;
-  for (int j = j0; j < j1; ++j, slot ^= 1) {
-    wait_and_meet<0>();
-    float next = 0.f;
-    if (j + 1 < j1) {
-      if (wave < 2) next = number(j + 1);
-      load(j + 1, slot ^ 1);
-    }
-    const int r0 = j * kStep;
-    if (w_real && r0 < w1.hi && r0 + kStep > w0.lo) {
-      const bool cut = r0 < w1.lo || r0 + kStep > w0.hi;
-      const int from = mine.lo - r0 - 4 * half, to = mine.hi - r0 - 4 * half;
-      const char* const qs = smem + slot * 2 * SLOT;
-      const char* const dos = qs + SLOT;
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        f32x16 p, ds;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 u = *reinterpret_cast<const float4*>(&stats[slot][0][32 * n + 8 * i + 4 * half]);
-          const float4 w = *reinterpret_cast<const float4*>(&stats[slot][1][32 * n + 8 * i + 4 * half]);
-          p[4 * i] = u.x; p[4 * i + 1] = u.y; p[4 * i + 2] = u.z; p[4 * i + 3] = u.w;
-          ds[4 * i] = w.x; ds[4 * i + 1] = w.y; ds[4 * i + 2] = w.z; ds[4 * i + 3] = w.w;
-        }
-#pragma unroll
-        for (int kc = 0; kc < KC; ++kc) {
-          p = Mma<T>::mma(L::row_frag(qs, rb, n, kc), kf[kc], p);
-          ds = Mma<T>::mma(L::row_frag(dos, rb, n, kc), vf[kc], ds);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          p[i] = exp2_(p[i] * g.c);
-          ds[i] *= p[i];
-        }
-        if (cut) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int at = 32 * n + 8 * (i / 4) + i % 4;
-            if (at < from || at >= to) p[i] = ds[i] = 0.f;
-          }
-        }
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          const Frag pf = Mma<T>::of(p, kk), sf = Mma<T>::of(ds, kk);
-#pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            dv[d] = Mma<T>::mma(L::col_frag(dos, cb, d, 2 * n + kk), pf, dv[d]);
-            dk[d] = Mma<T>::mma(L::col_frag(qs, cb, d, 2 * n + kk), sf, dk[d]);
-          }
-        }
-      }
-    }
-    if (j + 1 < j1 && wave < 2) stats[slot ^ 1][wave][lane] = wave == 0 && next == INFINITY ? -INFINITY : next;
-  }
-  if (!real) return;
-  T* const dkp = static_cast<T*>(g.dk) + (long)(s.k0 + key) * a.k_row + (long)kvh * a.k_head;
-  T* const dvp = static_cast<T*>(g.dv) + (long)(s.k0 + key) * a.v_row + (long)kvh * a.v_head;
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
+
+  // 32 rows against the wavefront's keys
+  auto step = [&](auto cut_, int slot, int r0, const PairLoad<T, DH>& next) {
+    constexpr bool CUT = decltype(cut_)::value;
+    const char* const qs = smem + slot * 2 * SLOT;
+    const char* const dos = qs + SLOT;
+    const float* const st = &stats[slot][0][32 * rw + 4 * half];
+    f32x16 p[NB], ds[NB];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int at = 32 * d + 8 * i + 4 * half;
-      if (at < a.dim) {
-        put4(dkp + at, dk[d][4 * i] * a.scale, dk[d][4 * i + 1] * a.scale, dk[d][4 * i + 2] * a.scale, dk[d][4 * i + 3] * a.scale);
-        put4(dvp + at, dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]);
+      const float4 u = *reinterpret_cast<const float4*>(st + 8 * i), w = *reinterpret_cast<const float4*>(st + kStep + 8 * i);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if (ES == 2) { p[b][4 * i] = u.x; p[b][4 * i + 1] = u.y; p[b][4 * i + 2] = u.z; p[b][4 * i + 3] = u.w; }
+        ds[b][4 * i] = w.x; ds[b][4 * i + 1] = w.y; ds[b][4 * i + 2] = w.z; ds[b][4 * i + 3] = w.w;
       }
     }
+    if (ES != 2)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) p[b] = f32x16{};
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      const Frag f = L::row_frag(qs, rb, rw, kc);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) p[b] = Mma<T>::mma(f, kf[b][kc], p[b]);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) next.piece(PER * kc + i);
+    }
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      const Frag f = L::row_frag(dos, rb, rw, kc);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if constexpr (V_LDS) ds[b] = Mma<T>::mma(f, L::row_frag(values, rb, kw * NB + b, kc), ds[b]);
+        else ds[b] = Mma<T>::mma(f, vf[b][kc], ds[b]);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      // (bf16: the products are summed on top of -lse / scale; in fp32 storage that would round them to its magnitude)
+      if constexpr (ES == 2) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[b][i] = exp2_(p[b][i] * g.c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 u = *reinterpret_cast<const float4*>(st + 8 * i);
+          p[b][4 * i] = exp2_(fmaf(p[b][4 * i], g.c, u.x));
+          p[b][4 * i + 1] = exp2_(fmaf(p[b][4 * i + 1], g.c, u.y));
+          p[b][4 * i + 2] = exp2_(fmaf(p[b][4 * i + 2], g.c, u.z));
+          p[b][4 * i + 3] = exp2_(fmaf(p[b][4 * i + 3], g.c, u.w));
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ds[b][i] *= p[b][i];
+      if constexpr (CUT) {
+        const Reach mine = rows_of(first + 32 * b + x);
+        const int from = mine.lo - r0 - 4 * half, to = mine.hi - r0 - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int at = 8 * (i / 4) + i % 4;
+          if (at < from || at >= to) p[b][i] = ds[b][i] = 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      Frag f[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) f[b] = Mma<T>::of(p[b], kk);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const Frag c = L::col_frag(dos, cb, d, 2 * rw + kk);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) dv[b][d] = Mma<T>::mma(c, f[b], dv[b][d]);
+      }
+    }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      Frag f[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) f[b] = Mma<T>::of(ds[b], kk);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const Frag c = L::col_frag(qs, cb, d, 2 * rw + kk);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) dk[b][d] = Mma<T>::mma(c, f[b], dk[b][d]);
+      }
+    }
+  };
+  int slot = 0, j = j0;
+  auto run = [&](auto cut_, int to) {
+    for (; j < to; ++j, slot ^= 1) {
+      wait_and_meet<0>();
+      const bool more = j + 1 < j1;
+      float number_next = 0.f;
+      if (more && wave < 2) number_next = number(j + 1);
+      step(cut_, slot, j * kStep + 32 * rw, fetch(j + 1, slot ^ 1, more));
+      if (more && wave < 2) keep(slot ^ 1, number_next);
+    }
+  };
+  // rows that some key does not see only at either end
+  const int all_from = cdiv(rows_of(key0 + KEYS - 1).lo, kStep), all_to = rows_of(key0).hi / kStep;
+  run(std::true_type{}, min(max(all_from, j0), j1));
+  run(std::false_type{}, min(max(all_to, j), j1));
+  run(std::true_type{}, j1);
+
+  // the other rows' sums: dk, then dv, through LDS
+  const float scale = a.scale;
+  T* const out[2] = {static_cast<T*>(g.dk) + (long)s.k0 * a.k_row + (long)kvh * a.k_head, static_cast<T*>(g.dv) + (long)s.k0 * a.v_row + (long)kvh * a.v_head};
+  const long row[2] = {a.k_row, a.v_row};
+  float4* const other = reinterpret_cast<float4*>(smem) + kw * NB * DB * 4 * kWave + lane;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    wait_and_meet<0>();
+    if (rw == 1)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x16& v = t ? dv[b][d] : dk[b][d];
+            other[((b * DB + d) * 4 + i) * kWave] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          }
+    wait_and_meet<0>();
+    if (rw == 0)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int key = first + 32 * b + x;
+        T* const to = out[t] + key * row[t];
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x16& v = t ? dv[b][d] : dk[b][d];
+            const float4 u = other[((b * DB + d) * 4 + i) * kWave];
+            const float f = t ? 1.f : scale;
+            const int at = 32 * d + 8 * i + 4 * half;
+            if (key < s.lk && at < a.dim) put4(to + at, (v[4 * i] + u.x) * f, (v[4 * i + 1] + u.y) * f, (v[4 * i + 2] + u.z) * f, (v[4 * i + 3] + u.w) * f);
+          }
+      }
+  }
 }
 
 template <typename T, int DH>
 int bwd(const BwdArgs& g, hipStream_t s) {
   const AttnShape& a = g.a;
   if (a.q_rows > 0) attn_bwd_q_kernel<T, DH><<<dim3((unsigned)(((long)a.q_rows * a.group / kRows + a.n_seq) * a.kv_heads)), dim3(256), 0, s>>>(g);
-  if (a.k_rows > 0) attn_bwd_kv_kernel<T, DH><<<dim3((unsigned)(((long)a.k_rows / kRows + a.n_seq) * a.kv_heads)), dim3(256), 0, s>>>(g);
+  if (a.k_rows > 0) attn_bwd_kv_kernel<T, DH><<<dim3((unsigned)(((long)a.k_rows / KvTile<T, DH>::kKeys + a.n_seq) * a.kv_heads)), dim3(256), 0, s>>>(g);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
 
