@@ -58,10 +58,14 @@ template <> struct Mma<float> {
 };
 
 __device__ __forceinline__ unsigned lds_address(void* p) { return uniform((unsigned)(unsigned long)(__attribute__((address_space(3))) char*)p); }
-// from `base` on, for offsets below 2^31
-__device__ __forceinline__ rsrc_t open_rsrc(unsigned long base, bool any = true) {
-  return rsrc_t{uniform((unsigned)base), uniform((unsigned)(base >> 32)), any ? 0x80000000u : 0u, 0x00020000u};
+// The resource of `bytes` bytes from `base` on for loads that stand in assembly.  Where one of its scalars comes out of a vector register, five wait states
+// have to pass before a load reads it; the compiler does not know that the load does, so they stand here (tests/test_lds_load_hazards.py looks at what is built).
+__device__ __forceinline__ rsrc_t rsrc_for_lds(unsigned long base, unsigned bytes) {
+  rsrc_t r = {uniform((unsigned)base), uniform((unsigned)(base >> 32)), uniform(bytes), 0x00020000u};
+  asm volatile("s_nop 4" : "+s"(r));
+  return r;
 }
+constexpr unsigned kOpen = 0x80000000u;      // bytes of a resource that is not to end: offsets are below 2^31
 
 // The order of a stretch of code with N matrix instructions, READS LDS reads and VALU other instructions to each: the first AHEAD
 // instructions' reads come first, the others' one instruction after another
@@ -131,7 +135,7 @@ struct Tile {
   }
   // kStep rows, at most `rows` of them real, from `base` on into LDS at `dst`; zeros beyond
   static __device__ __forceinline__ void load_rows(unsigned long base, long stride, int rows, int dim, unsigned dst, int wave, int lane) {
-    const rsrc_t rs = {uniform((unsigned)base), uniform((unsigned)(base >> 32)), uniform((unsigned)(max(min(rows, kStep), 0) * stride)), 0x00020000u};
+    const rsrc_t rs = rsrc_for_lds(base, (unsigned)(max(min(rows, kStep), 0) * stride));
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const unsigned o = load_off(wave, i, lane, stride, dim);
@@ -160,7 +164,7 @@ struct PairLoad {
     for (int i = 0; i < 2; ++i) {
       const unsigned long at = base[i] + (unsigned long)((long)j * kStep * stride[i]);
       const unsigned bytes = (unsigned)(max(min(rows - j * kStep, kStep), 0) * stride[i]);
-      rs[i] = rsrc_t{uniform((unsigned)at), uniform((unsigned)(at >> 32)), uniform(bytes), 0x00020000u};
+      rs[i] = rsrc_for_lds(at, bytes);
     }
   }
   // from resources that are there
@@ -180,6 +184,10 @@ struct PairLoad {
 
 // The last loads into LDS, before a block may end
 __device__ __forceinline__ void drain() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// This wavefront's loads but the newest N; its LDS reads
+template <int N>
+__device__ __forceinline__ void wait_for() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+__device__ __forceinline__ void wait_for_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ float both_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));

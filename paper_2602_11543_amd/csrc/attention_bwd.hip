@@ -218,8 +218,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kerne
   auto fetch = [&](int j, int slot, bool there) {
     const int r0 = j * kStep, query = r0 / G, rem = r0 - query * G;
     if (there && (j == j0 || rem != 0 || kStep % G != 0 || r0 + kStep > n_rows)) aim(rem, n_rows - r0);
-    return PairLoad<T, DH>(off, open_rsrc(q_base + (unsigned long)((long)query * a.q_row * ES), there),
-                           open_rsrc(d_base + (unsigned long)((long)query * a.heads * a.dim * ES), there), lds0 + (unsigned)(slot * 2 * SLOT), wave);
+    return PairLoad<T, DH>(off, rsrc_for_lds(q_base + (unsigned long)((long)query * a.q_row * ES), there ? kOpen : 0u),
+                           rsrc_for_lds(d_base + (unsigned long)((long)query * a.heads * a.dim * ES), there ? kOpen : 0u), lds0 + (unsigned)(slot * 2 * SLOT), wave);
   };
   constexpr int PER = PairLoad<T, DH>::kPieces / KC;
   // one row's number to a lane of the first two wavefronts, on its way while the step before is worked on
