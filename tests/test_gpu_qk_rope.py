@@ -259,3 +259,32 @@ def test_another_stream_and_a_graph():
         eager = call()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, (q, k, *p.views(grad), *dw))), i
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("kw", [dict(heads=16, kv=4, dim=128), dict(heads=5, kv=3, dim=64, interleaved=True), dict(heads=9, kv=9, dim=256, rot=64), dict(heads=30, kv=1, dim=64, norm=False)])
+def test_tensors_that_the_caches_do_not_hold(dtype, kw):
+    """More than 256 MB pass; the kernels for that take whole tokens."""
+    size = 4 if dtype == torch.float32 else 2
+    T = 300 * 2 ** 20 // (2 * size * (kw["heads"] + kw["kv"]) * kw["dim"]) + 3
+    p = Problem(T, dtype=dtype, seed=10, **kw)
+    p.check()
+    start = [torch.randn(p.dim, device="cuda") for _ in range(2)]
+    if p.qw is not None:
+        for a, b, c in zip(start, p.backward()[2], p.backward(accumulate=start)[2]):
+            assert torch.equal(a + b, c)
+    p.pos[T - 2] = -1
+    assert torch.isnan(p.forward()[1][T - 2, :, : p.rot]).all()
+
+
+def test_a_missing_position_stays_with_its_token():
+    """The gradients of the other tokens are what they were; those of the token and the weights' are NaN."""
+    for T in (50, 300 * 2 ** 20 // (2 * 2 * 4 * 64)):
+        p = Problem(T, heads=3, kv=1, dim=64, seed=11)
+        want = p.backward()
+        p.pos[7] = 10 ** 6
+        got = p.backward()
+        keep = torch.arange(T, device="cuda") != 7
+        for a, b in zip(got[:2], want[:2]):
+            assert torch.equal(a[keep], b[keep]) and torch.isnan(a[7]).all()
+        assert all(torch.isnan(w).all() for w in got[2])
