@@ -1,0 +1,126 @@
+"""The attention half of a block on the device: root-mean-square norm, projections, norm of queries' and keys' heads with the rotation by position, and causal
+attention over sequences of unequal length, forward and backward, with the optimizer step; and single tokens against a cache.  It holds the buffers and
+makes the calls; the products with the projections' matrices are plain library products."""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+from . import binding as S
+
+
+def rotation_table(n_pos, rot_dim, base=10000.0, device="cuda"):
+    """Cosines and sines of every position's angles, formed in 64 bits: [n_pos, rot_dim] as spes_qk_rope_fwd takes them."""
+    pair = torch.arange(rot_dim // 2, dtype=torch.float64, device=device)
+    angle = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * base ** (-2.0 / rot_dim * pair)
+    return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+class DeviceAttention:
+    """Weights, state and buffers for batches of T tokens.  Every node trains these matrices."""
+
+    def __init__(self, T, d_model, heads, kv_heads, head_dim, n_pos, dtype="bf16", rot_dim=None, window=0, seed=0, device="cuda"):
+        self.dt = S.SPES_F32 if dtype == "f32" else S.SPES_BF16
+        self.T, self.d, self.H, self.K, self.D, self.window, self.n_pos = T, d_model, heads, kv_heads, head_dim, window, n_pos
+        self.rot = head_dim if rot_dim is None else rot_dim
+        st, f32 = S.torch_dtype(self.dt), torch.float32
+        g = torch.Generator(device=device).manual_seed(seed)
+        new = lambda *s, t=f32: torch.empty(*s, dtype=t, device=device)  # noqa: E731
+        normal = lambda std, *s: (std * torch.randn(*s, device=device, generator=g)).to(st)  # noqa: E731
+        width = (heads + 2 * kv_heads) * head_dim
+        self.w = {"norm": torch.ones(d_model, dtype=st, device=device), "qkv": normal(d_model ** -0.5, width, d_model),
+                  "q": torch.ones(head_dim, dtype=st, device=device), "k": torch.ones(head_dim, dtype=st, device=device),
+                  "o": normal((heads * head_dim) ** -0.5, d_model, heads * head_dim)}
+        self.state = {n: dict(master=w.float().clone(), m=torch.zeros(w.shape, device=device), v=torch.zeros(w.shape, device=device)) for n, w in self.w.items()}
+        self.grad = {n: torch.zeros(w.shape, device=device) for n, w in self.w.items()}
+        self.table = rotation_table(n_pos, self.rot, device=device)
+        self.h, self.rstd, self.dx = new(T, d_model, t=st), new(T), new(T, d_model, t=st)
+        self.q, self.k = new(T, heads, head_dim, t=st), new(T, kv_heads, head_dim, t=st)
+        self.dq, self.dk = torch.empty_like(self.q), torch.empty_like(self.k)
+        self.o, self.lse, self.d_qkv = torch.empty_like(self.q), new(heads, T), new(T, width, t=st)
+        self.qk = S.qk_shape(T, heads, kv_heads, head_dim, self.rot, self.dt, 0, n_pos)
+        self.norm_scratch = new(S.spes_norm_scratch_bytes(T, d_model), t=torch.uint8)
+        self.qk_scratch = new(S.spes_qk_rope_scratch_bytes(self.qk), t=torch.uint8)
+        self.steps, self.cache = 0, None
+
+    def _heads(self, t):
+        """Views of a projection's output, or of its gradient: queries, keys, values."""
+        H, K, D = self.H, self.K, self.D
+        return t[:, : H * D].view(-1, H, D), t[:, H * D: (H + K) * D].view(-1, K, D), t[:, (H + K) * D:].view(-1, K, D)
+
+    def _scratch(self, shape, backward):
+        need = S.spes_attn_scratch_bytes(shape, backward)
+        if getattr(self, "attn_scratch", None) is None or self.attn_scratch.numel() < need:
+            self.attn_scratch = torch.empty(need, dtype=torch.uint8, device=self.h.device)
+        return self.attn_scratch
+
+    def forward(self, x, starts, pos):
+        """x [T, d]: the stream; starts [n + 1] i32: where its sequences begin, and the last one's end; pos [T] i32: a token's place in its
+        sequence.  Returns what this half adds to the stream.  A caller that captures the calls into a graph makes one eager call first, which
+        takes the scratch."""
+        T, d = self.T, self.d
+        S.spes_norm_fwd(S.SPES_NORM_RMS, T, d, self.dt, x, None, self.w["norm"], None, 1e-6, None, self.h, None, self.rstd)
+        self.qkv = self.h @ self.w["qkv"].t()
+        q, k, v = self._heads(self.qkv)
+        S.spes_qk_rope_fwd(self.qk, q, k, self.w["q"], self.w["k"], self.table, pos, self.q, self.k)
+        self.shape = S.attn_shape(starts.numel() - 1, T, T, self.H, self.K, self.D, self.dt, 1, self.window)
+        S.spes_attn_fwd(self.shape, self.q, self.k, v, starts, starts, None, self.o, self.lse, self._scratch(self.shape, 0))
+        return self.o.view(T, -1) @ self.w["o"].t()
+
+    def backward(self, d_add, x, starts, pos, d_stream=None, accumulate=0):
+        """d_add [T, d]: gradient of what the forward returned; d_stream: the one that reaches x along the stream.  Returns x's."""
+        T, d = self.T, self.d
+        product = lambda a, b: a.float().t() @ b.float()  # noqa: E731
+        w_o, w_qkv = product(d_add, self.o.view(T, -1)), None
+        d_o = (d_add @ self.w["o"]).view(T, self.H, self.D)
+        q, k, v = self._heads(self.qkv)
+        dq, dk, dv = self._heads(self.d_qkv)
+        S.spes_attn_bwd(self.shape, d_o, self.q, self.k, v, starts, starts, None, self.o, self.lse, self.dq, self.dk, dv, self._scratch(self.shape, 1))
+        S.spes_qk_rope_bwd(self.qk, self.dq, self.dk, q, k, self.w["q"], self.w["k"], self.table, pos, dq, dk, self.grad["q"], self.grad["k"], accumulate,
+                           self.qk_scratch)
+        w_qkv = product(self.d_qkv, self.h)
+        for n, w in (("o", w_o), ("qkv", w_qkv)):
+            if accumulate:
+                self.grad[n] += w
+            else:
+                self.grad[n] = w
+        dh = self.d_qkv @ self.w["qkv"]
+        S.spes_norm_bwd(S.SPES_NORM_RMS, T, d, self.dt, dh, x, self.w["norm"], None, self.rstd, d_stream, self.dx, self.grad["norm"], None, accumulate,
+                        self.norm_scratch)
+        return self.dx
+
+    def step(self, lr=1e-3, weight_decay=0.1):
+        self.steps += 1
+        for n, w in self.w.items():
+            s = self.state[n]
+            S.spes_masked_adamw(1, w.numel(), self.dt, w, np.ones(1, dtype=np.uint8), s["master"], s["m"], s["v"], self.grad[n].contiguous(), lr, 0.9, 0.95, 1e-8,
+                                weight_decay if w.dim() > 1 else 0.0, self.steps)
+
+    def start_cache(self, n_seq, room):
+        """Empty caches with room for `room` tokens of each of n_seq sequences."""
+        dev, st = self.h.device, S.torch_dtype(self.dt)
+        self.room, self.taken = room, 0
+        self.cache = [torch.empty(n_seq, room, self.K, self.D, dtype=st, device=dev) for _ in range(2)]
+        self.length = torch.zeros(n_seq, dtype=torch.int32, device=dev)
+        self.row0 = torch.arange(n_seq, dtype=torch.int32, device=dev) * room
+        self.q_start = torch.arange(n_seq + 1, dtype=torch.int32, device=dev)
+
+    def decode(self, x):
+        """x [n_seq, d]: each sequence's next token.  Its keys and values join the cache; returns what this half adds to the stream."""
+        n, H, K, D = x.shape[0], self.H, self.K, self.D
+        if self.cache is None or n != self.cache[0].shape[0] or self.taken >= min(self.room, self.n_pos):
+            raise S.SpesError("decode: no cache for this many sequences, or its room or the positions are used up")
+        self.taken += 1
+        new = lambda *s, t=x.dtype: torch.empty(*s, dtype=t, device=x.device)  # noqa: E731
+        h, q, k, o = new(n, self.d), new(n, H, D), new(n, K, D), new(n, H, D)
+        S.spes_norm_fwd(S.SPES_NORM_RMS, n, self.d, self.dt, x, None, self.w["norm"], None, 1e-6, None, h, None, new(n, t=torch.float32))
+        qp, kp, vp = self._heads(h @ self.w["qkv"].t())
+        S.spes_qk_rope_fwd(S.qk_shape(n, H, K, D, self.rot, self.dt, 0, self.n_pos), qp, kp, self.w["q"], self.w["k"], self.table, self.length, q, k)
+        rows = (self.row0 + self.length).long()
+        caches = [c.view(-1, K, D) for c in self.cache]
+        for c, t in zip(caches, (k, vp)):
+            c.index_copy_(0, rows, t)
+        self.length += 1
+        shape = S.attn_shape(n, n, n * self.room, H, K, D, self.dt, 1, self.window)
+        S.spes_attn_fwd(shape, q, *caches, self.q_start, self.row0, self.length, o, new(H, n, t=torch.float32), self._scratch(shape, 0))
+        return o.view(n, -1) @ self.w["o"].t()
