@@ -502,7 +502,7 @@ SPES_API int spes_qk_rope_bwd(const spes_qk_shape* shape, const void* dq, const 
  * infinity or a NaN in one can reach other rows of its sequence, whether they see it or not.
  * Products in bf16 storage take bf16 operands, the probabilities and their gradient among them, and are summed in fp32; in fp32 storage they are fp32.
  *
- *  Supported: head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, at most 1024; q_rows heads below 2^31; strides multiples of 16 bytes,
+ *  Supported: head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, at most 1024; q_rows heads and k_rows at most 2^31 - 2^16; strides multiples of 16 bytes,
  *  rows at most 2^20 elements apart, heads / kv_heads heads of q within 2^28 elements
  */
 typedef struct {

@@ -12,6 +12,8 @@ bool dtype_ok(int dtype) { return dtype == SPES_F32 || dtype == SPES_BF16; }
 constexpr int kMaxRopeDim = 256, kMaxHeadDim = 128, kMaxHeads = 1024;
 constexpr long kMaxRow = 1l << 20, kMaxGroup = 1l << 28;          // in elements: 32-bit byte offsets from a tile's first row
 
+constexpr long kMaxRows = (1l << 31) - (1l << 16);               // the number of a row a few tiles behind the last one still fits 32 bits
+
 bool stride_ok(int64_t stride, int dtype) { return stride % (dtype == SPES_F32 ? 4 : 8) == 0; }
 
 int qk_supported(const spes_qk_shape* p) {
@@ -45,7 +47,7 @@ int attn_supported(const spes_attn_shape* p) {
   if (p->q_row > kMaxRow || p->k_row > kMaxRow || p->v_row > kMaxRow) return SPES_ESHAPE;
   if (p->q_head > kMaxGroup / (p->heads / p->kv_heads)) return SPES_ESHAPE;
   // rows of all heads, and blocks of a launch
-  if ((long)p->q_rows * p->heads >= 1l << 31 || ((long)p->q_rows * p->heads / 4 + (long)p->n_seq * p->kv_heads) * 32 >= 1l << 31 ||
+  if ((long)p->q_rows * p->heads > kMaxRows || p->k_rows > kMaxRows || ((long)p->q_rows * p->heads / 4 + (long)p->n_seq * p->kv_heads) * 32 >= 1l << 31 ||
       ((long)p->k_rows / 128 + p->n_seq) * p->kv_heads >= 1l << 31)
     return SPES_ESHAPE;
   for (const int64_t stride : {p->q_row, p->q_head, p->k_row, p->k_head, p->v_row, p->v_head})

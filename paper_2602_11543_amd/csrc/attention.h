@@ -7,6 +7,11 @@
 // scores of one column, 8 (i / 4) + 4 (lane / 32) + i % 4 for its register i.  The contraction that follows runs over just these: as its order is free, a
 // lane's registers 0..7 and 8..15 are its operand fragments as they stand, and the other operand is read from LDS in the same order.
 #pragma once
+#ifndef TWOSETS
+#define TWOSETS 512
+#endif
+#include <algorithm>
+
 #include "lds_load.h"
 #include "kernels.h"
 
@@ -15,7 +20,6 @@ namespace attn {
 
 constexpr int kRows = 128;       // rows of a block of four wavefronts, 32 each
 constexpr int kStep = 64;        // keys (rows, in the keys' kernel) that pass through LDS at a time
-constexpr int kNone = 1 << 24;   // the number of a tile that no sequence has (2^30 keys: behind the last of them, or its loads are not used)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -79,6 +83,13 @@ __device__ __forceinline__ void interleave() {
     if (VALU) __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
   }
 }
+
+// Heads of up to 32, 64, 96 or 128 elements are computed as that many, in rows of 64 or 128 in LDS
+constexpr int tile_dim(int dim) { return dim <= 64 ? 64 : 128; }
+
+// Whether two sets of four wavefronts have room in LDS, and whether a launch of so many blocks is to have them
+template <typename T, int DC> constexpr bool kTwoSets = 2 * 4 * kStep * tile_dim(DC) * (int)sizeof(T) <= 144 * 1024;
+inline bool two_sets(long blocks, long rows, int n_seq) { return std::max<long>(blocks, n_seq) <= TWOSETS && rows >= 4l * kStep * n_seq; }
 
 // A tile in LDS: rows of DH elements, chunk c (16 bytes) of row r at position c ^ turn(r).  LDS has 64 banks of four bytes, a read of 16 bytes a lane
 // takes sixteen lanes at a time: sixteen rows at one chunk, and in the transposing reads four rows of 64 bytes (fp32: two of 128), meet every bank once.
@@ -155,19 +166,6 @@ struct PairLoad {
   const unsigned (&off)[2][L::kLoads];
   rsrc_t rs[2];
   unsigned dst;
-  // rows j kStep .. of `rows` rows, stride[i] bytes apart from base[i]; zeros beyond the last one (the resource ends there) and beyond a row's elements.
-  // Where there is no such tile the loads bring zeros: a loop issues them to its end, without a branch in the middle of its matrix instructions
-  __device__ __forceinline__ PairLoad(const unsigned (&off_)[2][L::kLoads], const unsigned long (&base)[2], const long (&stride)[2], int rows, int j, unsigned slot,
-                                      int wave)
-      : off(off_), dst(slot + (unsigned)(wave * L::kLoads * 1024)) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const unsigned long at = base[i] + (unsigned long)((long)j * kStep * stride[i]);
-      const unsigned bytes = (unsigned)(max(min(rows - j * kStep, kStep), 0) * stride[i]);
-      rs[i] = rsrc_for_lds(at, bytes);
-    }
-  }
-  // from resources that are there
   __device__ __forceinline__ PairLoad(const unsigned (&off_)[2][L::kLoads], const rsrc_t& first, const rsrc_t& second, unsigned slot, int wave)
       : off(off_), rs{first, second}, dst(slot + (unsigned)(wave * L::kLoads * 1024)) {}
   __device__ __forceinline__ void piece(int p) const {
@@ -179,6 +177,31 @@ struct PairLoad {
   __device__ __forceinline__ void all() const {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) piece(p);
+  }
+};
+
+// Where the tiles of two tensors stand in memory, one after the other.  All of it in scalars that are carried on by additions: formed anew
+// for every tile, with the products and limits that this takes, they cost a step of 64 keys and 64 elements a tenth of its time.
+struct TileStream {
+  unsigned long at[2];
+  long left[2], step[2];       // bytes: from the tile to the last row's end, and to the next tile
+  // tile j of rows `stride` bytes apart from `base`, of `rows` rows in all; `by` tiles ahead with every one
+  __device__ __forceinline__ TileStream(const unsigned long (&base)[2], const long (&stride)[2], int j, int rows, int by) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      at[i] = base[i] + (unsigned long)((long)j * kStep * stride[i]);
+      left[i] = ((long)rows - (long)j * kStep) * stride[i];
+      step[i] = (long)by * kStep * stride[i];
+    }
+  }
+  // of the tile that is next; it ends with the last row, and behind it loads bring zeros: loops issue them to their end, without a branch among the
+  // matrix instructions
+  __device__ __forceinline__ rsrc_t next(int i) {
+    const long bytes = left[i];
+    const rsrc_t r = rsrc_for_lds(at[i], bytes <= 0 ? 0u : bytes < (long)kOpen ? (unsigned)bytes : kOpen);
+    at[i] += (unsigned long)step[i];
+    left[i] -= step[i];
+    return r;
   }
 };
 

@@ -52,14 +52,18 @@ __device__ __forceinline__ void put_row(const FwdArgs& g, int part, long token, 
   if (half == 0) (whole ? g.lse : g.part_lse + (long)part * a.heads * a.q_rows)[(long)head * a.q_rows + token] = lse;
 }
 
-template <typename T, int DH>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(const FwdArgs g) {
+// 128 rows, 32 to each of four wavefronts.  With KS = 2 there are four more, and the two sets take every second step of keys and join what they have at the end:
+// half the steps one behind the other for launches that leave CUs empty.
+template <typename T, int DC, int KS>
+__global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(const FwdArgs g) {
+  constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DH / 16, DB = DH / 32, SLOT = kStep * L::kRowBytes;
-  __shared__ __align__(1024) char smem[4 * SLOT];            // keys and values, two of each
+  constexpr int ES = sizeof(T), KC = DC / 16, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  __shared__ __align__(1024) char smem[4 * KS * SLOT];       // keys and values, two of each for each set
+  __shared__ float2 stats[KS == 1 ? 1 : kRows];
   const AttnShape& a = g.a;
-  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), x = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 31, half = lane >> 5;
   const int part = blockIdx.x % g.parts, item = blockIdx.x / g.parts, kvh = item % a.kv_heads;
   Seq s;
   int tile, tiles;
@@ -102,8 +106,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(c
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int n = 0; n < L::kLoads; ++n) off[i][n] = L::load_off(wave, n, lane, stride[i], a.dim);
-  auto fetch = [&](int j, int slot) { return PairLoad<T, DH>(off, base, stride, s.lk, j, lds0 + (unsigned)(slot * 2 * SLOT), wave); };
-  constexpr int PER = PairLoad<T, DH>::kPieces / KC;
+  TileStream stream(base, stride, j0 + ks, min(s.lk, j1 * kStep), KS);
+  auto fetch = [&](int slot) {
+    const rsrc_t k = stream.next(0), v = stream.next(1);
+    return PairLoad<T, DH>(off, k, v, lds0 + (unsigned)((slot * KS + ks) * 2 * SLOT), wave);
+  };
+  constexpr int PIECES = PairLoad<T, DH>::kPieces;
 
   f32x16 acc[DB];
 #pragma unroll
@@ -111,33 +119,33 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(c
   float m = -INFINITY, l[4] = {0.f, 0.f, 0.f, 0.f};             // of this lane's row, in units of log2; l: this half's share
   const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
   settle(qf);
-  if (j0 < j1) fetch(j0, 0).all();
+  if (j0 < j1) fetch(0).all();
   int slot = 0;
-  for (int j = j0; j < j1; ++j, slot ^= 1) {
+  for (int first = j0; first < j1; first += KS, slot ^= 1) {
     wait_and_meet<0>();
-    const int key0 = j * kStep;
-    const PairLoad<T, DH> next = fetch(j + 1 < j1 ? j + 1 : kNone, slot ^ 1);
-    if (!w_real || key0 >= w1.hi || key0 + kStep <= w0.lo) {
+    const int j = first + ks, key0 = j * kStep;
+    const PairLoad<T, DH> next = fetch(slot ^ 1);
+    if (!w_real || (KS > 1 && j >= j1) || key0 >= w1.hi || key0 + kStep <= w0.lo) {
       next.all();
       continue;
     }
-    const char* const ks = smem + slot * 2 * SLOT;
-    const char* const vs = ks + SLOT;
+    const char* const kt = smem + (slot * KS + ks) * 2 * SLOT;
+    const char* const vt = kt + SLOT;
     f32x16 sc[2] = {f32x16{}, f32x16{}};
     Frag kf[3][2];             // read two steps ahead
 #pragma unroll
     for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
-      for (int n = 0; n < 2; ++n) kf[kc][n] = L::row_frag(ks, rb, n, kc);
+      for (int n = 0; n < 2; ++n) kf[kc][n] = L::row_frag(kt, rb, n, kc);
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
       if (kc + 2 < KC)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) kf[(kc + 2) % 3][n] = L::row_frag(ks, rb, n, kc + 2);
+        for (int n = 0; n < 2; ++n) kf[(kc + 2) % 3][n] = L::row_frag(kt, rb, n, kc + 2);
 #pragma unroll
       for (int n = 0; n < 2; ++n) sc[n] = Mma<T>::mma(kf[kc % 3][n], qf[kc], sc[n]);
 #pragma unroll
-      for (int p = 0; p < PER; ++p) next.piece(PER * kc + p);
+      for (int p = PIECES * kc / KC; p < PIECES * (kc + 1) / KC; ++p) next.piece(p);
     }
     if (key0 < w1.lo || key0 + kStep > w0.hi) {
       const int from = mine.lo - key0 - 4 * half, to = mine.hi - key0 - 4 * half;
@@ -176,12 +184,40 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(c
     for (int kk = 0; kk < 4; ++kk) {
       const Frag p = Mma<T>::of(sc[kk / 2], kk % 2);
 #pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] = Mma<T>::mma(L::col_frag(vs, cb, d, kk), p, acc[d]);
+      for (int d = 0; d < DB; ++d) acc[d] = Mma<T>::mma(L::col_frag(vt, cb, d, kk), p, acc[d]);
     }
   }
 
   drain();
-  const float sum = both_sum((l[0] + l[1]) + (l[2] + l[3]));
+  float sum = both_sum((l[0] + l[1]) + (l[2] + l[3]));
+  if constexpr (KS == 2) {
+    // the second set's to the first, both scaled to their common maximum
+    float4* const other = reinterpret_cast<float4*>(smem) + wave * DB * 4 * kWave + lane;
+    wait_and_meet<0>();
+    if (ks == 1) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[(d * 4 + i) * kWave] = make_float4(acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]);
+      if (half == 0) stats[wave * 32 + x] = make_float2(m, sum);
+    }
+    wait_and_meet<0>();
+    if (ks == 1) return;
+    const float2 st = stats[wave * 32 + x];
+    const float top = fmaxf(m, st.x), low = top == -INFINITY ? 0.f : top, f = exp2_(m - low), f1 = exp2_(st.x - low);
+    sum = sum * f + st.y * f1;
+    m = top;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 u = other[(d * 4 + i) * kWave];
+        acc[d][4 * i] = acc[d][4 * i] * f + u.x * f1;
+        acc[d][4 * i + 1] = acc[d][4 * i + 1] * f + u.y * f1;
+        acc[d][4 * i + 2] = acc[d][4 * i + 2] * f + u.z * f1;
+        acc[d][4 * i + 3] = acc[d][4 * i + 3] * f + u.w * f1;
+      }
+  }
   if (real) put_row<T, DB>(g, part, s.q0 + query, head, half, acc, sum, m);
 }
 
@@ -256,12 +292,13 @@ struct FewPlan {
   }
 };
 
-template <typename T, int DH>
-__global__ __launch_bounds__((64 * Few<T, DH>::kWaves)) void attn_few_kernel(const FwdArgs g) {
+template <typename T, int DC>
+__global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_kernel(const FwdArgs g) {
+  constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef Few<T, DH> W;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DH / 16, DB = DH / 32;
+  constexpr int ES = sizeof(T), KC = DC / 16, DB = DC / 32;
   __shared__ __align__(1024) char smem[W::kWaves * 4 * W::kSlot];
   __shared__ float2 stats[W::kWaves][kFewRows];
   const AttnShape& a = g.a;
@@ -495,7 +532,7 @@ static_assert(kMaxParts == 64, "two parts to a lane");
 
 // How a call is cut.  few: 32 rows at most to a sequence on the average, by the kernel for these.  Parts: so that few rows against many keys fill the chip.
 struct Cut { bool few; int parts, per; };
-Cut cut_of(const AttnShape& a) {
+Cut cut_of(int dtype, const AttnShape& a) {
   if (a.n_seq == 0 || a.q_rows == 0) return {false, 1, 1};
   const long rows = (long)a.q_rows * a.group, keys = a.k_rows / a.n_seq;
   if (rows <= (long)kFewRows * a.n_seq) {
@@ -503,39 +540,48 @@ Cut cut_of(const AttnShape& a) {
     return {true, (int)std::max<long>(1, std::min<long>({kMaxParts, 4 * kFewItems / tiles, a.k_rows / (kFewLeast * kFewStep)})), 1};
   }
   const long tiles = std::max<long>(cdiv(rows, kRows), std::min(a.n_seq, a.q_rows)) * a.kv_heads;
-  const int parts = (int)std::max<long>(1, std::min<long>({kMaxParts, 512 / tiles, keys / 256}));
+  const long held = dtype == SPES_F32 && a.dim > 64 ? 256 : 512;      // blocks that the chip holds: two to a CU, or one
+  const int parts = (int)std::max<long>(1, std::min<long>({kMaxParts, held / tiles, keys / 256}));
   return {false, parts, (int)cdiv(cdiv(std::max<long>(keys, 1), kStep), parts)};
 }
 
-template <typename T, int DH>
+template <typename T, int DC>
 int fwd(const FwdArgs& g, bool few, hipStream_t s) {
   const AttnShape& a = g.a;
   const long n = (long)a.q_rows * a.group;
   auto grid = [&](long per, int parts) { return dim3((unsigned)((n / per + a.n_seq) * a.kv_heads * parts)); };
   if (few) {
-    attn_few_kernel<T, DH><<<std::min<unsigned>(grid(kFewRows, g.parts).x, kFewBlocks), dim3(64 * Few<T, DH>::kWaves), 0, s>>>(g);
+    attn_few_kernel<T, DC><<<std::min<unsigned>(grid(kFewRows, g.parts).x, kFewBlocks), dim3(64 * Few<T, tile_dim(DC)>::kWaves), 0, s>>>(g);
     if (g.parts > 1) attn_join_kernel<T, 256, true><<<grid(1, 1), dim3(256), 0, s>>>(g);
   } else {
-    attn_fwd_kernel<T, DH><<<grid(kRows, g.parts), dim3(256), 0, s>>>(g);
+    bool two = false;
+    if constexpr (kTwoSets<T, DC>) two = two_sets(n / kRows * a.kv_heads * g.parts, a.k_rows / g.parts, a.n_seq);
+    if constexpr (kTwoSets<T, DC>)
+      if (two) attn_fwd_kernel<T, DC, 2><<<grid(kRows, g.parts), dim3(512), 0, s>>>(g);
+    if (!two) attn_fwd_kernel<T, DC, 1><<<grid(kRows, g.parts), dim3(256), 0, s>>>(g);
     if (g.parts > 1) attn_join_kernel<T, 32, false><<<grid(8, 1), dim3(256), 0, s>>>(g);
   }
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
+template <typename T>
+int fwd(const FwdArgs& g, bool few, hipStream_t s) {
+  const int dim = g.a.dim;
+  return dim <= 32 ? fwd<T, 32>(g, few, s) : dim <= 64 ? fwd<T, 64>(g, few, s) : dim <= 96 ? fwd<T, 96>(g, few, s) : fwd<T, 128>(g, few, s);
+}
 
 }  // namespace
 
-size_t attn_fwd_scratch_bytes(int, const AttnShape& a) {
-  const int parts = cut_of(a).parts;
+size_t attn_fwd_scratch_bytes(int dtype, const AttnShape& a) {
+  const int parts = cut_of(dtype, a).parts;
   return parts == 1 ? 16 : (size_t)parts * a.q_rows * a.heads * (a.dim + 1) * sizeof(float) + 16;
 }
 
 int launch_attn_fwd(int dtype, const AttnShape& a, const void* q, const void* k, const void* v, void* o, float* lse, void* scratch, hipStream_t s) {
-  const Cut cut = cut_of(a);
+  const Cut cut = cut_of(dtype, a);
   FwdArgs g = {a, q, k, v, o, lse, nullptr, nullptr, cut.parts, cut.per, a.scale * kLog2e};
   g.part_o = static_cast<float*>(scratch);
   g.part_lse = g.part_o + (size_t)g.parts * a.q_rows * a.heads * a.dim;
-  if (dtype == SPES_BF16) return a.dim <= 64 ? fwd<bf16_t, 64>(g, cut.few, s) : fwd<bf16_t, 128>(g, cut.few, s);
-  return a.dim <= 64 ? fwd<float, 64>(g, cut.few, s) : fwd<float, 128>(g, cut.few, s);
+  return dtype == SPES_BF16 ? fwd<bf16_t>(g, cut.few, s) : fwd<float>(g, cut.few, s);
 }
 
 }  // namespace spes

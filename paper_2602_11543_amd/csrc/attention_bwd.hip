@@ -21,14 +21,16 @@ struct BwdArgs {
   float c;
 };
 
-template <typename T, int DH>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel(const BwdArgs g) {
+// 128 rows; KS sets of four wavefronts as in the forward
+template <typename T, int DC, int KS>
+__global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel(const BwdArgs g) {
+  constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DH / 16, DB = DH / 32, SLOT = kStep * L::kRowBytes;
-  __shared__ __align__(1024) char smem[4 * SLOT];
+  constexpr int ES = sizeof(T), KC = DC / 16, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  __shared__ __align__(1024) char smem[4 * KS * SLOT];
   const AttnShape& a = g.a;
-  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), x = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 31, half = lane >> 5;
   const int kvh = blockIdx.x % a.kv_heads;
   Seq s;
   int tile, tiles;
@@ -68,7 +70,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
     }
   }
   delta = both_sum(delta);
-  if (real && half == 0) g.delta[(long)head * a.q_rows + token] = delta;
+  if (real && half == 0 && ks == 0) g.delta[(long)head * a.q_rows + token] = delta;
 
   const long stride[2] = {a.k_row * ES, a.v_row * ES};
   const unsigned long source[2] = {(unsigned long)g.k + (unsigned long)(s.k0 * stride[0] + (long)kvh * a.k_head * ES),
@@ -79,8 +81,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int n = 0; n < L::kLoads; ++n) off[i][n] = L::load_off(wave, n, lane, stride[i], a.dim);
-  auto fetch = [&](int j, int slot) { return PairLoad<T, DH>(off, source, stride, s.lk, j, lds0 + (unsigned)(slot * 2 * SLOT), wave); };
-  constexpr int PER = PairLoad<T, DH>::kPieces / KC;
+  TileStream stream(source, stride, j0 + ks, min(s.lk, j1 * kStep), KS);
+  auto fetch = [&](int slot) {
+    const rsrc_t k = stream.next(0), v = stream.next(1);
+    return PairLoad<T, DH>(off, k, v, lds0 + (unsigned)((slot * KS + ks) * 2 * SLOT), wave);
+  };
+  constexpr int PIECES = PairLoad<T, DH>::kPieces;
 
   f32x16 acc[DB];
 #pragma unroll
@@ -91,20 +97,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
   settle(df);
   settle(base);
   settle(delta);
-  if (j0 < j1) fetch(j0, 0).all();
+  if (j0 < j1) fetch(0).all();
   int slot = 0;
-  for (int j = j0; j < j1; ++j, slot ^= 1) {
+  for (int first = j0; first < j1; first += KS, slot ^= 1) {
     wait_and_meet<0>();
-    const int key0 = j * kStep;
-    const PairLoad<T, DH> next = fetch(j + 1 < j1 ? j + 1 : kNone, slot ^ 1);
-    if (!w_real || key0 >= w1.hi || key0 + kStep <= w0.lo) {
+    const int j = first + ks, key0 = j * kStep;
+    const PairLoad<T, DH> next = fetch(slot ^ 1);
+    if (!w_real || (KS > 1 && j >= j1) || key0 >= w1.hi || key0 + kStep <= w0.lo) {
       next.all();
       continue;
     }
     const bool cut = key0 < w1.lo || key0 + kStep > w0.hi;
     const int from = mine.lo - key0 - 4 * half, to = mine.hi - key0 - 4 * half;
-    const char* const ks = smem + slot * 2 * SLOT;
-    const char* const vs = ks + SLOT;
+    const char* const kt = smem + (slot * KS + ks) * 2 * SLOT;
+    const char* const vt = kt + SLOT;
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       f32x16 sc = f32x16{}, ds;
@@ -112,11 +118,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
       for (int i = 0; i < 16; ++i) ds[i] = -delta;
 #pragma unroll
       for (int kc = 0; kc < KC; ++kc) {
-        sc = Mma<T>::mma(L::row_frag(ks, rb, n, kc), qf[kc], sc);
-        ds = Mma<T>::mma(L::row_frag(vs, rb, n, kc), df[kc], ds);
+        sc = Mma<T>::mma(L::row_frag(kt, rb, n, kc), qf[kc], sc);
+        ds = Mma<T>::mma(L::row_frag(vt, rb, n, kc), df[kc], ds);
         if (n == 0)
 #pragma unroll
-          for (int p = 0; p < PER; ++p) next.piece(PER * kc + p);
+          for (int p = PIECES * kc / KC; p < PIECES * (kc + 1) / KC; ++p) next.piece(p);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) ds[i] *= exp2_(fmaf(sc[i], g.c, -base));
@@ -131,11 +137,32 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
       for (int kk = 0; kk < 2; ++kk) {
         const Frag f = Mma<T>::of(ds, kk);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) acc[d] = Mma<T>::mma(L::col_frag(ks, cb, d, 2 * n + kk), f, acc[d]);
+        for (int d = 0; d < DB; ++d) acc[d] = Mma<T>::mma(L::col_frag(kt, cb, d, 2 * n + kk), f, acc[d]);
       }
     }
   }
   drain();
+  if constexpr (KS == 2) {
+    float4* const other = reinterpret_cast<float4*>(smem) + wave * DB * 4 * kWave + lane;
+    wait_and_meet<0>();
+    if (ks == 1)
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[(d * 4 + i) * kWave] = make_float4(acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]);
+    wait_and_meet<0>();
+    if (ks == 1) return;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 u = other[(d * 4 + i) * kWave];
+        acc[d][4 * i] += u.x;
+        acc[d][4 * i + 1] += u.y;
+        acc[d][4 * i + 2] += u.z;
+        acc[d][4 * i + 3] += u.w;
+      }
+  }
   if (!real) return;
   T* const dq = static_cast<T*>(g.dq) + token * a.q_row + (long)head * a.q_head;
 #pragma unroll
@@ -147,31 +174,26 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel
     }
 }
 
-// Four wavefronts, two by two: two groups of NB x 32 keys, and in each one wavefront for the first 32 of the 64 rows that are in LDS and one for the
-// others, whose sums are joined at the end.
-template <typename T, int DH>
-struct KvTile {
-  static constexpr int NB = 1, kKeys = 2 * NB * 32;
-  static constexpr bool kValuesInLds = false;      // dk, dv and the keys take 320 of a lane's 512 registers, the values would take 64
-};
-
-template <typename T, int DH>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kernel(const BwdArgs g) {
+// Four wavefronts: two groups of 32 keys, and in each one wavefront for the first 32 of the 64 rows that are in LDS and one for the others, whose sums are
+// joined at the end.  (Four groups, 64 rows each: half the loads into LDS, but the second 32 rows cost more registers than there are, 128
+// elements: 12.6 ms in place of 4.1 for all of the backward below; 64 elements: 97 us in place of 83.)
+constexpr int kKeys = 64;
+template <typename T, int DC, int KS>
+__global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kernel(const BwdArgs g) {
+  constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DH / 16, DB = DH / 32, SLOT = kStep * L::kRowBytes, NB = KvTile<T, DH>::NB, KEYS = KvTile<T, DH>::kKeys;
-  __shared__ __align__(1024) char smem[4 * SLOT];
-  constexpr bool V_LDS = KvTile<T, DH>::kValuesInLds;
-  __shared__ __align__(1024) char values[V_LDS ? KEYS * L::kRowBytes : 16];
-  __shared__ __align__(16) float stats[2][2][kStep];         // of each slot's rows: -lse / scale (fp32: -lse log2 e), -delta
+  constexpr int ES = sizeof(T), KC = DC / 16, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  __shared__ __align__(1024) char smem[4 * KS * SLOT];
+  __shared__ __align__(16) float stats[2][KS][2][kStep];         // of each slot's rows: -lse / scale (fp32: -lse log2 e), -delta
   const AttnShape& a = g.a;
-  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), x = lane & 31, half = lane >> 5, kw = wave & 1, rw = wave >> 1;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 31, half = lane >> 5, kw = wave % 2, rw = wave / 2;
   const int kvh = blockIdx.x % a.kv_heads;
   Seq s;
   int tile, tiles;
-  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, KEYS, lane, s, tile, tiles)) return;
+  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, kKeys, lane, s, tile, tiles)) return;
 
-  const int G = a.group, n_rows = s.lq * G, key0 = tile * KEYS, first = key0 + kw * NB * 32, tail = s.lk - 1;
+  const int G = a.group, n_rows = s.lq * G, key0 = tile * kKeys, first = key0 + kw * 32, key = first + x, tail = s.lk - 1;
   // Rows [from, to) see a key: with causal masks r / G + lk - lq >= key, hence r >= (key - (lk - lq)) G, and likewise for the window
   auto rows_of = [&](int at) {
     Reach r = {0, n_rows};
@@ -182,20 +204,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kerne
     }
     return r;
   };
-  const int lo = rows_of(key0).lo, hi = rows_of(key0 + KEYS - 1).hi;
+  const int lo = rows_of(key0).lo, hi = rows_of(key0 + kKeys - 1).hi;
   const int j0 = lo / kStep, j1 = hi > lo ? cdiv(hi, kStep) : j0;
 
-  Frag kf[NB][KC], vf[NB][V_LDS ? 1 : KC];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int key = min(first + 32 * b + x, tail);
-    const T* const kp = static_cast<const T*>(g.k) + (long)(s.k0 + key) * a.k_row + (long)kvh * a.k_head + 8 * half;
-    const T* const vp = static_cast<const T*>(g.v) + (long)(s.k0 + key) * a.v_row + (long)kvh * a.v_head + 8 * half;
+  Frag kf[KC], vf[KC];
+  {
+    const T* const kp = static_cast<const T*>(g.k) + (long)(s.k0 + min(key, tail)) * a.k_row + (long)kvh * a.k_head + 8 * half;
+    const T* const vp = static_cast<const T*>(g.v) + (long)(s.k0 + min(key, tail)) * a.v_row + (long)kvh * a.v_head + 8 * half;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
       const bool in = 16 * kc + 8 * half < a.dim;
-      kf[b][kc] = in ? Mma<T>::load(kp + 16 * kc) : Mma<T>::zero();
-      if constexpr (!V_LDS) vf[b][kc] = in ? Mma<T>::load(vp + 16 * kc) : Mma<T>::zero();
+      kf[kc] = in ? Mma<T>::load(kp + 16 * kc) : Mma<T>::zero();
+      vf[kc] = in ? Mma<T>::load(vp + 16 * kc) : Mma<T>::zero();
     }
   }
 
@@ -205,6 +225,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kerne
   const unsigned lds0 = lds_address(smem);
   const unsigned magic = (1u << 22) / (unsigned)G + 1;       // n / G = n magic >> 22 for n < 64 + G, G <= 1024
   unsigned off[2][L::kLoads];
+#pragma unroll
+  for (int i = 0; i < L::kLoads; ++i) off[0][i] = off[1][i] = kOutOfRange;
   auto aim = [&](int rem, int left) {
 #pragma unroll
     for (int i = 0; i < L::kLoads; ++i) {
@@ -215,196 +237,186 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kerne
       off[1][i] = in ? q * (unsigned)(a.heads * a.dim * ES) + h * (unsigned)(a.dim * ES) + ch * 16 : kOutOfRange;
     }
   };
-  auto fetch = [&](int j, int slot, bool there) {
-    const int r0 = j * kStep, query = r0 / G, rem = r0 - query * G;
-    if (there && (j == j0 || rem != 0 || kStep % G != 0 || r0 + kStep > n_rows)) aim(rem, n_rows - r0);
-    return PairLoad<T, DH>(off, rsrc_for_lds(q_base + (unsigned long)((long)query * a.q_row * ES), there ? kOpen : 0u),
-                           rsrc_for_lds(d_base + (unsigned long)((long)query * a.heads * a.dim * ES), there ? kOpen : 0u), lds0 + (unsigned)(slot * 2 * SLOT), wave);
+  // the tile that is next: its first row is head `rem` of a query; both are carried on by additions, as in TileStream
+  const int by = KS * kStep, by_query = by / G, by_rem = by - by_query * G;
+  const long q_bytes = a.q_row * ES, d_bytes = (long)a.heads * a.dim * ES;
+  int row0 = (j0 + ks) * kStep, query0 = row0 / G, rem0 = row0 - query0 * G;
+  unsigned long q_at = q_base + (unsigned long)(query0 * q_bytes), d_at = d_base + (unsigned long)(query0 * d_bytes);
+  aim(rem0, n_rows - row0);
+  auto fetch = [&](int slot) {
+    const bool there = row0 < min(n_rows, j1 * kStep);
+    if (by_rem != 0 || (there && row0 + kStep > n_rows)) aim(rem0, max(n_rows - row0, 1));
+    const PairLoad<T, DH> load(off, rsrc_for_lds(q_at, there ? kOpen : 0u), rsrc_for_lds(d_at, there ? kOpen : 0u), lds0 + (unsigned)((slot * KS + ks) * 2 * SLOT), wave);
+    const int more = rem0 + by_rem >= G, queries = by_query + more;
+    row0 += by;
+    query0 += queries;
+    rem0 += by_rem - more * G;
+    q_at += (unsigned long)(queries * q_bytes);
+    d_at += (unsigned long)(queries * d_bytes);
+    return load;
   };
-  constexpr int PER = PairLoad<T, DH>::kPieces / KC;
-  // one row's number to a lane of the first two wavefronts, on its way while the step before is worked on
-  auto number = [&](int j) {
-    const int r = j * kStep + lane;
-    if (r >= n_rows) return wave == 0 ? -INFINITY : 0.f;
-    const long at = (long)(kvh * G + r % G) * a.q_rows + s.q0 + r / G;
-    return wave == 0 ? g.lse[at] : -g.delta[at];
+  // one row's number of that tile to a lane of the first two wavefronts, on its way while the step before is worked on
+  const float* const numbers = wave == 0 ? g.lse : g.delta;
+  const float factor = wave == 1 ? -1.f : ES == 2 ? -1.f / a.scale : -kLog2e;
+  auto number = [&]() {
+    const unsigned n = (unsigned)(lane + rem0), q = n * magic >> 22, h = n - q * G;
+    return row0 + lane < n_rows ? numbers[(long)(kvh * G + (int)h) * a.q_rows + s.q0 + query0 + (int)q] : wave == 0 ? -INFINITY : 0.f;
   };
   auto keep = [&](int slot, float v) {
-    if (wave == 0) v = v == -INFINITY ? -INFINITY : ES == 2 ? -v / a.scale : -v * kLog2e;      // a row without keys has no probabilities
-    if (wave < 2) stats[slot][wave][lane] = v;
+    if (wave < 2) stats[slot][ks][wave][lane] = wave == 0 && v == -INFINITY ? -INFINITY : v * factor;      // a row without keys has no probabilities
   };
 
-  f32x16 dk[NB][DB], dv[NB][DB];
+  f32x16 dk[DB], dv[DB];
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int d = 0; d < DB; ++d) dk[b][d] = dv[b][d] = f32x16{};
+  for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x16{};
   const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    settle(kf[b]);
-    if constexpr (!V_LDS) settle(vf[b]);
-  }
-  if constexpr (V_LDS)
-#pragma unroll
-    for (int t = 0; t < KEYS / kStep; ++t)
-      L::load_rows((unsigned long)g.v + (unsigned long)(((long)(s.k0 + key0 + t * kStep) * a.v_row + (long)kvh * a.v_head) * ES), a.v_row * ES,
-                   s.lk - key0 - t * kStep, a.dim, lds_address(values) + (unsigned)(t * SLOT), wave, lane);
+  settle(kf);
+  settle(vf);
   if (j0 < j1) {
-    fetch(j0, 0, true).all();
-    if (wave < 2) keep(0, number(j0));
+    float v = 0.f;
+    if (wave < 2) v = number();
+    fetch(0).all();
+    keep(0, v);
   }
+  const Reach mine = rows_of(key);
 
-  // 32 rows against the wavefront's keys
+  // the wavefront's 32 of the rows in LDS, the first of them the sequence's r0, against its keys.  The loads of the next rows go out on the way
   auto step = [&](auto cut_, int slot, int r0, const PairLoad<T, DH>& next) {
     constexpr bool CUT = decltype(cut_)::value;
-    const char* const qs = smem + slot * 2 * SLOT;
+    constexpr int PIECES = PairLoad<T, DH>::kPieces;
+    const int n = rw;
+    const char* const qs = smem + (slot * KS + ks) * 2 * SLOT;
     const char* const dos = qs + SLOT;
-    const float* const st = &stats[slot][0][32 * rw + 4 * half];
-    f32x16 p[NB], ds[NB];
+    const float* const st = &stats[slot][ks][0][32 * n + 4 * half];
+    f32x16 p = f32x16{}, ds;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float4 u = *reinterpret_cast<const float4*>(st + 8 * i), w = *reinterpret_cast<const float4*>(st + kStep + 8 * i);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        if (ES == 2) { p[b][4 * i] = u.x; p[b][4 * i + 1] = u.y; p[b][4 * i + 2] = u.z; p[b][4 * i + 3] = u.w; }
-        ds[b][4 * i] = w.x; ds[b][4 * i + 1] = w.y; ds[b][4 * i + 2] = w.z; ds[b][4 * i + 3] = w.w;
-      }
-    }
-    if (ES != 2)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) p[b] = f32x16{};
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc) {
-      const Frag f = L::row_frag(qs, rb, rw, kc);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) p[b] = Mma<T>::mma(f, kf[b][kc], p[b]);
-#pragma unroll
-      for (int i = 0; i < PER; ++i) next.piece(PER * kc + i);
+      if (ES == 2) { p[4 * i] = u.x; p[4 * i + 1] = u.y; p[4 * i + 2] = u.z; p[4 * i + 3] = u.w; }
+      ds[4 * i] = w.x; ds[4 * i + 1] = w.y; ds[4 * i + 2] = w.z; ds[4 * i + 3] = w.w;
     }
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const Frag f = L::row_frag(dos, rb, rw, kc);
+      p = Mma<T>::mma(L::row_frag(qs, rb, n, kc), kf[kc], p);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        if constexpr (V_LDS) ds[b] = Mma<T>::mma(f, L::row_frag(values, rb, kw * NB + b, kc), ds[b]);
-        else ds[b] = Mma<T>::mma(f, vf[b][kc], ds[b]);
+      for (int i = PIECES * kc / KC; i < PIECES * (kc + 1) / KC; ++i) next.piece(i);
+    }
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) ds = Mma<T>::mma(L::row_frag(dos, rb, n, kc), vf[kc], ds);
+    // (bf16: the products are summed on top of -lse / scale; in fp32 storage that would round them to its magnitude)
+    if constexpr (ES == 2) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = exp2_(p[i] * g.c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 u = *reinterpret_cast<const float4*>(st + 8 * i);
+        p[4 * i] = exp2_(fmaf(p[4 * i], g.c, u.x));
+        p[4 * i + 1] = exp2_(fmaf(p[4 * i + 1], g.c, u.y));
+        p[4 * i + 2] = exp2_(fmaf(p[4 * i + 2], g.c, u.z));
+        p[4 * i + 3] = exp2_(fmaf(p[4 * i + 3], g.c, u.w));
       }
     }
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      // (bf16: the products are summed on top of -lse / scale; in fp32 storage that would round them to its magnitude)
-      if constexpr (ES == 2) {
+    for (int i = 0; i < 16; ++i) ds[i] *= p[i];
+    if constexpr (CUT) {
+      const int from = mine.lo - r0 - 4 * half, to = mine.hi - r0 - 4 * half;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) p[b][i] = exp2_(p[b][i] * g.c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 u = *reinterpret_cast<const float4*>(st + 8 * i);
-          p[b][4 * i] = exp2_(fmaf(p[b][4 * i], g.c, u.x));
-          p[b][4 * i + 1] = exp2_(fmaf(p[b][4 * i + 1], g.c, u.y));
-          p[b][4 * i + 2] = exp2_(fmaf(p[b][4 * i + 2], g.c, u.z));
-          p[b][4 * i + 3] = exp2_(fmaf(p[b][4 * i + 3], g.c, u.w));
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) ds[b][i] *= p[b][i];
-      if constexpr (CUT) {
-        const Reach mine = rows_of(first + 32 * b + x);
-        const int from = mine.lo - r0 - 4 * half, to = mine.hi - r0 - 4 * half;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = 8 * (i / 4) + i % 4;
-          if (at < from || at >= to) p[b][i] = ds[b][i] = 0.f;
-        }
+      for (int i = 0; i < 16; ++i) {
+        const int at = 8 * (i / 4) + i % 4;
+        if (at < from || at >= to) p[i] = ds[i] = 0.f;
       }
     }
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      Frag f[NB];
+      const Frag f = Mma<T>::of(p, kk);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) f[b] = Mma<T>::of(p[b], kk);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const Frag c = L::col_frag(dos, cb, d, 2 * rw + kk);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) dv[b][d] = Mma<T>::mma(c, f[b], dv[b][d]);
-      }
+      for (int d = 0; d < DB; ++d) dv[d] = Mma<T>::mma(L::col_frag(dos, cb, d, 2 * n + kk), f, dv[d]);
     }
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      Frag f[NB];
+      const Frag f = Mma<T>::of(ds, kk);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) f[b] = Mma<T>::of(ds[b], kk);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const Frag c = L::col_frag(qs, cb, d, 2 * rw + kk);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) dk[b][d] = Mma<T>::mma(c, f[b], dk[b][d]);
-      }
+      for (int d = 0; d < DB; ++d) dk[d] = Mma<T>::mma(L::col_frag(qs, cb, d, 2 * n + kk), f, dk[d]);
     }
   };
+  // (KS = 2: the second set's last step may be behind the last row; its rows have no probabilities then, and its keys' sums are whole)
   int slot = 0, j = j0;
   auto run = [&](auto cut_, int to) {
-    for (; j < to; ++j, slot ^= 1) {
+    for (; j < to; j += KS, slot ^= 1) {
       wait_and_meet<0>();
-      const bool more = j + 1 < j1;
       float number_next = 0.f;
-      if (more && wave < 2) number_next = number(j + 1);
-      step(cut_, slot, j * kStep + 32 * rw, fetch(j + 1, slot ^ 1, more));
-      if (more && wave < 2) keep(slot ^ 1, number_next);
+      if (wave < 2) number_next = number();
+      const PairLoad<T, DH> next = fetch(slot ^ 1);
+      step(cut_, slot, (j + ks) * kStep + 32 * rw, next);
+      keep(slot ^ 1, number_next);
     }
   };
   // rows that some key does not see only at either end
-  const int all_from = cdiv(rows_of(key0 + KEYS - 1).lo, kStep), all_to = rows_of(key0).hi / kStep;
+  const int all_from = cdiv(rows_of(key0 + kKeys - 1).lo, kStep), all_to = rows_of(key0).hi / kStep;
   run(std::true_type{}, min(max(all_from, j0), j1));
-  run(std::false_type{}, min(max(all_to, j), j1));
+  run(std::false_type{}, min(max(all_to, j), j1) - (KS - 1));
   run(std::true_type{}, j1);
 
+  drain();
   // the other rows' sums: dk, then dv, through LDS
-  const float scale = a.scale;
-  T* const out[2] = {static_cast<T*>(g.dk) + (long)s.k0 * a.k_row + (long)kvh * a.k_head, static_cast<T*>(g.dv) + (long)s.k0 * a.v_row + (long)kvh * a.v_head};
-  const long row[2] = {a.k_row, a.v_row};
-  float4* const other = reinterpret_cast<float4*>(smem) + kw * NB * DB * 4 * kWave + lane;
+  const bool real = key < s.lk;
+  T* const out[2] = {static_cast<T*>(g.dk) + (long)(s.k0 + key) * a.k_row + (long)kvh * a.k_head,
+                     static_cast<T*>(g.dv) + (long)(s.k0 + key) * a.v_row + (long)kvh * a.v_head};
+  float4* const shared = reinterpret_cast<float4*>(smem) + lane;
+  auto at_ = [&](int set, int d, int i) { return ((set * 2 + kw) * DB * 4 + d * 4 + i) * kWave; };      // set: of the 2 KS - 1 others
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     wait_and_meet<0>();
-    if (rw == 1)
+    const int set = ks * 2 + rw;
+    if (set > 0)
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x16& v = t ? dv[b][d] : dk[b][d];
-            other[((b * DB + d) * 4 + i) * kWave] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          const f32x16& v = t ? dv[d] : dk[d];
+          shared[at_(set - 1, d, i)] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
     wait_and_meet<0>();
-    if (rw == 0)
+    if (set == 0)
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int key = first + 32 * b + x;
-        T* const to = out[t] + key * row[t];
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+        for (int i = 0; i < 4; ++i) {
+          const f32x16& v = t ? dv[d] : dk[d];
+          float4 y = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x16& v = t ? dv[b][d] : dk[b][d];
-            const float4 u = other[((b * DB + d) * 4 + i) * kWave];
-            const float f = t ? 1.f : scale;
-            const int at = 32 * d + 8 * i + 4 * half;
-            if (key < s.lk && at < a.dim) put4(to + at, (v[4 * i] + u.x) * f, (v[4 * i + 1] + u.y) * f, (v[4 * i + 2] + u.z) * f, (v[4 * i + 3] + u.w) * f);
+          for (int o = 0; o < 2 * KS - 1; ++o) {
+            const float4 u = shared[at_(o, d, i)];
+            y = make_float4(y.x + u.x, y.y + u.y, y.z + u.z, y.w + u.w);
           }
-      }
+          const float f = t ? 1.f : a.scale;
+          const int at = 32 * d + 8 * i + 4 * half;
+          if (real && at < a.dim) put4(out[t] + at, y.x * f, y.y * f, y.z * f, y.w * f);
+        }
   }
 }
 
-template <typename T, int DH>
+template <typename T, int DC>
 int bwd(const BwdArgs& g, hipStream_t s) {
   const AttnShape& a = g.a;
-  if (a.q_rows > 0) attn_bwd_q_kernel<T, DH><<<dim3((unsigned)(((long)a.q_rows * a.group / kRows + a.n_seq) * a.kv_heads)), dim3(256), 0, s>>>(g);
-  if (a.k_rows > 0) attn_bwd_kv_kernel<T, DH><<<dim3((unsigned)(((long)a.k_rows / KvTile<T, DH>::kKeys + a.n_seq) * a.kv_heads)), dim3(256), 0, s>>>(g);
+  const long rows = (long)a.q_rows * a.group, q_blocks = (rows / kRows + a.n_seq) * a.kv_heads, k_blocks = ((long)a.k_rows / kKeys + a.n_seq) * a.kv_heads;
+  bool two_q = false, two_k = false;
+  if constexpr (kTwoSets<T, DC>) {
+    two_q = two_sets(rows / kRows * a.kv_heads, a.k_rows, a.n_seq);
+    two_k = two_sets((long)a.k_rows / kKeys * a.kv_heads, rows, a.n_seq);
+    if (two_q && a.q_rows > 0) attn_bwd_q_kernel<T, DC, 2><<<dim3((unsigned)q_blocks), dim3(512), 0, s>>>(g);
+  }
+  if (!two_q && a.q_rows > 0) attn_bwd_q_kernel<T, DC, 1><<<dim3((unsigned)q_blocks), dim3(256), 0, s>>>(g);
+  if constexpr (kTwoSets<T, DC>)
+    if (two_k && a.k_rows > 0) attn_bwd_kv_kernel<T, DC, 2><<<dim3((unsigned)k_blocks), dim3(512), 0, s>>>(g);
+  if (!two_k && a.k_rows > 0) attn_bwd_kv_kernel<T, DC, 1><<<dim3((unsigned)k_blocks), dim3(256), 0, s>>>(g);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
+}
+template <typename T>
+int bwd(const BwdArgs& g, hipStream_t s) {
+  const int dim = g.a.dim;
+  return dim <= 32 ? bwd<T, 32>(g, s) : dim <= 64 ? bwd<T, 64>(g, s) : dim <= 96 ? bwd<T, 96>(g, s) : bwd<T, 128>(g, s);
 }
 
 }  // namespace
@@ -414,8 +426,7 @@ size_t attn_bwd_scratch_bytes(int, const AttnShape& a) { return (size_t)a.q_rows
 int launch_attn_bwd(int dtype, const AttnShape& a, const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse, void* dq,
                     void* dk, void* dv, void* scratch, hipStream_t s) {
   const BwdArgs g = {a, d_o, q, k, v, o, lse, dq, dk, dv, static_cast<float*>(scratch), a.scale * kLog2e};
-  if (dtype == SPES_BF16) return a.dim <= 64 ? bwd<bf16_t, 64>(g, s) : bwd<bf16_t, 128>(g, s);
-  return a.dim <= 64 ? bwd<float, 64>(g, s) : bwd<float, 128>(g, s);
+  return dtype == SPES_BF16 ? bwd<bf16_t>(g, s) : bwd<float>(g, s);
 }
 
 }  // namespace spes
