@@ -555,7 +555,7 @@ int fwd(const FwdArgs& g, bool few, hipStream_t s) {
     if (g.parts > 1) attn_join_kernel<T, 256, true><<<grid(1, 1), dim3(256), 0, s>>>(g);
   } else {
     bool two = false;
-    if constexpr (kTwoSets<T, DC>) two = two_sets(n / kRows * a.kv_heads * g.parts, a.k_rows / g.parts, a.n_seq);
+    if constexpr (kTwoSets<T, DC>) two = g.parts == 1 && two_sets(n / kRows * a.kv_heads, 512, a.k_rows, a.n_seq);
     if constexpr (kTwoSets<T, DC>)
       if (two) attn_fwd_kernel<T, DC, 2><<<grid(kRows, g.parts), dim3(512), 0, s>>>(g);
     if (!two) attn_fwd_kernel<T, DC, 1><<<grid(kRows, g.parts), dim3(256), 0, s>>>(g);

@@ -301,3 +301,18 @@ def test_nothing_to_do():
         torch.cuda.synchronize()
         for n, t in got.items():
             assert (t == SENTINEL).all(), n
+
+
+@pytest.mark.parametrize("dtype,dim", [(torch.bfloat16, 32), (torch.bfloat16, 64), (torch.bfloat16, 96), (torch.bfloat16, 128), (torch.float32, 32), (torch.float32, 64),
+                                       (torch.float32, 128)])
+@pytest.mark.parametrize("kw", [dict(), dict(causal=False), dict(window=100), dict(window=333, heads=3, kv=1), dict(heads=7, kv=1)])
+def test_sequences_long_enough_for_two_sets_of_wavefronts(dtype, dim, kw):
+    Problem([257, 640, 449], dtype=dtype, dim=dim, seed=dim, **kw).check()
+    Problem([300, 290], keys=[600, 290], dtype=dtype, dim=dim, gap=3, layout="heads", seed=dim, **kw).check()
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+def test_many_blocks(dtype):
+    """More than the chip holds at once, so one set of wavefronts to a block; sequences of unequal length."""
+    lens = [1500, 3, 700, 64, 257, 1]
+    Problem(lens, heads=32, kv=16, dim=64, dtype=dtype, seed=21).check()
