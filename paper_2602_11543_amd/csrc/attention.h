@@ -1,11 +1,16 @@
-// What the attention kernels share: how a problem is cut into tiles, tiles in LDS, operand fragments of the 32 x 32 matrix instructions.
+// What the attention kernels share: how a problem is cut into tiles, tiles in LDS, operand fragments of the 16 x 16 matrix instructions.
 //
 // Rows.  The heads that share keys stand side by side: row r of a sequence is query r / G under head kvh * G + r % G, G = heads / kv_heads, so a tile of rows
 // meets every key once for all of them, and a sum over the rows is one over the heads as well.
 //
-// Orientation.  Scores are formed as S^T = K Q^T (queries' kernels: keys down, rows across) or S = Q K^T (keys' kernel), so that a lane holds sixteen
-// scores of one column, 8 (i / 4) + 4 (lane / 32) + i % 4 for its register i.  The contraction that follows runs over just these: as its order is free, a
-// lane's registers 0..7 and 8..15 are its operand fragments as they stand, and the other operand is read from LDS in the same order.
+// Orientation.  Scores are formed as S^T = K Q^T (queries' kernels: keys down, rows across) or S = Q K^T (keys' kernel), 32 x 32 at a time as two by two
+// tiles, so that a lane (x = lane % 16, quad = lane / 16) holds of two columns, 16 j + x, the eight scores 16 i + 4 quad + 0..3.  The contraction that follows
+// runs over just these: as its order is free, a column's eight are the lane's operand fragment as they stand, and the other operand is read from
+// LDS in the same order.
+//
+// Why 16 x 16 x 32 and not 32 x 32 x 16: what bounds the large cases is power (32 heads of 128, 8 x 4096 tokens: the clock falls from 2.4 to 1.5 GHz), and the
+// smaller form moves half as many accumulators per multiply-add: backward of that 3.75 -> 3.65 ms, forward 1.13 -> 1.12; 2 x 2048 tokens, 12 heads of 64, forward
+// 33 -> 30 us.
 #pragma once
 #include <algorithm>
 
@@ -19,29 +24,27 @@ constexpr int kRows = 128;       // rows of a block of four wavefronts, 32 each
 constexpr int kStep = 64;        // keys (rows, in the keys' kernel) that pass through LDS at a time
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-typedef __attribute__((ext_vector_type(16))) float f32x16;
 struct f32x8 { float v[8]; };
+struct Acc { f32x4 t[2][2]; };       // 32 x 32: tile (i, j)
 
+// A fragment is 32 of the contraction for one row or column of sixteen: eight elements of each quarter of the lanes
 template <typename T> struct Mma;
 template <> struct Mma<bf16_t> {
-  typedef bf16x8 Frag;           // sixteen of the contraction: eight of each half of the lanes
-  static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, const f32x16& c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-  }
+  typedef bf16x8 Frag;
+  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ Frag zero() { return __builtin_bit_cast(Frag, make_uint4(0, 0, 0, 0)); }
   static __device__ __forceinline__ Frag load(const bf16_t* p) { return __builtin_bit_cast(Frag, *reinterpret_cast<const uint4*>(p)); }
-  // registers 8 n .. 8 n + 7 of a tile of results, rounded to the operands' type
-  static __device__ __forceinline__ Frag of(const f32x16& s, int n) {
-    return __builtin_bit_cast(Frag, make_uint4(pack_bf16x2(s[8 * n], s[8 * n + 1]), pack_bf16x2(s[8 * n + 2], s[8 * n + 3]),
-                                               pack_bf16x2(s[8 * n + 4], s[8 * n + 5]), pack_bf16x2(s[8 * n + 6], s[8 * n + 7])));
+  // a column's eight results, rounded to the operands' type
+  static __device__ __forceinline__ Frag of(const f32x4& a, const f32x4& b) {
+    return __builtin_bit_cast(Frag, make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])));
   }
   static __device__ __forceinline__ float get(const Frag& f, int j) { return (float)f[j]; }
 };
 template <> struct Mma<float> {
   typedef f32x8 Frag;
-  static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, f32x16 c) {
+  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
     return c;
   }
   static __device__ __forceinline__ Frag zero() { return Frag{}; }
@@ -49,14 +52,15 @@ template <> struct Mma<float> {
     const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
     return Frag{{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}};
   }
-  static __device__ __forceinline__ Frag of(const f32x16& s, int n) {
-    Frag f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f.v[j] = s[8 * n + j];
-    return f;
-  }
+  static __device__ __forceinline__ Frag of(const f32x4& a, const f32x4& b) { return Frag{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}}; }
   static __device__ __forceinline__ float get(const Frag& f, int j) { return f.v[j]; }
 };
+// row i of tiles: one fragment of the rows with both of the columns
+template <typename T>
+__device__ __forceinline__ void mma(const typename Mma<T>::Frag& a, const typename Mma<T>::Frag (&b)[2], f32x4 (&c)[2]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) c[j] = Mma<T>::mma(a, b[j], c[j]);
+}
 
 __device__ __forceinline__ unsigned lds_address(void* p) { return uniform((unsigned)(unsigned long)(__attribute__((address_space(3))) char*)p); }
 // The resource of `bytes` bytes from `base` on for loads that stand in assembly.  Where one of its scalars comes out of a vector register, five wait states
@@ -90,47 +94,49 @@ constexpr int tile_dim(int dim) { return dim <= 64 ? 64 : 128; }
 template <typename T, int DC> constexpr bool kTwoSets = 2 * 4 * kStep * tile_dim(DC) * (int)sizeof(T) <= 144 * 1024;
 inline bool two_sets(long blocks, long most, long steps_rows, int n_seq) { return std::max<long>(blocks, n_seq) <= most && steps_rows >= 4l * kStep * n_seq; }
 
-// A tile in LDS: rows of DH elements, chunk c (16 bytes) of row r at position c ^ turn(r).  LDS has 64 banks of four bytes, a read of 16 bytes a lane
-// takes sixteen lanes at a time: sixteen rows at one chunk, and in the transposing reads four rows of 64 bytes (fp32: two of 128), meet every bank once.
+// A tile in LDS: rows of DH elements, chunk c (16 bytes) of row r at position c ^ turn(r).  LDS has 64 banks of four bytes.  A read of 16 bytes a lane is
+// served sixteen lanes at a time, 0-3, 12-15, 20-27 and so on: eight rows at one chunk and the other eight at the next one.  The transposing reads take
+// eight rows of 32 bytes, and in fp32 64 lanes read four rows of 64 bytes, four rows apart.  Each of them meets every bank once (counted: no conflicts; with
+// rows 0-7 at even turns and 8-15 at odd ones in their order, every second read of 16 bytes was one).
 template <typename T, int DH>
 struct Tile {
   static constexpr int kRowBytes = DH * (int)sizeof(T), kChunks = kRowBytes / 16, kRowsPerLoad = 64 / kChunks;
   static __device__ __forceinline__ int turn(int r) {
-    if (sizeof(T) == 4) return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3);
-    if (DH == 64) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
-    return (r & 3) << 2 | ((r >> 2) & 3);
+    if (sizeof(T) == 4) return r & 15;
+    const int far = (r >> 3) & 1;
+    return DH == 64 ? (((r >> 1) & 3) ^ 2 * far) << 1 | far : ((r & 7) ^ 4 * far) << 1 | far;
   }
-  // fragments of rows: lane (x = lane % 32, h = lane / 32) takes elements 16 kc + 8 h .. + 7 of row 32 n + x
+  // fragments of rows: lane (x, quad) takes elements 32 kc + 8 quad .. + 7 of row 16 n + x
   static __device__ __forceinline__ unsigned row_base(int lane) {
-    const int x = lane & 31, h = lane >> 5;
-    return (unsigned)(x * kRowBytes + (((sizeof(T) == 4 ? 2 * h : h) ^ turn(x)) << 4));
+    const int x = lane & 15, quad = lane >> 4;
+    return (unsigned)(x * kRowBytes + (((sizeof(T) == 4 ? 2 * quad : quad) ^ turn(x)) << 4));
   }
   static __device__ __forceinline__ typename Mma<T>::Frag row_frag(const char* slot, unsigned base, int n, int kc) {
     if constexpr (sizeof(T) == 2) {
-      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(slot + (base ^ (unsigned)(kc << 5)) + n * 32 * kRowBytes));
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(slot + (base ^ (unsigned)(kc << 6)) + n * 16 * kRowBytes));
     } else {
-      const float4 p = *reinterpret_cast<const float4*>(slot + (base ^ (unsigned)((4 * kc) << 4)) + n * 32 * kRowBytes);
-      const float4 q = *reinterpret_cast<const float4*>(slot + (base ^ (unsigned)((4 * kc + 1) << 4)) + n * 32 * kRowBytes);
+      const float4 p = *reinterpret_cast<const float4*>(slot + (base ^ (unsigned)((8 * kc) << 4)) + n * 16 * kRowBytes);
+      const float4 q = *reinterpret_cast<const float4*>(slot + (base ^ (unsigned)((8 * kc + 1) << 4)) + n * 16 * kRowBytes);
       return f32x8{{p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w}};
     }
   }
-  // fragments of columns: lane (x, h) takes column 32 db + x of rows 16 kk + 4 h + 0..3 and 16 kk + 8 + 4 h + 0..3
+  // fragments of columns: lane (x, quad) takes column 16 n + x of rows 32 kk + 4 quad + 0..3 and 32 kk + 16 + 4 quad + 0..3
   static __device__ __forceinline__ unsigned col_base(int lane) {
-    const int h = lane >> 5;
-    if (sizeof(T) == 4) return (unsigned)(4 * h * kRowBytes + ((((lane & 31) >> 2) ^ (h << 3)) << 4) + (lane & 3) * 4);
-    const int s = lane & 15, r = 4 * h + (s >> 2);
-    return (unsigned)(r * kRowBytes + (((((lane >> 4) & 1) * 2 + ((s & 3) >> 1)) ^ turn(r)) << 4) + (s & 1) * 8);
+    const int x = lane & 15, quad = lane >> 4;
+    if (sizeof(T) == 4) return (unsigned)(4 * quad * kRowBytes + (((x >> 2) ^ (quad << 2)) << 4) + (x & 3) * 4);
+    const int r = 4 * quad + (x >> 2);
+    return (unsigned)(r * kRowBytes + ((((x & 3) >> 1) ^ turn(r)) << 4) + (x & 1) * 8);
   }
-  static __device__ __forceinline__ typename Mma<T>::Frag col_frag(const char* slot, unsigned base, int db, int kk) {
+  static __device__ __forceinline__ typename Mma<T>::Frag col_frag(const char* slot, unsigned base, int n, int kk) {
     if constexpr (sizeof(T) == 2) {
-      const uint2 p = lds_read_tr(reinterpret_cast<const bf16_t*>(slot + (base ^ (unsigned)(db << 6)) + 16 * kk * kRowBytes));
-      const uint2 q = lds_read_tr(reinterpret_cast<const bf16_t*>(slot + (base ^ (unsigned)(db << 6 | 32)) + (16 * kk + 8) * kRowBytes));
+      const char* const at = slot + (base ^ (unsigned)(n << 5)) + 32 * kk * kRowBytes;
+      const uint2 p = lds_read_tr(reinterpret_cast<const bf16_t*>(at)), q = lds_read_tr(reinterpret_cast<const bf16_t*>(at + 16 * kRowBytes));
       return __builtin_bit_cast(bf16x8, make_uint4(p.x, p.y, q.x, q.y));
     } else {
       f32x8 f;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        f.v[j] = *reinterpret_cast<const float*>(slot + (base ^ (unsigned)((8 * db ^ (j & 4) ^ (j & 3)) << 4)) + (16 * kk + (j & 3) + 8 * (j >> 2)) * kRowBytes);
+        f.v[j] = *reinterpret_cast<const float*>(slot + (base ^ (unsigned)((4 * n ^ (j & 3)) << 4)) + (32 * kk + (j & 3) + 16 * (j >> 2)) * kRowBytes);
       return f;
     }
   }
@@ -210,12 +216,17 @@ __device__ __forceinline__ void drain() { asm volatile("s_waitcnt vmcnt(0)" ::: 
 template <int N>
 __device__ __forceinline__ void wait_for() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 __device__ __forceinline__ void wait_for_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ float both_max(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+// over the four lanes of a column, in all of them
+__device__ __forceinline__ float quad_max(float v) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float both_sum(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+__device__ __forceinline__ float quad_sum(float v) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -235,15 +246,17 @@ __device__ __forceinline__ void settle(F (&f)[N]) {
     }
   }
 }
+template <typename F, int M, int N>
+__device__ __forceinline__ void settle(F (&f)[M][N]) {
+#pragma unroll
+  for (int i = 0; i < M; ++i) settle(f[i]);
+}
 __device__ __forceinline__ void settle(float& v) { asm volatile("" : "+v"(v)); }
 
 __device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ __forceinline__ void put4(bf16_t* p, float a, float b, float c, float d) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
 }
-__device__ __forceinline__ void put2(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
-__device__ __forceinline__ void put2(bf16_t* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(a, b); }
-
 // A sequence as the descriptors give it, cut to the rows that there are, so that whatever they hold no access leaves the tensors
 struct Seq { int q0, lq, k0, lk; };
 __device__ __forceinline__ Seq sequence(const AttnShape& a, int b) {
@@ -285,6 +298,17 @@ __device__ __forceinline__ bool find_tile(const AttnShape& a, int t, int per, in
   }
   return false;
 }
+
+// One of the two rows of a lane in the queries' kernels; a row behind the last one stands for that one, but is not real
+struct Row {
+  bool real;
+  int query, head;
+  __device__ __forceinline__ Row(int r, int rows, int G, int kvh) : real(r < rows) {
+    r = min(r, rows - 1);
+    query = r / G;
+    head = kvh * G + (r - query * G);
+  }
+};
 
 // Keys [lo, hi) that query i of a sequence sees
 struct Reach { int lo, hi; };

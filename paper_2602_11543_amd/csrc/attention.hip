@@ -30,9 +30,9 @@ __device__ __forceinline__ bool part_of(const FwdArgs& g, int part, int n, int& 
 }
 __device__ __forceinline__ int parts_used(const FwdArgs& g, int n) { return min(max(cdiv(n, g.per), 1), g.parts); }
 
-// A row's result: part of one, or the whole.  acc: DB tiles of O^T, the lane's column is the row
+// A row's result: part of one, or the whole.  The row is the lane's column j of the DB x 32 elements in acc
 template <typename T, int DB>
-__device__ __forceinline__ void put_row(const FwdArgs& g, int part, long token, int head, int half, const f32x16 (&acc)[DB], float sum, float m) {
+__device__ __forceinline__ void put_row(const FwdArgs& g, int part, long token, int head, int quad, const Acc (&acc)[DB], int j, float sum, float m) {
   const AttnShape& a = g.a;
   const float inv = sum == 0.f ? 0.f : 1.f / sum, lse = (m + log2f(sum)) * kLn2;
   const bool whole = g.parts == 1;
@@ -41,15 +41,15 @@ __device__ __forceinline__ void put_row(const FwdArgs& g, int part, long token, 
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int at = 32 * d + 8 * i + 4 * half;
-      const float4 v = make_float4(acc[d][4 * i] * inv, acc[d][4 * i + 1] * inv, acc[d][4 * i + 2] * inv, acc[d][4 * i + 3] * inv);
+    for (int i = 0; i < 2; ++i) {
+      const int at = 32 * d + 16 * i + 4 * quad;
+      const f32x4 v = acc[d].t[i][j] * inv;
       if (at < a.dim) {
-        if (whole) put4(op + at, v.x, v.y, v.z, v.w);
-        else put4(po + at, v.x, v.y, v.z, v.w);
+        if (whole) put4(op + at, v[0], v[1], v[2], v[3]);
+        else put4(po + at, v[0], v[1], v[2], v[3]);
       }
     }
-  if (half == 0) (whole ? g.lse : g.part_lse + (long)part * a.heads * a.q_rows)[(long)head * a.q_rows + token] = lse;
+  if (quad == 0) (whole ? g.lse : g.part_lse + (long)part * a.heads * a.q_rows)[(long)head * a.q_rows + token] = lse;
 }
 
 // 128 rows, 32 to each of four wavefronts.  With KS = 2 there are four more, and the two sets take every second step of keys and join what they have at the end:
@@ -59,27 +59,26 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
   constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DC / 16, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  constexpr int ES = sizeof(T), KC = DC / 32, DB = DC / 32, SLOT = kStep * L::kRowBytes;
   __shared__ __align__(1024) char smem[4 * KS * SLOT];       // keys and values, two of each for each set
   __shared__ float2 stats[KS == 1 ? 1 : kRows];
   const AttnShape& a = g.a;
-  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 15, quad = lane >> 4;
   const int part = blockIdx.x % g.parts, item = blockIdx.x / g.parts, kvh = item % a.kv_heads;
   Seq s;
   int tile, tiles;
   if (!find_tile<false>(a, item / a.kv_heads, kRows, lane, s, tile, tiles)) return;
   tile = tiles - 1 - tile;                                   // the longest first
 
-  // this lane's row, and what the block and the wavefront see between them
-  const int G = a.group, n_rows = s.lq * G, r0 = tile * kRows, row = r0 + wave * 32 + x;
-  const int query = min(row, n_rows - 1) / G, head = kvh * G + min(row, n_rows - 1) % G;
-  const bool real = row < n_rows;
-  const Reach mine = reach(a, s, query);
+  // this lane's two rows, and what the block and the wavefront see between them
+  const int G = a.group, n_rows = s.lq * G, r0 = tile * kRows, w_row = r0 + wave * 32;
+  const Row row[2] = {Row(w_row + x, n_rows, G, kvh), Row(w_row + 16 + x, n_rows, G, kvh)};
+  const Reach mine[2] = {reach(a, s, row[0].query), reach(a, s, row[1].query)};
   const int last = min(r0 + kRows, n_rows) - 1;
   const int lo = reach(a, s, r0 / G).lo, hi = reach(a, s, last / G).hi;
-  const int w_first = min(r0 + wave * 32, n_rows - 1) / G, w_last = min(r0 + wave * 32 + 31, n_rows - 1) / G;
+  const int w_first = min(w_row, n_rows - 1) / G, w_last = min(w_row + 31, n_rows - 1) / G;
   const Reach w0 = reach(a, s, w_first), w1 = reach(a, s, w_last);       // [w0.lo, w1.hi) is seen by some row, [w1.lo, w0.hi) by all
-  const bool w_real = r0 + wave * 32 < n_rows;
+  const bool w_real = w_row < n_rows;
   int j0 = lo / kStep, j1;
   {
     int from, to;
@@ -89,11 +88,12 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
   }
 
   // queries: the operand with the rows across, in registers
-  Frag qf[KC];
-  {
-    const T* const qp = static_cast<const T*>(g.q) + (long)(s.q0 + query) * a.q_row + (long)head * a.q_head + 8 * half;
+  Frag qf[KC][2];
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) qf[kc] = real && 16 * kc + 8 * half < a.dim ? Mma<T>::load(qp + 16 * kc) : Mma<T>::zero();
+  for (int j = 0; j < 2; ++j) {
+    const T* const qp = static_cast<const T*>(g.q) + (long)(s.q0 + row[j].query) * a.q_row + (long)row[j].head * a.q_head + 8 * quad;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) qf[kc][j] = row[j].real && 32 * kc + 8 * quad < a.dim ? Mma<T>::load(qp + 32 * kc) : Mma<T>::zero();
   }
 
   // keys and values on their way into LDS
@@ -111,12 +111,12 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
     const rsrc_t k = stream.next(0), v = stream.next(1);
     return PairLoad<T, DH>(off, k, v, lds0 + (unsigned)((slot * KS + ks) * 2 * SLOT), wave);
   };
-  constexpr int PIECES = PairLoad<T, DH>::kPieces;
+  constexpr int PIECES = PairLoad<T, DH>::kPieces, NS = 2 * KC;      // NS: steps of 32 keys and 32 elements
 
-  f32x16 acc[DB];
+  Acc acc[DB];
 #pragma unroll
-  for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
-  float m = -INFINITY, l[4] = {0.f, 0.f, 0.f, 0.f};             // of this lane's row, in units of log2; l: this half's share
+  for (int d = 0; d < DB; ++d) acc[d] = Acc{};
+  float m[2] = {-INFINITY, -INFINITY}, l[2][2] = {{0.f, 0.f}, {0.f, 0.f}};      // of the lane's rows, m in units of log2; l: this lane's share
   const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
   settle(qf);
   if (j0 < j1) fetch(0).all();
@@ -131,94 +131,118 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
     }
     const char* const kt = smem + (slot * KS + ks) * 2 * SLOT;
     const char* const vt = kt + SLOT;
-    f32x16 sc[2] = {f32x16{}, f32x16{}};
-    Frag kf[3][2];             // read two steps ahead
+    Acc sc[2] = {Acc{}, Acc{}};          // of 32 keys each
+    Frag kf[3][2];                       // read two steps ahead
 #pragma unroll
-    for (int kc = 0; kc < 2; ++kc)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int n = 0; n < 2; ++n) kf[kc][n] = L::row_frag(kt, rb, n, kc);
+      for (int i = 0; i < 2; ++i) kf[t][i] = L::row_frag(kt, rb, 2 * (t % 2) + i, t / 2);
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) {
-      if (kc + 2 < KC)
+    for (int t = 0; t < NS; ++t) {
+      if (t + 2 < NS)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) kf[(kc + 2) % 3][n] = L::row_frag(kt, rb, n, kc + 2);
+        for (int i = 0; i < 2; ++i) kf[(t + 2) % 3][i] = L::row_frag(kt, rb, 2 * ((t + 2) % 2) + i, (t + 2) / 2);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) sc[n] = Mma<T>::mma(kf[kc % 3][n], qf[kc], sc[n]);
+      for (int i = 0; i < 2; ++i) mma<T>(kf[t % 3][i], qf[t / 2], sc[t % 2].t[i]);
 #pragma unroll
-      for (int p = PIECES * kc / KC; p < PIECES * (kc + 1) / KC; ++p) next.piece(p);
+      for (int p = PIECES * t / NS; p < PIECES * (t + 1) / NS; ++p) next.piece(p);
     }
     if (key0 < w1.lo || key0 + kStep > w0.hi) {
-      const int from = mine.lo - key0 - 4 * half, to = mine.hi - key0 - 4 * half;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int from = mine[c].lo - key0 - 4 * quad, to = mine[c].hi - key0 - 4 * quad;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int at = 32 * n + 16 * i + e;
+              if (at < from || at >= to) sc[n].t[i][c][e] = -INFINITY;
+            }
+      }
+    }
+    float top[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      float half[2];                     // (two chains, as the sums below: one would be waited for)
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        half[n] = sc[n].t[0][c][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) half[n] = fmaxf(half[n], sc[n].t[e / 4][c][e % 4]);
+      }
+      top[c] = quad_max(fmaxf(half[0], half[1])) * g.c;
+    }
+    if (__any(top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bool raise = top[c] > m[c] + kLazy;
+        const float f = raise ? exp2_(m[c] - top[c]) : 1.f;
+        if (raise) m[c] = top[c];
+        l[c][0] *= f;
+        l[c][1] *= f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) acc[d].t[i][c] *= f;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const float low = m[c] == -INFINITY ? 0.f : m[c];
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = 32 * n + 8 * (i / 4) + i % 4;
-          if (at < from || at >= to) sc[n][i] = -INFINITY;
+        for (int e = 0; e < 8; ++e) {
+          const float v = exp2_(fmaf(sc[n].t[e / 4][c][e % 4], g.c, -low));
+          sc[n].t[e / 4][c][e % 4] = v;
+          l[c][n] += v;
         }
     }
-    float tops[4] = {sc[0][0], sc[0][8], sc[1][0], sc[1][8]};          // (four chains of eight, as the sums below: one chain would be waited for)
 #pragma unroll
-    for (int i = 1; i < 8; ++i)
+    for (int n = 0; n < 2; ++n) {
+      const Frag p[2] = {Mma<T>::of(sc[n].t[0][0], sc[n].t[1][0]), Mma<T>::of(sc[n].t[0][1], sc[n].t[1][1])};
 #pragma unroll
-      for (int u = 0; u < 4; ++u) tops[u] = fmaxf(tops[u], sc[u / 2][8 * (u % 2) + i]);
-    const float top = both_max(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * g.c;
-    if (__any(top > m + kLazy)) {
-      const bool raise = top > m + kLazy;
-      const float f = raise ? exp2_(m - top) : 1.f;
-      if (raise) m = top;
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) l[u] *= f;
-#pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] *= f;
-    }
-    const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[n][i] = exp2_(fmaf(sc[n][i], g.c, -base));
-        l[2 * n + i / 8] += sc[n][i];
-      }
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      const Frag p = Mma<T>::of(sc[kk / 2], kk % 2);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] = Mma<T>::mma(L::col_frag(vt, cb, d, kk), p, acc[d]);
+        for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(vt, cb, 2 * d + i, n), p, acc[d].t[i]);
     }
   }
 
   drain();
-  float sum = both_sum((l[0] + l[1]) + (l[2] + l[3]));
+  float sum[2] = {quad_sum(l[0][0] + l[0][1]), quad_sum(l[1][0] + l[1][1])};
   if constexpr (KS == 2) {
     // the second set's to the first, both scaled to their common maximum
-    float4* const other = reinterpret_cast<float4*>(smem) + wave * DB * 4 * kWave + lane;
+    f32x4* const other = reinterpret_cast<f32x4*>(smem) + wave * DB * 4 * kWave + lane;
     wait_and_meet<0>();
     if (ks == 1) {
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
+      for (int c = 0; c < 2; ++c) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) other[(d * 4 + i) * kWave] = make_float4(acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]);
-      if (half == 0) stats[wave * 32 + x] = make_float2(m, sum);
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) other[(d * 4 + i * 2 + c) * kWave] = acc[d].t[i][c];
+        if (quad == 0) stats[wave * 32 + 16 * c + x] = make_float2(m[c], sum[c]);
+      }
     }
     wait_and_meet<0>();
     if (ks == 1) return;
-    const float2 st = stats[wave * 32 + x];
-    const float top = fmaxf(m, st.x), low = top == -INFINITY ? 0.f : top, f = exp2_(m - low), f1 = exp2_(st.x - low);
-    sum = sum * f + st.y * f1;
-    m = top;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int c = 0; c < 2; ++c) {
+      const float2 st = stats[wave * 32 + 16 * c + x];
+      const float top = fmaxf(m[c], st.x), low = top == -INFINITY ? 0.f : top, f = exp2_(m[c] - low), f1 = exp2_(st.x - low);
+      sum[c] = sum[c] * f + st.y * f1;
+      m[c] = top;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 u = other[(d * 4 + i) * kWave];
-        acc[d][4 * i] = acc[d][4 * i] * f + u.x * f1;
-        acc[d][4 * i + 1] = acc[d][4 * i + 1] * f + u.y * f1;
-        acc[d][4 * i + 2] = acc[d][4 * i + 2] * f + u.z * f1;
-        acc[d][4 * i + 3] = acc[d][4 * i + 3] * f + u.w * f1;
-      }
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[d].t[i][c] = acc[d].t[i][c] * f + other[(d * 4 + i * 2 + c) * kWave] * f1;
+    }
   }
-  if (real) put_row<T, DB>(g, part, s.q0 + query, head, half, acc, sum, m);
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+    if (row[c].real) put_row<T, DB>(g, part, s.q0 + row[c].query, row[c].head, quad, acc, c, sum[c], m[c]);
 }
 
 // Few rows of a sequence (up to 32) against many keys: every wavefront goes over keys of its own, steps of 32, through LDS of its own, so nothing is waited
@@ -298,11 +322,11 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
   typedef Tile<T, DH> L;
   typedef Few<T, DH> W;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DC / 16, DB = DC / 32;
+  constexpr int ES = sizeof(T), KC = DC / 32, DB = DC / 32;
   __shared__ __align__(1024) char smem[W::kWaves * 4 * W::kSlot];
   __shared__ float2 stats[W::kWaves][kFewRows];
   const AttnShape& a = g.a;
-  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), x = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), x = lane & 15, quad = lane >> 4;
   const FewPlan plan(a, g.parts, lane);
   char* const mem = smem + wave * 4 * W::kSlot;
   const unsigned lds0 = lds_address(mem);
@@ -312,10 +336,9 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
   int tile, part, j0, j1;
   const int kvh = item % a.kv_heads;
   if (!plan.find(a, item / a.kv_heads, lane, s, tile, part, j0, j1)) return;
-  const int G = a.group, n_rows = s.lq * G, r0 = tile * kFewRows, row = r0 + x, last = min(r0 + kFewRows, n_rows) - 1;
-  const int query = min(row, last) / G, head = kvh * G + min(row, last) % G;
-  const bool real = row <= last;
-  const Reach mine = reach(a, s, query), first = reach(a, s, r0 / G), final = reach(a, s, last / G);
+  const int G = a.group, n_rows = s.lq * G, r0 = tile * kFewRows, last = min(r0 + kFewRows, n_rows) - 1;
+  const Row row[2] = {Row(r0 + x, n_rows, G, kvh), Row(r0 + 16 + x, n_rows, G, kvh)};
+  const Reach mine[2] = {reach(a, s, row[0].query), reach(a, s, row[1].query)}, first = reach(a, s, r0 / G), final = reach(a, s, last / G);
   // (of its sequence's steps, those that the tile sees)
   j0 = max(j0, first.lo / kFewStep);
   j1 = final.hi > first.lo ? min(j1, cdiv(final.hi, kFewStep)) : j0;
@@ -346,108 +369,136 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
   };
   int j = j0 + wave;
   // queries first: they are waited for by number of loads behind them
-  Frag qf[KC];
-  {
-    const T* const qp = static_cast<const T*>(g.q) + (long)(s.q0 + query) * a.q_row + (long)head * a.q_head + 8 * half;
+  Frag qf[KC][2];
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) qf[kc] = real && 16 * kc + 8 * half < a.dim ? Mma<T>::load(qp + 16 * kc) : Mma<T>::zero();
+  for (int c = 0; c < 2; ++c) {
+    const T* const qp = static_cast<const T*>(g.q) + (long)(s.q0 + row[c].query) * a.q_row + (long)row[c].head * a.q_head + 8 * quad;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) qf[kc][c] = row[c].real && 32 * kc + 8 * quad < a.dim ? Mma<T>::load(qp + 32 * kc) : Mma<T>::zero();
   }
   load(j, 0);
   settle(qf);
 
-  f32x16 acc[DB];
+  // (rows beyond sixteen, where there are any, are the lane's second)
+  const bool both = last - r0 >= 16;
+  Acc acc[DB];
 #pragma unroll
-  for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
-  float m = -INFINITY, l[2] = {0.f, 0.f};
+  for (int d = 0; d < DB; ++d) acc[d] = Acc{};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
   int slot = 0;
   for (; j < j1; j += W::kWaves, slot ^= 1) {
     load(j + W::kWaves, slot ^ 1);
     wait_for<2 * W::kLoads>();
     const int key0 = j * kFewStep;
-    const char* const ks = mem + slot * 2 * W::kSlot;
-    const char* const vs = ks + W::kSlot;
-    f32x16 sc = f32x16{};
+    const char* const kt = mem + slot * 2 * W::kSlot;
+    const char* const vt = kt + W::kSlot;
+    Acc sc = Acc{};
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) sc = Mma<T>::mma(L::row_frag(ks, rb, 0, kc), qf[kc], sc);
-    if (key0 < final.lo || key0 + kFewStep > first.hi) {
-      const int from = mine.lo - key0 - 4 * half, to = mine.hi - key0 - 4 * half;
+    for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int at = 8 * (i / 4) + i % 4;
-        if (at < from || at >= to) sc[i] = -INFINITY;
+      for (int i = 0; i < 2; ++i) {
+        const Frag f = L::row_frag(kt, rb, i, kc);
+        sc.t[i][0] = Mma<T>::mma(f, qf[kc][0], sc.t[i][0]);
+        if (both) sc.t[i][1] = Mma<T>::mma(f, qf[kc][1], sc.t[i][1]);
       }
+    const bool cut = key0 < final.lo || key0 + kFewStep > first.hi;
+    Frag p[2] = {Mma<T>::zero(), Mma<T>::zero()};
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      if (c == 1 && !both) break;
+      if (cut) {
+        const int from = mine[c].lo - key0 - 4 * quad, to = mine[c].hi - key0 - 4 * quad;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int at = 16 * (e / 4) + e % 4;
+          if (at < from || at >= to) sc.t[e / 4][c][e % 4] = -INFINITY;
+        }
+      }
+      float top = sc.t[0][c][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, sc.t[e / 4][c][e % 4]);
+      top = quad_max(top) * g.c;
+      if (__any(top > m[c] + kLazy)) {
+        const bool raise = top > m[c] + kLazy;
+        const float f = raise ? exp2_(m[c] - top) : 1.f;
+        if (raise) m[c] = top;
+        l[c] *= f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) acc[d].t[i][c] *= f;
+      }
+      const float low = m[c] == -INFINITY ? 0.f : m[c];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = exp2_(fmaf(sc.t[e / 4][c][e % 4], g.c, -low));
+        sc.t[e / 4][c][e % 4] = v;
+        l[c] += v;
+      }
+      p[c] = Mma<T>::of(sc.t[0][c], sc.t[1][c]);
     }
-    float tops[2] = {sc[0], sc[8]};
 #pragma unroll
-    for (int i = 1; i < 8; ++i)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) tops[u] = fmaxf(tops[u], sc[8 * u + i]);
-    const float top = both_max(fmaxf(tops[0], tops[1])) * g.c;
-    if (__any(top > m + kLazy)) {
-      const bool raise = top > m + kLazy;
-      const float f = raise ? exp2_(m - top) : 1.f;
-      if (raise) m = top;
-      l[0] *= f;
-      l[1] *= f;
-#pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] *= f;
-    }
-    const float low = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      sc[i] = exp2_(fmaf(sc[i], g.c, -low));
-      l[i / 8] += sc[i];
-    }
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      const Frag p = Mma<T>::of(sc, kk);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] = Mma<T>::mma(L::col_frag(vs, cb, d, kk), p, acc[d]);
-    }
+      for (int i = 0; i < 2; ++i) {
+        const Frag f = L::col_frag(vt, cb, 2 * d + i, 0);
+        acc[d].t[i][0] = Mma<T>::mma(f, p[0], acc[d].t[i][0]);
+        if (both) acc[d].t[i][1] = Mma<T>::mma(f, p[1], acc[d].t[i][1]);
+      }
     wait_for_reads();         // ahead of the loads that overwrite them
   }
   drain();
 
   // the wavefronts' sums, scaled to their common maximum
-  const float sum = both_sum(l[0] + l[1]);
-  if (half == 0) stats[wave][x] = make_float2(m, sum);
-  wait_and_meet<0>();
-  float top = -INFINITY, all = 0.f;
 #pragma unroll
-  for (int w = 0; w < W::kWaves; ++w) top = fmaxf(top, stats[w][x].x);
-  const float low = top == -INFINITY ? 0.f : top;
-#pragma unroll
-  for (int w = 0; w < W::kWaves; ++w) all += stats[w][x].y * exp2_(stats[w][x].x - low);
-  const float f = exp2_(m - low);
-  // slice DB / kWaves of the elements is joined by one wavefront: [wave][d][i][lane]
-  float4* const shared = reinterpret_cast<float4*>(smem);
-#pragma unroll
-  for (int d = 0; d < DB; ++d) {
-    acc[d] *= f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      shared[((wave * DB + d) * 4 + i) * kWave + lane] = make_float4(acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]);
+  for (int c = 0; c < 2; ++c) {
+    const float sum = quad_sum(l[c]);
+    if (quad == 0) stats[wave][16 * c + x] = make_float2(m[c], sum);
   }
   wait_and_meet<0>();
+  f32x4* const shared = reinterpret_cast<f32x4*>(smem) + lane;      // [wave][c][d][i][lane]
+  float low[2], all[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W::kWaves; ++w) top = fmaxf(top, stats[w][16 * c + x].x);
+    low[c] = top == -INFINITY ? 0.f : top;
+    all[c] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W::kWaves; ++w) all[c] += stats[w][16 * c + x].y * exp2_(stats[w][16 * c + x].x - low[c]);
+    const float f = exp2_(m[c] - low[c]);
+    if (c == 0 || both)
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) shared[(((wave * 2 + c) * DB + d) * 2 + i) * kWave] = acc[d].t[i][c] * f;
+  }
+  wait_and_meet<0>();
+  // each of the sixteen elements' quads of a column is joined by one wavefront
   const bool whole = g.parts == 1;
-  const float inv = all == 0.f ? 0.f : 1.f / all;
-  const long token = s.q0 + query;
-  float* const po = g.part_o + (((long)part * a.q_rows + token) * a.heads + head) * a.dim;
-  T* const op = static_cast<T*>(g.o) + (token * a.heads + head) * a.dim;
-  for (int t = wave; t < 4 * DB; t += W::kWaves) {
-    float4 v = shared[t * kWave + lane];
 #pragma unroll
-    for (int w = 1; w < W::kWaves; ++w) {
-      const float4 u = shared[(w * DB * 4 + t) * kWave + lane];
-      v = make_float4(v.x + u.x, v.y + u.y, v.z + u.z, v.w + u.w);
+  for (int c = 0; c < 2; ++c) {
+    if (c == 1 && !both) break;
+    const float inv = all[c] == 0.f ? 0.f : 1.f / all[c];
+    const long token = s.q0 + row[c].query;
+    float* const po = g.part_o + (((long)part * a.q_rows + token) * a.heads + row[c].head) * a.dim;
+    T* const op = static_cast<T*>(g.o) + (token * a.heads + row[c].head) * a.dim;
+    for (int t = wave; t < 2 * DB; t += W::kWaves) {
+      f32x4 v = shared[(c * DB * 2 + t) * kWave];
+#pragma unroll
+      for (int w = 1; w < W::kWaves; ++w) v += shared[((w * 2 + c) * DB * 2 + t) * kWave];
+      v *= inv;
+      const int at = 16 * t + 4 * quad;
+      if (row[c].real && at < a.dim) {
+        if (whole) put4(op + at, v[0], v[1], v[2], v[3]);
+        else put4(po + at, v[0], v[1], v[2], v[3]);
+      }
     }
-    const int at = 32 * (t / 4) + 8 * (t % 4) + 4 * half;
-    if (real && at < a.dim) {
-      if (whole) put4(op + at, v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-      else put4(po + at, v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-    }
+    // (a row without keys: its sum is nothing, and so is what its maximum is)
+    if (row[c].real && wave == 0 && quad == 0)
+      (whole ? g.lse : g.part_lse + (long)part * a.heads * a.q_rows)[(long)row[c].head * a.q_rows + token] = (low[c] + log2f(all[c])) * kLn2;
   }
-  if (real && wave == 0 && half == 0) (whole ? g.lse : g.part_lse + (long)part * a.heads * a.q_rows)[(long)head * a.q_rows + token] = (top + log2f(all)) * kLn2;
   wait_and_meet<0>();           // the next item's loads overwrite what has been read here
   }
 }

@@ -27,50 +27,51 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
   constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DC / 16, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  constexpr int ES = sizeof(T), KC = DC / 32, DB = DC / 32, SLOT = kStep * L::kRowBytes;
   __shared__ __align__(1024) char smem[4 * KS * SLOT];
   const AttnShape& a = g.a;
-  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 15, quad = lane >> 4;
   const int kvh = blockIdx.x % a.kv_heads;
   Seq s;
   int tile, tiles;
   if (!find_tile<false>(a, blockIdx.x / a.kv_heads, kRows, lane, s, tile, tiles)) return;
   tile = tiles - 1 - tile;                                   // the longest first
 
-  const int G = a.group, n_rows = s.lq * G, r0 = tile * kRows, row = r0 + wave * 32 + x;
-  const int query = min(row, n_rows - 1) / G, head = kvh * G + min(row, n_rows - 1) % G;
-  const bool real = row < n_rows;
-  const Reach mine = reach(a, s, query);
+  const int G = a.group, n_rows = s.lq * G, r0 = tile * kRows, w_row = r0 + wave * 32;
+  const Row row[2] = {Row(w_row + x, n_rows, G, kvh), Row(w_row + 16 + x, n_rows, G, kvh)};
+  const Reach mine[2] = {reach(a, s, row[0].query), reach(a, s, row[1].query)};
   const int last = min(r0 + kRows, n_rows) - 1;
   const int lo = reach(a, s, r0 / G).lo, hi = reach(a, s, last / G).hi;
-  const int w_first = min(r0 + wave * 32, n_rows - 1) / G, w_last = min(r0 + wave * 32 + 31, n_rows - 1) / G;
+  const int w_first = min(w_row, n_rows - 1) / G, w_last = min(w_row + 31, n_rows - 1) / G;
   const Reach w0 = reach(a, s, w_first), w1 = reach(a, s, w_last);
-  const bool w_real = r0 + wave * 32 < n_rows;
+  const bool w_real = w_row < n_rows;
   const int j0 = lo / kStep, j1 = hi > lo ? cdiv(hi, kStep) : j0;
-  const long token = s.q0 + query;
 
-  Frag qf[KC], df[KC];
-  float delta = 0.f;
-  {
-    const T* const qp = static_cast<const T*>(g.q) + token * a.q_row + (long)head * a.q_head + 8 * half;
-    const long at = (token * a.heads + head) * a.dim + 8 * half;
+  Frag qf[KC][2], df[KC][2];
+  float delta[2], base[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const long token = s.q0 + row[c].query, at = (token * a.heads + row[c].head) * a.dim + 8 * quad;
+    const T* const qp = static_cast<const T*>(g.q) + token * a.q_row + (long)row[c].head * a.q_head + 8 * quad;
     const T* const dp = static_cast<const T*>(g.d_o) + at;
     const T* const op = static_cast<const T*>(g.o) + at;
+    Frag of[KC];
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const bool in = real && 16 * kc + 8 * half < a.dim;
-      qf[kc] = in ? Mma<T>::load(qp + 16 * kc) : Mma<T>::zero();
-      df[kc] = in ? Mma<T>::load(dp + 16 * kc) : Mma<T>::zero();
+      const bool in = row[c].real && 32 * kc + 8 * quad < a.dim;
+      qf[kc][c] = in ? Mma<T>::load(qp + 32 * kc) : Mma<T>::zero();
+      df[kc][c] = in ? Mma<T>::load(dp + 32 * kc) : Mma<T>::zero();
+      of[kc] = in ? Mma<T>::load(op + 32 * kc) : Mma<T>::zero();
     }
+    base[c] = g.lse[(long)row[c].head * a.q_rows + token] * kLog2e;
+    delta[c] = 0.f;
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) {
-      const Frag of = real && 16 * kc + 8 * half < a.dim ? Mma<T>::load(op + 16 * kc) : Mma<T>::zero();
+    for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) delta = fmaf(Mma<T>::get(df[kc], j), Mma<T>::get(of, j), delta);
-    }
+      for (int e = 0; e < 8; ++e) delta[c] = fmaf(Mma<T>::get(df[kc][c], e), Mma<T>::get(of[kc], e), delta[c]);
+    delta[c] = quad_sum(delta[c]);
+    if (row[c].real && quad == 0 && ks == 0) g.delta[(long)row[c].head * a.q_rows + token] = delta[c];
   }
-  delta = both_sum(delta);
-  if (real && half == 0 && ks == 0) g.delta[(long)head * a.q_rows + token] = delta;
 
   const long stride[2] = {a.k_row * ES, a.v_row * ES};
   const unsigned long source[2] = {(unsigned long)g.k + (unsigned long)(s.k0 * stride[0] + (long)kvh * a.k_head * ES),
@@ -88,15 +89,17 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
   };
   constexpr int PIECES = PairLoad<T, DH>::kPieces;
 
-  f32x16 acc[DB];
+  Acc acc[DB];
 #pragma unroll
-  for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
+  for (int d = 0; d < DB; ++d) acc[d] = Acc{};
   const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
-  float base = g.lse[(long)head * a.q_rows + token] * kLog2e;
   settle(qf);
   settle(df);
-  settle(base);
-  settle(delta);
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    settle(base[c]);
+    settle(delta[c]);
+  }
   if (j0 < j1) fetch(0).all();
   int slot = 0;
   for (int first = j0; first < j1; first += KS, slot ^= 1) {
@@ -108,70 +111,76 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
       continue;
     }
     const bool cut = key0 < w1.lo || key0 + kStep > w0.hi;
-    const int from = mine.lo - key0 - 4 * half, to = mine.hi - key0 - 4 * half;
     const char* const kt = smem + (slot * KS + ks) * 2 * SLOT;
     const char* const vt = kt + SLOT;
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      f32x16 sc = f32x16{}, ds;
+      Acc sc = Acc{}, ds;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ds[i] = -delta;
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) ds.t[i][c] = f32x4{-delta[c], -delta[c], -delta[c], -delta[c]};
 #pragma unroll
       for (int kc = 0; kc < KC; ++kc) {
-        sc = Mma<T>::mma(L::row_frag(kt, rb, n, kc), qf[kc], sc);
-        ds = Mma<T>::mma(L::row_frag(vt, rb, n, kc), df[kc], ds);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mma<T>(L::row_frag(kt, rb, 2 * n + i, kc), qf[kc], sc.t[i]);
+          mma<T>(L::row_frag(vt, rb, 2 * n + i, kc), df[kc], ds.t[i]);
+        }
         if (n == 0)
 #pragma unroll
           for (int p = PIECES * kc / KC; p < PIECES * (kc + 1) / KC; ++p) next.piece(p);
       }
+      Frag f[2];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ds[i] *= exp2_(fmaf(sc[i], g.c, -base));
-      if (cut) {
+      for (int c = 0; c < 2; ++c) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = 32 * n + 8 * (i / 4) + i % 4;
-          if (at < from || at >= to) ds[i] = 0.f;
+        for (int e = 0; e < 8; ++e) ds.t[e / 4][c][e % 4] *= exp2_(fmaf(sc.t[e / 4][c][e % 4], g.c, -base[c]));
+        if (cut) {
+          const int from = mine[c].lo - key0 - 4 * quad, to = mine[c].hi - key0 - 4 * quad;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int at = 32 * n + 16 * (e / 4) + e % 4;
+            if (at < from || at >= to) ds.t[e / 4][c][e % 4] = 0.f;
+          }
         }
+        f[c] = Mma<T>::of(ds.t[0][c], ds.t[1][c]);
       }
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        const Frag f = Mma<T>::of(ds, kk);
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int d = 0; d < DB; ++d) acc[d] = Mma<T>::mma(L::col_frag(kt, cb, d, 2 * n + kk), f, acc[d]);
-      }
+        for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(kt, cb, 2 * d + i, n), f, acc[d].t[i]);
     }
   }
   drain();
   if constexpr (KS == 2) {
-    float4* const other = reinterpret_cast<float4*>(smem) + wave * DB * 4 * kWave + lane;
+    f32x4* const other = reinterpret_cast<f32x4*>(smem) + wave * DB * 4 * kWave + lane;
     wait_and_meet<0>();
     if (ks == 1)
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) other[(d * 4 + i) * kWave] = make_float4(acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]);
+        for (int i = 0; i < 4; ++i) other[(d * 4 + i) * kWave] = acc[d].t[i / 2][i % 2];
     wait_and_meet<0>();
     if (ks == 1) return;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 u = other[(d * 4 + i) * kWave];
-        acc[d][4 * i] += u.x;
-        acc[d][4 * i + 1] += u.y;
-        acc[d][4 * i + 2] += u.z;
-        acc[d][4 * i + 3] += u.w;
+      for (int i = 0; i < 4; ++i) acc[d].t[i / 2][i % 2] += other[(d * 4 + i) * kWave];
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    if (!row[c].real) continue;
+    T* const dq = static_cast<T*>(g.dq) + (long)(s.q0 + row[c].query) * a.q_row + (long)row[c].head * a.q_head;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int at = 32 * d + 16 * i + 4 * quad;
+        const f32x4 v = acc[d].t[i][c] * a.scale;
+        if (at < a.dim) put4(dq + at, v[0], v[1], v[2], v[3]);
       }
   }
-  if (!real) return;
-  T* const dq = static_cast<T*>(g.dq) + token * a.q_row + (long)head * a.q_head;
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int at = 32 * d + 8 * i + 4 * half;
-      if (at < a.dim) put4(dq + at, acc[d][4 * i] * a.scale, acc[d][4 * i + 1] * a.scale, acc[d][4 * i + 2] * a.scale, acc[d][4 * i + 3] * a.scale);
-    }
 }
 
 // Four wavefronts: two groups of 32 keys, and in each one wavefront for the first 32 of the 64 rows that are in LDS and one for the others, whose sums are
@@ -183,17 +192,18 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
   constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DC / 16, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  constexpr int ES = sizeof(T), KC = DC / 32, DB = DC / 32, SLOT = kStep * L::kRowBytes;
   __shared__ __align__(1024) char smem[4 * KS * SLOT];
   __shared__ __align__(16) float stats[2][KS][2][kStep];         // of each slot's rows: -lse / scale (fp32: -lse log2 e), -delta
   const AttnShape& a = g.a;
-  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 31, half = lane >> 5, kw = wave % 2, rw = wave / 2;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 15, quad = lane >> 4;
+  const int kw = wave % 2, rw = wave / 2;
   const int kvh = blockIdx.x % a.kv_heads;
   Seq s;
   int tile, tiles;
   if (!find_tile<true>(a, blockIdx.x / a.kv_heads, kKeys, lane, s, tile, tiles)) return;
 
-  const int G = a.group, n_rows = s.lq * G, key0 = tile * kKeys, first = key0 + kw * 32, key = first + x, tail = s.lk - 1;
+  const int G = a.group, n_rows = s.lq * G, key0 = tile * kKeys, first = key0 + kw * 32, tail = s.lk - 1;
   // Rows [from, to) see a key: with causal masks r / G + lk - lq >= key, hence r >= (key - (lk - lq)) G, and likewise for the window
   auto rows_of = [&](int at) {
     Reach r = {0, n_rows};
@@ -207,15 +217,17 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
   const int lo = rows_of(key0).lo, hi = rows_of(key0 + kKeys - 1).hi;
   const int j0 = lo / kStep, j1 = hi > lo ? cdiv(hi, kStep) : j0;
 
-  Frag kf[KC], vf[KC];
-  {
-    const T* const kp = static_cast<const T*>(g.k) + (long)(s.k0 + min(key, tail)) * a.k_row + (long)kvh * a.k_head + 8 * half;
-    const T* const vp = static_cast<const T*>(g.v) + (long)(s.k0 + min(key, tail)) * a.v_row + (long)kvh * a.v_head + 8 * half;
+  Frag kf[KC][2], vf[KC][2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int key = first + 16 * c + x;
+    const T* const kp = static_cast<const T*>(g.k) + (long)(s.k0 + min(key, tail)) * a.k_row + (long)kvh * a.k_head + 8 * quad;
+    const T* const vp = static_cast<const T*>(g.v) + (long)(s.k0 + min(key, tail)) * a.v_row + (long)kvh * a.v_head + 8 * quad;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const bool in = 16 * kc + 8 * half < a.dim;
-      kf[kc] = in ? Mma<T>::load(kp + 16 * kc) : Mma<T>::zero();
-      vf[kc] = in ? Mma<T>::load(vp + 16 * kc) : Mma<T>::zero();
+      const bool in = 32 * kc + 8 * quad < a.dim;
+      kf[kc][c] = in ? Mma<T>::load(kp + 32 * kc) : Mma<T>::zero();
+      vf[kc][c] = in ? Mma<T>::load(vp + 32 * kc) : Mma<T>::zero();
     }
   }
 
@@ -266,9 +278,9 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
     if (wave < 2) stats[slot][ks][wave][lane] = wave == 0 && v == -INFINITY ? -INFINITY : v * factor;      // a row without keys has no probabilities
   };
 
-  f32x16 dk[DB], dv[DB];
+  Acc dk[DB], dv[DB];
 #pragma unroll
-  for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x16{};
+  for (int d = 0; d < DB; ++d) dk[d] = dv[d] = Acc{};
   const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
   settle(kf);
   settle(vf);
@@ -278,67 +290,67 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
     fetch(0).all();
     keep(0, v);
   }
-  const Reach mine = rows_of(key);
+  const Reach mine[2] = {rows_of(first + x), rows_of(first + 16 + x)};
 
   // the wavefront's 32 of the rows in LDS, the first of them the sequence's r0, against its keys.  The loads of the next rows go out on the way
   auto step = [&](auto cut_, int slot, int r0, const PairLoad<T, DH>& next) {
     constexpr bool CUT = decltype(cut_)::value;
     constexpr int PIECES = PairLoad<T, DH>::kPieces;
-    const int n = rw;
     const char* const qs = smem + (slot * KS + ks) * 2 * SLOT;
     const char* const dos = qs + SLOT;
-    const float* const st = &stats[slot][ks][0][32 * n + 4 * half];
-    f32x16 p = f32x16{}, ds;
+    const float* const st = &stats[slot][ks][0][32 * rw + 4 * quad];
+    Acc p = Acc{}, ds;
+    f32x4 lse[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 u = *reinterpret_cast<const float4*>(st + 8 * i), w = *reinterpret_cast<const float4*>(st + kStep + 8 * i);
-      if (ES == 2) { p[4 * i] = u.x; p[4 * i + 1] = u.y; p[4 * i + 2] = u.z; p[4 * i + 3] = u.w; }
-      ds[4 * i] = w.x; ds[4 * i + 1] = w.y; ds[4 * i + 2] = w.z; ds[4 * i + 3] = w.w;
+    for (int i = 0; i < 2; ++i) {
+      lse[i] = *reinterpret_cast<const f32x4*>(st + 16 * i);
+      const f32x4 w = *reinterpret_cast<const f32x4*>(st + kStep + 16 * i);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (ES == 2) p.t[i][c] = lse[i];
+        ds.t[i][c] = w;
+      }
     }
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      p = Mma<T>::mma(L::row_frag(qs, rb, n, kc), kf[kc], p);
 #pragma unroll
-      for (int i = PIECES * kc / KC; i < PIECES * (kc + 1) / KC; ++i) next.piece(i);
+      for (int i = 0; i < 2; ++i) mma<T>(L::row_frag(qs, rb, 2 * rw + i, kc), kf[kc], p.t[i]);
+#pragma unroll
+      for (int n = PIECES * kc / KC; n < PIECES * (kc + 1) / KC; ++n) next.piece(n);
     }
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) ds = Mma<T>::mma(L::row_frag(dos, rb, n, kc), vf[kc], ds);
-    // (bf16: the products are summed on top of -lse / scale; in fp32 storage that would round them to its magnitude)
-    if constexpr (ES == 2) {
+    for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = exp2_(p[i] * g.c);
-    } else {
+      for (int i = 0; i < 2; ++i) mma<T>(L::row_frag(dos, rb, 2 * rw + i, kc), vf[kc], ds.t[i]);
+    Frag pf[2], sf[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 u = *reinterpret_cast<const float4*>(st + 8 * i);
-        p[4 * i] = exp2_(fmaf(p[4 * i], g.c, u.x));
-        p[4 * i + 1] = exp2_(fmaf(p[4 * i + 1], g.c, u.y));
-        p[4 * i + 2] = exp2_(fmaf(p[4 * i + 2], g.c, u.z));
-        p[4 * i + 3] = exp2_(fmaf(p[4 * i + 3], g.c, u.w));
+    for (int c = 0; c < 2; ++c) {
+      // (bf16: the products are summed on top of -lse / scale; in fp32 storage that would round them to its magnitude)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = p.t[e / 4][c][e % 4], u = ES == 2 ? exp2_(v * g.c) : exp2_(fmaf(v, g.c, lse[e / 4][e % 4]));
+        p.t[e / 4][c][e % 4] = u;
+        ds.t[e / 4][c][e % 4] *= u;
       }
-    }
+      if constexpr (CUT) {
+        const int from = mine[c].lo - r0 - 4 * quad, to = mine[c].hi - r0 - 4 * quad;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) ds[i] *= p[i];
-    if constexpr (CUT) {
-      const int from = mine.lo - r0 - 4 * half, to = mine.hi - r0 - 4 * half;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int at = 8 * (i / 4) + i % 4;
-        if (at < from || at >= to) p[i] = ds[i] = 0.f;
+        for (int e = 0; e < 8; ++e) {
+          const int at = 16 * (e / 4) + e % 4;
+          if (at < from || at >= to) p.t[e / 4][c][e % 4] = ds.t[e / 4][c][e % 4] = 0.f;
+        }
       }
+      pf[c] = Mma<T>::of(p.t[0][c], p.t[1][c]);
+      sf[c] = Mma<T>::of(ds.t[0][c], ds.t[1][c]);
     }
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      const Frag f = Mma<T>::of(p, kk);
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int d = 0; d < DB; ++d) dv[d] = Mma<T>::mma(L::col_frag(dos, cb, d, 2 * n + kk), f, dv[d]);
-    }
+      for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(dos, cb, 2 * d + i, rw), pf, dv[d].t[i]);
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      const Frag f = Mma<T>::of(ds, kk);
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int d = 0; d < DB; ++d) dk[d] = Mma<T>::mma(L::col_frag(qs, cb, d, 2 * n + kk), f, dk[d]);
-    }
+      for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(qs, cb, 2 * d + i, rw), sf, dk[d].t[i]);
   };
   // (KS = 2: the second set's last step may be behind the last row; its rows have no probabilities then, and its keys' sums are whole)
   int slot = 0, j = j0;
@@ -360,40 +372,36 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
 
   drain();
   // the other rows' sums: dk, then dv, through LDS
-  const bool real = key < s.lk;
-  T* const out[2] = {static_cast<T*>(g.dk) + (long)(s.k0 + key) * a.k_row + (long)kvh * a.k_head,
-                     static_cast<T*>(g.dv) + (long)(s.k0 + key) * a.v_row + (long)kvh * a.v_head};
-  float4* const shared = reinterpret_cast<float4*>(smem) + lane;
-  auto at_ = [&](int set, int d, int i) { return ((set * 2 + kw) * DB * 4 + d * 4 + i) * kWave; };      // set: of the 2 KS - 1 others
+  f32x4* const shared = reinterpret_cast<f32x4*>(smem) + lane;
+  auto place = [&](int set, int d, int i) { return ((set * 2 + kw) * DB * 4 + d * 4 + i) * kWave; };      // set: of the 2 KS - 1 others
+  const int set = ks * 2 + rw;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     wait_and_meet<0>();
-    const int set = ks * 2 + rw;
     if (set > 0)
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x16& v = t ? dv[d] : dk[d];
-          shared[at_(set - 1, d, i)] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        }
+        for (int i = 0; i < 4; ++i) shared[place(set - 1, d, i)] = (t ? dv[d] : dk[d]).t[i / 2][i % 2];
     wait_and_meet<0>();
     if (set == 0)
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
+      for (int c = 0; c < 2; ++c) {
+        const int key = first + 16 * c + x;
+        T* const out = t ? static_cast<T*>(g.dv) + (long)(s.k0 + key) * a.v_row + (long)kvh * a.v_head
+                         : static_cast<T*>(g.dk) + (long)(s.k0 + key) * a.k_row + (long)kvh * a.k_head;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x16& v = t ? dv[d] : dk[d];
-          float4 y = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int o = 0; o < 2 * KS - 1; ++o) {
-            const float4 u = shared[at_(o, d, i)];
-            y = make_float4(y.x + u.x, y.y + u.y, y.z + u.z, y.w + u.w);
+          for (int i = 0; i < 2; ++i) {
+            f32x4 y = (t ? dv[d] : dk[d]).t[i][c];
+#pragma unroll
+            for (int o = 0; o < 2 * KS - 1; ++o) y += shared[place(o, d, 2 * i + c)];
+            if (t == 0) y *= a.scale;
+            const int at = 32 * d + 16 * i + 4 * quad;
+            if (key < s.lk && at < a.dim) put4(out + at, y[0], y[1], y[2], y[3]);
           }
-          const float f = t ? 1.f : a.scale;
-          const int at = 32 * d + 8 * i + 4 * half;
-          if (real && at < a.dim) put4(out[t] + at, y.x * f, y.y * f, y.z * f, y.w * f);
-        }
+      }
   }
 }
 
