@@ -476,7 +476,8 @@ SPES_API int spes_qk_rope_fwd(const spes_qk_shape* shape, const void* q, const v
                               const void* k_weight, const float* table, const int32_t* pos, void* q_out,
                               void* k_out, void* stream);
 
-/* Its backward for the upstream gradients dq and dk of q_out and k_out.
+/* Its backward for the upstream gradients dq and dk of q_out and k_out.  A token whose position the table does not have gets gradients of NaN, and so do
+ * the weights.
  *
  *  dq        DEVICE [T, heads, head_dim]       dk  DEVICE [T, kv_heads, head_dim]
  *  q, k      as above (NULL is allowed without weights)
@@ -502,8 +503,9 @@ SPES_API int spes_qk_rope_bwd(const spes_qk_shape* shape, const void* dq, const 
  * infinity or a NaN in one can reach other rows of its sequence, whether they see it or not.
  * Products in bf16 storage take bf16 operands, the probabilities and their gradient among them, and are summed in fp32; in fp32 storage they are fp32.
  *
- *  Supported: head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, at most 1024; q_rows heads and k_rows at most 2^31 - 2^16; strides multiples of 16 bytes,
- *  rows at most 2^20 elements apart, heads / kv_heads heads of q within 2^28 elements
+ *  Supported: head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, at most 1024; q_rows heads at most 2^30, k_rows at most 2^31 - 2^16
+ *  (in the backward k_rows kv_heads at most 2^29), n_seq kv_heads at most 2^22; strides multiples of 16 bytes, rows at most 2^20 elements
+ *  apart, heads / kv_heads heads of q within 2^28 elements
  */
 typedef struct {
   int64_t q_row, q_head; /* elements from a token's q to the next one's, and from a head's to the next one's; of dq as well     */
@@ -534,7 +536,8 @@ SPES_API int spes_attn_fwd(const spes_attn_shape* shape, const void* q, const vo
  *
  *  d_o       DEVICE [q_rows, heads, head_dim]
  *  o, lse    as the forward left them; all other inputs as above
- *  dq        DEVICE out, laid out as q is;  dk, dv  DEVICE out, laid out as k and v are.  They are overwritten
+ *  dq        DEVICE out, laid out as q is;  dk, dv  DEVICE out, laid out as k and v are.  They are overwritten.  These layouts must not put two
+ *            elements into one place: rows lie beyond all heads of the one before, or heads beyond all rows
  *  scratch   DEVICE, spes_attn_scratch_bytes(shape, 1) bytes
  */
 SPES_API int spes_attn_bwd(const spes_attn_shape* shape, const void* d_o, const void* q, const void* k,

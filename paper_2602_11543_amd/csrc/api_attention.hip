@@ -13,6 +13,8 @@ constexpr int kMaxRopeDim = 256, kMaxHeadDim = 128, kMaxHeads = 1024;
 constexpr long kMaxRow = 1l << 20, kMaxGroup = 1l << 28;          // in elements: 32-bit byte offsets from a tile's first row
 
 constexpr long kMaxRows = (1l << 31) - (1l << 16);               // the number of a row a few tiles behind the last one still fits 32 bits
+// A launch has fewer than 2^32 threads: blocks of 256 for 128 rows of queries, or in the backward for 64 keys, and one more for each sequence
+constexpr long kMaxQueryRows = 1l << 30, kMaxKeyRows = 1l << 29, kMaxSeqs = 1l << 22;
 
 bool stride_ok(int64_t stride, int dtype) { return stride % (dtype == SPES_F32 ? 4 : 8) == 0; }
 
@@ -46,13 +48,20 @@ int attn_supported(const spes_attn_shape* p) {
     if (stride < p->head_dim) return SPES_EINVAL;
   if (p->q_row > kMaxRow || p->k_row > kMaxRow || p->v_row > kMaxRow) return SPES_ESHAPE;
   if (p->q_head > kMaxGroup / (p->heads / p->kv_heads)) return SPES_ESHAPE;
-  // rows of all heads, and blocks of a launch
-  if ((long)p->q_rows * p->heads > kMaxRows || p->k_rows > kMaxRows || ((long)p->q_rows * p->heads / 4 + (long)p->n_seq * p->kv_heads) * 32 >= 1l << 31 ||
-      ((long)p->k_rows / 128 + p->n_seq) * p->kv_heads >= 1l << 31)
-    return SPES_ESHAPE;
+  if ((long)p->q_rows * p->heads > kMaxQueryRows || p->k_rows > kMaxRows || (long)p->n_seq * p->kv_heads > kMaxSeqs) return SPES_ESHAPE;
   for (const int64_t stride : {p->q_row, p->q_head, p->k_row, p->k_head, p->v_row, p->v_head})
     if (!stride_ok(stride, p->dtype)) return SPES_EALIGN;
   return SPES_OK;
+}
+// The backward writes tensors that are laid out as q, k and v are: no two of their elements in one place
+bool apart(int64_t row, int64_t head, long rows, long heads, long dim) { return row >= (heads - 1) * head + dim || head >= (rows - 1) * row + dim; }
+int attn_bwd_supported(const spes_attn_shape* p) {
+  const int rc = attn_supported(p);
+  if (rc != SPES_OK) return rc;
+  if (!apart(p->q_row, p->q_head, p->q_rows, p->heads, p->head_dim) || !apart(p->k_row, p->k_head, p->k_rows, p->kv_heads, p->head_dim) ||
+      !apart(p->v_row, p->v_head, p->k_rows, p->kv_heads, p->head_dim))
+    return SPES_EINVAL;
+  return (long)p->k_rows * p->kv_heads > kMaxKeyRows ? SPES_ESHAPE : SPES_OK;
 }
 AttnShape shape_of(const spes_attn_shape& p, const int32_t* q_start, const int32_t* k_start, const int32_t* k_len) {
   return {q_start, k_start, k_len, p.q_row, p.q_head, p.k_row, p.k_head, p.v_row, p.v_head, p.n_seq, p.q_rows, p.k_rows, p.heads, p.kv_heads,
@@ -102,7 +111,7 @@ SPES_API int spes_qk_rope_bwd(const spes_qk_shape* shape, const void* dq, const 
 }
 
 SPES_API size_t spes_attn_scratch_bytes(const spes_attn_shape* shape, int32_t backward) {
-  if (attn_supported(shape) != SPES_OK) return 0;
+  if ((backward ? attn_bwd_supported(shape) : attn_supported(shape)) != SPES_OK) return 0;
   const AttnShape a = shape_of(*shape, nullptr, nullptr, nullptr);
   return backward ? attn_bwd_scratch_bytes(shape->dtype, a) : attn_fwd_scratch_bytes(shape->dtype, a);
 }
@@ -122,7 +131,7 @@ SPES_API int spes_attn_fwd(const spes_attn_shape* shape, const void* q, const vo
 SPES_API int spes_attn_bwd(const spes_attn_shape* shape, const void* d_o, const void* q, const void* k, const void* v, const int32_t* q_start,
                            const int32_t* k_start, const int32_t* k_len, const void* o, const float* lse, void* dq, void* dk, void* dv, void* scratch,
                            void* stream) {
-  const int rc = attn_supported(shape);
+  const int rc = attn_bwd_supported(shape);
   if (rc != SPES_OK) return rc;
   if (shape->n_seq == 0 || (shape->q_rows == 0 && shape->k_rows == 0)) return SPES_OK;
   if (!q_start || !k_start || !scratch || (shape->q_rows > 0 && (!d_o || !q || !o || !lse || !dq)) || (shape->k_rows > 0 && (!k || !v || !dk || !dv)))

@@ -72,19 +72,6 @@ __device__ __forceinline__ rsrc_t rsrc_for_lds(unsigned long base, unsigned byte
 }
 constexpr unsigned kOpen = 0x80000000u;      // bytes of a resource that is not to end: offsets are below 2^31
 
-// The order of a stretch of code with N matrix instructions, READS LDS reads and VALU other instructions to each: the first AHEAD
-// instructions' reads come first, the others' one instruction after another
-template <int N, int READS, int AHEAD, int VALU>
-__device__ __forceinline__ void interleave() {
-  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    if (i + AHEAD < N) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-    if (VALU) __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
-  }
-}
-
 // Heads of up to 32, 64, 96 or 128 elements are computed as that many, in rows of 64 or 128 in LDS
 constexpr int tile_dim(int dim) { return dim <= 64 ? 64 : 128; }
 

@@ -12,7 +12,6 @@
 namespace spes {
 namespace {
 
-
 constexpr int kMaxBlocks = 1024;         // of the backward: partial sums of queries or keys, one each
 
 struct Side {                            // queries or keys

@@ -138,3 +138,21 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     for args in ((x[:7], y), (x, y.float()), (x.transpose(0, 1).contiguous().transpose(0, 1), y), (x, y)):
         with pytest.raises(S.SpesError):
             S.spes_qk_rope_fwd(p, *args, None, None, None, None, None, None)
+
+
+def test_attention_limits_and_layouts_of_gradients():
+    """More rows, keys or sequences than a launch has blocks for; gradients of which two elements would have one place."""
+    fwd, bwd, need = LIB.spes_attn_fwd, LIB.spes_attn_bwd, LIB.spes_attn_scratch_bytes
+    need.restype, need.argtypes = sz, [vp, i32]
+    both = [dict(q_rows=2 ** 28 + 1), dict(n_seq=2 ** 21 + 1)]
+    backward = [(dict(k_rows=2 ** 28 + 1), ESHAPE), (dict(q_row=64, q_head=64), EINVAL), (dict(q_row=248), EINVAL), (dict(k_row=64), EINVAL),
+                (dict(k_head=128), EINVAL), (dict(v_row=120), EINVAL), (dict(v_row=64, v_head=64 * 95), EINVAL)]
+    for bad in both:
+        s = ctypes.byref(_attn(**bad))
+        assert need(s, 0) == 0 == need(s, 1) and fwd(s, *P[:9], None) == ESHAPE == bwd(s, *P[:13], None), bad
+    for bad, code in backward:
+        s = ctypes.byref(_attn(**bad))
+        assert need(s, 0) > 0 == need(s, 1) and bwd(s, *P[:13], None) == code, bad
+    for good in (dict(), dict(q_row=264), dict(q_head=72, q_row=3 * 72 + 64), dict(k_row=64, k_head=96 * 64), dict(v_row=256, v_head=64), dict(q_rows=1, q_row=64),
+                 dict(kv_heads=1, k_row=64, v_row=64)):
+        assert need(ctypes.byref(_attn(**good)), 1) > 0, good
