@@ -184,7 +184,9 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
 }
 
 // Four wavefronts: two groups of 32 keys, and in each one wavefront for the first 32 of the 64 rows that are in LDS and one for the others, whose sums are
-// joined at the end.  (Four groups, 64 rows each: half the loads into LDS, but the second 32 rows cost more registers than there are, 128
+// joined at the end.  The rows are gone over from the last one down: the blocks of a sequence's keys then begin at the same rows and find each other's in L2,
+// where from each block's first row on they are all over a sequence of which L2 holds half (8 x 4096 tokens, 32 / 8 heads of 128: 8 MB).
+// (Four groups, 64 rows each: half the loads into LDS, but the second 32 rows cost more registers than there are, 128
 // elements: 12.6 ms in place of 4.1 for all of the backward below; 64 elements: 97 us in place of 83.)
 constexpr int kKeys = 64;
 template <typename T, int DC, int KS>
@@ -249,22 +251,23 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
       off[1][i] = in ? q * (unsigned)(a.heads * a.dim * ES) + h * (unsigned)(a.dim * ES) + ch * 16 : kOutOfRange;
     }
   };
-  // the tile that is next: its first row is head `rem` of a query; both are carried on by additions, as in TileStream
+  // the tile that is next, from the last one down: its first row is head `rem` of a query; both are carried on by subtractions, as in TileStream by
+  // additions.  A set's last tile may be ahead of the first one: it is not there, and brings rows without probabilities.
   const int by = KS * kStep, by_query = by / G, by_rem = by - by_query * G;
   const long q_bytes = a.q_row * ES, d_bytes = (long)a.heads * a.dim * ES;
-  int row0 = (j0 + ks) * kStep, query0 = row0 / G, rem0 = row0 - query0 * G;
+  int row0 = (j1 - 1 - ks) * kStep, query0 = max(row0, 0) / G, rem0 = max(row0, 0) - query0 * G;
   unsigned long q_at = q_base + (unsigned long)(query0 * q_bytes), d_at = d_base + (unsigned long)(query0 * d_bytes);
   aim(rem0, n_rows - row0);
   auto fetch = [&](int slot) {
-    const bool there = row0 < min(n_rows, j1 * kStep);
-    if (by_rem != 0 || (there && row0 + kStep > n_rows)) aim(rem0, max(n_rows - row0, 1));
+    const bool there = row0 >= j0 * kStep;
+    if (there && (by_rem != 0 || row0 + by + kStep > n_rows)) aim(rem0, n_rows - row0);
     const PairLoad<T, DH> load(off, rsrc_for_lds(q_at, there ? kOpen : 0u), rsrc_for_lds(d_at, there ? kOpen : 0u), lds0 + (unsigned)((slot * KS + ks) * 2 * SLOT), wave);
-    const int more = rem0 + by_rem >= G, queries = by_query + more;
-    row0 += by;
-    query0 += queries;
-    rem0 += by_rem - more * G;
-    q_at += (unsigned long)(queries * q_bytes);
-    d_at += (unsigned long)(queries * d_bytes);
+    const int less = rem0 < by_rem, queries = by_query + less;
+    row0 -= by;
+    query0 -= queries;
+    rem0 += less * G - by_rem;
+    q_at -= (unsigned long)(queries * q_bytes);
+    d_at -= (unsigned long)(queries * d_bytes);
     return load;
   };
   // one row's number of that tile to a lane of the first two wavefronts, on its way while the step before is worked on
@@ -272,7 +275,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
   const float factor = wave == 1 ? -1.f : ES == 2 ? -1.f / a.scale : -kLog2e;
   auto number = [&]() {
     const unsigned n = (unsigned)(lane + rem0), q = n * magic >> 22, h = n - q * G;
-    return row0 + lane < n_rows ? numbers[(long)(kvh * G + (int)h) * a.q_rows + s.q0 + query0 + (int)q] : wave == 0 ? -INFINITY : 0.f;
+    return row0 >= j0 * kStep && row0 + lane < n_rows ? numbers[(long)(kvh * G + (int)h) * a.q_rows + s.q0 + query0 + (int)q] : wave == 0 ? -INFINITY : 0.f;
   };
   auto keep = [&](int slot, float v) {
     if (wave < 2) stats[slot][ks][wave][lane] = wave == 0 && v == -INFINITY ? -INFINITY : v * factor;      // a row without keys has no probabilities
@@ -352,23 +355,22 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
 #pragma unroll
       for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(qs, cb, 2 * d + i, rw), sf, dk[d].t[i]);
   };
-  // (KS = 2: the second set's last step may be behind the last row; its rows have no probabilities then, and its keys' sums are whole)
-  int slot = 0, j = j0;
+  int slot = 0, n = 0;           // n: tiles done, from the last one down
   auto run = [&](auto cut_, int to) {
-    for (; j < to; j += KS, slot ^= 1) {
+    for (; n < to; n += KS, slot ^= 1) {
       wait_and_meet<0>();
       float number_next = 0.f;
       if (wave < 2) number_next = number();
       const PairLoad<T, DH> next = fetch(slot ^ 1);
-      step(cut_, slot, (j + ks) * kStep + 32 * rw, next);
+      step(cut_, slot, (j1 - 1 - n - ks) * kStep + 32 * rw, next);
       keep(slot ^ 1, number_next);
     }
   };
   // rows that some key does not see only at either end
   const int all_from = cdiv(rows_of(key0 + kKeys - 1).lo, kStep), all_to = rows_of(key0).hi / kStep;
-  run(std::true_type{}, min(max(all_from, j0), j1));
-  run(std::false_type{}, min(max(all_to, j), j1) - (KS - 1));
-  run(std::true_type{}, j1);
+  run(std::true_type{}, min(j1 - all_to, j1 - j0));
+  run(std::false_type{}, min(j1 - all_from, j1 - j0) - (KS - 1));
+  run(std::true_type{}, j1 - j0);
 
   drain();
   // the other rows' sums: dk, then dv, through LDS
