@@ -314,17 +314,17 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
         ds.t[i][c] = w;
       }
     }
+    // operands from LDS in the order of their use, some of them on their way: sums and what is summed leave room for one in the first half, for three in the second
+    constexpr int HALF = 2 * KC;
+    auto row = [&](int t) { return L::row_frag(t < HALF ? qs : dos, rb, 2 * rw + t % 2, t % HALF / 2); };
+    Frag r[2] = {row(0), row(1)};
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) {
+    for (int t = 0; t < 2 * HALF; ++t) {
+      mma<T>(r[t % 2], (t < HALF ? kf : vf)[t % HALF / 2], (t < HALF ? p : ds).t[t % 2]);
+      if (t + 2 < 2 * HALF) r[t % 2] = row(t + 2);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) mma<T>(L::row_frag(qs, rb, 2 * rw + i, kc), kf[kc], p.t[i]);
-#pragma unroll
-      for (int n = PIECES * kc / KC; n < PIECES * (kc + 1) / KC; ++n) next.piece(n);
+      for (int n = PIECES * t / HALF; n < min(PIECES * (t + 1) / HALF, PIECES); ++n) next.piece(n);
     }
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) mma<T>(L::row_frag(dos, rb, 2 * rw + i, kc), vf[kc], ds.t[i]);
     Frag pf[2], sf[2];
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -346,14 +346,16 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
       pf[c] = Mma<T>::of(p.t[0][c], p.t[1][c]);
       sf[c] = Mma<T>::of(ds.t[0][c], ds.t[1][c]);
     }
+    constexpr int kAhead = 3;
+    auto column = [&](int t) { return L::col_frag(t < HALF ? dos : qs, cb, t % HALF, rw); };
+    Frag f[kAhead + 1];
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int t = 0; t < kAhead; ++t) f[t] = column(t);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(dos, cb, 2 * d + i, rw), pf, dv[d].t[i]);
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(qs, cb, 2 * d + i, rw), sf, dk[d].t[i]);
+    for (int t = 0; t < 2 * HALF; ++t) {
+      if (t + kAhead < 2 * HALF) f[(t + kAhead) % (kAhead + 1)] = column(t + kAhead);
+      mma<T>(f[t % (kAhead + 1)], t < HALF ? pf : sf, (t < HALF ? dv : dk)[t % HALF / 2].t[t % 2]);
+    }
   };
   int slot = 0, n = 0;           // n: tiles done, from the last one down
   auto run = [&](auto cut_, int to) {
