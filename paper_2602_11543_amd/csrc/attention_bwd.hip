@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
     const rsrc_t k = stream.next(0), v = stream.next(1);
     return PairLoad<T, DH>(off, k, v, lds0 + (unsigned)((slot * KS + ks) * 2 * SLOT), wave);
   };
-  constexpr int PIECES = PairLoad<T, DH>::kPieces;
+  constexpr int PIECES = PairLoad<T, DH>::kPieces, kAhead = 2;
 
   Acc acc[DB];
 #pragma unroll
@@ -120,16 +120,19 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int c = 0; c < 2; ++c) ds.t[i][c] = f32x4{-delta[c], -delta[c], -delta[c], -delta[c]};
+      // operands from LDS in the order of their use, two of them on their way
+      constexpr int ALL = 4 * KC;
+      auto line = [&](int t) { return L::row_frag(t % 2 ? vt : kt, rb, 2 * n + t / 2 % 2, t / 4); };
+      Frag r[kAhead + 1];
 #pragma unroll
-      for (int kc = 0; kc < KC; ++kc) {
+      for (int t = 0; t < kAhead; ++t) r[t] = line(t);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          mma<T>(L::row_frag(kt, rb, 2 * n + i, kc), qf[kc], sc.t[i]);
-          mma<T>(L::row_frag(vt, rb, 2 * n + i, kc), df[kc], ds.t[i]);
-        }
+      for (int t = 0; t < ALL; ++t) {
+        if (t + kAhead < ALL) r[(t + kAhead) % (kAhead + 1)] = line(t + kAhead);
+        mma<T>(r[t % (kAhead + 1)], (t % 2 ? df : qf)[t / 4], (t % 2 ? ds : sc).t[t / 2 % 2]);
         if (n == 0)
 #pragma unroll
-          for (int p = PIECES * kc / KC; p < PIECES * (kc + 1) / KC; ++p) next.piece(p);
+          for (int p = PIECES * t / ALL; p < PIECES * (t + 1) / ALL; ++p) next.piece(p);
       }
       Frag f[2];
 #pragma unroll
@@ -146,10 +149,14 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
         }
         f[c] = Mma<T>::of(ds.t[0][c], ds.t[1][c]);
       }
+      Frag k[kAhead + 1];
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
+      for (int d = 0; d < min(kAhead, 2 * DB); ++d) k[d] = L::col_frag(kt, cb, d, n);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(kt, cb, 2 * d + i, n), f, acc[d].t[i]);
+      for (int d = 0; d < 2 * DB; ++d) {
+        if (d + kAhead < 2 * DB) k[(d + kAhead) % (kAhead + 1)] = L::col_frag(kt, cb, d + kAhead, n);
+        mma<T>(k[d % (kAhead + 1)], f, acc[d / 2].t[d % 2]);
+      }
     }
   }
   drain();
