@@ -31,9 +31,10 @@ struct Acc { f32x4 t[2][2]; };       // 32 x 32: tile (i, j)
 template <typename T> struct Mma;
 template <> struct Mma<bf16_t> {
   typedef bf16x8 Frag;
-  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, const f32x4& c, bool = false) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ Frag zero() { return __builtin_bit_cast(Frag, make_uint4(0, 0, 0, 0)); }
   static __device__ __forceinline__ Frag load(const bf16_t* p) { return __builtin_bit_cast(Frag, *reinterpret_cast<const uint4*>(p)); }
+  static __device__ __forceinline__ Frag load_half(const bf16_t*) { return zero(); }       // (there are none)
   // a column's eight results, rounded to the operands' type
   static __device__ __forceinline__ Frag of(const f32x4& a, const f32x4& b) {
     return __builtin_bit_cast(Frag, make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])));
@@ -42,9 +43,10 @@ template <> struct Mma<bf16_t> {
 };
 template <> struct Mma<float> {
   typedef f32x8 Frag;
-  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c) {
+  static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c, bool half = false) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+    for (int j = 0; j < 8; ++j)
+      if (!half || j < 4) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
     return c;
   }
   static __device__ __forceinline__ Frag zero() { return Frag{}; }
@@ -52,14 +54,32 @@ template <> struct Mma<float> {
     const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
     return Frag{{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}};
   }
+  static __device__ __forceinline__ Frag load_half(const float* p) {
+    const float4 x = *reinterpret_cast<const float4*>(p);
+    return Frag{{x.x, x.y, x.z, x.w, 0.f, 0.f, 0.f, 0.f}};
+  }
   static __device__ __forceinline__ Frag of(const f32x4& a, const f32x4& b) { return Frag{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}}; }
   static __device__ __forceinline__ float get(const Frag& f, int j) { return f.v[j]; }
 };
 // row i of tiles: one fragment of the rows with both of the columns
 template <typename T>
-__device__ __forceinline__ void mma(const typename Mma<T>::Frag& a, const typename Mma<T>::Frag (&b)[2], f32x4 (&c)[2]) {
+__device__ __forceinline__ void mma(const typename Mma<T>::Frag& a, const typename Mma<T>::Frag (&b)[2], f32x4 (&c)[2], bool half = false) {
 #pragma unroll
-  for (int j = 0; j < 2; ++j) c[j] = Mma<T>::mma(a, b[j], c[j]);
+  for (int j = 0; j < 2; ++j) c[j] = Mma<T>::mma(a, b[j], c[j], half);
+}
+
+// A head is computed as DC elements: 32, 64, 96 or 128, and in fp32 also 48, 80 or 112, whose last fragment is a half: four elements of each quarter of the
+// lanes.  (fp32 products are what those kernels take their time for: heads of 80 in place of 96, 10 of them on 5 of keys, 2760 tokens, window of 700: 84 + 277 us
+// -> 74 + 236.)
+template <int DC> constexpr int kFrags = (DC + 31) / 32;
+template <int DC> constexpr bool last_half(int kc) { return DC % 32 != 0 && kc == kFrags<DC> - 1; }
+template <int DC> constexpr bool has_tile(int d, int i) { return 32 * d + 16 * i < DC; }       // of a head's columns, in Acc
+// fragment kc of the row at p
+template <typename T, int DC>
+__device__ __forceinline__ typename Mma<T>::Frag head_frag(const T* p, int kc, int quad, int dim, bool real) {
+  const bool half = last_half<DC>(kc);
+  const int at = 32 * kc + (half ? 4 : 8) * quad;
+  return !real || at >= dim ? Mma<T>::zero() : half ? Mma<T>::load_half(p + at) : Mma<T>::load(p + at);
 }
 
 __device__ __forceinline__ unsigned lds_address(void* p) { return uniform((unsigned)(unsigned long)(__attribute__((address_space(3))) char*)p); }
@@ -72,7 +92,7 @@ __device__ __forceinline__ rsrc_t rsrc_for_lds(unsigned long base, unsigned byte
 }
 constexpr unsigned kOpen = 0x80000000u;      // bytes of a resource that is not to end: offsets are below 2^31
 
-// Heads of up to 32, 64, 96 or 128 elements are computed as that many, in rows of 64 or 128 in LDS
+// in rows of 64 or 128 elements in LDS
 constexpr int tile_dim(int dim) { return dim <= 64 ? 64 : 128; }
 
 // Whether two sets of four wavefronts have room in LDS, and whether a launch of so many blocks is to have them: where there are at most `most`, and steps enough
@@ -93,17 +113,20 @@ struct Tile {
     const int far = (r >> 3) & 1;
     return DH == 64 ? (((r >> 1) & 3) ^ 2 * far) << 1 | far : ((r & 7) ^ 4 * far) << 1 | far;
   }
-  // fragments of rows: lane (x, quad) takes elements 32 kc + 8 quad .. + 7 of row 16 n + x
-  static __device__ __forceinline__ unsigned row_base(int lane) {
+  // fragments of rows: lane (x, quad) takes elements 32 kc + 8 quad .. + 7 of row 16 n + x, of half a fragment 32 kc + 4 quad .. + 3
+  struct Base { unsigned whole, half; };
+  static __device__ __forceinline__ Base row_base(int lane) {
     const int x = lane & 15, quad = lane >> 4;
-    return (unsigned)(x * kRowBytes + (((sizeof(T) == 4 ? 2 * quad : quad) ^ turn(x)) << 4));
+    auto at = [&](int chunk) { return (unsigned)(x * kRowBytes + ((chunk ^ turn(x)) << 4)); };
+    return Base{at(sizeof(T) == 4 ? 2 * quad : quad), at(quad)};
   }
-  static __device__ __forceinline__ typename Mma<T>::Frag row_frag(const char* slot, unsigned base, int n, int kc) {
+  static __device__ __forceinline__ typename Mma<T>::Frag row_frag(const char* slot, const Base& base, int n, int kc, bool half = false) {
     if constexpr (sizeof(T) == 2) {
-      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(slot + (base ^ (unsigned)(kc << 6)) + n * 16 * kRowBytes));
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(slot + (base.whole ^ (unsigned)(kc << 6)) + n * 16 * kRowBytes));
     } else {
-      const float4 p = *reinterpret_cast<const float4*>(slot + (base ^ (unsigned)((8 * kc) << 4)) + n * 16 * kRowBytes);
-      const float4 q = *reinterpret_cast<const float4*>(slot + (base ^ (unsigned)((8 * kc + 1) << 4)) + n * 16 * kRowBytes);
+      const float4 p = *reinterpret_cast<const float4*>(slot + ((half ? base.half : base.whole) ^ (unsigned)((8 * kc) << 4)) + n * 16 * kRowBytes);
+      if (half) return f32x8{{p.x, p.y, p.z, p.w, 0.f, 0.f, 0.f, 0.f}};
+      const float4 q = *reinterpret_cast<const float4*>(slot + (base.whole ^ (unsigned)((8 * kc + 1) << 4)) + n * 16 * kRowBytes);
       return f32x8{{p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w}};
     }
   }

@@ -30,18 +30,19 @@ __device__ __forceinline__ bool part_of(const FwdArgs& g, int part, int n, int& 
 }
 __device__ __forceinline__ int parts_used(const FwdArgs& g, int n) { return min(max(cdiv(n, g.per), 1), g.parts); }
 
-// A row's result: part of one, or the whole.  The row is the lane's column j of the DB x 32 elements in acc
-template <typename T, int DB>
-__device__ __forceinline__ void put_row(const FwdArgs& g, int part, long token, int head, int quad, const Acc (&acc)[DB], int j, float sum, float m) {
+// A row's result: part of one, or the whole.  The row is the lane's column j of the DC elements in acc
+template <typename T, int DC>
+__device__ __forceinline__ void put_row(const FwdArgs& g, int part, long token, int head, int quad, const Acc (&acc)[kFrags<DC>], int j, float sum, float m) {
   const AttnShape& a = g.a;
   const float inv = sum == 0.f ? 0.f : 1.f / sum, lse = (m + log2f(sum)) * kLn2;
   const bool whole = g.parts == 1;
   float* const po = g.part_o + (((long)part * a.q_rows + token) * a.heads + head) * a.dim;
   T* const op = static_cast<T*>(g.o) + (token * a.heads + head) * a.dim;
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+  for (int d = 0; d < kFrags<DC>; ++d)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      if (!has_tile<DC>(d, i)) continue;
       const int at = 32 * d + 16 * i + 4 * quad;
       const f32x4 v = acc[d].t[i][j] * inv;
       if (at < a.dim) {
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
   constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DC / 32, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  constexpr int ES = sizeof(T), KC = kFrags<DC>, DB = kFrags<DC>, SLOT = kStep * L::kRowBytes;
   __shared__ __align__(1024) char smem[4 * KS * SLOT];       // keys and values, two of each for each set
   __shared__ float2 stats[KS == 1 ? 1 : kRows];
   const AttnShape& a = g.a;
@@ -91,9 +92,9 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
   Frag qf[KC][2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const T* const qp = static_cast<const T*>(g.q) + (long)(s.q0 + row[j].query) * a.q_row + (long)row[j].head * a.q_head + 8 * quad;
+    const T* const qp = static_cast<const T*>(g.q) + (long)(s.q0 + row[j].query) * a.q_row + (long)row[j].head * a.q_head;
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) qf[kc][j] = row[j].real && 32 * kc + 8 * quad < a.dim ? Mma<T>::load(qp + 32 * kc) : Mma<T>::zero();
+    for (int kc = 0; kc < KC; ++kc) qf[kc][j] = head_frag<T, DC>(qp, kc, quad, a.dim, row[j].real);
   }
 
   // keys and values on their way into LDS
@@ -117,7 +118,8 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = Acc{};
   float m[2] = {-INFINITY, -INFINITY}, l[2][2] = {{0.f, 0.f}, {0.f, 0.f}};      // of the lane's rows, m in units of log2; l: this lane's share
-  const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
+  const typename L::Base rb = L::row_base(lane);
+  const unsigned cb = L::col_base(lane);
   settle(qf);
   if (j0 < j1) fetch(0).all();
   int slot = 0;
@@ -136,14 +138,14 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) kf[t][i] = L::row_frag(kt, rb, 2 * (t % 2) + i, t / 2);
+      for (int i = 0; i < 2; ++i) kf[t][i] = L::row_frag(kt, rb, 2 * (t % 2) + i, t / 2, last_half<DC>(t / 2));
 #pragma unroll
     for (int t = 0; t < NS; ++t) {
       if (t + 2 < NS)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) kf[(t + 2) % 3][i] = L::row_frag(kt, rb, 2 * ((t + 2) % 2) + i, (t + 2) / 2);
+        for (int i = 0; i < 2; ++i) kf[(t + 2) % 3][i] = L::row_frag(kt, rb, 2 * ((t + 2) % 2) + i, (t + 2) / 2, last_half<DC>((t + 2) / 2));
 #pragma unroll
-      for (int i = 0; i < 2; ++i) mma<T>(kf[t % 3][i], qf[t / 2], sc[t % 2].t[i]);
+      for (int i = 0; i < 2; ++i) mma<T>(kf[t % 3][i], qf[t / 2], sc[t % 2].t[i], last_half<DC>(t / 2));
 #pragma unroll
       for (int p = PIECES * t / NS; p < PIECES * (t + 1) / NS; ++p) next.piece(p);
     }
@@ -185,7 +187,8 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) acc[d].t[i][c] *= f;
+          for (int i = 0; i < 2; ++i)
+            if (has_tile<DC>(d, i)) acc[d].t[i][c] *= f;
       }
     }
 #pragma unroll
@@ -206,7 +209,8 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) mma<T>(L::col_frag(vt, cb, 2 * d + i, n), p, acc[d].t[i]);
+        for (int i = 0; i < 2; ++i)
+          if (has_tile<DC>(d, i)) mma<T>(L::col_frag(vt, cb, 2 * d + i, n), p, acc[d].t[i]);
     }
   }
 
@@ -242,7 +246,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
   }
 #pragma unroll
   for (int c = 0; c < 2; ++c)
-    if (row[c].real) put_row<T, DB>(g, part, s.q0 + row[c].query, row[c].head, quad, acc, c, sum[c], m[c]);
+    if (row[c].real) put_row<T, DC>(g, part, s.q0 + row[c].query, row[c].head, quad, acc, c, sum[c], m[c]);
 }
 
 // Few rows of a sequence (up to 32) against many keys: every wavefront goes over keys of its own, steps of 32, through LDS of its own, so nothing is waited
@@ -322,7 +326,7 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
   typedef Tile<T, DH> L;
   typedef Few<T, DH> W;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DC / 32, DB = DC / 32;
+  constexpr int ES = sizeof(T), KC = kFrags<DC>, DB = kFrags<DC>;
   __shared__ __align__(1024) char smem[W::kWaves * 4 * W::kSlot];
   __shared__ float2 stats[W::kWaves][kFewRows];
   const AttnShape& a = g.a;
@@ -330,7 +334,8 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
   const FewPlan plan(a, g.parts, lane);
   char* const mem = smem + wave * 4 * W::kSlot;
   const unsigned lds0 = lds_address(mem);
-  const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
+  const typename L::Base rb = L::row_base(lane);
+  const unsigned cb = L::col_base(lane);
   for (int item = blockIdx.x;; item += gridDim.x) {
   Seq s;
   int tile, part, j0, j1;
@@ -372,9 +377,9 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
   Frag qf[KC][2];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    const T* const qp = static_cast<const T*>(g.q) + (long)(s.q0 + row[c].query) * a.q_row + (long)row[c].head * a.q_head + 8 * quad;
+    const T* const qp = static_cast<const T*>(g.q) + (long)(s.q0 + row[c].query) * a.q_row + (long)row[c].head * a.q_head;
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) qf[kc][c] = row[c].real && 32 * kc + 8 * quad < a.dim ? Mma<T>::load(qp + 32 * kc) : Mma<T>::zero();
+    for (int kc = 0; kc < KC; ++kc) qf[kc][c] = head_frag<T, DC>(qp, kc, quad, a.dim, row[c].real);
   }
   load(j, 0);
   settle(qf);
@@ -397,9 +402,10 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
     for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const Frag f = L::row_frag(kt, rb, i, kc);
-        sc.t[i][0] = Mma<T>::mma(f, qf[kc][0], sc.t[i][0]);
-        if (both) sc.t[i][1] = Mma<T>::mma(f, qf[kc][1], sc.t[i][1]);
+        const bool half = last_half<DC>(kc);
+        const Frag f = L::row_frag(kt, rb, i, kc, half);
+        sc.t[i][0] = Mma<T>::mma(f, qf[kc][0], sc.t[i][0], half);
+        if (both) sc.t[i][1] = Mma<T>::mma(f, qf[kc][1], sc.t[i][1], half);
       }
     const bool cut = key0 < final.lo || key0 + kFewStep > first.hi;
     Frag p[2] = {Mma<T>::zero(), Mma<T>::zero()};
@@ -426,7 +432,8 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) acc[d].t[i][c] *= f;
+          for (int i = 0; i < 2; ++i)
+            if (has_tile<DC>(d, i)) acc[d].t[i][c] *= f;
       }
       const float low = m[c] == -INFINITY ? 0.f : m[c];
 #pragma unroll
@@ -441,6 +448,7 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        if (!has_tile<DC>(d, i)) continue;
         const Frag f = L::col_frag(vt, cb, 2 * d + i, 0);
         acc[d].t[i][0] = Mma<T>::mma(f, p[0], acc[d].t[i][0]);
         if (both) acc[d].t[i][1] = Mma<T>::mma(f, p[1], acc[d].t[i][1]);
@@ -617,6 +625,11 @@ int fwd(const FwdArgs& g, bool few, hipStream_t s) {
 template <typename T>
 int fwd(const FwdArgs& g, bool few, hipStream_t s) {
   const int dim = g.a.dim;
+  if constexpr (sizeof(T) == 4) {
+    if (dim > 32 && dim <= 48) return fwd<T, 48>(g, few, s);
+    if (dim > 64 && dim <= 80) return fwd<T, 80>(g, few, s);
+    if (dim > 96 && dim <= 112) return fwd<T, 112>(g, few, s);
+  }
   return dim <= 32 ? fwd<T, 32>(g, few, s) : dim <= 64 ? fwd<T, 64>(g, few, s) : dim <= 96 ? fwd<T, 96>(g, few, s) : fwd<T, 128>(g, few, s);
 }
 

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
   constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DC / 32, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  constexpr int ES = sizeof(T), KC = kFrags<DC>, DB = kFrags<DC>, SLOT = kStep * L::kRowBytes;
   __shared__ __align__(1024) char smem[4 * KS * SLOT];
   const AttnShape& a = g.a;
   const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 15, quad = lane >> 4;
@@ -51,17 +51,16 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
   float delta[2], base[2];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    const long token = s.q0 + row[c].query, at = (token * a.heads + row[c].head) * a.dim + 8 * quad;
-    const T* const qp = static_cast<const T*>(g.q) + token * a.q_row + (long)row[c].head * a.q_head + 8 * quad;
+    const long token = s.q0 + row[c].query, at = (token * a.heads + row[c].head) * a.dim;
+    const T* const qp = static_cast<const T*>(g.q) + token * a.q_row + (long)row[c].head * a.q_head;
     const T* const dp = static_cast<const T*>(g.d_o) + at;
     const T* const op = static_cast<const T*>(g.o) + at;
     Frag of[KC];
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const bool in = row[c].real && 32 * kc + 8 * quad < a.dim;
-      qf[kc][c] = in ? Mma<T>::load(qp + 32 * kc) : Mma<T>::zero();
-      df[kc][c] = in ? Mma<T>::load(dp + 32 * kc) : Mma<T>::zero();
-      of[kc] = in ? Mma<T>::load(op + 32 * kc) : Mma<T>::zero();
+      qf[kc][c] = head_frag<T, DC>(qp, kc, quad, a.dim, row[c].real);
+      df[kc][c] = head_frag<T, DC>(dp, kc, quad, a.dim, row[c].real);
+      of[kc] = head_frag<T, DC>(op, kc, quad, a.dim, row[c].real);
     }
     base[c] = g.lse[(long)row[c].head * a.q_rows + token] * kLog2e;
     delta[c] = 0.f;
@@ -92,7 +91,8 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
   Acc acc[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc[d] = Acc{};
-  const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
+  const typename L::Base rb = L::row_base(lane);
+  const unsigned cb = L::col_base(lane);
   settle(qf);
   settle(df);
 #pragma unroll
@@ -122,14 +122,14 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
         for (int c = 0; c < 2; ++c) ds.t[i][c] = f32x4{-delta[c], -delta[c], -delta[c], -delta[c]};
       // operands from LDS in the order of their use, two of them on their way
       constexpr int ALL = 4 * KC;
-      auto line = [&](int t) { return L::row_frag(t % 2 ? vt : kt, rb, 2 * n + t / 2 % 2, t / 4); };
+      auto line = [&](int t) { return L::row_frag(t % 2 ? vt : kt, rb, 2 * n + t / 2 % 2, t / 4, last_half<DC>(t / 4)); };
       Frag r[kAhead + 1];
 #pragma unroll
       for (int t = 0; t < kAhead; ++t) r[t] = line(t);
 #pragma unroll
       for (int t = 0; t < ALL; ++t) {
         if (t + kAhead < ALL) r[(t + kAhead) % (kAhead + 1)] = line(t + kAhead);
-        mma<T>(r[t % (kAhead + 1)], (t % 2 ? df : qf)[t / 4], (t % 2 ? ds : sc).t[t / 2 % 2]);
+        mma<T>(r[t % (kAhead + 1)], (t % 2 ? df : qf)[t / 4], (t % 2 ? ds : sc).t[t / 2 % 2], last_half<DC>(t / 4));
         if (n == 0)
 #pragma unroll
           for (int p = PIECES * t / ALL; p < PIECES * (t + 1) / ALL; ++p) next.piece(p);
@@ -151,10 +151,10 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
       }
       Frag k[kAhead + 1];
 #pragma unroll
-      for (int d = 0; d < min(kAhead, 2 * DB); ++d) k[d] = L::col_frag(kt, cb, d, n);
+      for (int d = 0; d < kAhead; ++d) k[d] = L::col_frag(kt, cb, d, n);
 #pragma unroll
-      for (int d = 0; d < 2 * DB; ++d) {
-        if (d + kAhead < 2 * DB) k[(d + kAhead) % (kAhead + 1)] = L::col_frag(kt, cb, d + kAhead, n);
+      for (int d = 0; d < DC / 16; ++d) {
+        if (d + kAhead < DC / 16) k[(d + kAhead) % (kAhead + 1)] = L::col_frag(kt, cb, d + kAhead, n);
         mma<T>(k[d % (kAhead + 1)], f, acc[d / 2].t[d % 2]);
       }
     }
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
   constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
-  constexpr int ES = sizeof(T), KC = DC / 32, DB = DC / 32, SLOT = kStep * L::kRowBytes;
+  constexpr int ES = sizeof(T), KC = kFrags<DC>, DB = kFrags<DC>, SLOT = kStep * L::kRowBytes;
   __shared__ __align__(1024) char smem[4 * KS * SLOT];
   __shared__ __align__(16) float stats[2][KS][2][kStep];         // of each slot's rows: -lse / scale (fp32: -lse log2 e), -delta
   const AttnShape& a = g.a;
@@ -230,13 +230,12 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     const int key = first + 16 * c + x;
-    const T* const kp = static_cast<const T*>(g.k) + (long)(s.k0 + min(key, tail)) * a.k_row + (long)kvh * a.k_head + 8 * quad;
-    const T* const vp = static_cast<const T*>(g.v) + (long)(s.k0 + min(key, tail)) * a.v_row + (long)kvh * a.v_head + 8 * quad;
+    const T* const kp = static_cast<const T*>(g.k) + (long)(s.k0 + min(key, tail)) * a.k_row + (long)kvh * a.k_head;
+    const T* const vp = static_cast<const T*>(g.v) + (long)(s.k0 + min(key, tail)) * a.v_row + (long)kvh * a.v_head;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const bool in = 32 * kc + 8 * quad < a.dim;
-      kf[kc][c] = in ? Mma<T>::load(kp + 32 * kc) : Mma<T>::zero();
-      vf[kc][c] = in ? Mma<T>::load(vp + 32 * kc) : Mma<T>::zero();
+      kf[kc][c] = head_frag<T, DC>(kp, kc, quad, a.dim, true);
+      vf[kc][c] = head_frag<T, DC>(vp, kc, quad, a.dim, true);
     }
   }
 
@@ -291,7 +290,8 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
   Acc dk[DB], dv[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) dk[d] = dv[d] = Acc{};
-  const unsigned rb = L::row_base(lane), cb = L::col_base(lane);
+  const typename L::Base rb = L::row_base(lane);
+  const unsigned cb = L::col_base(lane);
   settle(kf);
   settle(vf);
   if (j0 < j1) {
@@ -323,11 +323,11 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
     }
     // operands from LDS in the order of their use, some of them on their way: sums and what is summed leave room for one in the first half, for three in the second
     constexpr int HALF = 2 * KC;
-    auto row = [&](int t) { return L::row_frag(t < HALF ? qs : dos, rb, 2 * rw + t % 2, t % HALF / 2); };
+    auto row = [&](int t) { return L::row_frag(t < HALF ? qs : dos, rb, 2 * rw + t % 2, t % HALF / 2, last_half<DC>(t % HALF / 2)); };
     Frag r[2] = {row(0), row(1)};
 #pragma unroll
     for (int t = 0; t < 2 * HALF; ++t) {
-      mma<T>(r[t % 2], (t < HALF ? kf : vf)[t % HALF / 2], (t < HALF ? p : ds).t[t % 2]);
+      mma<T>(r[t % 2], (t < HALF ? kf : vf)[t % HALF / 2], (t < HALF ? p : ds).t[t % 2], last_half<DC>(t % HALF / 2));
       if (t + 2 < 2 * HALF) r[t % 2] = row(t + 2);
 #pragma unroll
       for (int n = PIECES * t / HALF; n < min(PIECES * (t + 1) / HALF, PIECES); ++n) next.piece(n);
@@ -353,15 +353,15 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
       pf[c] = Mma<T>::of(p.t[0][c], p.t[1][c]);
       sf[c] = Mma<T>::of(ds.t[0][c], ds.t[1][c]);
     }
-    constexpr int kAhead = 3;
-    auto column = [&](int t) { return L::col_frag(t < HALF ? dos : qs, cb, t % HALF, rw); };
+    constexpr int kAhead = 3, COLS = DC / 16;
+    auto column = [&](int t) { return L::col_frag(t < COLS ? dos : qs, cb, t % COLS, rw); };
     Frag f[kAhead + 1];
 #pragma unroll
     for (int t = 0; t < kAhead; ++t) f[t] = column(t);
 #pragma unroll
-    for (int t = 0; t < 2 * HALF; ++t) {
-      if (t + kAhead < 2 * HALF) f[(t + kAhead) % (kAhead + 1)] = column(t + kAhead);
-      mma<T>(f[t % (kAhead + 1)], t < HALF ? pf : sf, (t < HALF ? dv : dk)[t % HALF / 2].t[t % 2]);
+    for (int t = 0; t < 2 * COLS; ++t) {
+      if (t + kAhead < 2 * COLS) f[(t + kAhead) % (kAhead + 1)] = column(t + kAhead);
+      mma<T>(f[t % (kAhead + 1)], t < COLS ? pf : sf, (t < COLS ? dv : dk)[t % COLS / 2].t[t % COLS % 2]);
     }
   };
   int slot = 0, n = 0;           // n: tiles done, from the last one down
@@ -437,6 +437,11 @@ int bwd(const BwdArgs& g, hipStream_t s) {
 template <typename T>
 int bwd(const BwdArgs& g, hipStream_t s) {
   const int dim = g.a.dim;
+  if constexpr (sizeof(T) == 4) {
+    if (dim > 32 && dim <= 48) return bwd<T, 48>(g, s);
+    if (dim > 64 && dim <= 80) return bwd<T, 80>(g, s);
+    if (dim > 96 && dim <= 112) return bwd<T, 112>(g, s);
+  }
   return dim <= 32 ? bwd<T, 32>(g, s) : dim <= 64 ? bwd<T, 64>(g, s) : dim <= 96 ? bwd<T, 96>(g, s) : bwd<T, 128>(g, s);
 }
 

@@ -316,3 +316,10 @@ def test_many_blocks(dtype):
     """More than the chip holds at once, so one set of wavefronts to a block; sequences of unequal length."""
     lens = [1500, 3, 700, 64, 257, 1]
     Problem(lens, heads=32, kv=16, dim=64, dtype=dtype, seed=21).check()
+
+
+@pytest.mark.parametrize("dim", [16, 32, 48, 56, 80, 96, 104, 112, 120])
+@pytest.mark.parametrize("kw", [dict(lens=[150, 1, 70]), dict(lens=[90, 33], window=40, heads=3, kv=1, layout="packed"), dict(lens=[1, 2], keys=[700, 91], room=704, heads=6),
+                                dict(lens=[700], keys=[900], causal=False)])
+def test_widths_that_end_inside_a_fragment(dim, kw):
+    Problem(**{**dict(dim=dim, dtype=torch.float32, seed=dim), **kw}).check()
