@@ -8,9 +8,12 @@
 // runs over just these: as its order is free, a column's eight are the lane's operand fragment as they stand, and the other operand is read from
 // LDS in the same order.
 //
-// Why 16 x 16 x 32 and not 32 x 32 x 16: what bounds the large cases is power (32 heads of 128, 8 x 4096 tokens: the clock falls from 2.4 to 1.5 GHz), and the
-// smaller form moves half as many accumulators per multiply-add: backward of that 3.75 -> 3.65 ms, forward 1.13 -> 1.12; 2 x 2048 tokens, 12 heads of 64, forward
-// 33 -> 30 us.
+// Why 16 x 16 x 32 and not 32 x 32 x 16: what bounds the large cases is power (32 heads of 128, 8 x 4096 tokens, call after call: the clock falls from 2.4 to
+// 1.5 GHz), and the smaller form moves half as many accumulators per multiply-add: backward of that, when it was taken, 3.75 -> 3.65 ms, forward 1.13 -> 1.12;
+// 2 x 2048 tokens, 12 heads of 64, forward 33 -> 30 us.
+//
+// Operands in bf16 storage are bf16: probabilities and their gradient are rounded once, by at most 2^-9 of each, on their way into the products that sum them in
+// fp32.  dq and dk are then 2.5e-3 off (in norm), where rounding the exact ones to bf16 leaves 1.7e-3; nearly all of it is the one rounding of the gradient.
 #pragma once
 #include <algorithm>
 
@@ -95,11 +98,11 @@ constexpr unsigned kOpen = 0x80000000u;      // bytes of a resource that is not 
 // in rows of 64 or 128 elements in LDS
 constexpr int tile_dim(int dim) { return dim <= 64 ? 64 : 128; }
 
-// Whether two sets of four wavefronts have room in LDS, and whether a launch of so many blocks is to have them: where there are at most `most`, and steps enough
-// for both.  2 x 2048 tokens, 12 heads of 64: forward (384 blocks) 35 -> 33 us, gradients of queries (384) and keys (768) 82.5 -> 79 with two sets for the
-// first of them, 95 with two for both.
+// Whether two sets of four wavefronts have room in LDS, and whether a launch of so many blocks is to have them: where they leave half of the chip empty or
+// hold it for long steps one behind the other (512 blocks: two to a CU), and steps enough for both.  2 x 2048 tokens, 12 heads of 64: forward (384 blocks)
+// 42 -> 33 us, gradients of queries (384 blocks) and keys (768, which keep one set) 87 -> 79; with two sets for the 768 as well 95.
 template <typename T, int DC> constexpr bool kTwoSets = 2 * 4 * kStep * tile_dim(DC) * (int)sizeof(T) <= 144 * 1024;
-inline bool two_sets(long blocks, long most, long steps_rows, int n_seq) { return std::max<long>(blocks, n_seq) <= most && steps_rows >= 4l * kStep * n_seq; }
+inline bool two_sets(long blocks, long steps_rows, int n_seq) { return std::max<long>(blocks, n_seq) <= 512 && steps_rows >= 4l * kStep * n_seq; }
 
 // A tile in LDS: rows of DH elements, chunk c (16 bytes) of row r at position c ^ turn(r).  LDS has 64 banks of four bytes.  A read of 16 bytes a lane is
 // served sixteen lanes at a time, 0-3, 12-15, 20-27 and so on: eight rows at one chunk and the other eight at the next one.  The transposing reads take

@@ -21,7 +21,9 @@ struct BwdArgs {
   float c;
 };
 
-// 128 rows; KS sets of four wavefronts as in the forward
+// 128 rows; KS sets of four wavefronts as in the forward.  Queries and upstream gradients stay in registers, keys and values pass through LDS: each key tile is
+// read as rows for the scores and as columns for dq.  8 x 4096 tokens, 32 / 8 heads of 128, causal: 1.45 ms, 1.14 PFLOP/s of the 6 D operations a
+// pair, bound by power; 2 x 2048 tokens, 12 heads of 64: 39 us; fp32, 2760 tokens, 10 / 5 heads of 80, window of 700: 106.
 template <typename T, int DC, int KS>
 __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel(const BwdArgs g) {
   constexpr int DH = tile_dim(DC);
@@ -193,8 +195,9 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
 // Four wavefronts: two groups of 32 keys, and in each one wavefront for the first 32 of the 64 rows that are in LDS and one for the others, whose sums are
 // joined at the end.  The rows are gone over from the last one down: the blocks of a sequence's keys then begin at the same rows and find each other's in L2,
 // where from each block's first row on they are all over a sequence of which L2 holds half (8 x 4096 tokens, 32 / 8 heads of 128: 8 MB).
-// (Four groups, 64 rows each: half the loads into LDS, but the second 32 rows cost more registers than there are, 128
-// elements: 12.6 ms in place of 4.1 for all of the backward below; 64 elements: 97 us in place of 83.)
+// The same problems as above: 2.1 ms, 1.05 PFLOP/s of the 8 D operations a pair (a wavefront's sums, keys and values take 192 of its 256 registers, which
+// leaves little for operands ahead of their use); 43 us; 135.  (Four groups, 64 rows each: half the loads into LDS, but the second 32 rows cost
+// more registers than there are, with 128 elements all of the backward took 12.6 ms in place of 4.1 then; 64 elements: 97 us in place of 83.)
 constexpr int kKeys = 64;
 template <typename T, int DC, int KS>
 __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kernel(const BwdArgs g) {
@@ -422,10 +425,8 @@ int bwd(const BwdArgs& g, hipStream_t s) {
   const long rows = (long)a.q_rows * a.group, q_blocks = (rows / kRows + a.n_seq) * a.kv_heads, k_blocks = ((long)a.k_rows / kKeys + a.n_seq) * a.kv_heads;
   bool two_q = false, two_k = false;
   if constexpr (kTwoSets<T, DC>) {
-    two_q = two_sets(rows / kRows * a.kv_heads, 512, a.k_rows, a.n_seq);
-    // (beyond 64 elements a block of two sets takes the room of two blocks, so nothing is lost by them, and a long sequence's first keys, which all of its rows
-    // see, are done in half the steps: 16384 tokens in documents of 1 to 6011, 16 / 4 heads of 128, 1024 blocks: 990 -> 930 us; 4096 blocks 3.83 -> 4.13 ms)
-    two_k = two_sets((long)a.k_rows / kKeys * a.kv_heads, DC > 64 ? 1024 : 512, rows, a.n_seq);
+    two_q = two_sets(rows / kRows * a.kv_heads, a.k_rows, a.n_seq);
+    two_k = two_sets((long)a.k_rows / kKeys * a.kv_heads, rows, a.n_seq);
     if (two_q && a.q_rows > 0) attn_bwd_q_kernel<T, DC, 2><<<dim3((unsigned)q_blocks), dim3(512), 0, s>>>(g);
   }
   if (!two_q && a.q_rows > 0) attn_bwd_q_kernel<T, DC, 1><<<dim3((unsigned)q_blocks), dim3(256), 0, s>>>(g);
