@@ -422,24 +422,22 @@ def qk_shape(T, heads, kv_heads, head_dim, rot_dim, dtype, interleaved=0, n_pos=
 
 
 def _qk(shape, q, k):
-    """The shape with the strides of q and k, and their pointers."""
-    t = torch_dtype(shape.dtype)
-    qp, q_row, q_head = _heads(q, shape.T, shape.heads, shape.head_dim, t)
-    kp, k_row, k_head = _heads(k, shape.T, shape.kv_heads, shape.head_dim, t)
-    if q_head != shape.head_dim or k_head != shape.head_dim:
+    """The shape with the strides of q and k, their pointers, and what sizes the other tensors: type, tokens, heads, kv_heads, head_dim."""
+    T, H, K, D, t = shape.T, shape.heads, shape.kv_heads, shape.head_dim, torch_dtype(shape.dtype)
+    qp, q_row, q_head = _heads(q, T, H, D, t)
+    kp, k_row, k_head = _heads(k, T, K, D, t)
+    if q_head != D or k_head != D:
         raise SpesError("a token's heads must stand side by side")
     own = spes_qk_shape.from_buffer_copy(shape)
     own.q_row, own.k_row = q_row, k_row
-    return own, qp, kp
+    return own, qp, kp, (t, T, H, K, D)
 
 
 def spes_qk_rope_fwd(shape, q, k, q_weight, k_weight, table, pos, q_out, k_out, stream=None) -> None:
     """q and k may be views of the projection's output; their strides go into the call."""
-    t, D, f = torch_dtype(shape.dtype), shape.head_dim, torch.float32
-    own, qp, kp = _qk(shape, q, k)
-    _check(_lib.spes_qk_rope_fwd(own, qp, kp, _buf(q_weight, t, D), _buf(k_weight, t, D), _buf(table, f, shape.n_pos, shape.rot_dim),
-                                 _buf(pos, torch.int32, shape.T), _buf(q_out, t, shape.T, shape.heads, D), _buf(k_out, t, shape.T, shape.kv_heads, D),
-                                 _stream(stream)), "spes_qk_rope_fwd")
+    own, qp, kp, (t, T, H, K, D) = _qk(shape, q, k)
+    _check(_lib.spes_qk_rope_fwd(own, qp, kp, _buf(q_weight, t, D), _buf(k_weight, t, D), _buf(table, torch.float32, own.n_pos, own.rot_dim),
+                                 _buf(pos, torch.int32, T), _buf(q_out, t, T, H, D), _buf(k_out, t, T, K, D), _stream(stream)), "spes_qk_rope_fwd")
 
 
 def spes_qk_rope_scratch_bytes(shape) -> int:
@@ -449,14 +447,13 @@ def spes_qk_rope_scratch_bytes(shape) -> int:
 def spes_qk_rope_bwd(shape, dq, dk, q, k, q_weight, k_weight, table, pos, dq_in, dk_in, d_q_weight, d_k_weight, accumulate=0, scratch=None,
                      stream=None) -> None:
     """dq_in and dk_in may be views of the gradient of the projection's output, with the strides of q and k."""
-    t, D, f = torch_dtype(shape.dtype), shape.head_dim, torch.float32
-    own, op, okp = _qk(shape, dq_in, dk_in)
-    qp = _like(q, (own.q_row, D), shape.T, shape.heads, D, t)
-    kp = _like(k, (own.k_row, D), shape.T, shape.kv_heads, D, t)
-    _check(_lib.spes_qk_rope_bwd(own, _buf(dq, t, shape.T, shape.heads, D), _buf(dk, t, shape.T, shape.kv_heads, D), qp, kp, _buf(q_weight, t, D),
-                                 _buf(k_weight, t, D), _buf(table, f, shape.n_pos, shape.rot_dim), _buf(pos, torch.int32, shape.T), op, okp,
-                                 _buf(d_q_weight, f, D), _buf(d_k_weight, f, D), int(accumulate), _scratch(scratch, _lib.spes_qk_rope_scratch_bytes, shape),
-                                 _stream(stream)), "spes_qk_rope_bwd")
+    own, op, okp, (t, T, H, K, D) = _qk(shape, dq_in, dk_in)
+    f = torch.float32
+    qp = _like(q, (own.q_row, D), T, H, D, t)
+    kp = _like(k, (own.k_row, D), T, K, D, t)
+    _check(_lib.spes_qk_rope_bwd(own, _buf(dq, t, T, H, D), _buf(dk, t, T, K, D), qp, kp, _buf(q_weight, t, D), _buf(k_weight, t, D),
+                                 _buf(table, f, own.n_pos, own.rot_dim), _buf(pos, torch.int32, T), op, okp, _buf(d_q_weight, f, D), _buf(d_k_weight, f, D),
+                                 int(accumulate), _scratch(scratch, _lib.spes_qk_rope_scratch_bytes, shape), _stream(stream)), "spes_qk_rope_bwd")
 
 
 def attn_shape(n_seq, q_rows, k_rows, heads, kv_heads, head_dim, dtype, causal=1, window=0, scale=None) -> spes_attn_shape:
@@ -470,33 +467,30 @@ def spes_attn_scratch_bytes(shape, backward=0) -> int:
 
 
 def _attn(shape, q, k, v, q_start, k_start, k_len):
-    """The shape with the strides of q, k and v, and the pointers of these and of the descriptors."""
-    t, i, n, D = torch_dtype(shape.dtype), torch.int32, shape.n_seq, shape.head_dim
+    """The shape with the strides of q, k and v, the pointers of these and of the descriptors, and what sizes the other tensors: type, rows, heads, head_dim."""
+    t, i, n, rows, keys, H, K, D = torch_dtype(shape.dtype), torch.int32, shape.n_seq, shape.q_rows, shape.k_rows, shape.heads, shape.kv_heads, shape.head_dim
     own = spes_attn_shape.from_buffer_copy(shape)
-    qp, own.q_row, own.q_head = _heads(q, shape.q_rows, shape.heads, D, t)
-    kp, own.k_row, own.k_head = _heads(k, shape.k_rows, shape.kv_heads, D, t)
-    vp, own.v_row, own.v_head = _heads(v, shape.k_rows, shape.kv_heads, D, t)
-    return own, qp, kp, vp, _buf(q_start, i, n + 1), _buf(k_start, i, n + (k_len is None)), _buf(k_len, i, n)
+    qp, own.q_row, own.q_head = _heads(q, rows, H, D, t)
+    kp, own.k_row, own.k_head = _heads(k, keys, K, D, t)
+    vp, own.v_row, own.v_head = _heads(v, keys, K, D, t)
+    return (own, qp, kp, vp, _buf(q_start, i, n + 1), _buf(k_start, i, n + (k_len is None)), _buf(k_len, i, n)), (t, rows, H, D)
 
 
 def spes_attn_fwd(shape, q, k, v, q_start, k_start, k_len, o, lse, scratch, stream=None) -> None:
     """q, k and v may be views; their strides go into the call."""
-    t, D = torch_dtype(shape.dtype), shape.head_dim
-    own, *inputs = _attn(shape, q, k, v, q_start, k_start, k_len)
-    _check(_lib.spes_attn_fwd(own, *inputs, _buf(o, t, shape.q_rows, shape.heads, D), _buf(lse, torch.float32, shape.heads, shape.q_rows),
-                              _scratch(scratch, _lib.spes_attn_scratch_bytes, shape, 0), _stream(stream)), "spes_attn_fwd")
+    inputs, (t, rows, H, D) = _attn(shape, q, k, v, q_start, k_start, k_len)
+    _check(_lib.spes_attn_fwd(*inputs, _buf(o, t, rows, H, D), _buf(lse, torch.float32, H, rows), _scratch(scratch, _lib.spes_attn_scratch_bytes, shape, 0),
+                              _stream(stream)), "spes_attn_fwd")
 
 
 def spes_attn_bwd(shape, d_o, q, k, v, q_start, k_start, k_len, o, lse, dq, dk, dv, scratch, stream=None) -> None:
     """q, k and v may be views; dq, dk and dv are laid out as they are."""
-    t, D = torch_dtype(shape.dtype), shape.head_dim
-    own, *inputs = _attn(shape, q, k, v, q_start, k_start, k_len)
-    _check(_lib.spes_attn_bwd(own, _buf(d_o, t, shape.q_rows, shape.heads, D), *inputs, _buf(o, t, shape.q_rows, shape.heads, D),
-                              _buf(lse, torch.float32, shape.heads, shape.q_rows),
-                              _like(dq, (own.q_row, own.q_head), shape.q_rows, shape.heads, D, t),
-                              _like(dk, (own.k_row, own.k_head), shape.k_rows, shape.kv_heads, D, t),
-                              _like(dv, (own.v_row, own.v_head), shape.k_rows, shape.kv_heads, D, t),
-                              _scratch(scratch, _lib.spes_attn_scratch_bytes, shape, 1), _stream(stream)), "spes_attn_bwd")
+    (own, *inputs), (t, rows, H, D) = _attn(shape, q, k, v, q_start, k_start, k_len)
+    keys, K = own.k_rows, own.kv_heads
+    _check(_lib.spes_attn_bwd(own, _buf(d_o, t, rows, H, D), *inputs, _buf(o, t, rows, H, D), _buf(lse, torch.float32, H, rows),
+                              _like(dq, (own.q_row, own.q_head), rows, H, D, t), _like(dk, (own.k_row, own.k_head), keys, K, D, t),
+                              _like(dv, (own.v_row, own.v_head), keys, K, D, t), _scratch(scratch, _lib.spes_attn_scratch_bytes, shape, 1), _stream(stream)),
+           "spes_attn_bwd")
 
 
 def spes_profile_enable(on: bool) -> None:
