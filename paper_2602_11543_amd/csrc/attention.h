@@ -30,13 +30,16 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 struct f32x8 { float v[8]; };
 struct Acc { f32x4 t[2][2]; };       // 32 x 32: tile (i, j)
 
+// Sixteen bytes of device memory; the address space is said, since a flat load would be waited for as a read of LDS as well
+__device__ __forceinline__ f32x4 load_global(const void* p) { return *(const __attribute__((address_space(1))) f32x4*)p; }
+
 // A fragment is 32 of the contraction for one row or column of sixteen: eight elements of each quarter of the lanes
 template <typename T> struct Mma;
 template <> struct Mma<bf16_t> {
   typedef bf16x8 Frag;
   static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, const f32x4& c, bool = false) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ Frag zero() { return __builtin_bit_cast(Frag, make_uint4(0, 0, 0, 0)); }
-  static __device__ __forceinline__ Frag load(const bf16_t* p) { return __builtin_bit_cast(Frag, *reinterpret_cast<const uint4*>(p)); }
+  static __device__ __forceinline__ Frag load(const bf16_t* p) { return __builtin_bit_cast(Frag, load_global(p)); }
   static __device__ __forceinline__ Frag load_half(const bf16_t*) { return zero(); }       // (there are none)
   // a column's eight results, rounded to the operands' type
   static __device__ __forceinline__ Frag of(const f32x4& a, const f32x4& b) {
@@ -54,12 +57,12 @@ template <> struct Mma<float> {
   }
   static __device__ __forceinline__ Frag zero() { return Frag{}; }
   static __device__ __forceinline__ Frag load(const float* p) {
-    const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
-    return Frag{{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}};
+    const f32x4 x = load_global(p), y = load_global(p + 4);
+    return Frag{{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}};
   }
   static __device__ __forceinline__ Frag load_half(const float* p) {
-    const float4 x = *reinterpret_cast<const float4*>(p);
-    return Frag{{x.x, x.y, x.z, x.w, 0.f, 0.f, 0.f, 0.f}};
+    const f32x4 x = load_global(p);
+    return Frag{{x[0], x[1], x[2], x[3], 0.f, 0.f, 0.f, 0.f}};
   }
   static __device__ __forceinline__ Frag of(const f32x4& a, const f32x4& b) { return Frag{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}}; }
   static __device__ __forceinline__ float get(const Frag& f, int j) { return f.v[j]; }

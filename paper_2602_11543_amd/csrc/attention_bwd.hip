@@ -19,24 +19,36 @@ struct BwdArgs {
   void *dq, *dk, *dv;
   float* delta;         // [heads, q_rows]
   float c;
+  int q_tiles, k_tiles; // of rows and keys, each for all heads that share keys, at most
 };
+
+// delta = sum do o of a lane's row c, whose upstream gradient is in d
+template <typename T, int DC>
+__device__ __forceinline__ float delta_of(const typename Mma<T>::Frag (&d)[kFrags<DC>][2], int c, const T* o, int quad, int dim, bool real) {
+  float sum = 0.f;
+#pragma unroll
+  for (int kc = 0; kc < kFrags<DC>; ++kc) {
+    const typename Mma<T>::Frag of = head_frag<T, DC>(o, kc, quad, dim, real);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(Mma<T>::get(d[kc][c], e), Mma<T>::get(of, e), sum);
+  }
+  return quad_sum(sum);
+}
 
 // 128 rows; KS sets of four wavefronts as in the forward.  Queries and upstream gradients stay in registers, keys and values pass through LDS: each key tile is
 // read as rows for the scores and as columns for dq.  8 x 4096 tokens, 32 / 8 heads of 128, causal: 1.45 ms, 1.14 PFLOP/s of the 6 D operations a
 // pair, bound by power; 2 x 2048 tokens, 12 heads of 64: 39 us; fp32, 2760 tokens, 10 / 5 heads of 80, window of 700: 106.
-template <typename T, int DC, int KS>
-__global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel(const BwdArgs g) {
+template <typename T, int DC, int KS, bool KEEP>
+__device__ __forceinline__ void bwd_q(const BwdArgs& g, int item, int kvh, char* smem) {
   constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
   constexpr int ES = sizeof(T), KC = kFrags<DC>, DB = kFrags<DC>, SLOT = kStep * L::kRowBytes;
-  __shared__ __align__(1024) char smem[4 * KS * SLOT];
   const AttnShape& a = g.a;
   const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 15, quad = lane >> 4;
-  const int kvh = blockIdx.x % a.kv_heads;
   Seq s;
   int tile, tiles;
-  if (!find_tile<false>(a, blockIdx.x / a.kv_heads, kRows, lane, s, tile, tiles)) return;
+  if (!find_tile<false>(a, item, kRows, lane, s, tile, tiles)) return;
   tile = tiles - 1 - tile;                                   // the longest first
 
   const int G = a.group, n_rows = s.lq * G, r0 = tile * kRows, w_row = r0 + wave * 32;
@@ -57,21 +69,14 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
     const T* const qp = static_cast<const T*>(g.q) + token * a.q_row + (long)row[c].head * a.q_head;
     const T* const dp = static_cast<const T*>(g.d_o) + at;
     const T* const op = static_cast<const T*>(g.o) + at;
-    Frag of[KC];
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
       qf[kc][c] = head_frag<T, DC>(qp, kc, quad, a.dim, row[c].real);
       df[kc][c] = head_frag<T, DC>(dp, kc, quad, a.dim, row[c].real);
-      of[kc] = head_frag<T, DC>(op, kc, quad, a.dim, row[c].real);
     }
     base[c] = g.lse[(long)row[c].head * a.q_rows + token] * kLog2e;
-    delta[c] = 0.f;
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) delta[c] = fmaf(Mma<T>::get(df[kc][c], e), Mma<T>::get(of[kc], e), delta[c]);
-    delta[c] = quad_sum(delta[c]);
-    if (row[c].real && quad == 0 && ks == 0) g.delta[(long)row[c].head * a.q_rows + token] = delta[c];
+    delta[c] = delta_of<T, DC>(df, c, op, quad, a.dim, row[c].real);
+    if (KEEP && row[c].real && quad == 0 && ks == 0) g.delta[(long)row[c].head * a.q_rows + token] = delta[c];
   }
 
   const long stride[2] = {a.k_row * ES, a.v_row * ES};
@@ -199,21 +204,19 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_k
 // leaves little for operands ahead of their use); 43 us; 135.  (Four groups, 64 rows each: half the loads into LDS, but the second 32 rows cost
 // more registers than there are, with 128 elements all of the backward took 12.6 ms in place of 4.1 then; 64 elements: 97 us in place of 83.)
 constexpr int kKeys = 64;
+template <int KS> struct Stats { float of[2][KS][2][kStep]; };       // of each slot's rows: -lse / scale (fp32: -lse log2 e), -delta
 template <typename T, int DC, int KS>
-__global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kernel(const BwdArgs g) {
+__device__ __forceinline__ void bwd_kv(const BwdArgs& g, int item, int kvh, char* smem, Stats<KS>& stats) {
   constexpr int DH = tile_dim(DC);
   typedef Tile<T, DH> L;
   typedef typename Mma<T>::Frag Frag;
   constexpr int ES = sizeof(T), KC = kFrags<DC>, DB = kFrags<DC>, SLOT = kStep * L::kRowBytes;
-  __shared__ __align__(1024) char smem[4 * KS * SLOT];
-  __shared__ __align__(16) float stats[2][KS][2][kStep];         // of each slot's rows: -lse / scale (fp32: -lse log2 e), -delta
   const AttnShape& a = g.a;
   const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6) & 3, ks = (int)uniform(threadIdx.x >> 8), x = lane & 15, quad = lane >> 4;
   const int kw = wave % 2, rw = wave / 2;
-  const int kvh = blockIdx.x % a.kv_heads;
   Seq s;
   int tile, tiles;
-  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, kKeys, lane, s, tile, tiles)) return;
+  if (!find_tile<true>(a, item, kKeys, lane, s, tile, tiles)) return;
 
   const int G = a.group, n_rows = s.lq * G, key0 = tile * kKeys, first = key0 + kw * 32, tail = s.lk - 1;
   // Rows [from, to) see a key: with causal masks r / G + lk - lq >= key, hence r >= (key - (lk - lq)) G, and likewise for the window
@@ -287,7 +290,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
     return row0 >= j0 * kStep && row0 + lane < n_rows ? numbers[(long)(kvh * G + (int)h) * a.q_rows + s.q0 + query0 + (int)q] : wave == 0 ? -INFINITY : 0.f;
   };
   auto keep = [&](int slot, float v) {
-    if (wave < 2) stats[slot][ks][wave][lane] = wave == 0 && v == -INFINITY ? -INFINITY : v * factor;      // a row without keys has no probabilities
+    if (wave < 2) stats.of[slot][ks][wave][lane] = wave == 0 && v == -INFINITY ? -INFINITY : v * factor;      // a row without keys has no probabilities
   };
 
   Acc dk[DB], dv[DB];
@@ -311,7 +314,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
     constexpr int PIECES = PairLoad<T, DH>::kPieces;
     const char* const qs = smem + (slot * KS + ks) * 2 * SLOT;
     const char* const dos = qs + SLOT;
-    const float* const st = &stats[slot][ks][0][32 * rw + 4 * quad];
+    const float* const st = &stats.of[slot][ks][0][32 * rw + 4 * quad];
     Acc p = Acc{}, ds;
     f32x4 lse[2];
 #pragma unroll
@@ -419,20 +422,84 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
   }
 }
 
+template <typename T, int DC, int KS> constexpr int kLds = 4 * KS * kStep * Tile<T, tile_dim(DC)>::kRowBytes;
+template <typename T, int DC, int KS>
+__global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_q_kernel(const BwdArgs g) {
+  __shared__ __align__(1024) char smem[kLds<T, DC, KS>];
+  bwd_q<T, DC, KS, true>(g, blockIdx.x / g.a.kv_heads, blockIdx.x % g.a.kv_heads, smem);
+}
+template <typename T, int DC, int KS>
+__global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_kernel(const BwdArgs g) {
+  __shared__ __align__(1024) char smem[kLds<T, DC, KS>];
+  __shared__ __align__(16) Stats<KS> stats;
+  bwd_kv<T, DC, KS>(g, blockIdx.x / g.a.kv_heads, blockIdx.x % g.a.kv_heads, smem, stats);
+}
+
+// Both in one launch, behind one that forms delta: where each by itself leaves CUs empty towards its end, or all along.  Tiles of rows and of keys are dealt out
+// evenly, the longest of a sequence first.
 template <typename T, int DC>
-int bwd(const BwdArgs& g, hipStream_t s) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_both_kernel(const BwdArgs g) {
+  __shared__ __align__(1024) char smem[kLds<T, DC, 1>];
+  __shared__ __align__(16) Stats<1> stats;
+  const int item = blockIdx.x / g.a.kv_heads, kvh = blockIdx.x % g.a.kv_heads;
+  const long all = (long)g.q_tiles + g.k_tiles;
+  const int keys = (int)(item * (long)g.k_tiles / all), more = (int)((item + 1) * (long)g.k_tiles / all);      // key tiles ahead of this one, and with it
+  if (more > keys) bwd_kv<T, DC, 1>(g, keys, kvh, smem, stats);
+  else bwd_q<T, DC, 1, false>(g, item - keys, kvh, smem);
+}
+// (the same sums in the same order as in bwd_q)
+template <typename T, int DC>
+__global__ __launch_bounds__(256) void attn_bwd_delta_kernel(const BwdArgs g) {
   const AttnShape& a = g.a;
-  const long rows = (long)a.q_rows * a.group, q_blocks = (rows / kRows + a.n_seq) * a.kv_heads, k_blocks = ((long)a.k_rows / kKeys + a.n_seq) * a.kv_heads;
+  const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), x = lane & 15, quad = lane >> 4, kvh = blockIdx.x % a.kv_heads;
+  Seq s;
+  int tile, tiles;
+  if (!find_tile<false>(a, blockIdx.x / a.kv_heads, kRows, lane, s, tile, tiles)) return;
+  typename Mma<T>::Frag df[kFrags<DC>][2];
+  float delta[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const Row row(tile * kRows + wave * 32 + 16 * c + x, s.lq * a.group, a.group, kvh);
+    const long token = s.q0 + row.query, at = (token * a.heads + row.head) * a.dim;
+#pragma unroll
+    for (int kc = 0; kc < kFrags<DC>; ++kc) df[kc][c] = head_frag<T, DC>(static_cast<const T*>(g.d_o) + at, kc, quad, a.dim, row.real);
+    delta[c] = delta_of<T, DC>(df, c, static_cast<const T*>(g.o) + at, quad, a.dim, row.real);
+    if (row.real && quad == 0) g.delta[(long)row.head * a.q_rows + token] = delta[c];
+  }
+}
+
+// How many blocks, of both kernels, are launched as one; all of the backward, one after the other -> together.  fp32 always (what a launch can have): one block
+// to a CU whatever its kernel, 1001, 1500 and 259 tokens, 10 / 5 heads of 80, window of 700 237 -> 227 us; 2 x 1000, 12 heads of 64 185 -> 143; 16 x 2000, 16 / 4
+// of 80 5.82 -> 5.52 ms.  Long heads in bf16 up to eight times what the chip holds: 1 x 1000, 16 / 4 heads of 128 99 -> 87 us; 16 documents of 1 to 6011
+// tokens (3200 blocks) 811 -> 771, in another order 910 -> 800; 64 of up to 512 (3584) 208 -> 215; 8 x 4096, 32 / 8 heads (12400) 3.39 -> 3.50 ms.  Short ones,
+// whose queries' kernel alone has three wavefronts to a SIMD, up to what the chip holds: 2 x 150, 12 heads of 64 (120 blocks) 18 -> 15 us; 8 x 200 (636) 22.5 ->
+// 23.3; 32 of up to 1024 158 -> 175.
+template <typename T, int DC> constexpr long kTogether = sizeof(T) == 4 ? 1l << 23 : DC > 64 ? 4096 : 512;
+
+template <typename T, int DC>
+int bwd(BwdArgs g, hipStream_t s) {
+  const AttnShape& a = g.a;
+  const long rows = (long)a.q_rows * a.group;
+  g.q_tiles = (int)(a.q_rows > 0 ? rows / kRows + a.n_seq : 0);
+  g.k_tiles = (int)(a.k_rows > 0 ? (long)a.k_rows / kKeys + a.n_seq : 0);
+  auto grid = [&](long tiles) { return dim3((unsigned)(tiles * a.kv_heads)); };
+  if (g.q_tiles > 0 && g.k_tiles > 0 && ((long)g.q_tiles + g.k_tiles) * a.kv_heads <= kTogether<T, DC>) {
+    attn_bwd_delta_kernel<T, DC><<<grid(g.q_tiles), dim3(256), 0, s>>>(g);
+    attn_bwd_both_kernel<T, DC><<<grid((long)g.q_tiles + g.k_tiles), dim3(256), 0, s>>>(g);
+    return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
+  }
+  // (two sets where launches above the limit can be short of blocks)
+  constexpr bool kTwo = kTwoSets<T, DC> && kTogether<T, DC> <= 512;
   bool two_q = false, two_k = false;
-  if constexpr (kTwoSets<T, DC>) {
+  if constexpr (kTwo) {
     two_q = two_sets(rows / kRows * a.kv_heads, a.k_rows, a.n_seq);
     two_k = two_sets((long)a.k_rows / kKeys * a.kv_heads, rows, a.n_seq);
-    if (two_q && a.q_rows > 0) attn_bwd_q_kernel<T, DC, 2><<<dim3((unsigned)q_blocks), dim3(512), 0, s>>>(g);
+    if (two_q && g.q_tiles > 0) attn_bwd_q_kernel<T, DC, 2><<<grid(g.q_tiles), dim3(512), 0, s>>>(g);
   }
-  if (!two_q && a.q_rows > 0) attn_bwd_q_kernel<T, DC, 1><<<dim3((unsigned)q_blocks), dim3(256), 0, s>>>(g);
-  if constexpr (kTwoSets<T, DC>)
-    if (two_k && a.k_rows > 0) attn_bwd_kv_kernel<T, DC, 2><<<dim3((unsigned)k_blocks), dim3(512), 0, s>>>(g);
-  if (!two_k && a.k_rows > 0) attn_bwd_kv_kernel<T, DC, 1><<<dim3((unsigned)k_blocks), dim3(256), 0, s>>>(g);
+  if (!two_q && g.q_tiles > 0) attn_bwd_q_kernel<T, DC, 1><<<grid(g.q_tiles), dim3(256), 0, s>>>(g);
+  if constexpr (kTwo)
+    if (two_k && g.k_tiles > 0) attn_bwd_kv_kernel<T, DC, 2><<<grid(g.k_tiles), dim3(512), 0, s>>>(g);
+  if (!two_k && g.k_tiles > 0) attn_bwd_kv_kernel<T, DC, 1><<<grid(g.k_tiles), dim3(256), 0, s>>>(g);
   return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
 }
 template <typename T>
@@ -452,7 +519,7 @@ size_t attn_bwd_scratch_bytes(int, const AttnShape& a) { return (size_t)a.q_rows
 
 int launch_attn_bwd(int dtype, const AttnShape& a, const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse, void* dq,
                     void* dk, void* dv, void* scratch, hipStream_t s) {
-  const BwdArgs g = {a, d_o, q, k, v, o, lse, dq, dk, dv, static_cast<float*>(scratch), a.scale * kLog2e};
+  const BwdArgs g = {a, d_o, q, k, v, o, lse, dq, dk, dv, static_cast<float*>(scratch), a.scale * kLog2e, 0, 0};
   return dtype == SPES_BF16 ? bwd<bf16_t>(g, s) : bwd<float>(g, s);
 }
 

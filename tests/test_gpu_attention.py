@@ -323,3 +323,24 @@ def test_many_blocks(dtype):
                                 dict(lens=[700], keys=[900], causal=False)])
 def test_widths_that_end_inside_a_fragment(dim, kw):
     Problem(**{**dict(dim=dim, dtype=torch.float32, seed=dim), **kw}).check()
+
+
+@pytest.mark.parametrize("dim", [24, 64])
+@pytest.mark.parametrize("kw", [dict(), dict(causal=False), dict(window=90), dict(heads=80), dict(heads=120, window=200)])
+def test_gradients_of_two_launches_with_two_sets_of_wavefronts(dim, kw):
+    """More blocks than run at once, each launch's fewer."""
+    Problem([300, 290], dim=dim, **{**dict(heads=40, kv=40, seed=dim), **kw}).check()
+
+
+@pytest.mark.parametrize("dim", [72, 128])
+@pytest.mark.parametrize("kw", [dict(), dict(causal=False), dict(window=50), dict(heads=192)])
+def test_gradients_of_long_heads_in_two_launches(dim, kw):
+    lens = [1, 200, 64, 65, 129, 7, 90, 128, 33, 250, 12, 101, 64, 180, 5, 70]
+    Problem(lens, dim=dim, **{**dict(heads=64, kv=64, seed=dim), **kw}).check()
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("lens,keys", [([0, 0], [70, 33]), ([70, 33], [0, 0])])
+def test_gradients_without_queries_or_keys(dtype, lens, keys):
+    got = Problem(lens, keys=keys, dtype=dtype).check()
+    assert all((got[n] == 0).all() for n in ("dq", "dk", "dv"))
