@@ -532,7 +532,7 @@ SPES_API int spes_attn_fwd(const spes_attn_shape* shape, const void* q, const vo
                            const int32_t* q_start, const int32_t* k_start, const int32_t* k_len, void* o,
                            float* lse, void* scratch, void* stream);
 
-/* Its backward for the upstream gradient d_o of o.  The probabilities are formed again from q, k and lse.
+/* Its backward for the upstream gradient d_o of o.  The probabilities are formed again from q, k and lse, and sum d_o o is taken of o as it is stored.
  *
  *  d_o       DEVICE [q_rows, heads, head_dim]
  *  o, lse    as the forward left them; all other inputs as above
