@@ -522,7 +522,8 @@ typedef struct {
 } spes_attn_shape;
 
 /*  q         DEVICE [q_rows, heads, head_dim]     k, v  DEVICE [k_rows, kv_heads, head_dim], strides in the shape
- *  q_start   DEVICE [n_seq + 1] i32, ascending    k_start  DEVICE [n_seq + 1] i32 ([n_seq] with k_len)      k_len  DEVICE [n_seq] i32 or NULL
+ *  q_start   DEVICE [n_seq + 1] i32, ascending    k_start  DEVICE [n_seq + 1] i32, ascending (with k_len [n_seq], in any order)
+ *  k_len     DEVICE [n_seq] i32 or NULL
  *  o         DEVICE [q_rows, heads, head_dim] out
  *  lse       DEVICE [heads, q_rows] f32 out
  *  scratch   DEVICE, spes_attn_scratch_bytes(shape, 0) bytes

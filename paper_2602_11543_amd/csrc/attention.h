@@ -286,34 +286,56 @@ __device__ __forceinline__ Seq sequence(const AttnShape& a, int b) {
   return s;
 }
 
-// Item t of the list of all sequences' tiles, `per` rows (or keys) each: the sequence, and which of its tiles.  Every wavefront goes over the
-// sequences for itself, 64 at a time.  False beyond the list's end.
+// Slot t of the list of all sequences' tiles, `per` rows (or keys) each: the sequence, and which of its tiles.  Starts are ascending, so sequence b has the slots from
+// start[b] group / per + b on, which are as many as its tiles or one more, and is looked for by every wavefront for itself, 64 places at a time: once up to
+// 64 sequences, twice up to 4096.  (Sums over all sequences ahead: 2048 of 16 tokens, 16 / 4 heads of 128, 396 + 841 us ->
+// 140 + 384; 2 of 2048, 12 heads of 64, forward 31 -> 29.)  A cache's
+// starts have any order, so there these sums it is (only the keys' gradients ask).  False for a slot without a tile.
 template <bool KEYS>
 __device__ __forceinline__ bool find_tile(const AttnShape& a, int t, int per, int lane, Seq& seq, int& tile, int& tiles) {
-  int before = 0;
-  for (int b0 = 0; b0 < a.n_seq; b0 += kWave) {
-    const int b = b0 + lane;
-    Seq s = {0, 0, 0, 0};
-    if (b < a.n_seq) s = sequence(a, b);
-    const int n = KEYS ? cdiv(s.lk, per) : cdiv((long)s.lq * a.group, per);
-    int sum = n;
+  auto tiles_of = [&](const Seq& s) { return KEYS ? cdiv(s.lk, per) : cdiv(s.lq * a.group, per); };
+  Seq s = {0, 0, 0, 0};
+  int from, at;
+  if (KEYS && a.k_len) {
+    int b0 = 0, all = 0;
+    do {
+      t -= all;
+      if (b0 >= a.n_seq) return false;
+      s = b0 + lane < a.n_seq ? sequence(a, b0 + lane) : Seq{0, 0, 0, 0};
+      const int n = tiles_of(s);
+      int sum = n;
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int up = __shfl_up(sum, d, kWave);
-      if (lane >= d) sum += up;
+      for (int d = 1; d < kWave; d <<= 1) {
+        const int up = __shfl_up(sum, d, kWave);
+        if (lane >= d) sum += up;
+      }
+      all = __builtin_amdgcn_readlane(sum, kWave - 1);
+      from = sum - n;
+      at = __builtin_ctzl(__ballot(t < sum) | 1ul << 63);
+      b0 += kWave;
+    } while (t >= all);
+  } else {
+    const int* const start = KEYS ? a.k_start : a.q_start;
+    auto slot = [&](int b) { return KEYS ? min(max(start[b], 0), a.k_rows) / per + b : min(max(start[b], 0), a.q_rows) * a.group / per + b; };
+    int lo = 0, hi = a.n_seq;
+    while (hi - lo > kWave) {
+      const int step = cdiv(hi - lo, kWave), b = lo + lane * step;
+      const unsigned long before = __ballot(b < hi && slot(b) <= t);
+      if (before == 0) return false;
+      lo += (63 - __builtin_clzl(before)) * step;
+      hi = min(lo + step, hi);
     }
-    const unsigned long has = __ballot(t < before + sum);
-    if (has) {
-      const int at = __builtin_ctzl(has);
-      auto pick = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-      seq = Seq{pick(s.q0), pick(s.lq), pick(s.k0), pick(s.lk)};
-      tiles = pick(n);
-      tile = t - before - (pick(sum) - tiles);
-      return true;
-    }
-    before += __builtin_amdgcn_readlane(sum, kWave - 1);
+    if (lo + lane < hi) s = sequence(a, lo + lane);
+    from = (KEYS ? s.k0 : s.q0 * a.group) / per + lo + lane;
+    const unsigned long before = __ballot(lo + lane < hi && from <= t);
+    if (before == 0) return false;
+    at = 63 - __builtin_clzl(before);
   }
-  return false;
+  auto pick = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+  seq = Seq{pick(s.q0), pick(s.lq), pick(s.k0), pick(s.lk)};
+  tiles = tiles_of(seq);
+  tile = t - pick(from);
+  return tile < tiles;
 }
 
 // One of the two rows of a lane in the queries' kernels; a row behind the last one stands for that one, but is not real

@@ -344,3 +344,22 @@ def test_gradients_of_long_heads_in_two_launches(dim, kw):
 def test_gradients_without_queries_or_keys(dtype, lens, keys):
     got = Problem(lens, keys=keys, dtype=dtype).check()
     assert all((got[n] == 0).all() for n in ("dq", "dk", "dv"))
+
+
+@pytest.mark.parametrize("n,some", [(65, 3), (130, 1), (4097, 15), (4500, 17)])
+def test_many_sequences_most_of_them_empty(n, some):
+    lens = [0] * n
+    for i in range(0, n, some):
+        lens[i] = 1 + (7 * i) % 41
+    lens[n // 2] = 300
+    Problem(lens, heads=2, kv=1, dim=32, gap=5, seed=n).check()
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+def test_caches_in_any_order(dtype):
+    for n in (5, 70):
+        p = Problem([20 + i % 30 for i in range(n)], keys=[90] * n, room=97, heads=4, kv=2, gap=2, dtype=dtype, seed=n)
+        order = torch.randperm(n, generator=torch.Generator().manual_seed(n)).tolist()
+        p.k_start = p.k_start[order].contiguous()
+        p.seqs = [(q, lq, p.seqs[o][2], m) for (q, lq, _, m), o in zip(p.seqs, order)]
+        p.check()
