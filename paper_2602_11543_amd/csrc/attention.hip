@@ -17,6 +17,7 @@ struct FwdArgs {
   float *lse, *part_o, *part_lse;
   int parts, per;       // parts that a tile's keys are cut into at most, and steps of keys to a part (for few rows: see FewPlan)
   float c;              // scale log2 e: exponentials are of base two
+  int items;            // of few rows whose keys are not cut: places of tiles
 };
 
 constexpr int kFewRows = 32, kFewStep = 32, kMaxParts = 64;
@@ -267,6 +268,9 @@ struct Few {
 };
 // What the blocks of that kernel make of the descriptors, every one for itself: items of (tile of rows, part of its sequence's keys), all parts of one size
 // `per`, such that there are about kFewItems of them, so the work is even however unequal the sequences are.
+// With that many tiles their keys are not cut: the tiles are looked up, by up to eight times the blocks, which even out unequal sequences, and nothing is joined
+// (one token each of 256 sequences, 32 / 8 heads of 128, 500 keys: 145 us cut, 108 whole; 1024 of 250 298 -> 235; 128 of 1 to 4096 302 -> 271; with
+// the chip's blocks alone 115, 227 and 308; by attn_fwd_kernel 128, 225 and 288).
 // (The 32 sequences above: 49 us in all with 1024 items, two for each block, 52 with 512, 56 with 2048; with at least 4 or 16 steps to a part the same as with 8.)
 constexpr int kFewItems = 1024, kFewLeast = 8, kFewBlocks = 512;      // kFewLeast: steps to a part at least; kFewBlocks: what the chip holds
 struct Span { int tiles, j0, n; };      // of a sequence: tiles of rows, first step of keys that its queries see, steps
@@ -347,9 +351,15 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
   const unsigned cb = L::col_base(lane);
   for (int item = blockIdx.x;; item += gridDim.x) {
   Seq s;
-  int tile, part, j0, j1;
+  int tile, part = 0, j0 = 0, j1 = 1 << 30;
   const int kvh = item % a.kv_heads;
-  if (!plan.find(a, item / a.kv_heads, lane, s, tile, part, j0, j1)) return;
+  if (g.parts > 1) {
+    if (!plan.find(a, item / a.kv_heads, lane, s, tile, part, j0, j1)) return;
+  } else {
+    int tiles;
+    if (item >= g.items) return;
+    if (!find_tile<false>(a, item / a.kv_heads, kFewRows, lane, s, tile, tiles)) continue;
+  }
   const int G = a.group, n_rows = s.lq * G, r0 = tile * kFewRows, last = min(r0 + kFewRows, n_rows) - 1;
   const Row row[2] = {Row(r0 + x, n_rows, G, kvh), Row(r0 + 16 + x, n_rows, G, kvh)};
   const Reach mine[2] = {reach(a, s, row[0].query), reach(a, s, row[1].query)}, first = reach(a, s, r0 / G), final = reach(a, s, last / G);
@@ -607,7 +617,8 @@ Cut cut_of(int dtype, const AttnShape& a) {
   const long rows = (long)a.q_rows * a.group, keys = a.k_rows / a.n_seq;
   if (rows <= (long)kFewRows * a.n_seq) {
     const long tiles = std::max<long>(cdiv(rows, kFewRows), std::min(a.n_seq, a.q_rows)) * a.kv_heads;
-    return {true, (int)std::max<long>(1, std::min<long>({kMaxParts, 4 * kFewItems / tiles, a.k_rows / (kFewLeast * kFewStep)})), 1};
+    const long parts = tiles >= kFewItems ? 1 : std::min<long>({kMaxParts, 4 * kFewItems / tiles, a.k_rows / (kFewLeast * kFewStep)});
+    return {true, (int)std::max<long>(1, parts), 1};
   }
   const long tiles = std::max<long>(cdiv(rows, kRows), std::min(a.n_seq, a.q_rows)) * a.kv_heads;
   const long held = dtype == SPES_F32 && a.dim > 64 ? 256 : 512;      // blocks that the chip holds: two to a CU, or one
@@ -616,12 +627,13 @@ Cut cut_of(int dtype, const AttnShape& a) {
 }
 
 template <typename T, int DC>
-int fwd(const FwdArgs& g, bool few, hipStream_t s) {
+int fwd(FwdArgs g, bool few, hipStream_t s) {
   const AttnShape& a = g.a;
   const long n = (long)a.q_rows * a.group;
   auto grid = [&](long per, int parts) { return dim3((unsigned)((n / per + a.n_seq) * a.kv_heads * parts)); };
   if (few) {
-    attn_few_kernel<T, DC><<<std::min<unsigned>(grid(kFewRows, g.parts).x, kFewBlocks), dim3(64 * Few<T, tile_dim(DC)>::kWaves), 0, s>>>(g);
+    g.items = (int)grid(kFewRows, 1).x;
+    attn_few_kernel<T, DC><<<std::min<unsigned>(grid(kFewRows, g.parts).x, g.parts > 1 ? kFewBlocks : 8 * kFewBlocks), dim3(64 * Few<T, tile_dim(DC)>::kWaves), 0, s>>>(g);
     if (g.parts > 1) attn_join_kernel<T, 256, true><<<grid(1, 1), dim3(256), 0, s>>>(g);
   } else {
     bool two = false;
@@ -653,7 +665,7 @@ size_t attn_fwd_scratch_bytes(int dtype, const AttnShape& a) {
 
 int launch_attn_fwd(int dtype, const AttnShape& a, const void* q, const void* k, const void* v, void* o, float* lse, void* scratch, hipStream_t s) {
   const Cut cut = cut_of(dtype, a);
-  FwdArgs g = {a, q, k, v, o, lse, nullptr, nullptr, cut.parts, cut.per, a.scale * kLog2e};
+  FwdArgs g = {a, q, k, v, o, lse, nullptr, nullptr, cut.parts, cut.per, a.scale * kLog2e, 0};
   g.part_o = static_cast<float*>(scratch);
   g.part_lse = g.part_o + (size_t)g.parts * a.q_rows * a.heads * a.dim;
   return dtype == SPES_BF16 ? fwd<bf16_t>(g, cut.few, s) : fwd<float>(g, cut.few, s);

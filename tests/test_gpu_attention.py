@@ -363,3 +363,10 @@ def test_caches_in_any_order(dtype):
         p.k_start = p.k_start[order].contiguous()
         p.seqs = [(q, lq, p.seqs[o][2], m) for (q, lq, _, m), o in zip(p.seqs, order)]
         p.check()
+
+
+@pytest.mark.parametrize("dtype,dim", [(torch.bfloat16, 128), (torch.bfloat16, 40), (torch.float32, 80)])
+@pytest.mark.parametrize("n,kv", [(130, 8), (70, 16), (700, 8)])
+def test_single_tokens_of_many_sequences(dtype, dim, n, kv):
+    """Keys in parts of more than 64 sequences, and at 700 sequences whole, from more tiles than there are blocks."""
+    Problem([i % 2 + (i % 7 == 0) for i in range(n)], keys=[(37 * i) % 300 for i in range(n)], room=300, heads=2 * kv, kv=kv, dim=dim, dtype=dtype, gap=1, seed=n).check(backward=False)
