@@ -59,7 +59,7 @@ __device__ __forceinline__ void put_row(const FwdArgs& g, int part, long token, 
 // the other for launches that leave CUs empty.
 // Two wavefronts to a SIMD in bf16 (220 registers with heads of 128): one's matrix instructions run beside the other's exponentials.  32 heads of 128 (8 of
 // keys), 8 x 4096 tokens, causal: 1.11 ms, 0.99 PFLOP/s of what the mask leaves, bound by power (with zeros for data 0.89 ms; a library product of 8192^3
-// 1.27 PFLOP/s).  512 queries against 16000 keys: 148 us, 0.89 PFLOP/s.  12 heads of 64, 2 x 2048 tokens: 32 us; there exponentials and maxima take longer than the
+// 1.27 PFLOP/s).  512 queries against 16000 keys: 148 us, 0.89 PFLOP/s.  12 heads of 64, 2 x 2048 tokens: 30 us; there exponentials and maxima take longer than the
 // products.  fp32, 10 heads of 80, 2760 tokens, window of 700: 75 us; the matrix instructions of the longest block 55 of them.
 template <typename T, int DC, int KS>
 __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(const FwdArgs g) {
@@ -532,7 +532,7 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
 
 // The parts of a row's keys joined: weights exp(lse_p - lse).  LANES lanes to a row: 32 hold four elements each, and each 32 go over every
 // (LANES / 32)th part.  A launch of its own, so no block waits for another: 6 us for one token of 32 sequences (1024 rows of up to 19 parts), which is two
-// trips to memory one behind the other, and 11 for 512 queries of 32 heads in 4 parts (34 MB).
+// trips to memory one behind the other, and 10 for 512 queries of 32 heads in 4 parts (34 MB).
 template <typename T, int LANES, bool FEW>
 __global__ __launch_bounds__(256) void attn_join_kernel(const FwdArgs g) {
   constexpr int GROUPS = LANES / 32, PER_BLOCK = 256 / LANES;

@@ -38,7 +38,7 @@ __device__ __forceinline__ float delta_of(const typename Mma<T>::Frag (&d)[kFrag
 
 // 128 rows; KS sets of four wavefronts as in the forward.  Queries and upstream gradients stay in registers, keys and values pass through LDS: each key tile is
 // read as rows for the scores and as columns for dq.  8 x 4096 tokens, 32 / 8 heads of 128, causal: 1.45 ms, 1.14 PFLOP/s of the 6 D operations a
-// pair, bound by power; 2 x 2048 tokens, 12 heads of 64: 39 us.
+// pair, bound by power; 2 x 2048 tokens, 12 heads of 64: 36 us.
 template <typename T, int DC, int KS, bool KEEP>
 __device__ __forceinline__ void bwd_q(const BwdArgs& g, int item, int kvh, char* smem) {
   constexpr int DH = tile_dim(DC);
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
 
 // Both in one launch, behind one that forms delta: where each by itself leaves CUs empty towards its end, or all along.  Tiles of rows and of keys are dealt out
 // evenly, the longest of a sequence first.  fp32, 2760 tokens, 10 / 5 heads of 80, window of 700: 220 us behind 5 (106 and 135 one after the other); 16 documents of 1 to
-// 6011 tokens, 16 / 4 heads of 128: 790 behind 24.
+// 6011 tokens, 16 / 4 heads of 128: 780 to 810 behind 23.
 template <typename T, int DC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_both_kernel(const BwdArgs g) {
   __shared__ __align__(1024) char smem[kLds<T, DC, 1>];
