@@ -36,7 +36,8 @@ class DeviceAttention:
         self.table = rotation_table(n_pos, self.rot, device=device)
         self.h, self.rstd, self.dx = new(T, d_model, t=st), new(T), new(T, d_model, t=st)
         self.q, self.k = new(T, heads, head_dim, t=st), new(T, kv_heads, head_dim, t=st)
-        self.dq, self.dk = torch.empty_like(self.q), torch.empty_like(self.k)
+        self.d_heads = new(T * (heads + kv_heads) * head_dim, t=st)          # of q and k, one behind the other, so that one call clears both
+        self.dq, self.dk = self.d_heads[: self.q.numel()].view_as(self.q), self.d_heads[self.q.numel():].view_as(self.k)
         self.o, self.lse, self.d_qkv = torch.empty_like(self.q), new(heads, T), new(T, width, t=st)
         self.qk = S.qk_shape(T, heads, kv_heads, head_dim, self.rot, self.dt, 0, n_pos)
         self.norm_scratch = new(S.spes_norm_scratch_bytes(T, d_model), t=torch.uint8)
@@ -56,7 +57,8 @@ class DeviceAttention:
 
     def forward(self, x, starts, pos):
         """x [T, d]: the stream; starts [n + 1] i32: where its sequences begin, and the last one's end; pos [T] i32: a token's place in its
-        sequence.  Returns what this half adds to the stream.  A caller that captures the calls into a graph makes one eager call first, which
+        sequence.  Rows ahead of the first sequence and behind the last one (finite, with a place that the table has) get nothing added and add nothing to
+        the gradients.  Returns what this half adds to the stream.  A caller that captures the calls into a graph makes one eager call first, which
         takes the scratch."""
         T, d = self.T, self.d
         S.spes_norm_fwd(S.SPES_NORM_RMS, T, d, self.dt, x, None, self.w["norm"], None, 1e-6, None, self.h, None, self.rstd)
@@ -64,6 +66,9 @@ class DeviceAttention:
         q, k, v = self._heads(self.qkv)
         S.spes_qk_rope_fwd(self.qk, q, k, self.w["q"], self.w["k"], self.table, pos, self.q, self.k)
         self.shape = S.attn_shape(starts.numel() - 1, T, T, self.H, self.K, self.D, self.dt, 1, self.window)
+        # (attention leaves rows of no sequence as they are, and the products below go over all rows.  Cleared whole: which rows these are is known on the
+        # device alone; 32768 rows of 32 / 8 heads of 128 in bf16, o and the three gradients, 0.7 GB to write)
+        self.o.zero_()
         S.spes_attn_fwd(self.shape, self.q, self.k, v, starts, starts, None, self.o, self.lse, self._scratch(self.shape, 0))
         return self.o.view(T, -1) @ self.w["o"].t()
 
@@ -75,6 +80,8 @@ class DeviceAttention:
         d_o = (d_add @ self.w["o"]).view(T, self.H, self.D)
         q, k, v = self._heads(self.qkv)
         dq, dk, dv = self._heads(self.d_qkv)
+        self.d_heads.zero_()
+        dv.zero_()
         S.spes_attn_bwd(self.shape, d_o, self.q, self.k, v, starts, starts, None, self.o, self.lse, self.dq, self.dk, dv, self._scratch(self.shape, 1))
         S.spes_qk_rope_bwd(self.qk, self.dq, self.dk, q, k, self.w["q"], self.w["k"], self.table, pos, dq, dk, self.grad["q"], self.grad["k"], accumulate,
                            self.qk_scratch)

@@ -1,0 +1,64 @@
+"""The attention half of a block over the batches and tokens of a longer run: batches that do not fill its rows, graphs beside eager calls, caches that fill up."""
+import pytest
+import torch
+
+import paper_2602_11543_amd as S
+from paper_2602_11543_amd.attention import DeviceAttention
+from test_gpu_attention_block import TOL16, TOL32, far
+
+pytestmark = pytest.mark.gpu
+
+D_MODEL = 64
+
+
+def make(T, dtype="bf16", seed=1, **kw):
+    A = DeviceAttention(T, D_MODEL, **{**dict(heads=4, kv_heads=2, head_dim=32, n_pos=128, dtype=dtype, seed=seed), **kw})
+    g = torch.Generator(device="cuda").manual_seed(seed + 100)
+    for n in ("norm", "q", "k"):
+        A.w[n].copy_(1 + 0.2 * torch.randn(A.w[n].shape, device="cuda", generator=g))
+    return A
+
+
+def batch(A, starts, T=None, seed=2):
+    """x, d_add, starts, pos of T rows, the rows of no sequence among them."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    T = A.T if T is None else T
+    x, d_add = (torch.randn(T, D_MODEL, device="cuda", generator=g).to(A.h.dtype) for _ in range(2))
+    pos = torch.zeros(T, dtype=torch.int32)
+    for a, b in zip(starts[:-1], starts[1:]):
+        pos[a:b] = torch.arange(b - a)
+    return x, d_add, torch.tensor(starts, dtype=torch.int32, device="cuda"), pos.cuda()
+
+
+def call(A, x, d_add, starts, pos):
+    add = A.forward(x, starts, pos)
+    dx = A.backward(d_add, x, starts, pos)
+    return {"add": add.clone(), "dx": dx.clone(), **{n: t.clone() for n, t in A.grad.items()}}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("starts", [[0, 30, 70], [9, 40, 41, 90], [20, 20, 128], [5, 5], [0]])
+def test_rows_of_no_sequence_add_nothing(dtype, starts):
+    """Behind a batch that fills all rows, and on memory that holds anything, a batch that does not is what its rows alone are."""
+    tol = TOL32 if dtype == "f32" else TOL16
+    used, fresh = make(128, dtype), make(128, dtype)
+    call(used, *batch(used, [0, 50, 128], seed=3))
+    for t in (fresh.o, fresh.dq, fresh.dk, fresh.d_qkv, fresh.q, fresh.k):
+        t.fill_(float("nan"))
+    x, d_add, at, pos = batch(used, starts)
+    got, other = call(used, x, d_add, at, pos), call(fresh, x, d_add, at, pos)
+    for n in got:
+        assert torch.equal(got[n], other[n]), n
+    rows = slice(starts[0], starts[-1])
+    outside = torch.ones(128, dtype=torch.bool, device="cuda")
+    outside[rows] = False
+    for n in ("add", "dx"):
+        assert (got[n][outside] == 0).all(), n
+    count = starts[-1] - starts[0]
+    if count == 0:
+        assert all((t == 0).all() for t in got.values())
+        return
+    alone = make(count, dtype)
+    want = call(alone, x[rows].contiguous(), d_add[rows].contiguous(), at - starts[0], pos[rows].clone())
+    for n, t in want.items():
+        assert far(got[n][rows] if n in ("add", "dx") else got[n], t) < tol, n
