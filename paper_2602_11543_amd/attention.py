@@ -42,18 +42,20 @@ class DeviceAttention:
         self.qk = S.qk_shape(T, heads, kv_heads, head_dim, self.rot, self.dt, 0, n_pos)
         self.norm_scratch = new(S.spes_norm_scratch_bytes(T, d_model), t=torch.uint8)
         self.qk_scratch = new(S.spes_qk_rope_scratch_bytes(self.qk), t=torch.uint8)
-        self.steps, self.cache = 0, None
+        self.steps, self.cache, self.scratch = 0, None, {}
 
     def _heads(self, t):
         """Views of a projection's output, or of its gradient: queries, keys, values."""
         H, K, D = self.H, self.K, self.D
         return t[:, : H * D].view(-1, H, D), t[:, H * D: (H + K) * D].view(-1, K, D), t[:, (H + K) * D:].view(-1, K, D)
 
-    def _scratch(self, shape, backward):
-        need = S.spes_attn_scratch_bytes(shape, backward)
-        if getattr(self, "attn_scratch", None) is None or self.attn_scratch.numel() < need:
-            self.attn_scratch = torch.empty(need, dtype=torch.uint8, device=self.h.device)
-        return self.attn_scratch
+    def _scratch(self, shape, backward, use="batch"):
+        """Scratch for the call.  Captured graphs have the addresses of what was handed out, so a buffer that is outgrown is kept; each is twice the one
+        before at least, and those kept are not more than the newest one.  Single tokens have their own, which batches do not grow."""
+        need, kept = S.spes_attn_scratch_bytes(shape, backward), self.scratch.setdefault(use, [])
+        if not kept or kept[-1].numel() < need:
+            kept.append(torch.empty(max(need, 2 * kept[-1].numel() if kept else 0), dtype=torch.uint8, device=self.h.device))
+        return kept[-1]
 
     def forward(self, x, starts, pos):
         """x [T, d]: the stream; starts [n + 1] i32: where its sequences begin, and the last one's end; pos [T] i32: a token's place in its
@@ -129,5 +131,6 @@ class DeviceAttention:
             c.index_copy_(0, rows, t)
         self.length += 1
         shape = S.attn_shape(n, n, n * self.room, H, K, D, self.dt, 1, self.window)
-        S.spes_attn_fwd(shape, q, *caches, self.q_start, self.row0, self.length, o, new(H, n, t=torch.float32), self._scratch(shape, 0))
+        S.spes_attn_fwd(shape, q, *caches, self.q_start, self.row0, self.length, o, new(H, n, t=torch.float32),
+                        self._scratch(shape, 0, "tokens"))
         return o.view(n, -1) @ self.w["o"].t()

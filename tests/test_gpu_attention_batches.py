@@ -62,3 +62,35 @@ def test_rows_of_no_sequence_add_nothing(dtype, starts):
     want = call(alone, x[rows].contiguous(), d_add[rows].contiguous(), at - starts[0], pos[rows].clone())
     for n, t in want.items():
         assert far(got[n][rows] if n in ("add", "dx") else got[n], t) < tol, n
+
+
+def test_scratch_of_a_graph_stays_its_own():
+    """Tokens and batches that need more scratch, between the replays of a captured step of the same object; what they allocate is overwritten."""
+    A, B, many = make(128, n_pos=8000), make(128, n_pos=8000), [0, 1, 2, 64, 128]
+    one = batch(A, [0, 50, 128])
+
+    def step(m):
+        return m.forward(one[0], one[2], one[3]), m.backward(one[1], *(one[i] for i in (0, 2, 3)))
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(A)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        add, dx = step(A)
+    kept = []
+    for i in range(3):
+        A.start_cache(2, 2000 * (i + 1))
+        A.decode(one[0][:2])
+        need = S.attn_shape(2, 2, 4000 * (i + 1), A.H, A.K, A.D, A.dt, 1, 0)
+        assert S.spes_attn_scratch_bytes(need, 0) > S.spes_attn_scratch_bytes(A.shape, 1)
+        call(A, *batch(A, many, seed=6))
+        kept += [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (512, 2048, 4096, 1 << 16)]
+        mine = [t.clone() for t in kept]
+        one[0].mul_(-0.75)
+        graph.replay()
+        want, want_dx = step(B)
+        torch.cuda.synchronize()
+        assert torch.equal(add, want) and torch.equal(dx, want_dx), i
+        assert all(torch.equal(a, b) for a, b in zip(kept, mine)), i
