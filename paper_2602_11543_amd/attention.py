@@ -38,7 +38,8 @@ class DeviceAttention:
         self.q, self.k = new(T, heads, head_dim, t=st), new(T, kv_heads, head_dim, t=st)
         self.d_heads = new(T * (heads + kv_heads) * head_dim, t=st)          # of q and k, one behind the other, so that one call clears both
         self.dq, self.dk = self.d_heads[: self.q.numel()].view_as(self.q), self.d_heads[self.q.numel():].view_as(self.k)
-        self.o, self.lse, self.d_qkv = torch.empty_like(self.q), new(heads, T), new(T, width, t=st)
+        self.o, self.lse = torch.empty_like(self.q), new(heads, T)
+        self.qkv, self.d_qkv = new(T, width, t=st), new(T, width, t=st)
         self.qk = S.qk_shape(T, heads, kv_heads, head_dim, self.rot, self.dt, 0, n_pos)
         self.norm_scratch = new(S.spes_norm_scratch_bytes(T, d_model), t=torch.uint8)
         self.qk_scratch = new(S.spes_qk_rope_scratch_bytes(self.qk), t=torch.uint8)
@@ -64,7 +65,7 @@ class DeviceAttention:
         takes the scratch."""
         T, d = self.T, self.d
         S.spes_norm_fwd(S.SPES_NORM_RMS, T, d, self.dt, x, None, self.w["norm"], None, 1e-6, None, self.h, None, self.rstd)
-        self.qkv = self.h @ self.w["qkv"].t()
+        torch.mm(self.h, self.w["qkv"].t(), out=self.qkv)
         q, k, v = self._heads(self.qkv)
         S.spes_qk_rope_fwd(self.qk, q, k, self.w["q"], self.w["k"], self.table, pos, self.q, self.k)
         self.shape = S.attn_shape(starts.numel() - 1, T, T, self.H, self.K, self.D, self.dt, 1, self.window)
@@ -77,8 +78,14 @@ class DeviceAttention:
     def backward(self, d_add, x, starts, pos, d_stream=None, accumulate=0):
         """d_add [T, d]: gradient of what the forward returned; d_stream: the one that reaches x along the stream.  Returns x's."""
         T, d = self.T, self.d
-        product = lambda a, b: a.float().t() @ b.float()  # noqa: E731
-        w_o, w_qkv = product(d_add, self.o.view(T, -1)), None
+
+        def product(name, a, b):               # (into the gradient's own place: graphs and the optimizer step know it by that)
+            if accumulate:
+                self.grad[name] += a.float().t() @ b.float()
+            else:
+                torch.mm(a.float().t(), b.float(), out=self.grad[name])
+
+        product("o", d_add, self.o.view(T, -1))
         d_o = (d_add @ self.w["o"]).view(T, self.H, self.D)
         q, k, v = self._heads(self.qkv)
         dq, dk, dv = self._heads(self.d_qkv)
@@ -87,12 +94,7 @@ class DeviceAttention:
         S.spes_attn_bwd(self.shape, d_o, self.q, self.k, v, starts, starts, None, self.o, self.lse, self.dq, self.dk, dv, self._scratch(self.shape, 1))
         S.spes_qk_rope_bwd(self.qk, self.dq, self.dk, q, k, self.w["q"], self.w["k"], self.table, pos, dq, dk, self.grad["q"], self.grad["k"], accumulate,
                            self.qk_scratch)
-        w_qkv = product(self.d_qkv, self.h)
-        for n, w in (("o", w_o), ("qkv", w_qkv)):
-            if accumulate:
-                self.grad[n] += w
-            else:
-                self.grad[n] = w
+        product("qkv", self.d_qkv, self.h)
         dh = self.d_qkv @ self.w["qkv"]
         S.spes_norm_bwd(S.SPES_NORM_RMS, T, d, self.dt, dh, x, self.w["norm"], None, self.rstd, d_stream, self.dx, self.grad["norm"], None, accumulate,
                         self.norm_scratch)

@@ -94,3 +94,38 @@ def test_scratch_of_a_graph_stays_its_own():
         torch.cuda.synchronize()
         assert torch.equal(add, want) and torch.equal(dx, want_dx), i
         assert all(torch.equal(a, b) for a, b in zip(kept, mine)), i
+
+
+def test_a_graph_beside_eager_calls_of_the_same_object():
+    """What a replay leaves is where the optimizer step and an eager backward look for it, also behind eager calls."""
+    A, B = make(128), make(128)
+    first, second = batch(A, [0, 50, 128]), batch(A, [0, 100, 128], seed=4)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call(A, *first)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.forward(first[0], first[2], first[3])
+        A.backward(first[1], *(first[i] for i in (0, 2, 3)))
+    for i in range(3):
+        call(A, *second)
+        first[0].mul_(-1.25)
+        graph.replay()
+        want = call(B, *first)
+        torch.cuda.synchronize()
+        for n, t in A.grad.items():
+            assert torch.equal(t, want[n]), (i, n)
+        assert torch.equal(A.qkv, B.qkv) and torch.equal(A.dx, want["dx"]), i
+    # a graph of the backward alone, behind eager forward calls
+    A.forward(first[0], first[2], first[3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.backward(first[1], *(first[i] for i in (0, 2, 3)))
+    for i in range(3):
+        first[0].mul_(0.75)
+        A.forward(first[0], first[2], first[3])
+        graph.replay()
+        want = call(B, *first)
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, want[n]) for n, t in A.grad.items()), i
