@@ -121,7 +121,6 @@ class DeviceAttention:
         n, H, K, D = x.shape[0], self.H, self.K, self.D
         if self.cache is None or n != self.cache[0].shape[0] or self.taken >= min(self.room, self.n_pos):
             raise S.SpesError("decode: no cache for this many sequences, or its room or the positions are used up")
-        self.taken += 1
         new = lambda *s, t=x.dtype: torch.empty(*s, dtype=t, device=x.device)  # noqa: E731
         h, q, k, o = new(n, self.d), new(n, H, D), new(n, K, D), new(n, H, D)
         S.spes_norm_fwd(S.SPES_NORM_RMS, n, self.d, self.dt, x, None, self.w["norm"], None, 1e-6, None, h, None, new(n, t=torch.float32))
@@ -135,4 +134,5 @@ class DeviceAttention:
         shape = S.attn_shape(n, n, n * self.room, H, K, D, self.dt, 1, self.window)
         S.spes_attn_fwd(shape, q, *caches, self.q_start, self.row0, self.length, o, new(H, n, t=torch.float32),
                         self._scratch(shape, 0, "tokens"))
+        self.taken += 1
         return o.view(n, -1) @ self.w["o"].t()

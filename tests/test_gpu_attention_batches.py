@@ -129,3 +129,12 @@ def test_a_graph_beside_eager_calls_of_the_same_object():
         want = call(B, *first)
         torch.cuda.synchronize()
         assert all(torch.equal(t, want[n]) for n, t in A.grad.items()), i
+
+
+def test_a_refused_token_takes_no_room():
+    A = make(8)
+    x = torch.randn(2, D_MODEL, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).to(A.h.dtype)
+    A.start_cache(2, 1)
+    with pytest.raises(S.SpesError):
+        A.decode(x.float())
+    assert torch.isfinite(A.decode(x)).all() and A.length.tolist() == [1, 1]
