@@ -108,31 +108,44 @@ class DeviceAttention:
                                 weight_decay if w.dim() > 1 else 0.0, self.steps)
 
     def start_cache(self, n_seq, room):
-        """Empty caches with room for `room` tokens of each of n_seq sequences."""
+        """Empty caches with room for `room` tokens of each of n_seq sequences.  Caches of these sizes that are there already are emptied where they are, and
+        graphs that captured decode() go on with them; with others such graphs are not to be replayed any more."""
         dev, st = self.h.device, S.torch_dtype(self.dt)
-        self.room, self.taken = room, 0
-        self.cache = [torch.empty(n_seq, room, self.K, self.D, dtype=st, device=dev) for _ in range(2)]
+        row0 = torch.arange(n_seq, dtype=torch.int32, device=dev) * room
+        self.taken = 0
+        if self.cache is not None and self.cache[0].shape[:2] == (n_seq, room):
+            self.length.zero_()
+            self.next.copy_(row0)
+            return
+        self.room, self.limit = room, min(room, self.n_pos)
+        # one row more than there is room for takes what does not fit
+        self.rows = [torch.empty(n_seq * room + 1, self.K, self.D, dtype=st, device=dev) for _ in range(2)]
+        self.cache = [c[:-1].view(n_seq, room, self.K, self.D) for c in self.rows]
         self.length = torch.zeros(n_seq, dtype=torch.int32, device=dev)
-        self.row0 = torch.arange(n_seq, dtype=torch.int32, device=dev) * room
+        self.row0, self.next, self.spare = row0, row0.long(), torch.full((n_seq,), n_seq * room, dtype=torch.int64, device=dev)
         self.q_start = torch.arange(n_seq + 1, dtype=torch.int32, device=dev)
 
     def decode(self, x):
-        """x [n_seq, d]: each sequence's next token.  Its keys and values join the cache; returns what this half adds to the stream."""
+        """x [n_seq, d]: each sequence's next token.  Its keys and values join the cache; returns what this half adds to the stream.  A call may be captured into a
+        graph, behind an eager one, which takes the scratch.  Where replays, which the host does not count, go on beyond the room or the
+        positions, what they return is NaN and the caches stay as they are."""
         n, H, K, D = x.shape[0], self.H, self.K, self.D
-        if self.cache is None or n != self.cache[0].shape[0] or self.taken >= min(self.room, self.n_pos):
+        if self.cache is None or n != self.cache[0].shape[0] or self.taken >= self.limit:
             raise S.SpesError("decode: no cache for this many sequences, or its room or the positions are used up")
         new = lambda *s, t=x.dtype: torch.empty(*s, dtype=t, device=x.device)  # noqa: E731
         h, q, k, o = new(n, self.d), new(n, H, D), new(n, K, D), new(n, H, D)
         S.spes_norm_fwd(S.SPES_NORM_RMS, n, self.d, self.dt, x, None, self.w["norm"], None, 1e-6, None, h, None, new(n, t=torch.float32))
         qp, kp, vp = self._heads(h @ self.w["qkv"].t())
-        S.spes_qk_rope_fwd(S.qk_shape(n, H, K, D, self.rot, self.dt, 0, self.n_pos), qp, kp, self.w["q"], self.w["k"], self.table, self.length, q, k)
-        rows = (self.row0 + self.length).long()
-        caches = [c.view(-1, K, D) for c in self.cache]
-        for c, t in zip(caches, (k, vp)):
-            c.index_copy_(0, rows, t)
+        # (a position beyond the limit is none of the table's, and gives NaN)
+        S.spes_qk_rope_fwd(S.qk_shape(n, H, K, D, self.rot, self.dt, 0, self.limit), qp, kp, self.w["q"], self.w["k"], self.table, self.length, q, k)
+        at = torch.where(self.length < self.limit, self.next, self.spare)
+        for c, t in zip(self.rows, (k, vp)):
+            c.index_copy_(0, at, t)
         self.length += 1
+        self.next += 1
         shape = S.attn_shape(n, n, n * self.room, H, K, D, self.dt, 1, self.window)
-        S.spes_attn_fwd(shape, q, *caches, self.q_start, self.row0, self.length, o, new(H, n, t=torch.float32),
+        S.spes_attn_fwd(shape, q, *(c.view(-1, K, D) for c in self.cache), self.q_start, self.row0, self.length, o, new(H, n, t=torch.float32),
                         self._scratch(shape, 0, "tokens"))
-        self.taken += 1
+        if not torch.cuda.is_current_stream_capturing():
+            self.taken += 1
         return o.view(n, -1) @ self.w["o"].t()

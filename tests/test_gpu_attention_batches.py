@@ -138,3 +138,43 @@ def test_a_refused_token_takes_no_room():
     with pytest.raises(S.SpesError):
         A.decode(x.float())
     assert torch.isfinite(A.decode(x)).all() and A.length.tolist() == [1, 1]
+
+
+@pytest.mark.parametrize("room,n_pos", [(6, 128), (9, 6)])
+def test_replays_beyond_the_room_of_a_cache(room, n_pos):
+    """A captured token: up to the sixth what eager calls give, then NaN, with the caches as they were; emptied caches of the same size take the graph on."""
+    A, B = make(8, n_pos=n_pos), make(8, n_pos=n_pos)
+    x = torch.randn(6, 3, D_MODEL, device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)).to(A.h.dtype)
+    for m in (A, B):
+        m.start_cache(3, room)
+        for c in m.cache:
+            c.fill_(7.0)
+    token = x[0].clone()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        A.decode(token)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = A.decode(token)
+    assert A.taken == 1 and A.length.tolist() == [1, 1, 1]
+    for start in (1, 0):
+        if start:
+            B.decode(x[0])
+        else:
+            for m in (A, B):
+                m.start_cache(3, room)
+        for i in range(start, 6):
+            token.copy_(x[i])
+            graph.replay()
+            want = B.decode(x[i])
+            torch.cuda.synchronize()
+            assert torch.isfinite(out).all() and torch.equal(out, want), (start, i)
+        held = [c.clone() for c in A.cache]
+        for _ in range(4):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.isnan(out).all()
+        assert all(torch.equal(a, b) for a, b in zip(A.cache, held)) and all((c[:, 6:] == 7.0).all() for c in A.cache)
+    with pytest.raises(S.SpesError):
+        B.decode(x[0])
