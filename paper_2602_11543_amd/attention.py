@@ -17,7 +17,8 @@ def rotation_table(n_pos, rot_dim, base=10000.0, device="cuda"):
 
 
 class DeviceAttention:
-    """Weights, state and buffers for batches of T tokens.  Every node trains these matrices."""
+    """Weights, state and buffers for batches of T tokens.  Every node trains these matrices.  rot_dim: elements of a head that are rotated, all of them if
+    not given, 0 for none."""
 
     def __init__(self, T, d_model, heads, kv_heads, head_dim, n_pos, dtype="bf16", rot_dim=None, window=0, seed=0, device="cuda"):
         self.dt = S.SPES_F32 if dtype == "f32" else S.SPES_BF16
@@ -33,7 +34,7 @@ class DeviceAttention:
                   "o": normal((heads * head_dim) ** -0.5, d_model, heads * head_dim)}
         self.state = {n: dict(master=w.float().clone(), m=torch.zeros(w.shape, device=device), v=torch.zeros(w.shape, device=device)) for n, w in self.w.items()}
         self.grad = {n: torch.zeros(w.shape, device=device) for n, w in self.w.items()}
-        self.table = rotation_table(n_pos, self.rot, device=device)
+        self.table = rotation_table(n_pos, self.rot, device=device) if self.rot else None
         self.h, self.rstd, self.dx = new(T, d_model, t=st), new(T), new(T, d_model, t=st)
         self.q, self.k = new(T, heads, head_dim, t=st), new(T, kv_heads, head_dim, t=st)
         self.d_heads = new(T * (heads + kv_heads) * head_dim, t=st)          # of q and k, one behind the other, so that one call clears both
@@ -67,7 +68,7 @@ class DeviceAttention:
         S.spes_norm_fwd(S.SPES_NORM_RMS, T, d, self.dt, x, None, self.w["norm"], None, 1e-6, None, self.h, None, self.rstd)
         torch.mm(self.h, self.w["qkv"].t(), out=self.qkv)
         q, k, v = self._heads(self.qkv)
-        S.spes_qk_rope_fwd(self.qk, q, k, self.w["q"], self.w["k"], self.table, pos, self.q, self.k)
+        S.spes_qk_rope_fwd(self.qk, q, k, self.w["q"], self.w["k"], self.table, pos if self.rot else None, self.q, self.k)
         self.shape = S.attn_shape(starts.numel() - 1, T, T, self.H, self.K, self.D, self.dt, 1, self.window)
         # (attention leaves rows of no sequence as they are, and the products below go over all rows.  Cleared whole: which rows these are is known on the
         # device alone; 32768 rows of 32 / 8 heads of 128 in bf16, o and the three gradients, 0.7 GB to write)
@@ -92,8 +93,8 @@ class DeviceAttention:
         self.d_heads.zero_()
         dv.zero_()
         S.spes_attn_bwd(self.shape, d_o, self.q, self.k, v, starts, starts, None, self.o, self.lse, self.dq, self.dk, dv, self._scratch(self.shape, 1))
-        S.spes_qk_rope_bwd(self.qk, self.dq, self.dk, q, k, self.w["q"], self.w["k"], self.table, pos, dq, dk, self.grad["q"], self.grad["k"], accumulate,
-                           self.qk_scratch)
+        S.spes_qk_rope_bwd(self.qk, self.dq, self.dk, q, k, self.w["q"], self.w["k"], self.table, pos if self.rot else None, dq, dk, self.grad["q"], self.grad["k"],
+                           accumulate, self.qk_scratch)
         product("qkv", self.d_qkv, self.h)
         dh = self.d_qkv @ self.w["qkv"]
         S.spes_norm_bwd(S.SPES_NORM_RMS, T, d, self.dt, dh, x, self.w["norm"], None, self.rstd, d_stream, self.dx, self.grad["norm"], None, accumulate,
@@ -137,8 +138,12 @@ class DeviceAttention:
         S.spes_norm_fwd(S.SPES_NORM_RMS, n, self.d, self.dt, x, None, self.w["norm"], None, 1e-6, None, h, None, new(n, t=torch.float32))
         qp, kp, vp = self._heads(h @ self.w["qkv"].t())
         # (a position beyond the limit is none of the table's, and gives NaN)
-        S.spes_qk_rope_fwd(S.qk_shape(n, H, K, D, self.rot, self.dt, 0, self.limit), qp, kp, self.w["q"], self.w["k"], self.table, self.length, q, k)
-        at = torch.where(self.length < self.limit, self.next, self.spare)
+        S.spes_qk_rope_fwd(S.qk_shape(n, H, K, D, self.rot, self.dt, 0, self.limit), qp, kp, self.w["q"], self.w["k"], self.table,
+                           self.length if self.rot else None, q, k)
+        fits = self.length < self.limit
+        if not self.rot:
+            q.masked_fill_(~fits[:, None, None], float("nan"))
+        at = torch.where(fits, self.next, self.spare)
         for c, t in zip(self.rows, (k, vp)):
             c.index_copy_(0, at, t)
         self.length += 1

@@ -141,9 +141,10 @@ def test_a_refused_token_takes_no_room():
 
 
 @pytest.mark.parametrize("room,n_pos", [(6, 128), (9, 6)])
-def test_replays_beyond_the_room_of_a_cache(room, n_pos):
+@pytest.mark.parametrize("rot_dim", [None, 16, 0])
+def test_replays_beyond_the_room_of_a_cache(room, n_pos, rot_dim):
     """A captured token: up to the sixth what eager calls give, then NaN, with the caches as they were; emptied caches of the same size take the graph on."""
-    A, B = make(8, n_pos=n_pos), make(8, n_pos=n_pos)
+    A, B = (make(8, n_pos=n_pos, rot_dim=rot_dim) for _ in range(2))
     x = torch.randn(6, 3, D_MODEL, device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)).to(A.h.dtype)
     for m in (A, B):
         m.start_cache(3, room)
@@ -178,3 +179,16 @@ def test_replays_beyond_the_room_of_a_cache(room, n_pos):
         assert all(torch.equal(a, b) for a, b in zip(A.cache, held)) and all((c[:, 6:] == 7.0).all() for c in A.cache)
     with pytest.raises(S.SpesError):
         B.decode(x[0])
+
+
+def test_without_rotation():
+    """rot_dim 0: what a rotation by no angle gives; single tokens as the whole.  (Not bit for bit: where pairs are half of the head apart a lane has chunks p and
+    p + 2 of it, without rotation 2 p and 2 p + 1, so the sums over a head run in another order; within the allowance of the other tests then.)"""
+    A, B = make(40, rot_dim=0), make(40)
+    x, d_add, starts, pos = batch(A, [0, 30, 40])
+    got, want = call(A, x, d_add, starts, pos), call(B, x, d_add, starts, torch.zeros_like(pos))
+    for n in want:
+        assert far(got[n], want[n]) < TOL16, n
+    A.start_cache(1, 30)
+    single = torch.cat([A.decode(x[i: i + 1]) for i in range(30)])
+    assert far(single, got["add"][:30]) < TOL16
