@@ -16,6 +16,9 @@ constexpr long kMaxRows = (1l << 31) - (1l << 16);               // the number o
 // A launch has fewer than 2^32 threads: blocks of 256 for 128 rows of queries, or in the backward for 64 keys, and one more for each sequence
 constexpr long kMaxQueryRows = 1l << 30, kMaxKeyRows = 1l << 29, kMaxSeqs = 1l << 22;
 
+// The bf16 gradients of keys sum scores on top of -lse / scale, and ln of 2^31 keys over this is 2^124.4 (behind it lse / scale is a score's own sum of products)
+constexpr float kLeastScale = 0x1p-120f;
+
 bool stride_ok(int64_t stride, int dtype) { return stride % (dtype == SPES_F32 ? 4 : 8) == 0; }
 
 int qk_supported(const spes_qk_shape* p) {
@@ -61,6 +64,7 @@ int attn_bwd_supported(const spes_attn_shape* p) {
   if (!apart(p->q_row, p->q_head, p->q_rows, p->heads, p->head_dim) || !apart(p->k_row, p->k_head, p->k_rows, p->kv_heads, p->head_dim) ||
       !apart(p->v_row, p->v_head, p->k_rows, p->kv_heads, p->head_dim))
     return SPES_EINVAL;
+  if (p->dtype == SPES_BF16 && p->scale < kLeastScale) return SPES_EINVAL;
   return (long)p->k_rows * p->kv_heads > kMaxKeyRows ? SPES_ESHAPE : SPES_OK;
 }
 AttnShape shape_of(const spes_attn_shape& p, const int32_t* q_start, const int32_t* k_start, const int32_t* k_len) {
