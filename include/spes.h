@@ -518,7 +518,7 @@ typedef struct {
   int32_t dtype;         /* spes_dtype                                                                                          */
   int32_t causal;
   int32_t window;        /* 0: none; > 0 with causal only                                                                       */
-  float scale;           /* > 0, finite; in the backward of bf16 storage at least 2^-120                                        */
+  float scale;           /* > 0, at most 2^95; in the backward of bf16 storage at least 2^-120                                  */
 } spes_attn_shape;
 
 /*  q         DEVICE [q_rows, heads, head_dim]     k, v  DEVICE [k_rows, kv_heads, head_dim], strides in the shape

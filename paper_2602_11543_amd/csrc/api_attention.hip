@@ -1,6 +1,4 @@
 // C ABI of the attention half of a block: argument checks ahead of any launch.
-#include <cmath>
-
 #include "kernels.h"
 
 using namespace spes;
@@ -16,6 +14,8 @@ constexpr long kMaxRows = (1l << 31) - (1l << 16);               // the number o
 // A launch has fewer than 2^32 threads: blocks of 256 for 128 rows of queries, or in the backward for 64 keys, and one more for each sequence
 constexpr long kMaxQueryRows = 1l << 30, kMaxKeyRows = 1l << 29, kMaxSeqs = 1l << 22;
 
+// A score is the scale times a sum of up to 128 products, each off by as much as 2^-126 where it is denormal: under a larger scale by more than 2^-24 in all
+constexpr float kMostScale = 0x1p95f;
 // The bf16 gradients of keys sum scores on top of -lse / scale, and ln of 2^31 keys over this is 2^124.4 (behind it lse / scale is a score's own sum of products)
 constexpr float kLeastScale = 0x1p-120f;
 
@@ -43,7 +43,7 @@ bool angles_ok(const spes_qk_shape& p, const float* table, const int32_t* pos) {
 int attn_supported(const spes_attn_shape* p) {
   if (p == nullptr) return SPES_EINVAL;
   if (p->n_seq < 0 || p->q_rows < 0 || p->k_rows < 0 || p->heads < 1 || p->kv_heads < 1 || p->head_dim < 1 || !dtype_ok(p->dtype) || p->window < 0 ||
-      !std::isfinite(p->scale) || !(p->scale > 0.f))
+      !(p->scale > 0.f && p->scale <= kMostScale))
     return SPES_EINVAL;
   if (p->heads % p->kv_heads != 0 || (p->window > 0 && !p->causal)) return SPES_EINVAL;
   if (p->head_dim % 8 != 0 || p->head_dim > kMaxHeadDim || p->heads > kMaxHeads) return SPES_ESHAPE;

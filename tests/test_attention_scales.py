@@ -23,3 +23,14 @@ def test_small_scales_of_bf16_gradients():
         assert LIB.spes_attn_bwd(ctypes.byref(s), *P[:13], None) == EINVAL and S.spes_attn_scratch_bytes(s, 1) == 0, scale
         assert S.spes_attn_scratch_bytes(s, 0) > 0 and S.spes_attn_scratch_bytes(shape(scale, S.SPES_F32), 1) > 0, scale
     assert S.spes_attn_scratch_bytes(shape(2.0 ** -120, S.SPES_BF16), 1) > 0
+
+
+def test_large_scales():
+    """Their scores would come of products that fp32 does not hold to 24 bits, and from 1.39 2^127 on scale log2 e is no number."""
+    for scale in (3.4e38, 2.0 ** 127, 1.01 * 2.0 ** 95):
+        for dtype in (S.SPES_BF16, S.SPES_F32):
+            s = shape(scale, dtype)
+            assert LIB.spes_attn_fwd(ctypes.byref(s), *P[:9], None) == EINVAL == LIB.spes_attn_bwd(ctypes.byref(s), *P[:13], None), scale
+            assert S.spes_attn_scratch_bytes(s, 0) == 0 == S.spes_attn_scratch_bytes(s, 1), scale
+    for backward in (0, 1):
+        assert S.spes_attn_scratch_bytes(shape(2.0 ** 95, S.SPES_BF16), backward) > 0

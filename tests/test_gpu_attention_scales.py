@@ -17,3 +17,8 @@ def test_small_scales(dtype, size):
 def test_smaller_ones_where_nothing_is_divided_by_them():
     Problem([150], heads=2, kv=1, dim=64, dtype=torch.float32, scale=1e-38, seed=12).check()
     Problem([150], heads=2, kv=1, dim=64, scale=1e-38, seed=12).check(backward=False)
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+def test_large_scales(dtype):
+    Problem([150, 1, 70], heads=2, kv=1, dim=64, dtype=dtype, scale=2.0 ** 95, size=2.0 ** -49, seed=12).check()
