@@ -454,7 +454,7 @@ SPES_API int spes_masked_muon(int32_t n_experts, int32_t rows, int32_t cols, int
  * A pair is elements i and i + rot_dim / 2, or with `interleaved` elements 2 i and 2 i + 1; elements from rot_dim on are not rotated.
  * What angles the table holds is the caller's.  A position that it does not have gives NaN in what is rotated.
  *
- *  Supported: head_dim a multiple of 8, at most 256; rot_dim a multiple of 16, at most head_dim, or 0; T (heads + kv_heads) below 2^31
+ *  Supported: head_dim a multiple of 8, at most 256; rot_dim a multiple of 16, at most head_dim, or 0; heads + kv_heads at most 2^22, T times these below 2^31
  */
 typedef struct {
   int64_t q_row, k_row; /* elements from one token's q and k to the next one's, where the projection wrote them (a token's heads stand

@@ -8,6 +8,7 @@ namespace {
 bool dtype_ok(int dtype) { return dtype == SPES_F32 || dtype == SPES_BF16; }
 
 constexpr int kMaxRopeDim = 256, kMaxHeadDim = 128, kMaxHeads = 1024;
+constexpr long kMaxRopeHeads = 1l << 22;         // a token's elements, and the number of a head some rounds behind the last one, fit 32 bits
 constexpr long kMaxRow = 1l << 20, kMaxGroup = 1l << 28;          // in elements: 32-bit byte offsets from a tile's first row
 
 constexpr long kMaxRows = (1l << 31) - (1l << 16);               // the number of a row a few tiles behind the last one still fits 32 bits
@@ -27,7 +28,8 @@ int qk_supported(const spes_qk_shape* p) {
       !dtype_ok(p->dtype) || !(p->eps >= 0.f))
     return SPES_EINVAL;
   if (p->head_dim % 8 != 0 || p->head_dim > kMaxRopeDim || p->rot_dim % 16 != 0) return SPES_ESHAPE;
-  if (((long)p->heads + p->kv_heads) * p->T >= 1l << 31) return SPES_ESHAPE;
+  const long heads = (long)p->heads + p->kv_heads;
+  if (heads > kMaxRopeHeads || heads * p->T >= 1l << 31) return SPES_ESHAPE;
   if (p->q_row < (long)p->heads * p->head_dim || p->k_row < (long)p->kv_heads * p->head_dim) return SPES_EINVAL;
   return SPES_OK;
 }

@@ -156,3 +156,19 @@ def test_attention_limits_and_layouts_of_gradients():
     for good in (dict(), dict(q_row=264), dict(q_head=72, q_row=3 * 72 + 64), dict(k_row=64, k_head=96 * 64), dict(v_row=256, v_head=64), dict(q_rows=1, q_row=64),
                  dict(kv_heads=1, k_row=64, v_row=64)):
         assert need(ctypes.byref(_attn(**good)), 1) > 0, good
+
+
+def test_norm_and_rotation_of_more_heads_than_are_numbered():
+    """Kernels number a token's heads up to a few rounds behind the last one, and its elements, in 32 bits."""
+    fwd, bwd, need = LIB.spes_qk_rope_fwd, LIB.spes_qk_rope_bwd, LIB.spes_qk_rope_scratch_bytes
+    fwd.restype, fwd.argtypes = i32, [vp] * 10
+    bwd.restype, bwd.argtypes = i32, [vp] * 13 + [i32, vp, vp]
+    need.restype, need.argtypes = sz, [vp]
+    for heads, kv in ((2 ** 31 - 2, 1), (2 ** 22, 1), (1, 2 ** 22), (2 ** 21 + 1, 2 ** 21)):
+        s = S.qk_shape(1, 4, 2, 8, 0, S.SPES_BF16, 0, 0)
+        s.heads, s.kv_heads, s.q_row, s.k_row = heads, kv, 8 * heads, 8 * kv
+        r = ctypes.byref(s)
+        assert fwd(r, *P[:4], None, None, *P[4:6], None) == ESHAPE == bwd(r, *P[:6], None, None, *P[6:10], 0, P[10], None) and need(r) == 0, (heads, kv)
+    s.heads = s.kv_heads = 2 ** 21
+    s.q_row = s.k_row = 2 ** 24
+    assert need(ctypes.byref(s)) > 0
