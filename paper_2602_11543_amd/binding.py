@@ -184,6 +184,12 @@ def _heads(t: Optional[torch.Tensor], rows: int, heads: int, dim: int, dtype: to
     return t.data_ptr(), row if rows > 1 else heads * dim, head if heads > 1 else dim
 
 
+def _here(t: Optional[torch.Tensor]) -> None:
+    """A launch goes to the current device: a tensor of another one would be read there, if at all."""
+    if t is not None and t.get_device() != torch._C._cuda_getDevice():
+        raise SpesError("tensors must be on the current device")
+
+
 def _like(t: Optional[torch.Tensor], strides, *want):
     """Pointer of an output that is laid out as its input is."""
     p, *got = _heads(t, *want)
@@ -426,6 +432,7 @@ def _qk(shape, q, k):
     T, H, K, D, t = shape.T, shape.heads, shape.kv_heads, shape.head_dim, torch_dtype(shape.dtype)
     qp, q_row, q_head = _heads(q, T, H, D, t)
     kp, k_row, k_head = _heads(k, T, K, D, t)
+    _here(q)
     if q_head != D or k_head != D:
         raise SpesError("a token's heads must stand side by side")
     own = spes_qk_shape.from_buffer_copy(shape)
@@ -473,6 +480,7 @@ def _attn(shape, q, k, v, q_start, k_start, k_len):
     qp, own.q_row, own.q_head = _heads(q, rows, H, D, t)
     kp, own.k_row, own.k_head = _heads(k, keys, K, D, t)
     vp, own.v_row, own.v_head = _heads(v, keys, K, D, t)
+    _here(q)
     return (own, qp, kp, vp, _buf(q_start, i, n + 1), _buf(k_start, i, n + (k_len is None)), _buf(k_len, i, n)), (t, rows, H, D)
 
 
