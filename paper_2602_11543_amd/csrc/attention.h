@@ -40,7 +40,6 @@ template <> struct Mma<bf16_t> {
   static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, const f32x4& c, bool = false) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ Frag zero() { return __builtin_bit_cast(Frag, make_uint4(0, 0, 0, 0)); }
   static __device__ __forceinline__ Frag load(const bf16_t* p) { return __builtin_bit_cast(Frag, load_global(p)); }
-  static __device__ __forceinline__ Frag load_half(const bf16_t*) { return zero(); }       // (there are none)
   // a column's eight results, rounded to the operands' type
   static __device__ __forceinline__ Frag of(const f32x4& a, const f32x4& b) {
     return __builtin_bit_cast(Frag, make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])));
@@ -85,7 +84,10 @@ template <typename T, int DC>
 __device__ __forceinline__ typename Mma<T>::Frag head_frag(const T* p, int kc, int quad, int dim, bool real) {
   const bool half = last_half<DC>(kc);
   const int at = 32 * kc + (half ? 4 : 8) * quad;
-  return !real || at >= dim ? Mma<T>::zero() : half ? Mma<T>::load_half(p + at) : Mma<T>::load(p + at);
+  if (!real || at >= dim) return Mma<T>::zero();
+  if constexpr (DC % 32 != 0)
+    if (half) return Mma<T>::load_half(p + at);
+  return Mma<T>::load(p + at);
 }
 
 __device__ __forceinline__ unsigned lds_address(void* p) { return uniform((unsigned)(unsigned long)(__attribute__((address_space(3))) char*)p); }
@@ -165,17 +167,6 @@ struct Tile {
   static __device__ __forceinline__ unsigned load_off(int wave, int i, int lane, long stride, int dim) {
     const int r = load_row(wave, i, lane), ch = load_chunk(r, lane);
     return ch * (16 / (int)sizeof(T)) < dim ? (unsigned)(r * stride + ch * 16) : kOutOfRange;
-  }
-  // kStep rows, at most `rows` of them real, from `base` on into LDS at `dst`; zeros beyond
-  static __device__ __forceinline__ void load_rows(unsigned long base, long stride, int rows, int dim, unsigned dst, int wave, int lane) {
-    const rsrc_t rs = rsrc_for_lds(base, (unsigned)(max(min(rows, kStep), 0) * stride));
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const unsigned o = load_off(wave, i, lane, stride, dim);
-      const unsigned m = set_lds_dest(uniform(dst + (unsigned)((wave * kLoads + i) * 1024)));
-      one_instruction();
-      load_to_lds(rs, o, m);
-    }
   }
 };
 
@@ -353,7 +344,7 @@ struct Row {
 struct Reach { int lo, hi; };
 __device__ __forceinline__ Reach reach(const AttnShape& a, const Seq& s, int i) {
   if (!a.causal) return Reach{0, s.lk};
-  const int end = min(max(i + s.lk - s.lq + 1, 0), s.lk);
+  const int end = min(max(i - s.lq + 1 + s.lk, 0), s.lk);      // (in this order no sum passes 32 bits, with 2^31 keys either)
   return Reach{a.window > 0 ? max(end - a.window, 0) : 0, end};
 }
 
