@@ -470,13 +470,23 @@ __global__ __launch_bounds__(256) void attn_bwd_delta_kernel(const BwdArgs g) {
   }
 }
 
-// How many blocks, of both kernels, are launched as one; all of the backward, one after the other -> together.  fp32 always (what a launch can have): one block
-// to a CU whatever its kernel, 1001, 1500 and 259 tokens, 10 / 5 heads of 80, window of 700 237 -> 227 us; 2 x 1000, 12 heads of 64 185 -> 143; 16 x 2000, 16 / 4
-// of 80 5.82 -> 5.52 ms.  Long heads in bf16 up to eight times what the chip holds: 1 x 1000, 16 / 4 heads of 128 99 -> 87 us; 16 documents of 1 to 6011
-// tokens (3200 blocks) 811 -> 771, in another order 910 -> 800; 64 of up to 512 (3584) 208 -> 215; 8 x 4096, 32 / 8 heads (12400) 3.39 -> 3.50 ms.  Short ones,
-// whose queries' kernel alone has three wavefronts to a SIMD, up to what the chip holds: 2 x 150, 12 heads of 64 (120 blocks) 18 -> 15 us; 8 x 200 (636) 22.5 ->
-// 23.3; 32 of up to 1024 158 -> 175.
-template <typename T, int DC> constexpr long kTogether = sizeof(T) == 4 ? 1l << 23 : DC > 64 ? 4096 : 512;
+// How many blocks, of both kernels, are launched as one.  The whole backward in two launches takes so many times what it takes in one (means over batches of equal and of
+// unequal sequences, 16 / 4 heads of 128 in both types, in fp32 also 10 / 5 of 80, 12 of 64 and 16 of 32; the chip holds 256 or 512 blocks):
+//      blocks                                        256    512   1024   2048   4000
+//      averages of 64 to 768 tokens                 1.36   1.12   1.07   1.00   0.95   (0.45 to 1.36 at 4000: 125 x 128 tokens in fp32 547 in place of 1218 us, where
+//                                                                                       tiles of one kind all come to the same CUs)
+//      1024 and 2048                                1.38   1.24   1.17   1.05   1.00
+// 1001, 1500 and 259 tokens, 10 / 5 heads of 80 in fp32, window of 700: 247 us in two, 226 in one; 16 documents of 1 to 6011 tokens, 16 / 4 heads of 128 (3200 blocks)
+// 820 and 788; 64 of up to 512 (3600) 209 and 224; 16 x 2000, 16 / 4 of 80 in fp32 5640 and 5340; 8 x 4096, 32 / 8 of 128 (12400) 3390 and 3500.
+// Short heads in bf16, whose queries' kernel alone has three wavefronts to a SIMD: 2 x 150, 12 heads of 64 (120 blocks) 18 and 15; 8 x 200 (636) 22.5 and 23.3; 32
+// documents of up to 1024 158 and 175.
+constexpr long kLongAverage = 1000;
+template <typename T, int DC>
+long together(const AttnShape& a) {
+  if (sizeof(T) == 2 && DC <= 64) return 512;
+  if (a.q_rows < kLongAverage * a.n_seq) return 2048;
+  return sizeof(T) == 4 ? 1l << 23 : 4096;         // (fp32: what a launch can have)
+}
 
 template <typename T, int DC>
 int bwd(BwdArgs g, hipStream_t s) {
@@ -485,13 +495,13 @@ int bwd(BwdArgs g, hipStream_t s) {
   g.q_tiles = (int)(a.q_rows > 0 ? rows / kRows + a.n_seq : 0);
   g.k_tiles = (int)(a.k_rows > 0 ? (long)a.k_rows / kKeys + a.n_seq : 0);
   auto grid = [&](long tiles) { return dim3((unsigned)(tiles * a.kv_heads)); };
-  if (g.q_tiles > 0 && g.k_tiles > 0 && ((long)g.q_tiles + g.k_tiles) * a.kv_heads <= kTogether<T, DC>) {
+  if (g.q_tiles > 0 && g.k_tiles > 0 && ((long)g.q_tiles + g.k_tiles) * a.kv_heads <= together<T, DC>(a)) {
     attn_bwd_delta_kernel<T, DC><<<grid(g.q_tiles), dim3(256), 0, s>>>(g);
     attn_bwd_both_kernel<T, DC><<<grid((long)g.q_tiles + g.k_tiles), dim3(256), 0, s>>>(g);
     return hipGetLastError() == hipSuccess ? SPES_OK : SPES_EHIP;
   }
   // (two sets where launches above the limit can be short of blocks)
-  constexpr bool kTwo = kTwoSets<T, DC> && kTogether<T, DC> <= 512;
+  constexpr bool kTwo = kTwoSets<T, DC> && sizeof(T) == 2 && DC <= 64;
   bool two_q = false, two_k = false;
   if constexpr (kTwo) {
     two_q = two_sets(rows / kRows * a.kv_heads, a.k_rows, a.n_seq);

@@ -36,3 +36,18 @@ def test_launches_of_their_own(dim):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_as_many_places_of_shared_heads(dtype):
     Scattered([70, 1, 130, 33, 64, 90], keys=[80, 5, 0, 300, 64, 100], heads=4, kv=4, dim=40, dtype=dtype, causal=False, seed=1).check()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim", [40, 80, 128])
+@pytest.mark.parametrize("lens,times", [([128, 128], 160), ([70, 1, 130, 33], 100), ([1100, 900], 6)])
+def test_gradients_are_the_same_in_one_launch_and_in_two(dtype, dim, lens, times):
+    """A batch whose blocks run as one launch, and many of it in one batch, whose blocks do or do not."""
+    few = Problem(lens, heads=8, kv=4, dim=dim, dtype=dtype, seed=dim)
+    many = Problem(lens * times, heads=8, kv=4, dim=dim, dtype=dtype, seed=dim)
+    for name in ("q", "k", "v", "d_o"):
+        getattr(many, name).copy_(getattr(few, name).repeat(times, 1, 1))
+    f = few.forward()             # (of both: the forward of few blocks has its keys' sums in two sets)
+    want, got = few.backward(**f), many.backward(f["o"].repeat(times, 1, 1), f["lse"].repeat(1, times))
+    for name in ("dq", "dk", "dv"):
+        assert torch.equal(got[name], want[name].repeat(times, 1, 1)), name
