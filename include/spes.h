@@ -502,6 +502,8 @@ SPES_API int spes_qk_rope_bwd(const spes_qk_shape* shape, const void* dq, const 
  * hold is cut to the tensors' rows; queries of two sequences must not overlap, nor in the backward keys.  Rows of a sequence must be finite: an
  * infinity or a NaN in one can reach other rows of its sequence, whether they see it or not.
  * Products in bf16 storage take bf16 operands, the probabilities and their gradient among them, and are summed in fp32; in fp32 storage they are fp32.
+ * Lengths stay on the device, so a captured call takes new ones; how the work is cut follows from n_seq, q_rows and k_rows alone.  A batch of unlike sequences (a prompt
+ * beside single tokens), places of no queries, and chunks of queries in a cache with much more room than keys are answered all the same, but take longer.
  *
  *  Supported: head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, at most 1024; q_rows heads at most 2^30, k_rows at most 2^31 - 2^16
  *  (in the backward k_rows kv_heads at most 2^29), n_seq kv_heads at most 2^22; strides multiples of 16 bytes, rows at most 2^20 elements

@@ -12,8 +12,9 @@
 // 1.5 GHz), and the smaller form moves half as many accumulators per multiply-add: backward of that, when it was taken, 3.75 -> 3.65 ms, forward 1.13 -> 1.12;
 // 2 x 2048 tokens, 12 heads of 64, forward 33 -> 30 us.
 //
-// Operands in bf16 storage are bf16: probabilities and their gradient are rounded once, by at most 2^-9 of each, on their way into the products that sum them in
-// fp32.  dq and dk are then 2.5e-3 off (in norm), where rounding the exact ones to bf16 leaves 1.7e-3; nearly all of it is the one rounding of the gradient.
+// Operands in bf16 storage are bf16: probabilities and their gradient are rounded once, by at most 2^-8 of each, on their way into the products that sum them in
+// fp32, for the rate of bf16 products, which is eight times that of fp32 ones.  o is then 1.9e-3 to 2.4e-3 off (in norm), dq and dk 2.5e-3, where rounding the exact
+// ones to bf16 leaves 1.7e-3; nearly all of it is the one rounding of the gradient.
 #pragma once
 #include <algorithm>
 
@@ -104,9 +105,10 @@ constexpr unsigned kOpen = 0x80000000u;      // bytes of a resource that is not 
 constexpr int tile_dim(int dim) { return dim <= 64 ? 64 : 128; }
 
 // Whether two sets of four wavefronts have room in LDS, and whether a launch of so many blocks is to have them: where they leave half of the chip empty or
-// hold it for long steps one behind the other (512 blocks: two to a CU), and steps enough for both.  2 x 2048 tokens, 12 heads of 64: forward (384 blocks)
-// 42 -> 33 us, gradients of queries (384 blocks) and keys (768, which keep one set) 87 -> 79; with two sets for the 768 as well 95.  Steps: one sequence of 200
-// tokens, 12 heads of 64, forward 9.0 us, with two sets 9.7.
+// hold it for long steps one behind the other (512 blocks), and steps enough for both.  2 x 2048 tokens, 12 heads of 64: forward (384 blocks)
+// 42 -> 31 us, gradients of queries (384 blocks) and keys (768, which keep one set) 87 -> 79; with two sets for the 768 as well 95.  Steps: one sequence of 200
+// tokens, 12 heads of 64, forward 9.0 us, with two sets 9.7.  (Eight wavefronts with more than 128 registers, 140 and 164 there, are alone on a CU, so
+// 384 blocks are one and a half rounds.)
 template <typename T, int DC> constexpr bool kTwoSets = 2 * 4 * kStep * tile_dim(DC) * (int)sizeof(T) <= 144 * 1024;
 inline bool two_sets(long blocks, long steps_rows, int n_seq) { return std::max<long>(blocks, n_seq) <= 512 && steps_rows >= 4l * kStep * n_seq; }
 

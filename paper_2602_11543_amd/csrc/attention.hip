@@ -58,9 +58,10 @@ __device__ __forceinline__ void put_row(const FwdArgs& g, int part, long token, 
 // With KS = 2 there are four more wavefronts, and the two sets take every second step of keys and join what they have at the end: half the steps one behind
 // the other for launches that leave CUs empty.
 // Two wavefronts to a SIMD in bf16 (220 registers with heads of 128): one's matrix instructions run beside the other's exponentials.  32 heads of 128 (8 of
-// keys), 8 x 4096 tokens, causal: 1.11 ms, 0.99 PFLOP/s of what the mask leaves, bound by power (with zeros for data 0.89 ms; a library product of 8192^3
-// 1.27 PFLOP/s).  512 queries against 16000 keys: 148 us, 0.89 PFLOP/s.  12 heads of 64, 2 x 2048 tokens: 30 us; there exponentials and maxima take longer than the
-// products.  fp32, 10 heads of 80, 2760 tokens, window of 700: 75 us; the matrix instructions of the longest block 55 of them.
+// keys), 8 x 4096 tokens, causal: 1.10 to 1.19 ms, 0.92 to 1.00 PFLOP/s of what the mask leaves, bound by power (with zeros for data 0.89 ms; a library product of
+// 8192^3 1.22 to 1.27 PFLOP/s).  512 queries against 16000 keys: 147 to 160 us, 0.83 to 0.90 PFLOP/s.  12 heads of 64, 2 x 2048 tokens: 31 us; there exponentials and
+// maxima take longer than the products.  fp32, 10 heads of 80, 2760 tokens, window of 700: 76 us, one wavefront to a SIMD (263 registers, and LDS for one set, with rows
+// of 80 laid out as 128); the matrix instructions of the longest block 55 of them.
 template <typename T, int DC, int KS>
 __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_kernel(const FwdArgs g) {
   constexpr int DH = tile_dim(DC);
@@ -258,20 +259,22 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_fwd_ker
 // Few rows of a sequence (up to 32) against many keys, so bound by memory: every wavefront goes over keys of its own, steps of 32, through LDS of its own, so nothing is waited
 // for but the wavefront's own loads, of which the next step's are always on their way.  The wavefronts' sums meet in LDS at the end.
 // One token each of 32 sequences over 1 to 8192 keys, 32 / 8 heads of 128: 44 us, 5.2 TB/s, and 6 for joining the parts; one over 131071 keys, 16 / 4 heads:
-// 48 us, 5.6 TB/s, and 6 (a copy of 2 GiB 4.9 TB/s).  With the kernel above in its place 83 and 56 us in all instead of 49 and 54: its parts are cut for
-// sequences of average length, and all of a block waits for every step.
+// 48 us, 5.6 TB/s, and 6 (a copy of 2 GiB 4.9 TB/s).  With the kernel above in its place 83 and 56 us in all instead of 50 and 53: its parts are cut for
+// sequences of average length, and all of a block waits for every step.  fp32, where LDS holds one wavefront to a block and two to a CU: 126 us in all (3.6 TB/s)
+// and 203 (2.6), 256 sequences of 500 233 (4.5).
 template <typename T, int DH>
 struct Few {
   typedef Tile<T, DH> L;
   static constexpr int kSlot = kFewStep * L::kRowBytes, kLoads = kFewStep / L::kRowsPerLoad;      // of keys or values
-  static constexpr int kWaves = 64 * 1024 / (4 * kSlot) < 4 ? 64 * 1024 / (4 * kSlot) : 4;          // two slots of both each; two blocks to a CU
+  // two slots of both each; two blocks to a CU: in bf16 up to 64 elements two wavefronts to a SIMD, else one or none
+  static constexpr int kWaves = 64 * 1024 / (4 * kSlot) < 4 ? 64 * 1024 / (4 * kSlot) : 4;
 };
 // What the blocks of that kernel make of the descriptors, every one for itself: items of (tile of rows, part of its sequence's keys), all parts of one size
 // `per`, such that there are about kFewItems of them, so the work is even however unequal the sequences are.
 // With that many tiles their keys are not cut: the tiles are looked up, by up to eight times the blocks, which even out unequal sequences, and nothing is joined
-// (one token each of 256 sequences, 32 / 8 heads of 128, 500 keys: 145 us cut, 108 whole; 1024 of 250 298 -> 235; 128 of 1 to 4096 302 -> 271; with
+// (one token each of 256 sequences, 32 / 8 heads of 128, 500 keys: 145 us cut, 109 whole; 1024 of 250 298 -> 234; 128 of 1 to 4096 302 -> 271; with
 // the chip's blocks alone 115, 227 and 308; by attn_fwd_kernel 128, 225 and 288).
-// (The 32 sequences above: 49 us in all with 1024 items, two for each block, 52 with 512, 56 with 2048; with at least 4 or 16 steps to a part the same as with 8.)
+// (The 32 sequences above: 50 us in all with 1024 items, two for each block, 52 with 512, 56 with 2048; with at least 4 or 16 steps to a part the same as with 8.)
 constexpr int kFewItems = 1024, kFewLeast = 8, kFewBlocks = 512;      // kFewLeast: steps to a part at least; kFewBlocks: what the chip holds
 struct Span { int tiles, j0, n; };      // of a sequence: tiles of rows, first step of keys that its queries see, steps
 __device__ __forceinline__ Span span_of(const AttnShape& a, const Seq& s) {
@@ -532,7 +535,7 @@ __global__ __launch_bounds__((64 * Few<T, tile_dim(DC)>::kWaves)) void attn_few_
 
 // The parts of a row's keys joined: weights exp(lse_p - lse).  LANES lanes to a row: 32 hold four elements each, and each 32 go over every
 // (LANES / 32)th part.  A launch of its own, so no block waits for another: 6 us for one token of 32 sequences (1024 rows of up to 19 parts), which is two
-// trips to memory one behind the other, and 10 for 512 queries of 32 heads in 4 parts (34 MB).
+// trips to memory one behind the other, and 11 for 512 queries of 32 heads in 4 parts (34 MB).
 template <typename T, int LANES, bool FEW>
 __global__ __launch_bounds__(256) void attn_join_kernel(const FwdArgs g) {
   constexpr int GROUPS = LANES / 32, PER_BLOCK = 256 / LANES;
@@ -611,6 +614,9 @@ static_assert(kMaxParts == 64, "two parts to a lane");
 
 // How a call is cut.  few: 32 rows at most to a sequence on the average, by the kernel for these.  Parts: so that few rows against many keys fill the chip
 // (512 queries of 32 heads against 16000 keys, 128 tiles: 219 us whole, 150 in 4 parts with the launch that joins them).
+// The host knows averages and the room of a cache, not lengths.  What that costs: the 512 queries in a cache with room for 131072 have all of their keys in the first part
+// and take 449 us; beside 512 on 512 keys, 512 on 120000 take 1670 in place of 985; 31 single tokens of the 32 sequences above take 45 us, a prompt of 1000 on 8192 keys 148, and
+// both in one batch 222.
 struct Cut { bool few; int parts, per; };
 Cut cut_of(int dtype, const AttnShape& a) {
   if (a.n_seq == 0 || a.q_rows == 0) return {false, 1, 1};

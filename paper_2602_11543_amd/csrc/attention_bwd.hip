@@ -37,8 +37,8 @@ __device__ __forceinline__ float delta_of(const typename Mma<T>::Frag (&d)[kFrag
 }
 
 // 128 rows; KS sets of four wavefronts as in the forward.  Queries and upstream gradients stay in registers, keys and values pass through LDS: each key tile is
-// read as rows for the scores and as columns for dq.  8 x 4096 tokens, 32 / 8 heads of 128, causal: 1.45 ms, 1.14 PFLOP/s of the 6 D operations a
-// pair, bound by power; 2 x 2048 tokens, 12 heads of 64: 36 us.
+// read as rows for the scores and as columns for dq.  8 x 4096 tokens, 32 / 8 heads of 128, causal: 1.43 to 1.47 ms, 1.12 to 1.16 PFLOP/s of the 6 D operations a
+// pair, bound by power; 2 x 2048 tokens, 12 heads of 64: 37 us.
 template <typename T, int DC, int KS, bool KEEP>
 __device__ __forceinline__ void bwd_q(const BwdArgs& g, int item, int kvh, char* smem) {
   constexpr int DH = tile_dim(DC);
@@ -201,8 +201,8 @@ __device__ __forceinline__ void bwd_q(const BwdArgs& g, int item, int kvh, char*
 // Four wavefronts: two groups of 32 keys, and in each one wavefront for the first 32 of the 64 rows that are in LDS and one for the others, whose sums are
 // joined at the end.  The rows are gone over from the last one down: the blocks of a sequence's keys then begin at the same rows and find each other's in L2,
 // where from each block's first row on they are all over a sequence of which L2 holds half (8 x 4096 tokens, 32 / 8 heads of 128: 8 MB).
-// The same problems as above: 2.1 ms, 1.05 PFLOP/s of the 8 D operations a pair (a wavefront's sums, keys and values take 192 of its 256 registers, which
-// leaves little for operands ahead of their use); 43 us.  (Four groups, 64 rows each: half the loads into LDS, but the second 32 rows cost
+// The same problems as above: 2.07 to 2.14 ms, 1.03 to 1.06 PFLOP/s of the 8 D operations a pair (a wavefront's sums, keys and values take 192 of its 256 registers, which
+// leaves little for operands ahead of their use: with 128 elements in bf16 26 registers are spilled, 100 bytes a lane); 44 us.  (Four groups, 64 rows each: half the loads into LDS, but the second 32 rows cost
 // more registers than there are, with 128 elements all of the backward took 12.6 ms in place of 4.1 then; 64 elements: 97 us in place of 83.)
 constexpr int kKeys = 64;
 template <int KS> struct Stats { float of[2][KS][2][kStep]; };       // of each slot's rows: -lse / scale (fp32: -lse log2 e), -delta
@@ -437,8 +437,8 @@ __global__ __launch_bounds__(256 * KS, sizeof(T) == 2 ? 2 : 1) void attn_bwd_kv_
 }
 
 // Both in one launch, behind one that forms delta: where each by itself leaves CUs empty towards its end, or all along.  Tiles of rows and of keys are dealt out
-// evenly, the longest of a sequence first.  fp32, 2760 tokens, 10 / 5 heads of 80, window of 700: 220 us behind 5 (106 and 135 one after the other); 16 documents of 1 to
-// 6011 tokens, 16 / 4 heads of 128: 780 to 810 behind 23.
+// evenly, the longest of a sequence first.  fp32, 2760 tokens, 10 / 5 heads of 80, window of 700: 222 to 225 us behind 5 (106 and 135 one after the other); 16 documents
+// of 1 to 6011 tokens, 16 / 4 heads of 128: 813 to 879 behind 23, as a profiler sees them one by one; both launches 770 to 825 in a row of calls.
 template <typename T, int DC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attn_bwd_both_kernel(const BwdArgs g) {
   __shared__ __align__(1024) char smem[kLds<T, DC, 1>];

@@ -128,8 +128,8 @@ __device__ __forceinline__ void turn(float* v, const float* c, const float* s, b
 }
 
 // Tensors that pass through the caches (and so carry the non-temporal hint): a wavefront goes over a token's heads, 64 / LG at a time, U such rounds at
-// once, with the angles in registers: queries' rounds first, then keys'.  32768 tokens, 32 + 8 heads of 128 in bf16: 118 us (5.7 TB/s) and
-// 188 (5.4), memory; the whole step 303 us, with a head to LG lanes as below 341.
+// once, with the angles in registers: queries' rounds first, then keys'.  32768 tokens, 32 + 8 heads of 128 in bf16: 116 to 119 us (5.7 TB/s) and
+// 183 to 200 (5.0 to 5.5), memory; the whole step 304 us, with a head to LG lanes as below 341.
 template <typename T, int LG, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void qk_rope_fwd_kernel(const QkArgs g) {
   constexpr int NG = kWave / LG, U = sizeof(T) == 2 ? 4 : 2;
@@ -287,8 +287,8 @@ __global__ __launch_bounds__(256) void qk_rope_bwd_kernel(const QkArgs g) {
 }
 
 // Tensors that the caches hold: LG lanes to a head, heads one behind the other, blocks of queries and blocks of keys.  Short launches, in which what
-// counts is how little a wavefront has to fetch before its first store (4096 tokens, 12 + 12 heads of 64: 8.1 and 11.0 us, 3.1 and 3.4 TB/s out of the Infinity
-// Cache; the whole step 24.5 us, with the kernels above 27).
+// counts is how little a wavefront has to fetch before its first store (4096 tokens, 12 + 12 heads of 64: 7.9 and 11.0 us, 3.2 and 3.4 TB/s out of the Infinity
+// Cache; the whole step 21.7 to 24.5 us, with the kernels above 27).
 template <typename T, int LG, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void qk_flat_fwd_kernel(const QkArgs g) {
   const bool keys = (int)blockIdx.x >= g.side[0].blocks;
