@@ -51,6 +51,9 @@ class DeviceAttention:
         H, K, D = self.H, self.K, self.D
         return t[:, : H * D].view(-1, H, D), t[:, H * D: (H + K) * D].view(-1, K, D), t[:, (H + K) * D:].view(-1, K, D)
 
+    def _shape(self, starts):
+        return S.attn_shape(starts.numel() - 1, self.T, self.T, self.H, self.K, self.D, self.dt, 1, self.window)
+
     def _scratch(self, shape, backward, use="batch"):
         """Scratch for the call.  Captured graphs have the addresses of what was handed out, so a buffer that is outgrown is kept; each is twice the one
         before at least, and those kept are not more than the newest one.  Single tokens have their own, which batches do not grow."""
@@ -69,15 +72,16 @@ class DeviceAttention:
         torch.mm(self.h, self.w["qkv"].t(), out=self.qkv)
         q, k, v = self._heads(self.qkv)
         S.spes_qk_rope_fwd(self.qk, q, k, self.w["q"], self.w["k"], self.table, pos if self.rot else None, self.q, self.k)
-        self.shape = S.attn_shape(starts.numel() - 1, T, T, self.H, self.K, self.D, self.dt, 1, self.window)
+        shape = self._shape(starts)
         # (attention leaves rows of no sequence as they are, and the products below go over all rows.  Cleared whole: which rows these are is known on the
         # device alone; 32768 rows of 32 / 8 heads of 128 in bf16, o and the three gradients, 0.7 GB to write)
         self.o.zero_()
-        S.spes_attn_fwd(self.shape, self.q, self.k, v, starts, starts, None, self.o, self.lse, self._scratch(self.shape, 0))
+        S.spes_attn_fwd(shape, self.q, self.k, v, starts, starts, None, self.o, self.lse, self._scratch(shape, 0))
         return self.o.view(T, -1) @ self.w["o"].t()
 
     def backward(self, d_add, x, starts, pos, d_stream=None, accumulate=0):
-        """d_add [T, d]: gradient of what the forward returned; d_stream: the one that reaches x along the stream.  Returns x's."""
+        """d_add [T, d]: gradient of what the last forward returned, x, starts and pos as they were for that; d_stream: the one that reaches x along the
+        stream.  Returns x's."""
         T, d = self.T, self.d
 
         def product(name, a, b):               # (into the gradient's own place: graphs and the optimizer step know it by that)
@@ -92,7 +96,8 @@ class DeviceAttention:
         dq, dk, dv = self._heads(self.d_qkv)
         self.d_heads.zero_()
         dv.zero_()
-        S.spes_attn_bwd(self.shape, d_o, self.q, self.k, v, starts, starts, None, self.o, self.lse, self.dq, self.dk, dv, self._scratch(self.shape, 1))
+        shape = self._shape(starts)
+        S.spes_attn_bwd(shape, d_o, self.q, self.k, v, starts, starts, None, self.o, self.lse, self.dq, self.dk, dv, self._scratch(shape, 1))
         S.spes_qk_rope_bwd(self.qk, self.dq, self.dk, q, k, self.w["q"], self.w["k"], self.table, pos if self.rot else None, dq, dk, self.grad["q"], self.grad["k"],
                            accumulate, self.qk_scratch)
         product("qkv", self.d_qkv, self.h)

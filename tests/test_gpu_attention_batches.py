@@ -84,7 +84,7 @@ def test_scratch_of_a_graph_stays_its_own():
         A.start_cache(2, 2000 * (i + 1))
         A.decode(one[0][:2])
         need = S.attn_shape(2, 2, 4000 * (i + 1), A.H, A.K, A.D, A.dt, 1, 0)
-        assert S.spes_attn_scratch_bytes(need, 0) > S.spes_attn_scratch_bytes(A.shape, 1)
+        assert S.spes_attn_scratch_bytes(need, 0) > S.spes_attn_scratch_bytes(S.attn_shape(2, 128, 128, A.H, A.K, A.D, A.dt, 1, 0), 1)
         call(A, *batch(A, many, seed=6))
         kept += [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (512, 2048, 4096, 1 << 16)]
         mine = [t.clone() for t in kept]
@@ -192,3 +192,19 @@ def test_without_rotation():
     A.start_cache(1, 30)
     single = torch.cat([A.decode(x[i: i + 1]) for i in range(30)])
     assert far(single, got["add"][:30]) < TOL16
+
+
+def test_a_backward_goes_by_the_sequences_that_it_is_given():
+    """A replayed forward of three sequences behind an eager one of a single sequence, then an eager backward of the three."""
+    A, B = make(128), make(128)
+    three, one = batch(A, [0, 40, 90, 128]), batch(A, [0, 128], seed=8)
+    A.forward(three[0], three[2], three[3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.forward(three[0], three[2], three[3])
+    A.forward(one[0], one[2], one[3])
+    graph.replay()
+    dx = A.backward(three[1], *(three[i] for i in (0, 2, 3)))
+    want = call(B, *three)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, want["dx"]) and all(torch.equal(t, want[n]) for n, t in A.grad.items())
