@@ -117,6 +117,8 @@ class DeviceAttention:
         """Empty caches with room for `room` tokens of each of n_seq sequences.  Caches of these sizes that are there already are emptied where they are, and
         graphs that captured decode() go on with them; with others such graphs are not to be replayed any more."""
         dev, st = self.h.device, S.torch_dtype(self.dt)
+        if n_seq < 0 or room < 0 or n_seq * room > 2 ** 31 - 2 ** 16:          # (as many rows as spes_attn_fwd takes)
+            raise S.SpesError("start_cache: more rows than a cache can have")
         row0 = torch.arange(n_seq, dtype=torch.int32, device=dev) * room
         self.taken = 0
         if self.cache is not None and self.cache[0].shape[:2] == (n_seq, room):
