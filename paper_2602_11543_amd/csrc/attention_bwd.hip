@@ -471,11 +471,12 @@ __global__ __launch_bounds__(256) void attn_bwd_delta_kernel(const BwdArgs g) {
 }
 
 // How many blocks, of both kernels, are launched as one.  The whole backward in two launches takes so many times what it takes in one (means over batches of equal and of
-// unequal sequences, 16 / 4 heads of 128 in both types, in fp32 also 10 / 5 of 80, 12 of 64 and 16 of 32; the chip holds 256 or 512 blocks):
+// unequal sequences, 16 / 4 heads of 128 in both types, in fp32 also 10 / 5 of 80 and 12 of 64; the chip holds 256 or 512 blocks):
 //      blocks                                        256    512   1024   2048   4000
-//      averages of 64 to 768 tokens                 1.36   1.12   1.07   1.00   0.95   (0.45 to 1.36 at 4000: 125 x 128 tokens in fp32 547 in place of 1218 us, where
+//      averages of 64 to 768 tokens                 1.35   1.10   1.06   0.97   0.92   (0.45 to 1.36 at 4000: 125 x 128 tokens in fp32 547 in place of 1218 us, where
 //                                                                                       tiles of one kind all come to the same CUs)
-//      1024 and 2048                                1.38   1.24   1.17   1.05   1.00
+//      1024 and 2048                                1.38   1.22   1.14   1.05   0.99
+//      fp32, 16 heads of 32, 64 to 1024             1.40   1.27   1.17   1.11   1.07
 // 1001, 1500 and 259 tokens, 10 / 5 heads of 80 in fp32, window of 700: 247 us in two, 226 in one; 16 documents of 1 to 6011 tokens, 16 / 4 heads of 128 (3200 blocks)
 // 820 and 788; 64 of up to 512 (3600) 209 and 224; 16 x 2000, 16 / 4 of 80 in fp32 5640 and 5340; 8 x 4096, 32 / 8 of 128 (12400) 3390 and 3500.
 // Short heads in bf16, whose queries' kernel alone has three wavefronts to a SIMD: 2 x 150, 12 heads of 64 (120 blocks) 18 and 15; 8 x 200 (636) 22.5 and 23.3; 32
@@ -484,7 +485,7 @@ constexpr long kLongAverage = 1000;
 template <typename T, int DC>
 long together(const AttnShape& a) {
   if (sizeof(T) == 2 && DC <= 64) return 512;
-  if (a.q_rows < kLongAverage * a.n_seq) return 2048;
+  if (DC > 48 && a.q_rows < kLongAverage * a.n_seq) return 1536;
   return sizeof(T) == 4 ? 1l << 23 : 4096;         // (fp32: what a launch can have)
 }
 
